@@ -311,6 +311,68 @@ hydra_status hydra_token_logprobs_kl(const void* logits_actor, const void* logit
                                      float* lse_ref, void* stream);
 
 /*
+ * Token statistics of rows of logits for the update side and for serving (§2 "Stage 3: PPO": the
+ * ratio r(theta) needs the sampled tokens' log-probabilities under the new parameters; the paper
+ * names no entropy bonus, the entropy is for those who add one or watch it). Per row z of V logits:
+ *     m = max_v z_v,  c = log sum_v exp(z_v - m)
+ *     logp     = (z[id] - m) - c
+ *     entropy  = -sum_v p_v log p_v,  p_v = exp(z_v - m - c)
+ *     norm     = (m, c)           their sum is the log-sum-exp; hydra_token_logprobs_entropy_grad
+ *                                 takes the pair, which stays exact where |m| is large
+ *     top_ids, top_logp           the top_k likeliest tokens with their log-probabilities, in
+ *                                 descending order; equal logits by ascending index
+ * Arguments:
+ *   logits  : [S*L, V] rows of dtype logits_dtype (HYDRA_F32 or HYDRA_BF16) at row stride
+ *             ld >= V elements; any row may start at any element (16-byte rows are not needed).
+ *   ids     : int32 [S*L] token ids in [0, V) for logp; may be NULL without logp.
+ *   lengths : int32 [S] valid tokens per sequence, 0..L; NULL means all L.
+ *   top_k   : 0..32, at most V.
+ *   logp, entropy fp32 [S*L], norm fp32 [S*L, 2]: outputs, each may be NULL; top_ids int32 and
+ *             top_logp fp32 [S*L, top_k], ignored with top_k == 0. At least one output is wanted.
+ * Rows t >= len: not read; logp, entropy, norm and top_logp 0, top_ids -1.
+ * Masked logits: -inf is a token that cannot be drawn (logp -inf, 0 in the entropy; among the top
+ * behind all others). A row of nothing but -inf has logp -inf, entropy 0, norm (-inf, 0) and top_logp
+ * -inf. The type's lowest value is a number like any other. A NaN or +inf logit makes the row's
+ * logp, entropy, norm[1] and top_logp NaN; top_ids then counts NaN as the largest.
+ * Bits: sums are fp32 and depend on nothing but the row's values, V, top_k > 0, its start modulo 16
+ * bytes and the number of rows S*L.
+ * Errors: logits_dtype or top_k -> HYDRA_ERR_RANGE; S, L < 0, S*L >= 2^31, V < 1, V > 2^30 or
+ * ld < V -> HYDRA_ERR_SHAPE; a needed pointer or every output NULL -> HYDRA_ERR_NULL; logits not
+ * aligned to its element -> HYDRA_ERR_ALIGN; id out of range -> device error 0x201 and logp NaN;
+ * length out of range -> device error 0x202, clamped. S*L == 0 is a no-op.
+ */
+hydra_status hydra_token_logprobs_entropy(const void* logits, int logits_dtype, int64_t S, int64_t L,
+                                          int64_t V, int64_t ld, const int32_t* ids,
+                                          const int32_t* lengths, int64_t top_k, float* logp,
+                                          float* entropy, float* norm, int32_t* top_ids,
+                                          float* top_logp, void* stream);
+
+/*
+ * Gradient of hydra_token_logprobs_entropy's logp and entropy with respect to the logits, given the
+ * gradients of a loss with respect to them (grad_logp as hydra_ppo_loss writes it):
+ *     dlogits[v] = grad_logp ([v == id] - p_v) - grad_entropy p_v (log p_v + entropy)
+ * Arguments:
+ *   logits, ids, lengths, S, L, V, ld : as the forward call. ids may be NULL without grad_logp.
+ *   norm      : fp32 [S*L, 2] and entropy : fp32 [S*L], as the forward call wrote them (entropy may
+ *               be NULL without grad_entropy).
+ *   grad_logp, grad_entropy : fp32 [S*L], either may be NULL (0), not both.
+ *   dlogits   : [S*L, V] rows of grad_dtype (HYDRA_F32, or HYDRA_BF16: fp32 rounded once) at row
+ *               stride ld_d >= V. dlogits == logits of the same dtype and stride works in place;
+ *               other overlaps are not allowed. Columns from V on are left as they were.
+ * Rows t >= len and rows of nothing but -inf are written 0 (rows t >= len are not read). A token at
+ * -inf has p = 0. An id out of range writes NaN to its row (device error 0x201).
+ * Errors: as the forward call, and grad_dtype, or dlogits == logits with another dtype or stride ->
+ * HYDRA_ERR_RANGE; ld_d < V, or S*L rows of V beyond 2^31 thread blocks (of up to 4096 logits of a
+ * row) -> HYDRA_ERR_SHAPE.
+ */
+hydra_status hydra_token_logprobs_entropy_grad(const void* logits, int logits_dtype, int64_t S,
+                                               int64_t L, int64_t V, int64_t ld, const int32_t* ids,
+                                               const int32_t* lengths, const float* norm,
+                                               const float* entropy, const float* grad_logp,
+                                               const float* grad_entropy, void* dlogits,
+                                               int grad_dtype, int64_t ld_d, void* stream);
+
+/*
  * The dual LM head and the log-probabilities in one pass, without materialising logits:
  * equal to hydra_lora_linear(h_off, h_on, ..., W_lm, A, B, r, s, z_ref, z_actor, HYDRA_F32)
  * followed by hydra_token_logprobs_kl(z_actor, z_ref, ...), up to the fp32 summation order.
@@ -411,6 +473,45 @@ hydra_status hydra_ppo_adv_moments(const float* advantages, const int32_t* lengt
  * d = mean_b - mean_a. No device work. Errors: k < 0 -> HYDRA_ERR_SHAPE; NULL out (or NULL
  * moments with k > 0) -> HYDRA_ERR_NULL; a negative or NaN n or M2 -> HYDRA_ERR_RANGE. */
 hydra_status hydra_ppo_merge_moments(const double* moments, int64_t k, double* out);
+
+/* One gradient tensor of a list: numel dense elements of dtype (HYDRA_F32 or HYDRA_BF16) at grad,
+ * and where its clipped values go (out == grad: in place; unused by hydra_grad_norm). */
+typedef struct hydra_grad_tensor {
+  const void* grad;
+  void* out;
+  int64_t numel;
+  int64_t dtype;
+} hydra_grad_tensor;
+
+/*
+ * Global norm of a list of gradient tensors, as one update of a LoRA set has hundreds of:
+ *     norm = sqrt(sum of g^2 over all elements of all tensors)
+ *     coef = min(1, max_norm / (norm + 1e-6)), and 1 where the norm is not finite
+ * and hydra_clip_grad_norm also writes out = g coef to every tensor (fp32 product, rounded once to
+ * dtype). A norm that is not finite leaves the values as they were: the caller sees it in norm_out.
+ *   tensors  : HOST array of n entries (device pointers inside), read during the call only: a
+ *              captured call keeps the addresses. Types may be mixed, pointers need no more than
+ *              their element's alignment, empty tensors (numel 0) are skipped.
+ *   max_norm : > 0; +inf measures only.
+ *   norm_out : device fp32 [2] = (norm, coef).
+ *   workspace: device, 16-byte aligned, >= hydra_grad_norm_workspace_size() bytes, caller-owned; no
+ *              initial contents required; calls sharing a workspace must be stream-ordered.
+ * A tensor's squares are summed in fp32 over runs of some dozens of elements and in fp64 beyond, in an
+ * order that depends on nothing but the list and the device: equal calls give equal bits. No fp32
+ * element is too large or too small for its square.
+ * An out range may not overlap any other range of the list, read or written (the same tensor twice
+ * among them); hydra_grad_norm, which only reads, counts a tensor listed twice twice.
+ * Errors: n < 0, n >= 2^31, a numel < 0 or >= 2^40 -> HYDRA_ERR_SHAPE; max_norm or a dtype, or
+ * overlapping ranges -> HYDRA_ERR_RANGE; NULL norm_out, list or (numel > 0) tensor -> HYDRA_ERR_NULL;
+ * a pointer not aligned to its element -> HYDRA_ERR_ALIGN; small or misaligned workspace ->
+ * HYDRA_ERR_WORKSPACE. n == 0 writes (0, 1).
+ */
+size_t hydra_grad_norm_workspace_size(void);
+hydra_status hydra_grad_norm(const hydra_grad_tensor* tensors, int64_t n, float max_norm, float* norm_out,
+                             void* workspace, size_t workspace_bytes, void* stream);
+hydra_status hydra_clip_grad_norm(const hydra_grad_tensor* tensors, int64_t n, float max_norm,
+                                  float* norm_out, void* workspace, size_t workspace_bytes,
+                                  void* stream);
 
 /* ===================================================================================
  * Llama decoder pieces and the full scoring pass (the paper runs Llama 7b, §4; the pass

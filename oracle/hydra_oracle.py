@@ -502,6 +502,69 @@ def ppo_loss(logp_new, logp_old, adv, returns, values, lengths, clip_eps=0.2, wh
     }
 
 
+def token_stats(z, ids, lengths, S, L, k=0):
+    """Log-probability of ids, entropy, (max, log-sum) and the k likeliest tokens of each row of
+    z [S*L, V]; ids None: no log-probabilities. Rows t >= len: 0, and -1 among the tokens. -inf is a
+    token that cannot be drawn; a row of nothing else has logp -inf, entropy 0, norm (-inf, 0)."""
+    z = np.asarray(z, dtype=np.float64)
+    live = _live_rows(lengths, S, L)
+    m = z.max(axis=1, keepdims=True)
+    empty = m == -np.inf
+    with np.errstate(invalid="ignore", over="ignore"):
+        t = np.where(empty, -np.inf, z - m)
+    total = np.exp(t).sum(axis=1, keepdims=True)
+    log_sum = np.log(np.where(empty, 1.0, total))
+    lp = t - log_sum
+    p = np.exp(lp)
+    out = {"entropy": np.where(live, -(p * np.where(p > 0, lp, 0.0)).sum(axis=1), 0.0),
+           "norm": np.where(live[:, None], np.concatenate([m, log_sum], axis=1), 0.0)}
+    if ids is not None:
+        picked = lp[np.arange(S * L), np.asarray(ids, dtype=np.int64)]
+        out["logp"] = np.where(live, picked, 0.0)
+    if k:
+        order = np.argsort(-z, axis=1, kind="stable")[:, :k]
+        out["top_ids"] = np.where(live[:, None], order, -1)
+        out["top_logp"] = np.where(live[:, None], np.take_along_axis(lp, order, axis=1), 0.0)
+    return out
+
+
+def token_stats_grad(z, ids, lengths, S, L, grad_logp=None, grad_entropy=None):
+    """Gradient of sum(grad_logp * logp + grad_entropy * entropy) of token_stats in z: with p the
+    row's probabilities, dlogp/dz_v = [v = id] - p_v and dH/dz_v = -p_v (log p_v + H). 0 in rows
+    t >= len and in rows of nothing but -inf."""
+    z = np.asarray(z, dtype=np.float64)
+    rows = np.arange(S * L)
+    m = z.max(axis=1, keepdims=True)
+    live = _live_rows(lengths, S, L) & (m[:, 0] > -np.inf)
+    with np.errstate(invalid="ignore", over="ignore"):
+        lp = z - m
+    lp = lp - np.log(np.exp(lp).sum(axis=1, keepdims=True))
+    p = np.exp(lp)
+    lp = np.where(p > 0, lp, 0.0)
+    d = np.zeros_like(z)
+    if grad_logp is not None:
+        d -= p * np.asarray(grad_logp, dtype=np.float64)[:, None]
+        d[rows, np.asarray(ids, dtype=np.int64)] += grad_logp
+    if grad_entropy is not None:
+        h = -(p * lp).sum(axis=1, keepdims=True)
+        d -= np.asarray(grad_entropy, dtype=np.float64)[:, None] * p * (lp + h)
+    return np.where(live[:, None], d, 0.0)
+
+
+def _live_rows(lengths, S, L):
+    n = np.full(S, L) if lengths is None else np.asarray(lengths, dtype=np.int64)
+    return (np.arange(L)[None, :] < n.reshape(S, 1)).reshape(-1)
+
+
+def clip_grad_norm(grads, max_norm):
+    """(norm, coefficient, clipped): norm of all elements of all arrays, coefficient
+    min(1, max_norm / (norm + 1e-6)) (1 where the norm is not finite), and the arrays times it."""
+    g = [np.asarray(x, dtype=np.float64) for x in grads]
+    norm = float(np.sqrt(sum(float((x * x).sum()) for x in g)))
+    coef = min(1.0, max_norm / (norm + 1e-6)) if np.isfinite(norm) else 1.0
+    return norm, coef, [x * coef for x in g]
+
+
 # ---------------------------------------------------------------------------
 # Generation with the actor (Alg. 1 and 2: the actor samples each sequence for T steps;
 # J-Hydra-PPO keeps the critic head's values while sampling)

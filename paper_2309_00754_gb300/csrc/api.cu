@@ -3,7 +3,10 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <mutex>
+#include <new>
+#include <vector>
 
 #include "../../include/hydra.h"
 #include "common.cuh"
@@ -128,6 +131,70 @@ hydra_status lora_linear_impl(const void* x_off, const void* x_on, int64_t M, in
   }
   const int rc = use_gemv ? hydra::launch_dual_lora_gemv(g, st) : hydra::launch_dual_lora_gemm_tc(g, st);
   return rc == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+// Rows of logits: [S * L] of V at stride ld. Element indices within a row stay in 32 bits.
+bool token_rows_ok(int64_t S, int64_t L, int64_t V, int64_t ld) {
+  return S >= 0 && L >= 0 && S < (1LL << 31) && L < (1LL << 31) && S * L < (1LL << 31) && V >= 1 &&
+         V <= (1LL << 30) && ld >= V;
+}
+
+// A tensor's memory range in a list of gradients.
+struct Span {
+  uintptr_t lo, hi;
+  bool written;
+};
+
+// Whether a range that is written overlaps any other one.
+bool spans_clash(std::vector<Span>& v) {
+  const auto before = [](const Span& a, const Span& b) { return a.lo < b.lo; };
+  if (!std::is_sorted(v.begin(), v.end(), before)) std::sort(v.begin(), v.end(), before);
+  uintptr_t end = 0, end_written = 0;
+  for (const Span& s : v) {
+    if (s.lo < (s.written ? end : end_written)) return true;
+    end = std::max(end, s.hi);
+    if (s.written) end_written = std::max(end_written, s.hi);
+  }
+  return false;
+}
+
+hydra_status grad_norm_impl(const hydra_grad_tensor* tensors, int64_t n, float max_norm, float* norm_out,
+                            bool clip, void* workspace, size_t workspace_bytes, void* stream) {
+  if (n < 0 || n >= (1LL << 31)) return HYDRA_ERR_SHAPE;
+  if (!(max_norm > 0.f)) return HYDRA_ERR_RANGE;
+  if (norm_out == nullptr || (n > 0 && tensors == nullptr)) return HYDRA_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(norm_out) % 4 != 0) return HYDRA_ERR_ALIGN;
+  if (workspace == nullptr || workspace_bytes < hydra::grad_norm_workspace_bytes() ||
+      !aligned16(workspace))
+    return HYDRA_ERR_WORKSPACE;
+  std::vector<hydra::GradTensor> list;
+  try {
+    std::vector<Span> spans;
+    list.reserve(static_cast<size_t>(n));
+    if (clip) spans.reserve(2 * static_cast<size_t>(n));
+    for (int64_t i = 0; i < n; ++i) {
+      const hydra_grad_tensor& t = tensors[i];
+      if (t.dtype != HYDRA_F32 && t.dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
+      if (t.numel < 0 || t.numel >= (1LL << 40)) return HYDRA_ERR_SHAPE;
+      if (t.numel == 0) continue;
+      if (t.grad == nullptr || (clip && t.out == nullptr)) return HYDRA_ERR_NULL;
+      const uintptr_t size = t.dtype == HYDRA_BF16 ? 2 : 4, bytes = size * static_cast<uintptr_t>(t.numel);
+      const uintptr_t src = reinterpret_cast<uintptr_t>(t.grad), dst = reinterpret_cast<uintptr_t>(t.out);
+      if (src % size != 0 || (clip && dst % size != 0)) return HYDRA_ERR_ALIGN;
+      list.push_back({t.grad, t.out, t.numel, t.dtype == HYDRA_BF16});
+      if (clip) {
+        spans.push_back({dst, dst + bytes, true});
+        if (src != dst) spans.push_back({src, src + bytes, false});
+      }
+    }
+    if (clip && spans_clash(spans)) return HYDRA_ERR_RANGE;
+  } catch (const std::bad_alloc&) {
+    return HYDRA_ERR_SHAPE;  // no host memory for a list of this length
+  }
+  return hydra::launch_grad_norm(list.data(), static_cast<int64_t>(list.size()), max_norm, norm_out, clip,
+                                 workspace, static_cast<cudaStream_t>(stream)) == 0
+             ? HYDRA_OK
+             : HYDRA_ERR_CUDA;
 }
 
 // One warp waits on an mbarrier that nothing ever arrives on, through the bounded wait that
@@ -462,6 +529,94 @@ hydra_status hydra_token_logprobs_kl(const void* logits_actor, const void* logit
                                          static_cast<cudaStream_t>(stream)) == 0
              ? HYDRA_OK
              : HYDRA_ERR_CUDA;
+}
+
+hydra_status hydra_token_logprobs_entropy(const void* logits, int logits_dtype, int64_t S, int64_t L,
+                                          int64_t V, int64_t ld, const int32_t* ids,
+                                          const int32_t* lengths, int64_t top_k, float* logp,
+                                          float* entropy, float* norm, int32_t* top_ids,
+                                          float* top_logp, void* stream) {
+  if (logits_dtype != HYDRA_F32 && logits_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
+  if (!token_rows_ok(S, L, V, ld)) return HYDRA_ERR_SHAPE;
+  if (top_k < 0 || top_k > hydra::kTokenTopMax || top_k > V) return HYDRA_ERR_RANGE;
+  if (S == 0 || L == 0) return HYDRA_OK;
+  if (logits == nullptr || (logp != nullptr && ids == nullptr)) return HYDRA_ERR_NULL;
+  if (top_k > 0 && (top_ids == nullptr || top_logp == nullptr)) return HYDRA_ERR_NULL;
+  if (logp == nullptr && entropy == nullptr && norm == nullptr && top_k == 0) return HYDRA_ERR_NULL;
+  const size_t size = logits_dtype == HYDRA_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(logits) % size != 0) return HYDRA_ERR_ALIGN;
+  hydra::TokenStatsArgs a;
+  a.logits = logits;
+  a.bf16 = logits_dtype == HYDRA_BF16;
+  a.S = S;
+  a.L = L;
+  a.V = V;
+  a.ld = ld;
+  a.ids = ids;
+  a.lengths = lengths;
+  a.top_k = top_k;
+  a.logp = logp;
+  a.entropy = entropy;
+  a.norm = norm;
+  a.top_ids = top_ids;
+  a.top_logp = top_logp;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_token_stats(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+hydra_status hydra_token_logprobs_entropy_grad(const void* logits, int logits_dtype, int64_t S,
+                                               int64_t L, int64_t V, int64_t ld, const int32_t* ids,
+                                               const int32_t* lengths, const float* norm,
+                                               const float* entropy, const float* grad_logp,
+                                               const float* grad_entropy, void* dlogits,
+                                               int grad_dtype, int64_t ld_d, void* stream) {
+  if (logits_dtype != HYDRA_F32 && logits_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
+  if (grad_dtype != HYDRA_F32 && grad_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
+  if (!token_rows_ok(S, L, V, ld) || ld_d < V) return HYDRA_ERR_SHAPE;
+  if (S == 0 || L == 0) return HYDRA_OK;
+  if (S * L > ((1LL << 31) - 1) / hydra::token_stats_grad_tiles(V)) return HYDRA_ERR_SHAPE;
+  if (logits == nullptr || norm == nullptr || dlogits == nullptr) return HYDRA_ERR_NULL;
+  if (grad_logp == nullptr && grad_entropy == nullptr) return HYDRA_ERR_NULL;
+  if ((grad_logp != nullptr && ids == nullptr) || (grad_entropy != nullptr && entropy == nullptr))
+    return HYDRA_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(logits) % (logits_dtype == HYDRA_BF16 ? 2 : 4) != 0 ||
+      reinterpret_cast<uintptr_t>(dlogits) % (grad_dtype == HYDRA_BF16 ? 2 : 4) != 0)
+    return HYDRA_ERR_ALIGN;
+  // in place every element is read and written by one thread; any other shape of it would race
+  if (logits == dlogits && (logits_dtype != grad_dtype || ld != ld_d)) return HYDRA_ERR_RANGE;
+  hydra::TokenStatsGradArgs a;
+  a.logits = logits;
+  a.bf16 = logits_dtype == HYDRA_BF16;
+  a.S = S;
+  a.L = L;
+  a.V = V;
+  a.ld = ld;
+  a.ids = ids;
+  a.lengths = lengths;
+  a.norm = norm;
+  a.entropy = entropy;
+  a.grad_logp = grad_logp;
+  a.grad_entropy = grad_entropy;
+  a.dlogits = dlogits;
+  a.grad_bf16 = grad_dtype == HYDRA_BF16;
+  a.ld_d = ld_d;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_token_stats_grad(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+size_t hydra_grad_norm_workspace_size(void) { return hydra::grad_norm_workspace_bytes(); }
+
+hydra_status hydra_grad_norm(const hydra_grad_tensor* tensors, int64_t n, float max_norm, float* norm_out,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  return grad_norm_impl(tensors, n, max_norm, norm_out, false, workspace, workspace_bytes, stream);
+}
+
+hydra_status hydra_clip_grad_norm(const hydra_grad_tensor* tensors, int64_t n, float max_norm,
+                                  float* norm_out, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+  return grad_norm_impl(tensors, n, max_norm, norm_out, true, workspace, workspace_bytes, stream);
 }
 
 hydra_status ppo_gae(const float* rewards, const float* values, const int32_t* lengths, int64_t S,

@@ -150,6 +150,56 @@ int launch_ppo_loss(const float* logp_new, const float* logp_old, const float* a
 constexpr int kPpoMaxMomentBlocks = 1024;
 constexpr int kPpoMaxLossBlocks = 1024;
 
+// Token statistics of rows of logits and their gradient (logprobs_entropy.cu). Rows [S * L] of V
+// logits at stride ld, fp32 or (bf16) bf16; NULL outputs are skipped.
+struct TokenStatsArgs {
+  const void* logits;
+  bool bf16;
+  int64_t S, L, V, ld;
+  const int32_t* ids;      // used for logp
+  const int32_t* lengths;  // or NULL
+  int64_t top_k;           // 0: no alternatives
+  float* logp;
+  float* entropy;
+  float* norm;  // [S * L][2] (max, log sum exp(z - max))
+  int32_t* top_ids;
+  float* top_logp;
+  int* err;
+};
+constexpr int kTokenTopMax = 32;
+int launch_token_stats(const TokenStatsArgs& a, cudaStream_t stream);
+struct TokenStatsGradArgs {
+  const void* logits;
+  bool bf16;
+  int64_t S, L, V, ld;
+  const int32_t* ids;
+  const int32_t* lengths;
+  const float* norm;
+  const float* entropy;       // used with grad_entropy
+  const float* grad_logp;     // or NULL
+  const float* grad_entropy;  // or NULL
+  void* dlogits;              // rows at stride ld_d, fp32 or (grad_bf16) bf16
+  bool grad_bf16;
+  int64_t ld_d;
+  int* err;
+};
+// CTAs a row takes: S * L * tiles must stay below 2^31
+int64_t token_stats_grad_tiles(int64_t V);
+int launch_token_stats_grad(const TokenStatsGradArgs& a, cudaStream_t stream);
+
+// Global norm of a list of tensors and clipping (grad_clip.cu); ws holds one fp64 partial a CTA.
+struct GradTensor {
+  const void* grad;
+  void* out;
+  int64_t numel;
+  int bf16;
+};
+constexpr int kGradMaxBlocks = 1216;
+size_t grad_norm_workspace_bytes();
+// norm_out [2] = (norm, coefficient); scale: out = grad * coefficient as well
+int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm_out, bool scale, void* ws,
+                     cudaStream_t st);
+
 // The full pass's stacked linear over ns row-stacked streams (score_llama.cu): rows [0, T)
 // of x are the LoRA-off stream, [T, 2T) the LoRA-on stream (LoRA set A, B; u receives its
 // down-projection) and, for ns == 3, [2T, 3T) a third stream with the set A2, B2 (u2). epi:

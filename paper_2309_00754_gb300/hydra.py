@@ -59,6 +59,15 @@ _SIGNATURES = {
     "hydra_token_logprobs_kl": (ctypes.c_int, [_vp, _vp, ctypes.c_int, _c_i64, _c_i64, _c_i64,
                                                _c_i64, _vp, _vp, _vp, ctypes.c_float, _vp, _vp,
                                                _vp, _vp, _vp, _vp]),
+    "hydra_token_logprobs_entropy": (ctypes.c_int, [_vp, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64,
+                                                    _vp, _vp, _c_i64, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "hydra_token_logprobs_entropy_grad": (ctypes.c_int, [_vp, ctypes.c_int, _c_i64, _c_i64, _c_i64,
+                                                         _c_i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                                         ctypes.c_int, _c_i64, _vp]),
+    "hydra_grad_norm_workspace_size": (ctypes.c_size_t, []),
+    "hydra_grad_norm": (ctypes.c_int, [_vp, _c_i64, ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]),
+    "hydra_clip_grad_norm": (ctypes.c_int, [_vp, _c_i64, ctypes.c_float, _vp, _vp, ctypes.c_size_t,
+                                            _vp]),
     "ppo_gae": (ctypes.c_int, [_vp, _vp, _vp, _c_i64, _c_i64, ctypes.c_float, ctypes.c_float, _vp,
                                _vp, _vp]),
     "hydra_ppo_workspace_size": (ctypes.c_size_t, []),
@@ -68,6 +77,10 @@ _SIGNATURES = {
                                              _vp]),
     "hydra_ppo_merge_moments": (ctypes.c_int, [_vp, _c_i64, _vp]),
 }
+
+
+class GradTensorC(ctypes.Structure):
+    _fields_ = [("grad", _vp), ("out", _vp), ("numel", _c_i64), ("dtype", _c_i64)]
 
 
 class LlamaConfigC(ctypes.Structure):
@@ -206,6 +219,25 @@ def _req(t, dtype, name):
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+def _on_device(*tensors):
+    """Refuse tensors of another device than the current one, whose stream the call would not order."""
+    now = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    for t in tensors:
+        if t is not None and t.device.index != now:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{now}")
+
+
+def _rows_of(t, rows, name):
+    """Row stride of [rows, V] logits or their gradient: rows may stand apart, elements may not."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dim() != 2 or t.shape[0] != rows:
+        raise ValueError(f"{name} must have {rows} rows, got shape {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} rows must be unit-stride")
+    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
 
 
 def device_error(clear: bool = True) -> int:
@@ -420,6 +452,60 @@ def hydra_token_logprobs_kl(logits_actor, logits_ref, ids, lengths, seq_score, b
         _p(reward_tok), _p(lse_actor), _p(lse_ref), _stream(stream)))
 
 
+def _per_row(rows, *named):
+    for t, n in named:
+        _req(t, torch.float32, n)
+        if t is not None and t.numel() != (2 * rows if n == "norm" else rows):
+            raise ValueError(f"{n} must have {'[rows, 2]' if n == 'norm' else 'one'} element(s) per row of {rows}")
+
+
+def hydra_token_logprobs_entropy(logits, ids, lengths, S, L, logp=None, entropy=None, norm=None,
+                                 top_ids=None, top_logp=None, stream=None):
+    """Per row of logits [S*L, V] (fp32 or bf16, rows may stand apart): log-probability of ids (int32
+    [S*L]), entropy, norm = (max, log-sum) [S*L, 2], and the top_ids.shape[1] likeliest tokens
+    (int32 ids and fp32 log-probabilities [S*L, k]). Outputs are preallocated, any may be None."""
+    rows = S * L
+    dt = _out_dtype(logits, "logits")
+    ld = _rows_of(logits, rows, "logits")
+    _req(ids, torch.int32, "ids")
+    _req(lengths, torch.int32, "lengths")
+    _req(top_ids, torch.int32, "top_ids")
+    _req(top_logp, torch.float32, "top_logp")
+    _per_row(rows, (logp, "logp"), (entropy, "entropy"), (norm, "norm"))
+    k = 0 if top_ids is None else top_ids.shape[-1]
+    for t, n, size in ((ids, "ids", rows), (lengths, "lengths", S), (top_ids, "top_ids", rows * k),
+                       (top_logp, "top_logp", rows * k)):
+        if t is not None and t.numel() != size:
+            raise ValueError(f"{n} must have {size} elements, got {t.numel()}")
+    _on_device(logits, ids, lengths, logp, entropy, norm, top_ids, top_logp)
+    _check("hydra_token_logprobs_entropy", load().hydra_token_logprobs_entropy(
+        _p(logits), dt, S, L, logits.shape[1], ld, _p(ids), _p(lengths), k, _p(logp), _p(entropy),
+        _p(norm), _p(top_ids), _p(top_logp), _stream(stream)))
+
+
+def hydra_token_logprobs_entropy_grad(logits, ids, lengths, S, L, norm, entropy, grad_logp,
+                                      grad_entropy, dlogits, stream=None):
+    """dlogits [S*L, V] (fp32 or bf16; logits itself: in place) from the gradients of a loss with
+    respect to hydra_token_logprobs_entropy's logp and entropy (either None: 0), whose norm and
+    entropy outputs it takes."""
+    rows = S * L
+    dt, dt_d = _out_dtype(logits, "logits"), _out_dtype(dlogits, "dlogits")
+    ld, ld_d = _rows_of(logits, rows, "logits"), _rows_of(dlogits, rows, "dlogits")
+    if dlogits.shape[1] != logits.shape[1]:
+        raise ValueError("dlogits and logits must have the same columns")
+    _req(ids, torch.int32, "ids")
+    _req(lengths, torch.int32, "lengths")
+    _per_row(rows, (norm, "norm"), (entropy, "entropy"), (grad_logp, "grad_logp"),
+             (grad_entropy, "grad_entropy"))
+    for t, n, size in ((ids, "ids", rows), (lengths, "lengths", S)):
+        if t is not None and t.numel() != size:
+            raise ValueError(f"{n} must have {size} elements, got {t.numel()}")
+    _on_device(logits, ids, lengths, norm, entropy, grad_logp, grad_entropy, dlogits)
+    _check("hydra_token_logprobs_entropy_grad", load().hydra_token_logprobs_entropy_grad(
+        _p(logits), dt, S, L, logits.shape[1], ld, _p(ids), _p(lengths), _p(norm), _p(entropy),
+        _p(grad_logp), _p(grad_entropy), _p(dlogits), dt_d, ld_d, _stream(stream)))
+
+
 def ppo_gae(rewards, values, lengths, gamma, lam, advantages, returns, stream=None):
     """GAE advantages and returns over [S, L] fp32 rewards/values (lengths int32 [S] or None)."""
     for t, n in ((rewards, "rewards"), (values, "values"), (advantages, "advantages"),
@@ -493,6 +579,54 @@ def all_reduce_adv_moments(moments, group=None):
     merged = ppo_merge_moments(torch.stack(parts))
     moments.copy_(merged.to(moments.device))
     return moments
+
+
+class GradList:
+    """The gradient tensors of an update (fp32 or bf16, contiguous) as hydra_grad_norm and
+    hydra_clip_grad_norm take them, with the tensors that receive the clipped values (None: in
+    place). Built once and kept as long as the buffers: it holds references to them."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if len(self.outs) != len(self.grads):
+            raise ValueError(f"{len(self.grads)} gradients, but {len(self.outs)} outputs")
+        self.c = (GradTensorC * max(1, len(self.grads)))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            _req(g, g.dtype, f"grads[{i}]")
+            _req(o, g.dtype, f"outs[{i}]")
+            if o.shape != g.shape:
+                raise ValueError(f"outs[{i}] has shape {tuple(o.shape)}, its gradient {tuple(g.shape)}")
+            self.c[i] = GradTensorC(_p(g), _p(o), g.numel(), _out_dtype(g, f"grads[{i}]"))
+        self.devices = {t.device.index for t in (*self.grads, *self.outs)}
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def grad_norm_workspace_size():
+    return int(load().hydra_grad_norm_workspace_size())
+
+
+def _grad_norm(fn, tensors, max_norm, norm_out, workspace, stream):
+    _req(norm_out, torch.float32, "norm_out")
+    if norm_out.numel() != 2:
+        raise ValueError("norm_out must have two elements")
+    _on_device(norm_out, workspace)
+    if not tensors.devices <= {norm_out.device.index}:
+        raise ValueError(f"gradients on devices {sorted(tensors.devices)}, norm_out on {norm_out.device}")
+    _check(fn, getattr(load(), fn)(tensors.c, len(tensors), float(max_norm), _p(norm_out), _p(workspace),
+                                   workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def hydra_grad_norm(tensors, max_norm, norm_out, workspace, stream=None):
+    """norm_out (fp32 [2]) = the global norm of a GradList and min(1, max_norm / (norm + 1e-6))."""
+    _grad_norm("hydra_grad_norm", tensors, max_norm, norm_out, workspace, stream)
+
+
+def hydra_clip_grad_norm(tensors, max_norm, norm_out, workspace, stream=None):
+    """hydra_grad_norm, and every gradient times that coefficient into its output."""
+    _grad_norm("hydra_clip_grad_norm", tensors, max_norm, norm_out, workspace, stream)
 
 
 # ----------------------------------------------------------------------------- Llama pieces

@@ -1,0 +1,393 @@
+"""Token statistics (log-probability, entropy, top alternatives) and their gradient against the
+fp64 oracle, at the sizes, strides and masks where they can go wrong.
+
+Tolerances, with u = 2^-24 (half a step of fp32). A row's sum of exp(z - m) is added up in chains of
+at most V / 128 + 32 terms and a tree; each term carries the rounding of z - m (relative error u of
+the difference, so |z - m| u of the term, and p |log p| adds up to the entropy, at most log V <= 19),
+of its product with log2 e (the same again) and of ex2 (2 ulp = 4 u): the sum is off by at most
+    tol_s = (V / 128 + 32 + 2 * 19 + 8) u  relative,
+    logp   (z_id - m) - c:  tol_s + 2 u (|z_id - m| + |c|) + u |logp|
+    entropy c - w / s:      tol_s + (2 tol_s + 4 u) entropy + 2 u |c|
+    gradient, given norm and entropy rounded to fp32: p is off by e_p = u (4 |log p| + |c| + 8) relative,
+        the weight g_logp + g_entropy (log p + H) by 4 u of the magnitudes in it; and the result is
+        rounded to its type (half a step, eps / 2). ex2 flushes probabilities under 2^-126: 2e-38 of
+        the weights."""
+import numpy as np
+import pytest
+import torch
+
+import oracle as O
+from paper_2309_00754_gb300 import build as B
+from paper_2309_00754_gb300 import hydra as H
+from tests.helpers import dev_f32, dev_i32, host_f64
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+INF = float("inf")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    B.build()
+    H.load()
+    H.device_error(clear=True)
+    yield
+    assert H.device_error(clear=True) == 0
+
+
+def rows_of(values, dtype, ld=None, shift=0):
+    """Device rows of `values` at stride ld, the first `shift` elements behind a 16-byte boundary; NaN around."""
+    n, v = values.shape
+    ld = ld or v
+    buf = torch.full((n * ld + shift + 8,), float("nan"), dtype=dtype, device="cuda")
+    out = buf[shift:shift + n * ld].view(n, ld)
+    out[:, :v] = torch.from_numpy(values).cuda().to(dtype)
+    return out[:, :v], buf
+
+
+def make(seed, S, L, V, dtype, mask=None, spread=3.0, ld=None, shift=0):
+    """(device logits, the fp64 values they hold, ids, lengths): ragged, the first sequence whole, the last empty."""
+    rng = np.random.default_rng(seed)
+    z = rng.normal(0, spread, (S * L, V)) * 10 ** rng.uniform(-1, 0.5, (S * L, 1))
+    if mask is not None:
+        low = -INF if mask == "inf" else float(torch.finfo(dtype).min)
+        z[rng.random((S * L, V)) < 0.7] = low
+        z[::5] = np.where(np.arange(V) == V // 2, 1.5, low)  # one token left
+        z[2::5] = low                                       # nothing left
+    dev, buf = rows_of(z, dtype, ld, shift)
+    lengths = rng.integers(0, L + 1, S)
+    lengths[0], lengths[-1] = L, (0 if S > 1 else L)
+    return dev, host_f64(dev), rng.integers(0, V, S * L), lengths, buf
+
+
+def run_stats(z, ids, lengths, S, L, k):
+    rows = S * L
+    nan = lambda *s: torch.full(s, float("nan"), device="cuda")  # noqa: E731
+    o = {"logp": nan(rows), "entropy": nan(rows), "norm": nan(rows, 2)}
+    if k:
+        o["top_ids"] = torch.full((rows, k), -7, dtype=torch.int32, device="cuda")
+        o["top_logp"] = nan(rows, k)
+    H.hydra_token_logprobs_entropy(z, None if ids is None else dev_i32(ids), None if lengths is None else dev_i32(lengths),
+                                   S, L, **o)
+    return o
+
+
+def close(got, want, tol, what):
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    bad = ~same & ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (what, np.argwhere(bad)[:4], got[bad][:4], want[bad][:4])
+
+
+def tol_sum(V):
+    return (V / 128 + 32 + 2 * 19 + 8) * U
+
+
+def check_stats(o, z, ids, lengths, S, L, k):
+    V = z.shape[1]
+    r = O.token_stats(z, ids, lengths, S, L, k)
+    ts, c = tol_sum(V), np.abs(np.where(np.isfinite(r["norm"][:, 1]), r["norm"][:, 1], 0))
+    shift = lambda lp: ts + 2 * U * (np.abs(np.where(np.isfinite(lp), lp, 0)) + 2 * c) + U * np.abs(np.where(np.isfinite(lp), lp, 0))  # noqa: E731
+    norm = host_f64(o["norm"])
+    assert np.array_equal(norm[:, 0], r["norm"][:, 0])
+    close(norm[:, 1], r["norm"][:, 1], ts + 2 * U * c, "log-sum")
+    if ids is not None:
+        close(host_f64(o["logp"]), r["logp"], shift(r["logp"]), "logp")
+    close(host_f64(o["entropy"]), r["entropy"], ts + (2 * ts + 4 * U) * r["entropy"] + 2 * U * c, "entropy")
+    if k:
+        assert np.array_equal(o["top_ids"].cpu().numpy(), r["top_ids"])
+        close(host_f64(o["top_logp"]), r["top_logp"], ts + 3 * U * np.abs(np.where(np.isfinite(r["top_logp"]), r["top_logp"], 0))
+              + 4 * U * c[:, None], "top_logp")
+
+
+SIZES = [  # S, L, V, ld, shift, k
+    (1, 1, 1, 1, 0, 1),
+    (2, 3, 2, 5, 1, 2),
+    (3, 2, 31, 31, 0, 31),
+    (1, 4, 32, 33, 3, 32),
+    (2, 2, 257, 257, 0, 32),
+    (3, 5, 1000, 1000, 0, 20),
+    (2, 3, 1001, 1003, 1, 8),
+    (2, 2, 2048, 2048, 0, 1),
+    (2, 2, 4095, 4097, 2, 32),
+    (3, 3, 8191, 8192, 0, 5),
+    (1, 1, 32000, 32000, 0, 20),
+    (5, 3, 32000, 32008, 0, 0),
+    (2, 5, 32001, 32001, 7, 32),
+    (1, 2, 131071, 131073, 1, 20),
+    (1, 1, 262147, 262147, 5, 32),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("mask", [None, "inf", "lowest"])
+@pytest.mark.parametrize("S,L,V,ld,shift,k", SIZES)
+def test_stats_parity(S, L, V, ld, shift, k, mask, dtype):
+    z, values, ids, lengths, _ = make(V + S, S, L, V, DTYPES[dtype], mask, ld=ld, shift=shift)
+    check_stats(run_stats(z, ids, lengths, S, L, k), values, ids, lengths, S, L, k)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 9, 18, 19, 37, 38, 75, 76, 77, 150, 151, 152, 153, 303, 305, 700, 1300])
+def test_stats_by_number_of_rows(rows):
+    """However many CTAs share a row."""
+    z, values, ids, _, _ = make(rows, rows, 1, 5003, torch.bfloat16)
+    check_stats(run_stats(z, ids, None, rows, 1, 7), values, ids, None, rows, 1, 7)
+
+
+@pytest.mark.parametrize("rows", [1, 40, 400])
+def test_top_of_rows_with_ties_and_clusters(rows):
+    """Equal values everywhere, ascending and descending rows, the best in one thread's slots only, more
+    equal candidates than are ranked at once, zeros of both signs."""
+    V, k = 40000, 32
+    base = np.zeros((rows, V))
+    i = np.arange(V)
+    kinds = [np.zeros(V), i * 2.0 ** -10, -i * 2.0 ** -10, np.where(i % 2 == 0, 0.0, -0.0), np.where(i % 7 == 3, 1.0, 0.0),
+             np.where((i // 8) % 256 == 17, 4.0, 0.0), np.where((i // 4) % 256 == 200, 4.0 + (i % 5), -1.0),
+             np.where((i // 8) % 2048 < 40, 1.0 + (i % 3), 0.0), np.where(i >= V - 3, 9.0, 2.0),
+             np.where((i // 4) % 512 < 33, 1.0 + i * 2.0 ** -12, 0.0)]
+    for n in range(rows):
+        base[n] = kinds[n % len(kinds)]
+    for dtype in (torch.float32, torch.bfloat16):
+        z, _ = rows_of(base, dtype, V + 3, 1)
+        o = {"top_ids": torch.full((rows, k), -7, dtype=torch.int32, device="cuda"),
+             "top_logp": torch.full((rows, k), float("nan"), device="cuda")}
+        H.hydra_token_logprobs_entropy(z, None, None, rows, 1, **o)
+        r = O.token_stats(host_f64(z), None, None, rows, 1, k)
+        assert np.array_equal(o["top_ids"].cpu().numpy(), r["top_ids"])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_stats_of_large_and_infinite_logits(dtype):
+    """Large magnitudes cancel exactly; NaN and +inf make the row NaN and come first among the top."""
+    V = 3001
+    rng = np.random.default_rng(3)
+    z = rng.normal(0, 1, (6, V))
+    z[0] += 30000.0
+    z[1] -= 30000.0
+    z[2, 100], z[2, 2000] = 1e38, 1e38
+    z[3] = -3e38
+    z[4, 77] = INF
+    z[5, 55], z[5, 99] = float("nan"), INF
+    dev, _ = rows_of(z, DTYPES[dtype])
+    values = host_f64(dev)
+    ids = rng.integers(0, V, 6)
+    o = run_stats(dev, ids, None, 6, 1, 4)
+    top = {k: v[:4] for k, v in o.items()}
+    check_stats(top, values[:4], ids[:4], None, 4, 1, 4)
+    for key in ("logp", "entropy"):
+        assert torch.isnan(o[key][4:]).all()
+    assert torch.isnan(o["norm"][4:, 1]).all() and torch.isnan(o["top_logp"][4:]).all()
+    assert o["top_ids"][4, 0] == 77 and o["top_ids"][5, :2].tolist() == [55, 99]
+
+
+def test_stats_outputs_one_by_one_and_dead_rows():
+    """Each output alone equals it among all; rows behind a sequence's end are not read (NaN there)."""
+    S, L, V, k = 3, 4, 5001, 6
+    z, values, ids, lengths, _ = make(11, S, L, V, torch.float32)
+    dead = np.arange(L)[None] >= lengths[:, None]
+    z[torch.from_numpy(dead.reshape(-1)).cuda()] = float("nan")
+    every = run_stats(z, ids, lengths, S, L, k)
+    assert not np.isnan(host_f64(every["logp"])).any()
+    for name in ("logp", "entropy", "norm"):
+        one = torch.full_like(every[name], float("nan"))
+        H.hydra_token_logprobs_entropy(z, dev_i32(ids) if name == "logp" else None, dev_i32(lengths), S, L, **{name: one})
+        plain = run_stats(z, ids, lengths, S, L, 0)[name]
+        assert torch.equal(one, plain)
+
+
+def test_stats_bad_id_and_bad_length_are_reported():
+    z, values, ids, _, _ = make(12, 2, 3, 2001, torch.bfloat16)
+    for bad in (-1, 2001, 1 << 30):
+        wrong = ids.copy()
+        wrong[1] = bad
+        o = run_stats(z, wrong, None, 2, 3, 2)
+        assert H.device_error(clear=True) == 0x201
+        assert np.isnan(host_f64(o["logp"])[1]) and not np.isnan(np.delete(host_f64(o["logp"]), 1)).any()
+    for bad, rows in ((-1, 0), (4, 3)):
+        o = run_stats(z, ids, np.array([3, bad]), 2, 3, 2)
+        assert H.device_error(clear=True) == 0x202
+        check_stats(o, values, ids, np.array([3, rows]), 2, 3, 2)
+
+
+# ---------------------------------------------------------------- gradient
+
+
+def run_grad(z, ids, lengths, S, L, norm, entropy, gl, gh, out_dtype, ld=None, shift=0, into=None):
+    d, buf = (into, None) if into is not None else rows_of(np.full((S * L, z.shape[1]), 7.0), out_dtype, ld, shift)
+    f = lambda a: None if a is None else dev_f32(a)  # noqa: E731
+    H.hydra_token_logprobs_entropy_grad(z, None if ids is None else dev_i32(ids),
+                                        None if lengths is None else dev_i32(lengths), S, L, f(norm), f(entropy), f(gl),
+                                        f(gh), d)
+    return d, buf
+
+
+def check_grad(d, z, ids, lengths, S, L, r, gl, gh, extra=0.0):
+    want = O.token_stats_grad(z, ids, lengths, S, L, gl, gh)
+    got = host_f64(d)
+    with np.errstate(invalid="ignore", over="ignore"):
+        lp = np.where(r["norm"][:, :1] > -INF, z - r["norm"][:, :1], -INF) - r["norm"][:, 1:]
+    p = np.exp(lp)
+    a = np.minimum(np.abs(lp), 256.0)
+    c, h = np.abs(r["norm"][:, 1:]), r["entropy"][:, None]
+    weight = (0 if gl is None else np.abs(gl)[:, None]) + (0 if gh is None else np.abs(gh)[:, None] * (a + h + 1))
+    half = torch.finfo(d.dtype).eps / 2
+    tol = p * weight * (U * (4 * a + c + 12) + extra) + half * (1 + 2.0 ** -6) * np.abs(want) + 4e-38 * (weight + 1)
+    if gl is not None:  # 1 - p of the drawn token moves as p does
+        rows = np.arange(len(want))
+        tol[rows, ids] += 4 * U * np.abs(gl)
+    if d.dtype == torch.bfloat16:
+        tol += 2.0 ** -133  # the smallest step
+    close(got, want, tol, "gradient")
+
+
+GRAD_SIZES = [  # S, L, V, ld, shift, ld_d, shift_d
+    (1, 1, 1, 1, 0, 1, 0),
+    (2, 3, 7, 9, 1, 9, 1),
+    (2, 2, 8, 8, 0, 8, 0),
+    (3, 7, 1001, 1001, 0, 1001, 0),
+    (3, 2, 1001, 1001, 3, 1005, 3),
+    (2, 2, 4096, 4096, 0, 4096, 0),
+    (2, 2, 4097, 4099, 1, 4099, 2),   # the two rows start apart on the 16-byte grid
+    (2, 3, 8195, 8200, 4, 8200, 4),
+    (1, 2, 32000, 32000, 0, 32000, 0),
+    (1, 1, 131073, 131073, 0, 131073, 5),
+]
+
+
+@pytest.mark.parametrize("types", ["f32/f32", "f32/bf16", "bf16/bf16", "bf16/f32"])
+@pytest.mark.parametrize("mask", [None, "inf", "lowest"])
+@pytest.mark.parametrize("S,L,V,ld,shift,ld_d,shift_d", GRAD_SIZES)
+def test_grad_parity(S, L, V, ld, shift, ld_d, shift_d, mask, types):
+    t_in, t_out = (DTYPES[x] for x in types.split("/"))
+    z, values, ids, lengths, _ = make(V + 3 * S, S, L, V, t_in, mask, ld=ld, shift=shift)
+    rng = np.random.default_rng(V)
+    gl, gh = (rng.normal(size=S * L).astype(np.float32) for _ in range(2))
+    r = O.token_stats(values, None, None, S, L)
+    for a, b in ((gl, gh), (gl, None), (None, gh)):
+        d, buf = run_grad(z, ids if a is not None else None, lengths, S, L, r["norm"], r["entropy"] if b is not None else None,
+                          a, b, t_out, ld_d, shift_d)
+        check_grad(d, values, ids, lengths, S, L, r, None if a is None else a.astype(float), None if b is None else b.astype(float))
+        outside = buf.clone()
+        outside[shift_d:shift_d + S * L * ld_d].view(S * L, ld_d)[:, :V] = float("nan")
+        assert torch.isnan(outside).all()  # nothing beyond the columns was written
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ld,shift", [(5000, 0), (5003, 1)])
+def test_grad_in_place_has_the_same_bits(dtype, ld, shift):
+    S, L, V = 3, 4, 5000
+    z, values, ids, lengths, _ = make(21, S, L, V, DTYPES[dtype], "inf", ld=ld, shift=shift)
+    gl, gh = np.linspace(-1, 1, S * L), np.full(S * L, -0.01)
+    r = O.token_stats(values, None, None, S, L)
+    d, _ = run_grad(z, ids, lengths, S, L, r["norm"], r["entropy"], gl, gh, DTYPES[dtype], ld, shift)
+    run_grad(z, ids, lengths, S, L, r["norm"], r["entropy"], gl, gh, None, into=z)
+    assert torch.equal(z, d)
+
+
+def test_grad_against_differences():
+    """The kernel's gradient against central differences of the oracle's loss: with steps of 1e-4
+    the differences are off by 1e-8 / 6 times a third derivative under 10, the kernel by fp32."""
+    S, L, V = 2, 2, 23
+    z, values, ids, _, _ = make(31, S, L, V, torch.float32, spread=1.0)
+    gl, gh = np.array([0.5, -1.0, 2.0, 0.1]), np.array([0.3, 0.2, -0.7, 1.0])
+    o = run_stats(z, ids, None, S, L, 0)
+    d, _ = run_grad(z, ids, None, S, L, host_f64(o["norm"]), host_f64(o["entropy"]), gl, gh, torch.float32)
+
+    def loss(y):
+        r = O.token_stats(y, ids, None, S, L)
+        return (gl * r["logp"] + gh * r["entropy"]).sum()
+
+    for i in range(S * L):
+        for v in range(V):
+            up, down = values.copy(), values.copy()
+            up[i, v] += 1e-4
+            down[i, v] -= 1e-4
+            assert abs((loss(up) - loss(down)) / 2e-4 - host_f64(d)[i, v]) <= 1e-6
+
+
+def test_grad_bad_id_writes_nan_and_is_reported():
+    z, values, ids, _, _ = make(12, 2, 3, 2001, torch.bfloat16)
+    ids[1] = 2001
+    r = O.token_stats(values, None, None, 2, 3)
+    d, _ = run_grad(z, ids, None, 2, 3, r["norm"], r["entropy"], np.ones(6), None, torch.float32)
+    assert H.device_error(clear=True) == 0x201
+    assert torch.isnan(d[1]).all() and not torch.isnan(d[[0, 2, 3, 4, 5]]).any()
+
+
+# ---------------------------------------------------------------- as they are used
+
+
+def _update(z, ids, lengths, S, L, o, g):
+    """Losses of the new log-probabilities and their gradient in the logits: the calls of one minibatch."""
+    H.hydra_token_logprobs_entropy(z, ids, lengths, S, L, o["logp"], o["entropy"], o["norm"])
+    H.hydra_ppo_loss(o["logp"].view(S, L), g["old"], g["adv"], g["ret"], g["val"], lengths, 0.2, False, o["gl"].view(S, L),
+                     o["gv"], o["stats"], o["ws"])
+    H.hydra_token_logprobs_entropy_grad(z, ids, lengths, S, L, o["norm"], o["entropy"], o["gl"], g["gh"], o["d"])
+
+
+def _update_state(S, L, V, dtype, seed=41):
+    z, values, ids, lengths, _ = make(seed, S, L, V, dtype)
+    rng = np.random.default_rng(seed)
+    f = lambda *s: dev_f32(rng.normal(size=s))  # noqa: E731
+    old = O.token_stats(values, ids, None, S, L)["logp"].reshape(S, L) + rng.normal(0, 0.1, (S, L))
+    g = {"old": dev_f32(old), "adv": f(S, L), "ret": f(S, L), "val": f(S, L), "gh": dev_f32(np.full(S * L, -0.01 / 30))}
+    nan = lambda *s, dtype=torch.float32: torch.full(s, float("nan"), dtype=dtype, device="cuda")  # noqa: E731
+    o = {"logp": nan(S * L), "entropy": nan(S * L), "norm": nan(S * L, 2), "gl": nan(S * L), "gv": nan(S, L),
+         "stats": nan(7, dtype=torch.float64), "d": nan(S * L, V, dtype=dtype),
+         "ws": torch.empty(H.ppo_workspace_size(), dtype=torch.uint8, device="cuda")}
+    return z, values, ids, lengths, o, g
+
+
+def test_minibatch_from_logits_to_their_gradient():
+    S, L, V = 4, 30, 4003
+    z, values, ids, lengths, o, g = _update_state(S, L, V, torch.float32)
+    _update(z, dev_i32(ids), dev_i32(lengths), S, L, o, g)
+    gl, gh = host_f64(o["gl"]), host_f64(g["gh"])
+    loss = O.ppo_loss(host_f64(o["logp"]).reshape(S, L), host_f64(g["old"]), host_f64(g["adv"]), host_f64(g["ret"]),
+                      host_f64(g["val"]), lengths)
+    np.testing.assert_allclose(gl.reshape(S, L), loss["grad_logp"], rtol=1e-5, atol=1e-6 * np.abs(loss["grad_logp"]).max())
+    check_grad(o["d"], values, ids, lengths, S, L, O.token_stats(values, None, None, S, L), gl, gh, extra=8 * tol_sum(V))
+
+
+def test_captured_graph_and_other_stream():
+    """The same calls captured and replayed over new logits, and on another stream, give the same bits."""
+    S, L, V = 3, 5, 33000
+    z, values, ids, lengths, o, g = _update_state(S, L, V, torch.bfloat16)
+    ids, lengths = dev_i32(ids), dev_i32(lengths)
+    _update(z, ids, lengths, S, L, o, g)
+    want = {k: o[k].clone() for k in ("logp", "entropy", "norm", "gl", "d")}
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        _update(z, ids, lengths, S, L, o, g)
+    keep = z.clone()
+    z.zero_()
+    graph.replay()
+    z.copy_(keep)
+    graph.replay()
+    assert all(torch.equal(o[k], want[k]) for k in want)
+    for k in want:
+        o[k].fill_(float("nan"))
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _update(z, ids, lengths, S, L, o, g)
+    side.synchronize()
+    assert all(torch.equal(o[k], want[k]) for k in want)
+
+
+def test_rows_far_into_a_large_buffer():
+    """Offsets beyond 2^31 elements: the last of three rows 1.2e9 elements apart."""
+    S, V, ld = 3, 1001, 1_200_000_001
+    buf = torch.empty(2 * ld + V, dtype=torch.bfloat16, device="cuda")
+    z = buf.as_strided((S, V), (ld, 1))
+    z.copy_(torch.randn(S, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)))
+    ids = np.array([0, 500, 1000])
+    o = run_stats(z, ids, None, S, 1, 5)
+    values = host_f64(z)
+    check_stats(o, values, ids, None, S, 1, 5)
+    r = O.token_stats(values, None, None, S, 1)
+    run_grad(z, ids, None, S, 1, r["norm"], r["entropy"], np.ones(S), np.ones(S), None, into=z)
+    check_grad(z, values, ids, None, S, 1, r, np.ones(S), np.ones(S))
