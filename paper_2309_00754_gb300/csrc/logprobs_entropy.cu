@@ -4,28 +4,43 @@
 // Forward, per row z of V logits, one pass with a running maximum (Milakov & Gimelshein 2018):
 //     m = max z,  s = sum exp(z - m),  w = sum exp(z - m) (z - m)
 //     logp = (z[id] - m) - log s,  entropy = log s - w / s
-// Both terms of the entropy are at least 0, so nothing cancels; keeping m and log s apart keeps
-// log-probabilities exact where |m| is large (a vocabulary masked with the type's lowest value).
+// Both terms of the entropy are at least 0; keeping m and log s apart keeps log-probabilities exact
+// where |m| is large (a vocabulary masked with the type's lowest value).
 //
-// The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps the
-// best of the slots (16-byte groups of logits) that it read. The k best elements of the row lie in
-// the k threads whose best come first in that order: an element of another thread has k better
-// ones before it. Those threads' slots alone are read again, and the few elements not behind the
-// k-th best thread's best are ranked by counting.
+// The rows come through a ring of 16 KB stages that one warp fills with bulk copies, rows ahead of the
+// eight warps that sum them: 256 threads with a maximum and two sums each, whose parts one warp puts
+// together. Four CTAs an SM take every 608th row. 2 % of the threads' time is waiting where the row is
+// fp32 (4096 x 32000: 76.5 us, all of the measured HBM rate); bf16 needs 8.4 instructions an element
+// (8192 x 32000: 83 us, 93 %). Few rows are shared by clusters, which meet in the first CTA's memory.
+//
+// The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps its best
+// value of each eighth of the row. A bound that k of the 256 threads reach holds for the k-th best element,
+// too; the eighths that reach it, about k, are read again, and the few elements not behind it are ranked by
+// counting. Three warps of a CTA do that, a row each, while the others are in the next rows, as it takes
+// 3 to 8 us, most of it one step waiting for the one before. Two such CTAs fit an SM (8192 x 32000 bf16,
+// k = 8: 103 us; in the summing threads themselves 130, with one such warp a CTA 160).
 //
 // Backward, with p = exp((z - m) - log s):
 //     dz[v] = g_logp (1[v = id] - p_v) - g_entropy p_v (log p_v + entropy)
+#include <algorithm>
+
 #include "common.cuh"
 #include "kernels.h"
 
 namespace hydra {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kCandidates = 512;  // elements ranked at once
+constexpr int kSummers = 256;  // threads of a CTA that sum a row; one more warp fetches it
+constexpr int kWarps = kSummers / 32;
+constexpr int kSlotsEach = 4;  // slots a thread takes of a stage
+constexpr int kStageSlots = kSummers * kSlotsEach;
+constexpr int kStages = 3;
+constexpr int kClusterMax = 8;
+constexpr int kEnders = 3;        // warps of a CTA that finish rows where tokens are selected
+constexpr int kSegments = 8;      // of a row's stages, with a best value of each thread
+constexpr int kCandidates = 252;  // elements ranked at once
 constexpr float kInf = __builtin_huge_valf(), kNan = __builtin_nanf("");
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // exp of anything below is 0 in fp32; a finite stand-in keeps 0 * (z - m) from being 0 * -inf
 constexpr float kFloor = -256.f;
 
@@ -34,10 +49,37 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-
-__device__ __forceinline__ float exp_fast(float x) {  // 2 ulp of ex2, x <= 0
+__device__ __forceinline__ uint32_t max_nan_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp
   float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x * kLog2e));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * kLog2e); }
+
+// two fp32 values an instruction
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
   return r;
 }
 
@@ -66,19 +108,17 @@ struct Row {
   }
   // index of a slot's first element (below 0 in the first slot)
   __device__ __forceinline__ int first(int j) const { return j * E - a; }
-  __device__ __forceinline__ uint4 load_full(int j) const {
-    return *reinterpret_cast<const uint4*>(p + first(j));
-  }
-  __device__ __forceinline__ void load(int j, float (&f)[E]) const {
-    if (j >= full_lo && j < full_hi) {
-      unpack(load_full(j), f);
-    } else {
+  __device__ __forceinline__ uint4 load_full(int j) const { return *reinterpret_cast<const uint4*>(p + first(j)); }
+  // a slot from memory, -inf in the places before and behind the row
+  __device__ __forceinline__ uint4 load(int j) const {
+    if (j >= full_lo && j < full_hi) return load_full(j);
+    alignas(16) T v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int i = first(j) + e;
-        f[e] = i >= 0 && i < V ? to_f(p[i]) : -kInf;
-      }
+    for (int e = 0; e < E; ++e) {
+      const int i = first(j) + e;
+      v[e] = i >= 0 && i < V ? p[i] : from_f<T>(-kInf);
     }
+    return *reinterpret_cast<uint4*>(v);
   }
   __device__ static __forceinline__ void unpack(const uint4& v, float (&f)[E]) {
     const uint32_t r[4] = {v.x, v.y, v.z, v.w};
@@ -87,10 +127,18 @@ struct Row {
       if constexpr (E == 4) {
         f[q] = __uint_as_float(r[q]);
       } else {
-        const float2 x = unpack_bf16x2(r[q]);
-        f[2 * q] = x.x;
-        f[2 * q + 1] = x.y;
+        f[2 * q] = __uint_as_float(r[q] << 16);
+        f[2 * q + 1] = __uint_as_float(r[q] & 0xffff0000u);
       }
+    }
+  }
+  __device__ static __forceinline__ float max_of(const uint4& v) {
+    if constexpr (E == 4) {
+      return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
+                     max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+    } else {
+      const uint32_t m = max_nan_bf16x2(max_nan_bf16x2(v.x, v.y), max_nan_bf16x2(v.z, v.w));
+      return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
   }
 };
@@ -110,35 +158,151 @@ __device__ __forceinline__ uint64_t rank_key(uint32_t key, int index) {
   return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(~index);
 }
 
-struct Stats {  // running maximum, sum of exp(z - m), sum of exp(z - m) (z - m)
-  float m = -kInf, s = 0.f, w = 0.f;
+__device__ __forceinline__ float warp_max_nan(float v) {
+  float r;
+  asm("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
 
-  // nm is the new maximum (NaN if there is a NaN)
-  __device__ __forceinline__ void rescale(float nm) {
-    const float d = max_nan(m - nm, kFloor);
-    const float c = exp_fast(d);
+// m = max z, s = sum 2^x, w = sum 2^x x with x = (z - m) log2 e, of parts of a row
+struct Stats {
+  float m, s, w;
+  // over the first `lanes` lanes of a warp, whose others hold (-inf, 0, 0); every one of them has the result
+  __device__ __forceinline__ void merge_lanes(int lanes) {
+    const float nm = warp_max_nan(m);
+    const float d = fmaxf(m - nm, kFloor) * kLog2e;  // -inf less -inf is NaN: the sums are 0
+    const float c = exp2_fast(d);
     w = c * (w + s * d);
     s *= c;
     m = nm;
+#pragma unroll
+    for (int off = lanes / 2; off > 0; off >>= 1) {
+      s += __shfl_xor_sync(0xffffffffu, s, off);
+      w += __shfl_xor_sync(0xffffffffu, w, off);
+    }
   }
-  __device__ __forceinline__ void merge(float m2, float s2, float w2) {
-    const float nm = max_nan(m, m2);
-    // both -inf: the difference is NaN, the sums 0
-    const float d1 = fmaxf(m - nm, kFloor), d2 = fmaxf(m2 - nm, kFloor);
-    const float c1 = exp_fast(d1), c2 = exp_fast(d2);
-    w = c1 * (w + s * d1) + c2 * (w2 + s2 * d2);
-    s = s * c1 + s2 * c2;
-    m = nm;
+};
+
+// A thread's running statistics. One fma gives x: z log2 e - ref with ref = m' log2 e rounded, m' a maximum of the
+// row so far that is not raised before another passes it by kAhead: a row has few stages, and one that has just
+// begun raises its maximum in nearly every one (for some lane of a warp). What ref is beside m log2 e, its rounding among
+// it, is taken out at the end (rebase).
+constexpr float kAhead = 8.f;  // of log2: sums of 2^8 times the terms, and 8 steps of 2^-24 in the entropy
+template <typename T>
+struct Running {
+  float m = -kInf;      // the maximum
+  float from = -kInf;   // m'
+  float limit = -kInf;  // above it m' is raised
+  bool huge = true;     // ref's rounding would not be small beside 1, or m' is -inf: (z - m') log2 e instead
+  uint64_t nref = 0;    // -ref twice; huge: -m', 0 for -inf
+  uint32_t low = 0;     // not huge: values below it (fp32, or bf16 twice) count as it, which is 0: 0 * x stays 0
+  uint64_t s = 0, w = 0;
+
+  __device__ __forceinline__ void raise(float nm) {  // m' to nm, NaN if there is a NaN
+    const bool h = fabsf(nm) >= 0x1p20f;
+    const float ref = h ? nm : nm * kLog2e;
+    const float d = max_nan(h || huge ? (from - nm) * kLog2e : -unpack2(nref).x - ref, kFloor * kLog2e);
+    const float c = exp2_fast(d);
+    w = fma2(s, pack2(d, d), w);
+    s = fma2(s, pack2(c, c), 0);
+    w = fma2(w, pack2(c, c), 0);
+    from = nm;
+    nref = pack2(-ref, -ref);
+    huge = h;
+    limit = h ? nm : nm + kAhead * kLn2;
+    const float l = nm + kFloor - 0x1p-6f * fabsf(nm);
+    low = sizeof(T) == 4 ? __float_as_uint(l) : pack_bf16x2(l, l);
+  }
+
+  __device__ __forceinline__ static float max_of(const uint32_t* r, int n) {  // of 4 n registers
+    if constexpr (sizeof(T) == 4) {
+      float x = __uint_as_float(r[0]);
+#pragma unroll
+      for (int i = 1; i < 4 * n; ++i) x = max_nan(x, __uint_as_float(r[i]));
+      return x;
+    } else {
+      uint32_t x = r[0];
+#pragma unroll
+      for (int i = 1; i < 4 * n; ++i) x = max_nan_bf16x2(x, r[i]);
+      return max_nan(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+    }
+  }
+
+  __device__ __forceinline__ void add_pair(uint64_t z2, uint64_t log2e) {
+    const uint64_t x2 = fma2(z2, log2e, nref);
+    const float2 x = unpack2(x2);
+    const uint64_t e2 = pack2(exp2_fast(x.x), exp2_fast(x.y));
+    s = add2(s, e2);
+    w = fma2(e2, x2, w);
+  }
+  // 4 n registers of values, whose largest is cm
+  template <int n>
+  __device__ __forceinline__ void add(const uint32_t* r, float cm, uint64_t log2e) {
+    if (!(cm <= limit)) raise(cm);
+    m = max_nan(m, cm);
+    if (!huge) {
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4 * n; i += 2)
+          add_pair(pack2(max_nan(__uint_as_float(r[i]), __uint_as_float(low)),
+                         max_nan(__uint_as_float(r[i + 1]), __uint_as_float(low))), log2e);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4 * n; ++i) {
+          const uint32_t c = max_nan_bf16x2(r[i], low);
+          add_pair(pack2(__uint_as_float(c << 16), __uint_as_float(c & 0xffff0000u)), log2e);
+        }
+      }
+    } else {
+      const float base = -unpack2(nref).x;
+#pragma unroll 1
+      for (int u = 0; u < n; ++u) {
+        float f[Row<T>::E];
+        uint4 v;
+        if constexpr (n == 1) {
+          v = make_uint4(r[0], r[1], r[2], r[3]);
+        } else {  // without indexing registers
+          v = make_uint4(0, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < n; ++i)
+            if (i == u) v = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+        }
+        Row<T>::unpack(v, f);
+#pragma unroll
+        for (int e = 0; e < Row<T>::E; e += 2) {
+          const float x0 = max_nan(f[e] - base, kFloor) * kLog2e, x1 = max_nan(f[e + 1] - base, kFloor) * kLog2e;
+          const uint64_t e2 = pack2(exp2_fast(x0), exp2_fast(x1));
+          s = add2(s, e2);
+          w = fma2(e2, pack2(x0, x1), w);
+        }
+      }
+    }
+  }
+  // the sums relative to m itself
+  __device__ __forceinline__ Stats rebase() const {
+    const float2 sp = unpack2(s), wp = unpack2(w);
+    Stats r{m, sp.x + sp.y, wp.x + wp.y};
+    if (!huge) {
+      const float d = fmaf(m, kLog2e, unpack2(nref).x);  // one rounding, of a number up to kAhead
+      const float c = exp2_fast(-d);
+      r.w = c * (r.w - r.s * d);
+      r.s *= c;
+    }
+    return r;
   }
 };
 
 __device__ __forceinline__ uint64_t shfl_xor64(uint64_t v, int mask) {
   return __shfl_xor_sync(0xffffffffu, static_cast<unsigned long long>(v), mask);
 }
+__device__ __forceinline__ uint32_t shfl(uint32_t v, int from) { return __shfl_sync(0xffffffffu, v, from); }
+__device__ __forceinline__ uint64_t shfl(uint64_t v, int from) {
+  return __shfl_sync(0xffffffffu, static_cast<unsigned long long>(v), from);
+}
 __device__ __forceinline__ uint64_t max64(uint64_t a, uint64_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint64_t min64(uint64_t a, uint64_t b) { return a < b ? a : b; }
 
-// Bitonic network over a warp, one key a lane, lane 0 the largest.
+// Bitonic networks over a warp, one key a lane, lane 0 the largest.
 __device__ __forceinline__ uint64_t bitonic_merge(uint64_t v, int lane) {
 #pragma unroll
   for (int j = 16; j > 0; j >>= 1) {
@@ -159,199 +323,623 @@ __device__ __forceinline__ uint64_t sort_warp(uint64_t v, int lane) {
   }
   return v;
 }
+// The same over 32-bit keys.
+__device__ __forceinline__ uint32_t bitonic_merge(uint32_t v, int lane) {
+#pragma unroll
+  for (int j = 16; j > 0; j >>= 1) {
+    const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
+    v = lane & j ? min(v, o) : max(v, o);
+  }
+  return v;
+}
+__device__ __forceinline__ uint32_t sort_warp(uint32_t v, int lane) {
+#pragma unroll
+  for (int size = 2; size <= 32; size <<= 1) {
+#pragma unroll
+    for (int j = size >> 1; j > 0; j >>= 1) {
+      const uint32_t o = __shfl_xor_sync(0xffffffffu, v, j);
+      v = ((lane & j) == 0) == ((lane & size) == 0) ? max(v, o) : min(v, o);
+    }
+  }
+  return v;
+}
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
+__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return max64(a, b); }
 
-struct TopShared {
-  uint64_t list[kWarps][32];
-  uint64_t cand[kCandidates];
-  uint64_t floor;  // elements behind it are not among the k best
-  int count;
+// A barrier of the summing threads.
+__device__ __forceinline__ void summers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSummers) : "memory"); }
+
+// A bound that at least k of 256 keys reach, or 0 where fewer than k are not 0: the k-th largest of the best of 64
+// groups of four. list[w] holds a key a lane.
+template <typename K>
+__device__ __forceinline__ K kth_bound(const K (*list)[32], int k, int lane) {
+  K a = 0, b = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps / 2; ++w) {
+    a = larger(a, list[w][lane]);
+    b = larger(b, list[w + kWarps / 2][lane]);
+  }
+  a = sort_warp(a, lane);
+  b = sort_warp(b, lane);
+  a = bitonic_merge(larger(a, static_cast<K>(shfl(b, 31 - lane))), lane);
+  return shfl(a, k - 1);
+}
+
+__device__ __forceinline__ void st_cluster_f32(const float* local, uint32_t rank, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_rank(smem_u32(local), rank)), "f"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster_u64(const uint64_t* local, uint32_t rank, uint64_t v) {
+  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(local), rank)), "l"(v) : "memory");
+}
+// [p, p + bytes) to shared memory at dst, all on 16-byte boundaries; its bytes arrive on `bar`
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* p, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "l"(reinterpret_cast<uint64_t>(p)), "r"(bytes), "r"(bar)
+               : "memory");
+}
+
+// What a stage holds: slots [j0, j0 + n) of a row; n < 0 ends the work.
+struct alignas(16) Stage {
+  unsigned row;
+  int j0, n_flags, id;
+};
+// beside n: the row's first and last stage in this CTA, the last of a segment, and which one
+constexpr int kFirst = 1 << 16, kLast = 1 << 17, kSegmentEnd = 1 << 18, kSegmentShift = 20;
+
+struct Shared {
+  unsigned char ring[kStages][kStageSlots * 16];
+  Stage stage[kStages];
+  uint64_t full[kStages], drained[kStages], others;
+  float red[kEnders][3][kWarps];
+  float cluster_stats[kClusterMax][3];
+  int abort_flag;
+};
+// What the summers leave of a row for one of the enders, and what that warp works with.
+struct End {
+  uint4 hit[128];                         // slots that hold candidates: G a lane
+  union alignas(16) {
+    uint64_t cand[kCandidates + 4];       // elements that may be among the best
+    uint64_t list[kWarps][32];            // before them: keys with slots
+  };
+  uint64_t best[32];                      // this CTA's k best elements
+  alignas(8) __nv_bfloat16 segment[kSegments][kSummers];  // each summer's best value of a segment, rounded up
+  uint32_t key[kWarps][32];               // order_key of its best value of all, 0 where it has none
+  int slot[kWarps][32];                   // and its first slot of the first stage that holds that
+  int hit_slot[128];
+  uint16_t asked[kSummers];               // summers that hold candidates
+  uint16_t owner[kSegments * 32];         // segments that do, of 32 of them
+  unsigned row;
+  int id;                                 // the row's token
+  bool end;                               // no row is left
+  uint64_t done, free;
+};
+struct SharedTop {
+  End end[kEnders];
+  // a cluster has one row, for the first ender: the other's segments hold what its CTAs send
+  __device__ __forceinline__ uint64_t* cluster_best(unsigned rank) {
+    return reinterpret_cast<uint64_t*>(end[1].segment) + rank * 32;
+  }
+};
+static_assert(kClusterMax * 32 * sizeof(uint64_t) <= sizeof(End::segment), "the keys of a cluster");
+static_assert(4 * (sizeof(Shared) + 1024) <= 228 * 1024 && 2 * (sizeof(Shared) + sizeof(SharedTop) + 1024) <= 228 * 1024,
+              "CTAs an SM");
+template <bool kTop>
+constexpr size_t shared_bytes() { return sizeof(Shared) + (kTop ? sizeof(SharedTop) : 0); }
+template <bool kTop>
+constexpr int block_threads() { return kSummers + 32 + (kTop ? kEnders * 32 : 0); }
+template <bool kTop>
+constexpr int ctas_per_sm() { return kTop ? 2 : 4; }
+
+// A row's slots in this CTA of a cluster of 1 << bits.
+struct Part {
+  int lo, hi;
+  __device__ __forceinline__ Part(int n_slots, unsigned rank, unsigned bits) {
+    lo = static_cast<int>(static_cast<unsigned>(n_slots) * static_cast<unsigned long long>(rank) >> bits);
+    hi = static_cast<int>(static_cast<unsigned>(n_slots) * static_cast<unsigned long long>(rank + 1) >> bits);
+  }
 };
 
-template <typename T, bool kTop>
-__global__ void __launch_bounds__(kThreads)
-    token_stats_kernel(const T* __restrict__ logits, long long ld, int L, int V,
-                       const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, int k,
-                       float* __restrict__ logp, float* __restrict__ entropy, float* __restrict__ norm,
-                       int32_t* __restrict__ top_ids, float* __restrict__ top_logp, int* err) {
-  constexpr int E = Row<T>::E;
-  constexpr int U = 4;
-  pdl_wait();
-  pdl_launch_dependents();
-  const long long row = blockIdx.x;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int sq = static_cast<int>(row / L);
-  const int t = static_cast<int>(row - static_cast<long long>(sq) * L);
-  int n = lengths ? lengths[sq] : L;
-  if (n < 0 || n > L) {
-    if (tid == 0) record_error(err, kDevBadLength);
-    n = n < 0 ? 0 : L;
-  }
-  if (t >= n) {
-    if (tid == 0) {
-      if (logp) logp[row] = 0.f;
-      if (entropy) entropy[row] = 0.f;
-      if (norm) norm[2 * row] = norm[2 * row + 1] = 0.f;
-    }
-    if (kTop && tid < k) {
-      top_ids[row * k + tid] = -1;
-      top_logp[row * k + tid] = 0.f;
-    }
-    return;
-  }
-  const Row<T> r(logits + row * ld, V);
-  Stats st;
-  uint32_t best = 0;
-  int best_slot = 0;
-  for (int j0 = tid; j0 < r.n_slots; j0 += U * kThreads) {
-    float f[U][E], vm[U];
-    const bool whole = j0 >= r.full_lo && j0 + (U - 1) * kThreads < r.full_hi;
+// Stages of a segment of a row's part.
+__device__ __forceinline__ int segment_stages(const Part& part) {
+  return ((part.hi - part.lo + kStageSlots - 1) / kStageSlots + kSegments - 1) / kSegments;
+}
+
+// The sum of v over the lanes below, and over all of them.
+__device__ __forceinline__ int scan(int v, int lane, int& total) {
+  int sum = v;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * kThreads;
-      if (whole) {
-        Row<T>::unpack(r.load_full(j), f[u]);
-      } else if (j < r.n_slots) {
-        r.load(j, f[u]);
+  for (int off = 1; off < 32; off <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, sum, off);
+    sum += lane >= off ? o : 0;
+  }
+  total = __shfl_sync(0xffffffffu, sum, 31);
+  return sum - v;
+}
+
+// The k best of the row's slots [part.lo, part.hi), best first, one a lane (0 behind the last). By one warp, whose
+// every step waits for the one before it: a vote or a branch for each of many things would cost more than
+// their loads (8 us a row instead of 3), so each lane works out what it adds and one scan places it.
+template <typename T>
+__device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Part& part, int k, int lane) {
+  constexpr int E = Row<T>::E, G = 4;
+  // Values alone first: every summer at or above the bound is asked, every element there is taken. With many equal
+  // values, or fewer summers or values than k, slots decide between equal ones.
+  uint32_t least = kth_bound(e.key, k, lane);
+  uint64_t slot_floor = 0, floor = static_cast<uint64_t>(least) << 32;
+  bool ties = least <= order_key(-kInf), ask = true;
+  const int stages = segment_stages(part), each = stages * kSlotsEach;
+  // a summer's slots of a segment by as many lanes, up to 32
+  const int bits = each <= 4 ? 2 : each <= 8 ? 3 : each <= 16 ? 4 : 5, at_once = 32 >> bits;
+  const int full_hi = min(part.hi, r.full_hi);
+  int asked = 0;
+  for (;;) {
+    if (ask) {
+      uint32_t is = 0;  // a bit for each warp's summer of this lane
+      if (!ties) {
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) is |= (e.key[w][lane] >= least ? 1u : 0u) << w;
       } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[u][e] = -kInf;
-      }
-    }
-    float cm = -kInf;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      vm[u] = f[u][0];
-#pragma unroll
-      for (int e = 1; e < E; ++e) vm[u] = max_nan(vm[u], f[u][e]);
-      cm = max_nan(cm, vm[u]);
-    }
-    if (!(cm <= st.m) || (kTop && best == 0)) {
-      if (kTop) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const uint32_t key = order_key(vm[u]);
-          if (key > best && j0 + u * kThreads < r.n_slots) {
-            best = key;
-            best_slot = j0 + u * kThreads;
-          }
+        uint64_t(*list)[32] = e.list;
+#pragma unroll 1
+        for (int w = 0; w < kWarps; ++w) {
+          const uint32_t key = e.key[w][lane];
+          int slot = e.slot[w][lane];
+          // the stage's first slot that holds it
+          for (int u = 1; key != 0 && u < kSlotsEach && order_key(Row<T>::max_of(r.load(slot))) != key; ++u) slot += kSummers;
+          list[w][lane] = key != 0 ? rank_key(key, slot) : 0;
         }
+        __syncwarp();
+        slot_floor = max64(1, kth_bound(list, k, lane));
+        least = static_cast<uint32_t>(slot_floor >> 32);
+        floor = 0;
+#pragma unroll 1
+        for (int w = 0; w < kWarps; ++w) is |= (list[w][lane] >= slot_floor ? 1u : 0u) << w;
       }
-      if (!(cm <= st.m)) st.rescale(max_nan(st.m, cm));
+      for (int at = scan(__popc(is), lane, asked); is != 0; is &= is - 1)
+        e.asked[at++] = static_cast<uint16_t>((__ffs(is) - 1) * 32 + lane);
+      __syncwarp();
+      ask = false;
     }
-    const float base = st.m == -kInf ? 0.f : st.m;
+    int found = 0;
+    for (int x0 = 0; x0 < asked; x0 += 32) {
+      // their segments that hold candidates: up to kSegments a lane
+      const int summer = x0 + lane < asked ? e.asked[x0 + lane] : 0;
+      uint32_t is = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+      for (int q = 0; q < kSegments; ++q)
+        if (part.lo + q * stages * kStageSlots + summer < part.hi) is |= (order_key(__bfloat162float(e.segment[q][summer])) >= least ? 1u : 0u) << q;
+      if (x0 + lane >= asked) is = 0;
+      int owners;
+      for (int at = scan(__popc(is), lane, owners); is != 0; is &= is - 1)
+        e.owner[at++] = static_cast<uint16_t>((__ffs(is) - 1) << 10 | summer);
+      __syncwarp();
+#pragma unroll 1
+      for (int i0 = 0; i0 < each; i0 += 1 << bits) {
+        const int i = i0 + (lane & ((1 << bits) - 1));
+#pragma unroll 1
+        for (int g0 = 0; g0 < owners; g0 += G * at_once) {
+          uint4 v[G];
+          int j[G];
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float d = max_nan(f[u][e] - base, kFloor);
-        const float x = exp_fast(d);
-        st.s += x;
-        st.w += x * d;
-      }
-    }
-  }
-
-  __shared__ float red[3][kWarps];
-  __shared__ float row_norm[2];
+          for (int g = 0; g < G; ++g) {
+            const int o = g0 + g * at_once + (lane >> bits);
+            j[g] = part.hi;
+            if (o < owners && i < each)
+              j[g] = part.lo + (e.owner[o] >> 10) * stages * kStageSlots + (e.owner[o] & 1023) + i * kSummers;
+            if (j[g] >= r.full_lo && j[g] < full_hi) v[g] = r.load_full(j[g]);
+          }
+          // the row's first and last slot, where it has them in part
+          bool in_part = false;
 #pragma unroll
-  for (int off = 16; off > 0; off >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, st.m, off), s2 = __shfl_xor_sync(0xffffffffu, st.s, off),
-                w2 = __shfl_xor_sync(0xffffffffu, st.w, off);
-    st.merge(m2, s2, w2);
-  }
-  if (lane == 0) {
-    red[0][warp] = st.m;
-    red[1][warp] = st.s;
-    red[2][warp] = st.w;
-  }
-  __shared__ TopShared top;
-  uint64_t mine = 0;
-  if (kTop) {
-    mine = sort_warp(best == 0 ? 0 : rank_key(best, best_slot), lane);
-    top.list[warp][lane] = mine;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    st = Stats();
-    for (int q = 0; q < kWarps; ++q) st.merge(red[0][q], red[1][q], red[2][q]);
-    const bool empty = st.m == -kInf;  // nothing but -inf
-    const float ls = empty ? 0.f : logf(st.s);
-    row_norm[0] = st.m;
-    row_norm[1] = ls;
-    if (norm) {
-      norm[2 * row] = st.m;
-      norm[2 * row + 1] = ls;
-    }
-    if (entropy) entropy[row] = empty ? 0.f : ls - st.w / st.s;
-    if (logp) {
-      const int id = ids[row];
-      if (id < 0 || id >= V) {
-        record_error(err, kDevBadTokenId);
-        logp[row] = kNan;
-      } else {
-        logp[row] = empty ? -kInf : (to_f(r.p[id]) - st.m) - ls;
-      }
-    }
-  }
-  if constexpr (kTop) {
-
-    // the 32 best of the threads' bests, in warp 0
-    for (int half = kWarps / 2; half > 0; half >>= 1) {
-      if (warp < half) {
-        mine = bitonic_merge(max64(mine, top.list[warp + half][31 - lane]), lane);
-        top.list[warp][lane] = mine;
-      }
-      __syncthreads();
-    }
-    const uint64_t slot_floor = top.list[0][k - 1];  // 0 where fewer threads than k hold anything
-    if (tid == 0) top.floor = 0;
-    for (;;) {
-      if (tid == 0) top.count = 0;
-      __syncthreads();
-      const uint64_t floor = top.floor;
-      for (int g = warp; g < k; g += kWarps) {
-        const uint64_t key = top.list[0][g];
-        if (key == 0) break;
-        const int owner = static_cast<int>(~static_cast<uint32_t>(key)) % kThreads;
-        for (int j = owner + lane * kThreads; j < r.n_slots; j += 32 * kThreads) {
-          float f[E];
-          r.load(j, f);
-  #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int i = r.first(j) + e;
-            const uint32_t key_e = order_key(f[e]);
-            if (i >= 0 && i < V && rank_key(key_e, j) >= slot_floor && rank_key(key_e, i) >= floor) {
-              const int at = atomicAdd(&top.count, 1);
-              if (at < kCandidates) top.cand[at] = rank_key(key_e, i);
+          for (int g = 0; g < G; ++g) in_part |= j[g] < part.hi && (j[g] < r.full_lo || j[g] >= full_hi);
+          if (__any_sync(0xffffffffu, in_part)) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+              if (j[g] < part.hi && (j[g] < r.full_lo || j[g] >= full_hi)) v[g] = r.load(j[g]);
+          }
+          // the slots that hold some, in a row; then their elements, a slot a lane
+          int hits = 0;
+#pragma unroll
+          for (int g = 0; g < G; ++g)
+            if (j[g] >= part.hi || order_key(Row<T>::max_of(v[g])) < least) j[g] = -1; else ++hits;
+          int slots;
+          int at = scan(hits, lane, slots);
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            if (j[g] < 0) continue;
+            e.hit[at] = v[g];
+            e.hit_slot[at++] = j[g];
+          }
+          __syncwarp();
+          for (int h0 = 0; h0 < slots; h0 += 32) {
+            const bool holds = h0 + lane < slots;
+            const int slot = holds ? e.hit_slot[h0 + lane] : 0;
+            const uint4 x = holds ? e.hit[h0 + lane] : make_uint4(0, 0, 0, 0);
+            float f[E];
+            Row<T>::unpack(x, f);
+            uint32_t mask = 0;
+            if (holds) {
+              const int first = r.first(slot);
+              if (!ties) {
+#pragma unroll
+                for (int q = 0; q < E; ++q) mask |= (order_key(f[q]) >= least ? 1u : 0u) << q;
+              } else {
+#pragma unroll
+                for (int q = 0; q < E; ++q) {
+                  const uint32_t key = order_key(f[q]);
+                  mask |= (rank_key(key, slot) >= slot_floor && rank_key(key, first + q) >= floor ? 1u : 0u) << q;
+                }
+              }
+              if (first < 0) mask &= ~0u << -first;
+              if (first + E > r.V) mask &= (1u << (r.V - first)) - 1;
+            }
+            int more;
+            int c = found + scan(__popc(mask), lane, more);
+            found += more;
+            for (; mask != 0; mask &= mask - 1, ++c) {
+              const int q = __ffs(mask) - 1;
+              if (c < kCandidates)
+                e.cand[c] = rank_key(order_key(to_f(reinterpret_cast<const T*>(&e.hit[h0 + lane])[q])), r.first(slot) + q);
             }
           }
+          __syncwarp();
         }
       }
-      __syncthreads();
-      const int count = top.count, held = min(count, kCandidates);
-      for (int c = tid; c < held; c += kThreads) {
-        const uint64_t key = top.cand[c];
-        int rank = 0;
-        for (int o = 0; o < held; ++o) rank += top.cand[o] > key;
-        if (count > kCandidates) {
-          // more than fit: the k-th best of those held is a higher floor, which leaves out the rest
-          if (rank == k - 1) top.floor = key;
-        } else if (rank < k) {
-          const float v = order_value(static_cast<uint32_t>(key >> 32));
-          const float m = row_norm[0];
-          top_ids[row * k + rank] = static_cast<int>(~static_cast<uint32_t>(key));
-          top_logp[row * k + rank] = m == -kInf ? -kInf : (v - m) - row_norm[1];
-        }
+    }
+    const int held = min(found, kCandidates);
+    if (lane < 4) e.cand[held + lane] = 0;
+    e.best[lane] = 0;
+    __syncwarp();
+    uint64_t raise = 0;
+    for (int c = lane; c < held; c += 32) {
+      const uint64_t mine = e.cand[c];
+      int place = 0;
+#pragma unroll 2
+      for (int o = 0; o < held; o += 4) {
+        const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(&e.cand[o]),
+                         y = *reinterpret_cast<const ulonglong2*>(&e.cand[o + 2]);
+        place += (x.x > mine) + (x.y > mine) + (y.x > mine) + (y.y > mine);
       }
-      if (count <= kCandidates) return;
-      __syncthreads();
+      if (place < k) e.best[place] = mine;
+      if (place == k - 1) raise = mine;
+    }
+    __syncwarp();
+    if (found <= kCandidates) return e.best[lane];
+    // more than fit: the k-th best of those held is a higher floor, which leaves out the rest
+    if (ties) {
+      const uint32_t who = __ballot_sync(0xffffffffu, raise != 0);
+      floor = shfl(raise, __ffs(who) - 1);
+    } else {
+      ask = ties = true;
     }
   }
 }
 
+// What a call gives for a row.
+struct Outputs {
+  float* logp;
+  float* entropy;
+  float* norm;
+  int32_t* top_ids;
+  float* top_logp;
+  int k;
+
+  __device__ __forceinline__ void dead(unsigned row) const {
+    if (logp) logp[row] = 0.f;
+    if (entropy) entropy[row] = 0.f;
+    if (norm) norm[2ll * row] = norm[2ll * row + 1] = 0.f;
+    for (int x = 0; x < k; ++x) {
+      top_ids[static_cast<long long>(row) * k + x] = -1;
+      top_logp[static_cast<long long>(row) * k + x] = 0.f;
+    }
+  }
+  // by a warp; st.m in every lane, the rest in lane 0, `top` one of the best a lane
+  template <bool kTop>
+  __device__ __forceinline__ void live(unsigned row, const Stats& st, float z_id, uint64_t top, int lane) const {
+    const float m = st.m, sum = __shfl_sync(0xffffffffu, st.s, 0);
+    const bool empty = m == -kInf;  // nothing but -inf
+    const float ls = empty ? 0.f : logf(sum);
+    if (lane == 0) {
+      if (norm) {
+        norm[2ll * row] = m;
+        norm[2ll * row + 1] = ls;
+      }
+      if (entropy) entropy[row] = empty ? 0.f : ls - kLn2 * (st.w / sum);
+      if (logp) logp[row] = empty && z_id == z_id ? -kInf : (z_id - m) - ls;
+    }
+    if (kTop && lane < k) {
+      const float x = order_value(static_cast<uint32_t>(top >> 32));
+      top_ids[static_cast<long long>(row) * k + lane] = static_cast<int>(~static_cast<uint32_t>(top));
+      top_logp[static_cast<long long>(row) * k + lane] = empty ? -kInf : (x - m) - ls;
+    }
+  }
+};
+
+// A CTA's part of a row, by a warp: written out, or in a cluster sent to its first CTA, which writes the whole.
+template <bool kTop>
+__device__ __forceinline__ void finish(Shared& sh, SharedTop& top, const Outputs& out, unsigned row, Stats st, float z_id,
+                                       uint64_t best, unsigned rank, unsigned cs, int lane, int* err) {
+  if (cs > 1) {
+    if (rank != 0) {
+      if (lane == 0) {
+        st_cluster_f32(&sh.cluster_stats[rank][0], 0, st.m);
+        st_cluster_f32(&sh.cluster_stats[rank][1], 0, st.s);
+        st_cluster_f32(&sh.cluster_stats[rank][2], 0, st.w);
+      }
+      if constexpr (kTop) st_cluster_u64(top.cluster_best(rank) + lane, 0, best);
+      asm volatile("fence.acq_rel.cluster;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.others), 0));
+      return;
+    }
+    if (!warp_wait_cluster_bounded(smem_u32(&sh.others), 0, &sh.abort_flag, err, kDevTimeoutEpilogue)) st.m = kNan;
+    if (lane > 0) {
+      st = Stats{-kInf, 0.f, 0.f};
+      if (lane < static_cast<int>(cs)) st = Stats{sh.cluster_stats[lane][0], sh.cluster_stats[lane][1], sh.cluster_stats[lane][2]};
+    }
+    st.merge_lanes(kClusterMax);
+    if constexpr (kTop) {
+      uint64_t list[kClusterMax] = {best};
+#pragma unroll
+      for (int c = 1; c < kClusterMax; ++c) list[c] = c < static_cast<int>(cs) ? top.cluster_best(c)[c % 2 ? 31 - lane : lane] : 0;
+#pragma unroll
+      for (int half = kClusterMax / 2; half > 0; half >>= 1) {
+#pragma unroll
+        for (int c = 0; c < half; ++c) {
+          // the second of a pair backwards
+          list[c] = bitonic_merge(max64(list[2 * c], list[2 * c + 1]), lane);
+          if (half > 1 && c % 2) list[c] = shfl(list[c], 31 - lane);
+        }
+      }
+      best = list[0];
+    }
+  }
+  out.live<kTop>(row, st, z_id, best, lane);
+}
+
+// Clusters of one CTA take every gridDim.x-th row in turn, larger ones one row that their CTAs share. The last
+// warp of a CTA fetches the slots of its rows, stage by stage, and the others sum them.
+template <typename T, bool kTop>
+__global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
+    token_stats_kernel(const T* __restrict__ logits, long long ld, unsigned rows, unsigned L, int V,
+                       const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, unsigned bits,
+                       const Outputs out, int* err) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  Shared& sh = *reinterpret_cast<Shared*>(raw);
+  SharedTop& top = *reinterpret_cast<SharedTop*>(raw + sizeof(Shared));  // with kTop
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const unsigned cs = 1u << bits, rank = bits > 0 ? cluster_rank() : 0;
+  if (tid == 0) {
+    for (int q = 0; q < kStages; ++q) {
+      mbar_init(smem_u32(&sh.full[q]), 1);
+      mbar_init(smem_u32(&sh.drained[q]), kWarps);
+    }
+    mbar_init(smem_u32(&sh.others), cs > 1 ? cs - 1 : 1);
+    if constexpr (kTop)
+      for (int f = 0; f < kEnders; ++f) {
+        mbar_init(smem_u32(&top.end[f].done), kWarps);
+        mbar_init(smem_u32(&top.end[f].free), 1);
+      }
+    sh.abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (cs > 1) cluster_sync_all(); else __syncthreads();
+  pdl_wait();
+  pdl_launch_dependents();
+
+  if (warp == kWarps) {
+    // ------------------------------------------------------------------ fetch
+    const unsigned step = gridDim.x >> bits;
+    int q = 0;
+    uint32_t parity = 1;  // of a stage's last release; none in the first round
+    bool wrapped = false;
+    auto acquire = [&]() {
+      return !wrapped || warp_wait_bounded(smem_u32(&sh.drained[q]), parity, &sh.abort_flag, err, kDevTimeoutProducer);
+    };
+    auto advance = [&]() {
+      __syncwarp();
+      if (++q == kStages) {
+        q = 0;
+        parity ^= 1;
+        wrapped = true;
+      }
+    };
+    // 32 of the rows at a time, one a lane: whether it holds a token, and which
+    for (unsigned long long base = blockIdx.x >> bits; base < rows; base += 32ull * step) {
+      const unsigned long long mine = base + static_cast<unsigned long long>(lane) * step;
+      bool live = mine < rows;
+      int id = 0;
+      if (live) {
+        const unsigned row = static_cast<unsigned>(mine);
+        if (out.logp) id = ids[row];
+        if (lengths != nullptr) {
+          const unsigned sq = row / L, t = row - sq * L;
+          const int n = lengths[sq];
+          if ((n < 0 || n > static_cast<int>(L)) && rank == 0) record_error(err, kDevBadLength);
+          live = n > static_cast<int>(L) || static_cast<int>(t) < n;
+        }
+        if (!live && rank == 0) out.dead(row);
+      }
+      for (uint32_t todo = __ballot_sync(0xffffffffu, live); todo != 0; todo &= todo - 1) {
+        const int l = __ffs(todo) - 1;
+        const unsigned row = static_cast<unsigned>(base + static_cast<unsigned long long>(l) * step);
+        const int row_id = __shfl_sync(0xffffffffu, id, l);
+        const Row<T> r(logits + row * ld, V);
+        const Part part(r.n_slots, rank, bits);
+        int j0 = part.lo, segment = 0, left = segment_stages(part);
+        do {  // a part without slots has a stage, too
+          if (!acquire()) return;
+          if (lane == 0) {
+            const int j1 = min(j0 + kStageSlots, part.hi), lo = max(j0, r.full_lo), hi = min(j1, r.full_hi);
+            unsigned char* dst = sh.ring[q];
+            // the row's first and last slot, where it has them in part
+            if (j0 < min(lo, j1)) *reinterpret_cast<uint4*>(dst) = r.load(j0);
+            if (hi < j1 && j1 > lo) *reinterpret_cast<uint4*>(dst + (j1 - 1 - j0) * 16) = r.load(j1 - 1);
+            sh.stage[q] = Stage{row, j0,
+                                (j1 - j0) | (j0 == part.lo ? kFirst : 0) | (j1 == part.hi ? kLast : 0) |
+                                    (left <= 1 || j1 == part.hi ? kSegmentEnd : 0) | segment << kSegmentShift,
+                                row_id};
+            const uint32_t bytes = hi > lo ? static_cast<uint32_t>(hi - lo) * 16 : 0;
+            mbar_arrive_expect_tx(smem_u32(&sh.full[q]), bytes);
+            if (bytes > 0) bulk_load(smem_u32(dst + (lo - j0) * 16), r.p + r.first(lo), bytes, smem_u32(&sh.full[q]));
+          }
+          advance();
+          j0 += kStageSlots;
+          if (--left == 0) {
+            left = segment_stages(part);
+            ++segment;
+          }
+        } while (j0 < part.hi);
+      }
+    }
+    if (!acquire()) return;
+    if (lane == 0) {
+      sh.stage[q] = Stage{0, 0, -1, 0};
+      mbar_arrive(smem_u32(&sh.full[q]));
+    }
+    return;
+  }
+
+  if (kTop && warp > kWarps) {
+    // ------------------------------------------------------------------ ends of rows
+    const int f = warp - kWarps - 1;
+    End& e = top.end[f];
+    for (uint32_t parity = 0;; parity ^= 1) {
+      if (!warp_wait_bounded(smem_u32(&e.done), parity, &sh.abort_flag, err, kDevTimeoutEpilogue) || e.end) return;
+      const unsigned row = e.row;
+      const Row<T> r(logits + row * ld, V);
+      float z_id = kNan;
+      if (lane == 0 && rank == 0 && out.logp) {
+        if (e.id < 0 || e.id >= V) record_error(err, kDevBadTokenId); else z_id = to_f(r.p[e.id]);
+      }
+      Stats st = lane < kWarps ? Stats{sh.red[f][0][lane], sh.red[f][1][lane], sh.red[f][2][lane]} : Stats{-kInf, 0.f, 0.f};
+      st.merge_lanes(32);
+      const uint64_t best = select_top<T>(e, r, Part(r.n_slots, rank, bits), out.k, lane);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&e.free));
+      finish<kTop>(sh, top, out, row, st, z_id, best, rank, cs, lane, err);
+    }
+  }
+
+  // -------------------------------------------------------------------- sums
+  int q = 0, buf = 0;
+  uint32_t parity = 0, used = 0;  // used: bit 0 of how often both buffers were filled, bit 1 whether they were
+  float z_id = 0.f;
+  uint64_t log2e;  // twice; kept, as it is not built again for every pair
+  asm volatile("mov.b64 %0, {%1, %1};" : "=l"(log2e) : "f"(kLog2e));
+  Running<T> run;
+  int best_slot = 0;       // the thread's first slot of the first stage that holds its maximum
+  float segment = -kInf;  // its maximum of the segment so far
+  for (;;) {
+    if (!mbar_wait_bounded(smem_u32(&sh.full[q]), parity, &sh.abort_flag, err, kDevTimeoutEpilogue)) return;
+    const Stage in = sh.stage[q];
+    if (in.n_flags < 0) break;
+    const int n = in.n_flags & (kFirst - 1), j = in.j0 + tid;
+    if (in.n_flags & kFirst) {
+      run = Running<T>();
+      best_slot = j;
+      if (kTop && (used & 2) && !warp_wait_bounded(smem_u32(&top.end[buf].free), used & 1, &sh.abort_flag, err, kDevTimeoutDrain))
+        return;
+      if (!kTop && tid == 0 && rank == 0 && out.logp) {
+        z_id = kNan;
+        if (in.id < 0 || in.id >= V) record_error(err, kDevBadTokenId); else z_id = to_f(logits[in.row * ld + in.id]);
+      }
+    }
+    const uint4* src = reinterpret_cast<const uint4*>(sh.ring[q]) + tid;
+    float cm = -kInf;
+    const float before = run.m;
+    if (n == kStageSlots) {
+      uint32_t v[4 * kSlotsEach];
+#pragma unroll
+      for (int u = 0; u < kSlotsEach; ++u) {
+        const uint4 x = src[u * kSummers];
+        v[4 * u] = x.x;
+        v[4 * u + 1] = x.y;
+        v[4 * u + 2] = x.z;
+        v[4 * u + 3] = x.w;
+      }
+      cm = run.max_of(v, kSlotsEach);
+      run.template add<kSlotsEach>(v, cm, log2e);
+    } else {
+#pragma unroll 1
+      for (int u = 0; tid + u * kSummers < n; ++u) {
+        const uint4 x = src[u * kSummers];
+        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+        const float slot_max = run.max_of(v, 1);
+        run.template add<1>(v, slot_max, log2e);
+        cm = max_nan(cm, slot_max);
+      }
+    }
+    if (kTop && !(cm <= before) && before == before) best_slot = j;
+    if constexpr (kTop) {
+      segment = max_nan(segment, cm);
+      if (in.n_flags & kSegmentEnd) {
+        top.end[buf].segment[in.n_flags >> kSegmentShift][tid] = __float2bfloat16_ru(segment);
+        segment = -kInf;
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&sh.drained[q]));
+    if (++q == kStages) {
+      q = 0;
+      parity ^= 1;
+    }
+    if (!(in.n_flags & kLast)) continue;
+
+    Stats st = run.rebase();
+    const float value = run.m;
+    st.merge_lanes(32);
+    if constexpr (kTop) {
+      End& e = top.end[buf];
+      // a summer without slots: its first slot would be behind the part's end, which is where the last stage ends
+      e.key[warp][lane] = best_slot < in.j0 + n ? order_key(value) : 0;
+      e.slot[warp][lane] = best_slot;
+      if (tid == 0) {
+        e.row = in.row;
+        e.id = in.id;
+        e.end = false;
+      }
+    }
+    if (lane == 0) {
+      sh.red[buf][0][warp] = st.m;
+      sh.red[buf][1][warp] = st.s;
+      sh.red[buf][2][warp] = st.w;
+    }
+    if constexpr (kTop) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&top.end[buf].done));
+    } else {
+      summers_sync();
+      if (warp == 0) {
+        st = lane < kWarps ? Stats{sh.red[buf][0][lane], sh.red[buf][1][lane], sh.red[buf][2][lane]} : Stats{-kInf, 0.f, 0.f};
+        st.merge_lanes(32);
+        finish<kTop>(sh, top, out, in.row, st, z_id, 0, rank, cs, lane, err);
+      }
+    }
+    if (++buf == kEnders) {
+      buf = 0;
+      used = used == 0 ? 2 : used ^ 1;
+    }
+  }
+  if constexpr (kTop) {
+    for (int f = 0; f < kEnders; ++f) {  // the enders may go
+      End& e = top.end[buf];
+      if ((used & 2) && !warp_wait_bounded(smem_u32(&e.free), used & 1, &sh.abort_flag, err, kDevTimeoutDrain)) return;
+      if (tid == 0) e.end = true;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&e.done));
+      if (++buf == kEnders) {
+        buf = 0;
+        used = used == 0 ? 2 : used ^ 1;
+      }
+    }
+  }
+}
+
+constexpr int kGradThreads = 256;
 constexpr int kUnit = 8;      // elements a thread turns at once
 constexpr int kUnitsEach = 2;
-constexpr int kTile = kThreads * kUnit * kUnitsEach;
+constexpr int kTile = kGradThreads * kUnit * kUnitsEach;
 
 template <typename T>
 __device__ __forceinline__ void load_unit(const T* p, float (&f)[kUnit]) {
@@ -376,7 +964,7 @@ __device__ __forceinline__ void store_unit(__nv_bfloat16* p, const float (&f)[kU
 // One CTA per tile of a row. Units lie on the 16-byte grid of both arrays where their rows start
 // alike on it (`a` elements before the row); else every element goes by itself.
 template <typename TI, typename TO>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kGradThreads)
     token_stats_grad_kernel(const TI* logits, long long ld, int L, int V, int tiles,
                             const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths,
                             const float* __restrict__ norm, const float* __restrict__ entropy,
@@ -427,7 +1015,7 @@ __global__ void __launch_bounds__(kThreads)
   if (together) {
 #pragma unroll
     for (int u = 0; u < kUnitsEach; ++u) {
-      const long long i0 = static_cast<long long>(tile) * kTile + (u * kThreads + tid) * kUnit - a;
+      const long long i0 = static_cast<long long>(tile) * kTile + (u * kGradThreads + tid) * kUnit - a;
       if (i0 >= V) return;
       const int i = static_cast<int>(i0);
       if (i >= 0 && i0 + kUnit <= V) {
@@ -446,18 +1034,83 @@ __global__ void __launch_bounds__(kThreads)
   } else {
     const long long i0 = static_cast<long long>(tile) * kTile - a;
     const int hi = static_cast<int>(min(i0 + kTile, static_cast<long long>(V)));
-    for (int i = static_cast<int>(max(i0, 0LL)) + tid; i < hi; i += kThreads)
+    for (int i = static_cast<int>(max(i0, 0LL)) + tid; i < hi; i += kGradThreads)
       d[i] = from_f<TO>(live ? value(to_f(z[i]), i) : 0.f);
   }
 }
 
-template <typename T>
+template <typename T, bool kTop>
+cudaLaunchConfig_t stats_config(unsigned clusters, int cs, cudaStream_t stream, cudaLaunchAttribute (&attr)[2]) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(clusters * static_cast<unsigned>(cs));
+  cfg.blockDim = dim3(block_threads<kTop>());
+  cfg.dynamicSmemBytes = shared_bytes<kTop>();
+  cfg.stream = stream;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(cs);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cfg;
+}
+
+// Clusters of 1 << bits CTAs that the device holds at once (0: none, or it does not say, which is not kept).
+template <typename T, bool kTop>
+int clusters_held(int dev, int bits) {
+  static int held[64][4];  // and one more
+  int& h = held[dev][bits];
+  if (h > 0) return h - 1;
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = stats_config<T, kTop>(1, 1 << bits, nullptr, attr);
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, token_stats_kernel<T, kTop>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  h = n + 1;
+  return n;
+}
+
+// How many CTAs share a row (as a power of two): the most of which the device holds a cluster for every row,
+// where a row is long enough. A cluster costs 0.6 us (1.3 where tokens are selected, whose lists are merged), and
+// one CTA reads 128 KB in about 2. Of eight / four / two / one CTAs, us in a graph: 1 x 32000 fp32 3.9 / 4.3 /
+// 5.1 / 5.8, 64 x 128001 bf16 8.4 / 8.2 / 8.9 / 12.4, 1 x 8000 fp32 3.5 / 3.7 / 3.9 / 3.4; with eight tokens 32 x
+// 32000 bf16 9.1 / 7.9 / 8.4 / 7.6, 19 x 128001 bf16 9.6 / 10.3 / 12.3 / 14.6, 64 x 128001 20.8 / 11.9 / 12.8 / 14.9.
+template <typename T, bool kTop>
+int cluster_bits(int64_t rows, int64_t V, int dev) {
+  for (int bits = 3; bits > 0; --bits) {
+    const int64_t least = 48 * 1024 * (kTop ? kClusterMax >> bits : 1);
+    if (V * static_cast<int64_t>(sizeof(T)) >= least && rows <= clusters_held<T, kTop>(dev, bits)) return bits;
+  }
+  return 0;
+}
+
+template <typename T, bool kTop>
 int launch_stats(const TokenStatsArgs& a, cudaStream_t stream) {
-  const auto kernel = a.top_k > 0 ? token_stats_kernel<T, true> : token_stats_kernel<T, false>;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(a.S * a.L)), dim3(kThreads), 0, stream,
-                    static_cast<const T*>(a.logits), static_cast<long long>(a.ld), static_cast<int>(a.L),
-                    static_cast<int>(a.V), a.ids, a.lengths, static_cast<int>(a.top_k), a.logp, a.entropy,
-                    a.norm, a.top_ids, a.top_logp, a.err) == cudaSuccess
+  static bool attr_set[64] = {false};  // the shared-memory limit is a per-device attribute
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(token_stats_kernel<T, kTop>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(shared_bytes<kTop>())) != cudaSuccess)
+      return -1;
+    attr_set[dev] = true;
+  }
+  const int64_t rows = a.S * a.L;
+  const int bits = cluster_bits<T, kTop>(rows, a.V, dev);
+  const int64_t resident = static_cast<int64_t>(ctas_per_sm<kTop>()) * std::max(1, sm_count());
+  cudaLaunchAttribute attr[2];
+  const cudaLaunchConfig_t cfg =
+      stats_config<T, kTop>(static_cast<unsigned>(bits > 0 ? rows : std::min(rows, resident)), 1 << bits, stream, attr);
+  return cudaLaunchKernelEx(&cfg, token_stats_kernel<T, kTop>, static_cast<const T*>(a.logits),
+                            static_cast<long long>(a.ld), static_cast<unsigned>(rows), static_cast<unsigned>(a.L),
+                            static_cast<int>(a.V), a.ids, a.lengths, static_cast<unsigned>(bits),
+                            Outputs{a.logp, a.entropy, a.norm, a.top_ids, a.top_logp, static_cast<int>(a.top_k)},
+                            a.err) == cudaSuccess
              ? 0
              : -3;
 }
@@ -466,7 +1119,7 @@ template <typename TI, typename TO>
 int launch_grad(const TokenStatsGradArgs& a, cudaStream_t stream) {
   const int64_t tiles = token_stats_grad_tiles(a.V);
   return launch_pdl(token_stats_grad_kernel<TI, TO>, dim3(static_cast<unsigned>(a.S * a.L * tiles)),
-                    dim3(kThreads), 0, stream, static_cast<const TI*>(a.logits), static_cast<long long>(a.ld),
+                    dim3(kGradThreads), 0, stream, static_cast<const TI*>(a.logits), static_cast<long long>(a.ld),
                     static_cast<int>(a.L), static_cast<int>(a.V), static_cast<int>(tiles), a.ids, a.lengths,
                     a.norm, a.entropy, a.grad_logp, a.grad_entropy, static_cast<TO*>(a.dlogits),
                     static_cast<long long>(a.ld_d), a.err) == cudaSuccess
@@ -477,7 +1130,8 @@ int launch_grad(const TokenStatsGradArgs& a, cudaStream_t stream) {
 }  // namespace
 
 int launch_token_stats(const TokenStatsArgs& a, cudaStream_t stream) {
-  return a.bf16 ? launch_stats<__nv_bfloat16>(a, stream) : launch_stats<float>(a, stream);
+  if (a.top_k > 0) return a.bf16 ? launch_stats<__nv_bfloat16, true>(a, stream) : launch_stats<float, true>(a, stream);
+  return a.bf16 ? launch_stats<__nv_bfloat16, false>(a, stream) : launch_stats<float, false>(a, stream);
 }
 
 // the row's first unit may start up to kUnit - 1 elements before it

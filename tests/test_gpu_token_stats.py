@@ -7,7 +7,9 @@ the difference, so |z - m| u of the term, and p |log p| adds up to the entropy, 
 of its product with log2 e (the same again) and of ex2 (2 ulp = 4 u): the sum is off by at most
     tol_s = (V / 128 + 32 + 2 * 19 + 8) u  relative,
     logp   (z_id - m) - c:  tol_s + 2 u (|z_id - m| + |c|) + u |logp|
-    entropy c - w / s:      tol_s + (2 tol_s + 4 u) entropy + 2 u |c|
+    entropy c - w / s:      tol_s + (2 tol_s + 4 u) entropy + 2 u |c|; both may be sums relative to a number up to
+        8 steps of 2 below m, which adds 8 times their own error (V / 1024 + 9 u: a quarter of a thread's V / 256
+        terms in each of four chains), less than tol_s
     gradient, given norm and entropy rounded to fp32: p is off by e_p = u (4 |log p| + |c| + 8) relative,
         the weight g_logp + g_entropy (log p + H) by 4 u of the magnitudes in it; and the result is
         rounded to its type (half a step, eps / 2). ex2 flushes probabilities under 2^-126: 2e-38 of
