@@ -36,6 +36,7 @@ constexpr int kSlotsEach = 4;  // slots a thread takes of a stage
 constexpr int kStageSlots = kSummers * kSlotsEach;
 constexpr int kStages = 3;
 constexpr int kClusterMax = 8;
+constexpr int kEvenMax = 128;     // sequences whose live rows are counted
 constexpr int kEnders = 3;        // warps of a CTA that finish rows where tokens are selected
 constexpr int kSegments = 8;      // of a row's stages, with a best value of each thread
 constexpr int kCandidates = 252;  // elements ranked at once
@@ -92,6 +93,17 @@ __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
+// Order of logits as unsigned integers: NaN first, then descending, -0 equal to 0. No value maps to 0.
+constexpr uint32_t kNanKey = 0xffffffffu;
+__device__ __forceinline__ uint32_t order_key(float v) {
+  if (v != v) return kNanKey;
+  const int b = __float_as_int(v + 0.f);
+  return b < 0 ? ~static_cast<uint32_t>(b) : static_cast<uint32_t>(b) | 0x80000000u;
+}
+__device__ __forceinline__ float order_value(uint32_t k) {
+  if (k == kNanKey) return kNan;
+  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
+}
 // A row's elements in slots of 16 bytes on the address grid: slot j holds elements
 // [j E - a, j E - a + E), the first and the last of them possibly in part.
 template <typename T>
@@ -132,6 +144,18 @@ struct Row {
       }
     }
   }
+  // a bit for each element of slot j whose order_key is not below `least`
+  __device__ __forceinline__ uint32_t at_least(const uint4& v, int j, uint32_t least) const {
+    float f[E];
+    unpack(v, f);
+    uint32_t mask = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) mask |= (order_key(f[e]) >= least ? 1u : 0u) << e;
+    const int i = first(j);
+    if (i < 0) mask &= ~0u << -i;
+    if (i + E > V) mask &= (1u << (V - i)) - 1;
+    return mask;
+  }
   __device__ static __forceinline__ float max_of(const uint4& v) {
     if constexpr (E == 4) {
       return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
@@ -143,16 +167,6 @@ struct Row {
   }
 };
 
-// Order of logits as unsigned integers: NaN first, then descending, -0 equal to 0. No value maps to 0.
-__device__ __forceinline__ uint32_t order_key(float v) {
-  if (v != v) return 0xffffffffu;
-  const int b = __float_as_int(v + 0.f);
-  return b < 0 ? ~static_cast<uint32_t>(b) : static_cast<uint32_t>(b) | 0x80000000u;
-}
-__device__ __forceinline__ float order_value(uint32_t k) {
-  if (k == 0xffffffffu) return kNan;
-  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-}
 // larger: better value, or the same at a lower index
 __device__ __forceinline__ uint64_t rank_key(uint32_t key, int index) {
   return static_cast<uint64_t>(key) << 32 | static_cast<uint32_t>(~index);
@@ -238,6 +252,7 @@ struct Running {
   // 4 n registers of values, whose largest is cm
   template <int n>
   __device__ __forceinline__ void add(const uint32_t* r, float cm, uint64_t log2e) {
+    if (cm == -kInf) return;  // nothing but masked logits
     if (!(cm <= limit)) raise(cm);
     m = max_nan(m, cm);
     if (!huge) {
@@ -311,18 +326,6 @@ __device__ __forceinline__ uint64_t bitonic_merge(uint64_t v, int lane) {
   }
   return v;
 }
-__device__ __forceinline__ uint64_t sort_warp(uint64_t v, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 32; size <<= 1) {
-#pragma unroll
-    for (int j = size >> 1; j > 0; j >>= 1) {
-      const uint64_t o = shfl_xor64(v, j);
-      const bool descending = (lane & size) == 0;
-      v = ((lane & j) == 0) == descending ? max64(v, o) : min64(v, o);
-    }
-  }
-  return v;
-}
 // The same over 32-bit keys.
 __device__ __forceinline__ uint32_t bitonic_merge(uint32_t v, int lane) {
 #pragma unroll
@@ -343,25 +346,21 @@ __device__ __forceinline__ uint32_t sort_warp(uint32_t v, int lane) {
   }
   return v;
 }
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return max(a, b); }
-__device__ __forceinline__ uint64_t larger(uint64_t a, uint64_t b) { return max64(a, b); }
-
 // A barrier of the summing threads.
 __device__ __forceinline__ void summers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSummers) : "memory"); }
 
 // A bound that at least k of 256 keys reach, or 0 where fewer than k are not 0: the k-th largest of the best of 64
 // groups of four. list[w] holds a key a lane.
-template <typename K>
-__device__ __forceinline__ K kth_bound(const K (*list)[32], int k, int lane) {
-  K a = 0, b = 0;
+__device__ __forceinline__ uint32_t kth_bound(const uint32_t (*list)[32], int k, int lane) {
+  uint32_t a = 0, b = 0;
 #pragma unroll
   for (int w = 0; w < kWarps / 2; ++w) {
-    a = larger(a, list[w][lane]);
-    b = larger(b, list[w + kWarps / 2][lane]);
+    a = max(a, list[w][lane]);
+    b = max(b, list[w + kWarps / 2][lane]);
   }
   a = sort_warp(a, lane);
   b = sort_warp(b, lane);
-  a = bitonic_merge(larger(a, static_cast<K>(shfl(b, 31 - lane))), lane);
+  a = bitonic_merge(max(a, shfl(b, 31 - lane)), lane);
   return shfl(a, k - 1);
 }
 
@@ -392,19 +391,16 @@ struct Shared {
   uint64_t full[kStages], drained[kStages], others;
   float red[kEnders][3][kWarps];
   float cluster_stats[kClusterMax][3];
+  int before[kEvenMax];  // live rows of the sequences before one
   int abort_flag;
 };
 // What the summers leave of a row for one of the enders, and what that warp works with.
 struct End {
-  uint4 hit[128];                         // slots that hold candidates: G a lane
-  union alignas(16) {
-    uint64_t cand[kCandidates + 4];       // elements that may be among the best
-    uint64_t list[kWarps][32];            // before them: keys with slots
-  };
+  uint4 hit[128];                         // slots that hold candidates: four a lane
+  uint64_t cand[kCandidates + 4];         // elements that may be among the best
   uint64_t best[32];                      // this CTA's k best elements
   alignas(8) __nv_bfloat16 segment[kSegments][kSummers];  // each summer's best value of a segment, rounded up
   uint32_t key[kWarps][32];               // order_key of its best value of all, 0 where it has none
-  int slot[kWarps][32];                   // and its first slot of the first stage that holds that
   int hit_slot[128];
   uint16_t asked[kSummers];               // summers that hold candidates
   uint16_t owner[kSegments * 32];         // segments that do, of 32 of them
@@ -462,52 +458,34 @@ __device__ __forceinline__ int scan(int v, int lane, int& total) {
 template <typename T>
 __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Part& part, int k, int lane) {
   constexpr int E = Row<T>::E, G = 4;
-  // Values alone first: every summer at or above the bound is asked, every element there is taken. With many equal
-  // values, or fewer summers or values than k, slots decide between equal ones.
-  uint32_t least = kth_bound(e.key, k, lane);
-  uint64_t slot_floor = 0, floor = static_cast<uint64_t>(least) << 32;
-  bool ties = least <= order_key(-kInf), ask = true;
   const int stages = segment_stages(part), each = stages * kSlotsEach;
   // a summer's slots of a segment by as many lanes, up to 32
   const int bits = each <= 4 ? 2 : each <= 8 ? 3 : each <= 16 ? 4 : 5, at_once = 32 >> bits;
   const int full_hi = min(part.hi, r.full_hi);
-  int asked = 0;
+  const uint32_t lowest = order_key(-kInf);
+  uint32_t bound = kth_bound(e.key, k, lane);  // at least k values are not below it
+  // Every value from the bound on is taken, or, where more equal the bound than can be ranked (masked logits often do),
+  // every value above it; those that equal it then follow by index.
+  bool above = bound == lowest;
   for (;;) {
-    if (ask) {
-      uint32_t is = 0;  // a bit for each warp's summer of this lane
-      if (!ties) {
+    const bool none = above && bound == kNanKey;  // is above it
+    const uint32_t least = above ? bound + 1 : max(bound, 1u);
+    e.best[lane] = 0;
+    int asked, found = 0;
+    uint32_t is = 0;  // a bit for each warp's summer of this lane
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) is |= (e.key[w][lane] >= least ? 1u : 0u) << w;
-      } else {
-        uint64_t(*list)[32] = e.list;
-#pragma unroll 1
-        for (int w = 0; w < kWarps; ++w) {
-          const uint32_t key = e.key[w][lane];
-          int slot = e.slot[w][lane];
-          // the stage's first slot that holds it
-          for (int u = 1; key != 0 && u < kSlotsEach && order_key(Row<T>::max_of(r.load(slot))) != key; ++u) slot += kSummers;
-          list[w][lane] = key != 0 ? rank_key(key, slot) : 0;
-        }
-        __syncwarp();
-        slot_floor = max64(1, kth_bound(list, k, lane));
-        least = static_cast<uint32_t>(slot_floor >> 32);
-        floor = 0;
-#pragma unroll 1
-        for (int w = 0; w < kWarps; ++w) is |= (list[w][lane] >= slot_floor ? 1u : 0u) << w;
-      }
-      for (int at = scan(__popc(is), lane, asked); is != 0; is &= is - 1)
-        e.asked[at++] = static_cast<uint16_t>((__ffs(is) - 1) * 32 + lane);
-      __syncwarp();
-      ask = false;
-    }
-    int found = 0;
+    for (int w = 0; w < kWarps; ++w) is |= (!none && e.key[w][lane] >= least ? 1u : 0u) << w;
+    for (int at = scan(__popc(is), lane, asked); is != 0; is &= is - 1)
+      e.asked[at++] = static_cast<uint16_t>((__ffs(is) - 1) * 32 + lane);
+    __syncwarp();
     for (int x0 = 0; x0 < asked; x0 += 32) {
       // their segments that hold candidates: up to kSegments a lane
       const int summer = x0 + lane < asked ? e.asked[x0 + lane] : 0;
-      uint32_t is = 0;
+      is = 0;
 #pragma unroll
       for (int q = 0; q < kSegments; ++q)
-        if (part.lo + q * stages * kStageSlots + summer < part.hi) is |= (order_key(__bfloat162float(e.segment[q][summer])) >= least ? 1u : 0u) << q;
+        if (part.lo + q * stages * kStageSlots + summer < part.hi)
+          is |= (order_key(__bfloat162float(e.segment[q][summer])) >= least ? 1u : 0u) << q;
       if (x0 + lane >= asked) is = 0;
       int owners;
       for (int at = scan(__popc(is), lane, owners); is != 0; is &= is - 1)
@@ -520,18 +498,16 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
         for (int g0 = 0; g0 < owners; g0 += G * at_once) {
           uint4 v[G];
           int j[G];
+          bool in_part = false;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
             const int o = g0 + g * at_once + (lane >> bits);
             j[g] = part.hi;
             if (o < owners && i < each)
               j[g] = part.lo + (e.owner[o] >> 10) * stages * kStageSlots + (e.owner[o] & 1023) + i * kSummers;
-            if (j[g] >= r.full_lo && j[g] < full_hi) v[g] = r.load_full(j[g]);
+            if (j[g] >= r.full_lo && j[g] < full_hi) v[g] = r.load_full(j[g]); else in_part |= j[g] < part.hi;
           }
           // the row's first and last slot, where it has them in part
-          bool in_part = false;
-#pragma unroll
-          for (int g = 0; g < G; ++g) in_part |= j[g] < part.hi && (j[g] < r.full_lo || j[g] >= full_hi);
           if (__any_sync(0xffffffffu, in_part)) {
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -552,27 +528,9 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
           }
           __syncwarp();
           for (int h0 = 0; h0 < slots; h0 += 32) {
-            const bool holds = h0 + lane < slots;
-            const int slot = holds ? e.hit_slot[h0 + lane] : 0;
-            const uint4 x = holds ? e.hit[h0 + lane] : make_uint4(0, 0, 0, 0);
-            float f[E];
-            Row<T>::unpack(x, f);
+            const int slot = h0 + lane < slots ? e.hit_slot[h0 + lane] : 0;
             uint32_t mask = 0;
-            if (holds) {
-              const int first = r.first(slot);
-              if (!ties) {
-#pragma unroll
-                for (int q = 0; q < E; ++q) mask |= (order_key(f[q]) >= least ? 1u : 0u) << q;
-              } else {
-#pragma unroll
-                for (int q = 0; q < E; ++q) {
-                  const uint32_t key = order_key(f[q]);
-                  mask |= (rank_key(key, slot) >= slot_floor && rank_key(key, first + q) >= floor ? 1u : 0u) << q;
-                }
-              }
-              if (first < 0) mask &= ~0u << -first;
-              if (first + E > r.V) mask &= (1u << (r.V - first)) - 1;
-            }
+            if (h0 + lane < slots) mask = r.at_least(e.hit[h0 + lane], slot, least);
             int more;
             int c = found + scan(__popc(mask), lane, more);
             found += more;
@@ -586,11 +544,14 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
         }
       }
     }
+    if (found > kCandidates && !above) {
+      above = true;
+      continue;
+    }
     const int held = min(found, kCandidates);
     if (lane < 4) e.cand[held + lane] = 0;
-    e.best[lane] = 0;
     __syncwarp();
-    uint64_t raise = 0;
+    uint64_t kth = 0;
     for (int c = lane; c < held; c += 32) {
       const uint64_t mine = e.cand[c];
       int place = 0;
@@ -600,19 +561,38 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
                          y = *reinterpret_cast<const ulonglong2*>(&e.cand[o + 2]);
         place += (x.x > mine) + (x.y > mine) + (y.x > mine) + (y.y > mine);
       }
-      if (place < k) e.best[place] = mine;
-      if (place == k - 1) raise = mine;
+      if (place < k && found <= kCandidates) e.best[place] = mine;
+      if (place == k - 1) kth = mine;
     }
     __syncwarp();
-    if (found <= kCandidates) return e.best[lane];
-    // more than fit: the k-th best of those held is a higher floor, which leaves out the rest
-    if (ties) {
-      const uint32_t who = __ballot_sync(0xffffffffu, raise != 0);
-      floor = shfl(raise, __ffs(who) - 1);
-    } else {
-      ask = ties = true;
+    if (found <= kCandidates) {
+      if (above && found < k) break;
+      return e.best[lane];
     }
+    // more than fit: the k-th best of those held is a higher bound
+    const uint32_t who = __ballot_sync(0xffffffffu, kth != 0);
+    bound = static_cast<uint32_t>(shfl(kth, __ffs(who) - 1) >> 32);
+    above = false;
   }
+  // the first values that equal the bound, in the segments that may hold some
+  int place = __popc(__ballot_sync(0xffffffffu, e.best[lane] != 0));
+  for (int j0 = part.lo; j0 < part.hi && place < k; j0 += 32) {
+    const int j = j0 + lane, in = j - part.lo;
+    const bool may = j < part.hi && order_key(__bfloat162float(e.segment[in / (stages * kStageSlots)][in % kSummers])) >= bound;
+    if (!__any_sync(0xffffffffu, may)) continue;
+    uint32_t mask = 0;
+    if (may) {
+      const uint4 v = r.load(j);
+      mask = r.at_least(v, j, bound);
+      if (bound != kNanKey) mask &= ~r.at_least(v, j, bound + 1);
+    }
+    int more;
+    int at = place + scan(__popc(mask), lane, more);
+    for (; mask != 0 && at < k; mask &= mask - 1, ++at) e.best[at] = rank_key(bound, r.first(j) + __ffs(mask) - 1);
+    place += more;
+  }
+  __syncwarp();
+  return e.best[lane];
 }
 
 // What a call gives for a row.
@@ -744,25 +724,64 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
         wrapped = true;
       }
     };
+    // Of few sequences the rows that hold a token are dealt evenly, by their number among these: a CTA's every 608th
+    // row may hold one each time, or never (1000 live rows of 4 x 400, 32000 fp32: 29.2 us, 25.1 so).
+    const unsigned seqs = rows / L;
+    const bool even = bits == 0 && lengths != nullptr && seqs <= kEvenMax && gridDim.x < rows;
+    unsigned items = rows;
+    if (even) {
+      int len[kEvenMax / 32], sum = 0, all;
+#pragma unroll
+      for (int x = 0; x < kEvenMax / 32; ++x) {
+        const unsigned sq = lane * (kEvenMax / 32) + x;
+        len[x] = 0;
+        if (sq < seqs) {
+          const int n = lengths[sq];
+          if (n < 0 || n > static_cast<int>(L)) record_error(err, kDevBadLength);
+          len[x] = min(max(n, 0), static_cast<int>(L));
+        }
+        sum += len[x];
+      }
+      int before = scan(sum, lane, all);
+#pragma unroll
+      for (int x = 0; x < kEvenMax / 32; ++x) {
+        sh.before[lane * (kEvenMax / 32) + x] = before;
+        before += len[x];
+      }
+      items = all;
+      __syncwarp();
+    }
+    auto live_row = [&](unsigned row, bool report) {
+      if (lengths == nullptr) return true;
+      const unsigned sq = row / L, t = row - sq * L;
+      const int n = lengths[sq];
+      if ((n < 0 || n > static_cast<int>(L)) && report) record_error(err, kDevBadLength);
+      return n > static_cast<int>(L) || static_cast<int>(t) < n;
+    };
     // 32 of the rows at a time, one a lane: whether it holds a token, and which
-    for (unsigned long long base = blockIdx.x >> bits; base < rows; base += 32ull * step) {
-      const unsigned long long mine = base + static_cast<unsigned long long>(lane) * step;
-      bool live = mine < rows;
+    for (unsigned long long base = blockIdx.x >> bits; base < items; base += 32ull * step) {
+      const unsigned long long item = base + static_cast<unsigned long long>(lane) * step;
+      unsigned row_l = static_cast<unsigned>(item);
+      bool live = item < items;
       int id = 0;
       if (live) {
-        const unsigned row = static_cast<unsigned>(mine);
-        if (out.logp) id = ids[row];
-        if (lengths != nullptr) {
-          const unsigned sq = row / L, t = row - sq * L;
-          const int n = lengths[sq];
-          if ((n < 0 || n > static_cast<int>(L)) && rank == 0) record_error(err, kDevBadLength);
-          live = n > static_cast<int>(L) || static_cast<int>(t) < n;
+        if (even) {  // the last sequence with no more rows before it
+          int lo = 0, hi = kEvenMax;
+          while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (sh.before[mid] <= static_cast<int>(item)) lo = mid; else hi = mid;
+          }
+          row_l = lo * L + static_cast<unsigned>(item) - sh.before[lo];
         }
-        if (!live && rank == 0) out.dead(row);
+        if (out.logp) id = ids[row_l];
+        if (!even) {
+          live = live_row(row_l, rank == 0);
+          if (!live && rank == 0) out.dead(row_l);
+        }
       }
       for (uint32_t todo = __ballot_sync(0xffffffffu, live); todo != 0; todo &= todo - 1) {
         const int l = __ffs(todo) - 1;
-        const unsigned row = static_cast<unsigned>(base + static_cast<unsigned long long>(l) * step);
+        const unsigned row = __shfl_sync(0xffffffffu, row_l, l);
         const int row_id = __shfl_sync(0xffffffffu, id, l);
         const Row<T> r(logits + row * ld, V);
         const Part part(r.n_slots, rank, bits);
@@ -797,6 +816,9 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
       sh.stage[q] = Stage{0, 0, -1, 0};
       mbar_arrive(smem_u32(&sh.full[q]));
     }
+    if (even)
+      for (unsigned long long row = blockIdx.x + static_cast<unsigned long long>(lane) * step; row < rows; row += 32ull * step)
+        if (!live_row(static_cast<unsigned>(row), false)) out.dead(static_cast<unsigned>(row));
     return;
   }
 
@@ -828,16 +850,16 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
   uint64_t log2e;  // twice; kept, as it is not built again for every pair
   asm volatile("mov.b64 %0, {%1, %1};" : "=l"(log2e) : "f"(kLog2e));
   Running<T> run;
-  int best_slot = 0;       // the thread's first slot of the first stage that holds its maximum
-  float segment = -kInf;  // its maximum of the segment so far
+  float segment = -kInf;  // the thread's maximum of the segment so far
+  bool holds = false;     // whether it has any slot
   for (;;) {
     if (!mbar_wait_bounded(smem_u32(&sh.full[q]), parity, &sh.abort_flag, err, kDevTimeoutEpilogue)) return;
     const Stage in = sh.stage[q];
     if (in.n_flags < 0) break;
-    const int n = in.n_flags & (kFirst - 1), j = in.j0 + tid;
+    const int n = in.n_flags & (kFirst - 1);
     if (in.n_flags & kFirst) {
       run = Running<T>();
-      best_slot = j;
+      holds = tid < n;  // a summer without a slot in the first stage has none
       if (kTop && (used & 2) && !warp_wait_bounded(smem_u32(&top.end[buf].free), used & 1, &sh.abort_flag, err, kDevTimeoutDrain))
         return;
       if (!kTop && tid == 0 && rank == 0 && out.logp) {
@@ -847,7 +869,6 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
     }
     const uint4* src = reinterpret_cast<const uint4*>(sh.ring[q]) + tid;
     float cm = -kInf;
-    const float before = run.m;
     if (n == kStageSlots) {
       uint32_t v[4 * kSlotsEach];
 #pragma unroll
@@ -870,7 +891,6 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
         cm = max_nan(cm, slot_max);
       }
     }
-    if (kTop && !(cm <= before) && before == before) best_slot = j;
     if constexpr (kTop) {
       segment = max_nan(segment, cm);
       if (in.n_flags & kSegmentEnd) {
@@ -891,9 +911,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
     st.merge_lanes(32);
     if constexpr (kTop) {
       End& e = top.end[buf];
-      // a summer without slots: its first slot would be behind the part's end, which is where the last stage ends
-      e.key[warp][lane] = best_slot < in.j0 + n ? order_key(value) : 0;
-      e.slot[warp][lane] = best_slot;
+      e.key[warp][lane] = holds ? order_key(value) : 0;
       if (tid == 0) {
         e.row = in.row;
         e.id = in.id;
