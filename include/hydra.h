@@ -362,8 +362,8 @@ hydra_status hydra_token_logprobs_entropy(const void* logits, int logits_dtype, 
  * Rows t >= len and rows of nothing but -inf are written 0 (rows t >= len are not read). A token at
  * -inf has p = 0. An id out of range writes NaN to its row (device error 0x201).
  * Errors: as the forward call, and grad_dtype, or dlogits == logits with another dtype or stride ->
- * HYDRA_ERR_RANGE; ld_d < V, or S*L rows of V beyond 2^31 thread blocks (of up to 4096 logits of a
- * row) -> HYDRA_ERR_SHAPE.
+ * HYDRA_ERR_RANGE; ld_d < V, or S*L rows of V beyond 2^32 tiles (of up to 2048 logits of a row) ->
+ * HYDRA_ERR_SHAPE.
  */
 hydra_status hydra_token_logprobs_entropy_grad(const void* logits, int logits_dtype, int64_t S,
                                                int64_t L, int64_t V, int64_t ld, const int32_t* ids,

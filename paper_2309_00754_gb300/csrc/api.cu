@@ -575,7 +575,7 @@ hydra_status hydra_token_logprobs_entropy_grad(const void* logits, int logits_dt
   if (grad_dtype != HYDRA_F32 && grad_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
   if (!token_rows_ok(S, L, V, ld) || ld_d < V) return HYDRA_ERR_SHAPE;
   if (S == 0 || L == 0) return HYDRA_OK;
-  if (S * L > ((1LL << 31) - 1) / hydra::token_stats_grad_tiles(V)) return HYDRA_ERR_SHAPE;
+  if (S * L > ((1LL << 32) - 1) / hydra::token_stats_grad_tiles(V)) return HYDRA_ERR_SHAPE;
   if (logits == nullptr || norm == nullptr || dlogits == nullptr) return HYDRA_ERR_NULL;
   if (grad_logp == nullptr && grad_entropy == nullptr) return HYDRA_ERR_NULL;
   if ((grad_logp != nullptr && ids == nullptr) || (grad_entropy != nullptr && entropy == nullptr))

@@ -4,13 +4,16 @@
 //     norm = sqrt(sum over all tensors and elements of g^2)
 //     coef = min(1, max_norm / (norm + 1e-6)), 1 where the norm is not finite;  out = g coef
 //
-// Two launches: every CTA sums the squares of a contiguous range of chunks and writes one fp64
-// partial; every CTA of the second pass adds all partials in the same fixed order and scales its
-// range. The tensors' addresses travel as a kernel parameter, so that a captured call stands by itself.
+// Two launches: every CTA sums the squares of a contiguous range of 16 KB chunks and writes one
+// partial sum; every CTA of the second pass adds all partials in the same fixed order and scales its
+// range, from its end, whose chunks L2 still holds. The tensors' addresses travel as a kernel parameter, so
+// that a captured call stands by itself.
 //
-// Squares are summed in fp32 over a thread's elements of a chunk and in fp64 beyond. A chunk whose
-// fp32 sum leaves [2^-80, 2^120] while its elements are not all zero is summed again in fp64,
-// where no square of an fp32 value overflows or vanishes.
+// Squares are summed in fp32 over a thread's elements of a chunk, and these sums as pairs of fp32 numbers with
+// their rounding errors (Knuth 1969): fp64 runs at a hundredth of the fp32 rate here (393 chunks of fp32: 21 us
+// with fp64 sums over CTAs). A chunk whose fp32 sum leaves [2^-80, 2^90] while its elements are not all
+// zero is summed again in fp64, where no square of an fp32 value overflows or vanishes, and only then is anything
+// beyond it done in fp64.
 #include <algorithm>
 
 #include "common.cuh"
@@ -20,9 +23,15 @@ namespace hydra {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kCtasPerSm = 4;  // (six: 205 MB of fp32 140 us, eight 163, for 95)
 constexpr int kChunkBytes = 16384;
-constexpr int kTableMax = 960;  // tensors of one launch: 30 KB of parameters
-constexpr double kEps = 1e-6;
+constexpr int kVecs = kChunkBytes / 16 / kThreads;  // of a thread in a whole chunk
+// Of a longer list the last of every CTA's range, where the second pass begins, is to stay in L2; the rest and the outputs
+// leave it first (102 MB of fp32 53.5 -> 48.8 us, 205 MB 100.4 -> 96.3, 822 MB 390 -> 386; the norm alone 21.5 -> 21.4,
+// 37.1 -> 32.1, 128 -> 125).
+constexpr int kKeepBytes = 64 << 20;
+constexpr int kTableMax = 880;  // tensors of one launch: 30 KB of parameters
+constexpr float kEps = 1e-6f;
 
 struct Entry {
   const void* src;
@@ -31,8 +40,10 @@ struct Entry {
   int first;  // first chunk
   int bf16;
 };
+// A launch's parameters. A search for a CTA's first tensor would be a chain of constant-cache misses.
 template <int kCap>
 struct Table {
+  uint16_t start[kGradMaxBlocks];  // of each CTA, the tensor of its first chunk
   Entry e[kCap];
 };
 
@@ -77,61 +88,113 @@ __device__ __forceinline__ void unpack(const uint4& v, float (&f)[16 / sizeof(T)
   }
 }
 
-// f(value) over this thread's elements of a chunk
-template <typename T, typename F>
-__device__ __forceinline__ void for_each(const Chunk<T>& c, F f) {
-  constexpr int E = Chunk<T>::E;
-#pragma unroll
-  for (int q = 0; q < kChunkBytes / 16 / kThreads; ++q) {
-    const int v = threadIdx.x + q * kThreads;
-    if (v < c.vecs) {
-      float x[E];
-      unpack<T>(*reinterpret_cast<const uint4*>(c.src + c.head + v * E), x);
-#pragma unroll
-      for (int e = 0; e < E; ++e) f(x[e]);
-    }
-  }
-  // up to E - 1 elements at either end
-  const int t = threadIdx.x;
-  const int tail = c.head + c.vecs * E;
-  if (t < c.head) f(to_f(c.src[t]));
-  if (t < c.n - tail) f(to_f(c.src[tail + t]));
+// (not volatile: then the compiler holds them in registers that the loads want)
+__device__ __forceinline__ uint64_t policy_first() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
-
-template <typename T>
-__device__ __forceinline__ double square_sum(const Chunk<T>& c) {
-  float s = 0.f;
-  uint32_t any = 0;
-  for_each(c, [&](float x) {
-    s = fmaf(x, x, s);
-    any |= __float_as_uint(x) << 1;
-  });
-  if (any == 0 || (s >= 0x1p-80f && s <= 0x1p120f)) return s;
-  double d = 0.0;
-  for_each(c, [&](float x) { d += static_cast<double>(x) * x; });
-  return d;
+__device__ __forceinline__ uint64_t policy_normal() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
+  return p;
 }
-
-__device__ __forceinline__ double block_sum(double v, double* red) {
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = 0.0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) v += red[w];
+__device__ __forceinline__ uint4 load16(const void* p, uint64_t policy) {
+  uint4 v;
+  asm volatile("ld.global.L2::cache_hint.v4.u32 {%0, %1, %2, %3}, [%4], %5;"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p), "l"(policy)
+               : "memory");
   return v;
 }
+__device__ __forceinline__ void store16(void* p, const uint4& v, uint64_t policy) {
+  asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1, %2, %3, %4}, %5;" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z),
+               "r"(v.w), "l"(policy)
+               : "memory");
+}
 
-// the tensor that chunk c belongs to: the last one that starts at or before it (empty ones have no chunk)
-template <int kCap>
-__device__ __forceinline__ int find(const Table<kCap>& t, int n, int c) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (t.e[mid].first <= c) lo = mid; else hi = mid;
+// A sum hi + lo, exact to twice the bits of fp32; the order of two does not change what they add up to.
+struct Sum {
+  float hi = 0.f, lo = 0.f;
+  __device__ __forceinline__ void add(float v, float v_lo) {
+    const float sum = hi + v, part = sum - hi;
+    lo = (lo + v_lo) + ((hi - (sum - part)) + (v - part));
+    hi = sum;
   }
-  return lo;
+};
+
+// A thread's sum of squares, and those that would not do in fp32.
+struct Squares {
+  Sum sum;
+  double d = 0.0;
+
+  template <typename T>
+  __device__ __forceinline__ void add(const Chunk<T>& c, uint64_t policy) {
+    constexpr int E = Chunk<T>::E;
+    const int t = threadIdx.x, tail = c.head + c.vecs * E;
+    uint4 v[kVecs];
+    float ends[2] = {0.f, 0.f};  // up to E - 1 elements at either end
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) {
+      v[q] = make_uint4(0, 0, 0, 0);
+      if (t + q * kThreads < c.vecs) v[q] = load16(c.src + c.head + (t + q * kThreads) * E, policy);
+    }
+    if (t < c.head) ends[0] = to_f(c.src[t]);
+    if (t < c.n - tail) ends[1] = to_f(c.src[tail + t]);
+    float s = ends[0] * ends[0] + ends[1] * ends[1];
+    uint32_t any = __float_as_uint(ends[0]) | __float_as_uint(ends[1]);
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q) {
+      float x[E];
+      unpack<T>(v[q], x);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s = fmaf(x[e], x[e], s);
+      any |= v[q].x | v[q].y | v[q].z | v[q].w;
+    }
+    const uint32_t signs = sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
+    if ((any & ~signs) == 0 || (s >= 0x1p-80f && s <= 0x1p90f)) {
+      sum.add(s, 0.f);
+      return;
+    }
+    d += static_cast<double>(ends[0]) * ends[0] + static_cast<double>(ends[1]) * ends[1];
+#pragma unroll 1
+    for (int q = 0; q < kVecs; ++q) {
+      if (t + q * kThreads >= c.vecs) break;
+      const T* p = c.src + c.head + (t + q * kThreads) * E;
+#pragma unroll 1
+      for (int e = 0; e < E; ++e) d += static_cast<double>(to_f(p[e])) * to_f(p[e]);
+    }
+  }
+};
+
+// A CTA's sum, or another part of it: `d` is 0 but where fp32 would not do.
+struct alignas(16) Partial {
+  Sum sum;
+  double d;
+};
+
+struct BlockShared {
+  Sum sum[kThreads / 32];
+  double d[kThreads / 32];
+};
+// The threads' parts added up, in every thread; their order is fixed.
+__device__ __forceinline__ Partial block_sum(Sum s, double d, BlockShared& sh) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1)
+    s.add(__shfl_xor_sync(0xffffffffu, s.hi, off), __shfl_xor_sync(0xffffffffu, s.lo, off));
+  if (lane == 0) sh.sum[warp] = s;
+  const bool wide = __syncthreads_or(__double_as_longlong(d) != 0);
+  Partial r{sh.sum[0], 0.0};
+#pragma unroll
+  for (int w = 1; w < kThreads / 32; ++w) r.sum.add(sh.sum[w].hi, sh.sum[w].lo);
+  if (wide) {
+    for (int off = 16; off > 0; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+    if (lane == 0) sh.d[warp] = d;
+    __syncthreads();
+    for (int w = 0; w < kThreads / 32; ++w) r.d += sh.d[w];
+  }
+  return r;
 }
 
 // chunks [b chunks / grid, (b + 1) chunks / grid) of a launch
@@ -143,19 +206,30 @@ __device__ __forceinline__ int range_at(int chunks, unsigned b) {
 template <int kCap>
 __global__ void __launch_bounds__(kThreads)
     grad_square_kernel(const __grid_constant__ Table<kCap> table, int n, int chunks, int add,
-                       double* __restrict__ partial) {
-  __shared__ double red[kThreads / 32];
+                       Partial* __restrict__ partial) {
+  __shared__ BlockShared sh;
+  const int c0 = range_at(chunks, blockIdx.x), c1 = range_at(chunks, blockIdx.x + 1);
+  int i = table.start[blockIdx.x];
   pdl_wait();
   pdl_launch_dependents();
-  const int c0 = range_at(chunks, blockIdx.x), c1 = range_at(chunks, blockIdx.x + 1);
-  double sum = 0.0;
-  for (int c = c0, i = find(table, n, c0); c < c1; ++c) {
+  Squares squares;
+  const int keep = kKeepBytes / kChunkBytes / gridDim.x;
+  const uint64_t first = policy_first();
+  for (int c = c0; c < c1; ++c) {
     while (i + 1 < n && table.e[i + 1].first <= c) ++i;
     const Entry& e = table.e[i];
-    sum += e.bf16 ? square_sum(Chunk<__nv_bfloat16>(e, c)) : square_sum(Chunk<float>(e, c));
+    const uint64_t policy = c >= c1 - keep ? policy_normal() : first;
+    if (e.bf16) squares.add(Chunk<__nv_bfloat16>(e, c), policy); else squares.add(Chunk<float>(e, c), policy);
   }
-  sum = block_sum(sum, red);
-  if (threadIdx.x == 0) partial[blockIdx.x] = add ? partial[blockIdx.x] + sum : sum;
+  Partial p = block_sum(squares.sum, squares.d, sh);
+  if (threadIdx.x == 0) {
+    if (add) {
+      const Partial before = partial[blockIdx.x];
+      p.sum.add(before.sum.hi, before.sum.lo);
+      p.d += before.d;
+    }
+    partial[blockIdx.x] = p;
+  }
 }
 
 // A coefficient of 1 copies: a product would give NaN another bit pattern.
@@ -183,13 +257,14 @@ __device__ __forceinline__ void scale_chunk(const Entry& e, int ci, float coef) 
   T* dst = static_cast<T*>(e.dst) + (c.src - static_cast<const T*>(e.src));
   const int t = threadIdx.x;
   if (((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(c.src)) & 15) == 0) {
+    uint4 x[kVecs];
 #pragma unroll
-    for (int q = 0; q < kChunkBytes / 16 / kThreads; ++q) {
-      const int v = t + q * kThreads;
-      if (v < c.vecs)
-        *reinterpret_cast<uint4*>(dst + c.head + v * E) =
-            scaled<T>(*reinterpret_cast<const uint4*>(c.src + c.head + v * E), coef);
-    }
+    for (int q = 0; q < kVecs; ++q)
+      if (t + q * kThreads < c.vecs) x[q] = load16(c.src + c.head + (t + q * kThreads) * E, policy_first());
+#pragma unroll
+    for (int q = 0; q < kVecs; ++q)
+      if (t + q * kThreads < c.vecs)
+        store16(dst + c.head + (t + q * kThreads) * E, scaled<T>(x[q], coef), policy_first());
     const int tail = c.head + c.vecs * E;
     if (t < c.head) dst[t] = scaled(c.src[t], coef);
     if (t < c.n - tail) dst[tail + t] = scaled(c.src[tail + t], coef);
@@ -198,64 +273,76 @@ __device__ __forceinline__ void scale_chunk(const Entry& e, int ci, float coef) 
   }
 }
 
-__device__ __forceinline__ double norm_of(const double* partial, int n, double* red) {
-  double s = 0.0;
-  for (int i = threadIdx.x; i < n; i += kThreads) s += partial[i];
-  return sqrt(block_sum(s, red));
-}
-__device__ __forceinline__ float coef_of(double norm, float max_norm) {
-  if (!isfinite(norm)) return 1.f;
-  return static_cast<float>(fmin(1.0, static_cast<double>(max_norm) / (norm + kEps)));
+struct Norm {
+  float norm, coef;
+};
+__device__ __forceinline__ Norm norm_of(const Partial* partial, int n, float max_norm, BlockShared& sh) {
+  Sum s;
+  double d = 0.0;
+  for (int i = threadIdx.x; i < n; i += kThreads) {
+    const Partial p = partial[i];
+    s.add(p.sum.hi, p.sum.lo);
+    if (__double_as_longlong(p.d) != 0) d += p.d;
+  }
+  const Partial all = block_sum(s, d, sh);
+  if (__double_as_longlong(all.d) == 0) {
+    const float norm = sqrtf(all.sum.hi + all.sum.lo);
+    return Norm{norm, fminf(1.f, max_norm / (norm + kEps))};
+  }
+  const double norm = sqrt(all.d + all.sum.hi + all.sum.lo);
+  return Norm{static_cast<float>(norm),
+              isfinite(norm) ? static_cast<float>(fmin(1.0, static_cast<double>(max_norm) / (norm + kEps))) : 1.f};
 }
 
 template <int kCap>
 __global__ void __launch_bounds__(kThreads)
     grad_scale_kernel(const __grid_constant__ Table<kCap> table, int n, int chunks,
-                      const double* __restrict__ partial, int n_partials, float max_norm,
+                      const Partial* __restrict__ partial, int n_partials, float max_norm,
                       float* __restrict__ norm_out) {
-  __shared__ double red[kThreads / 32];
+  __shared__ BlockShared sh;
+  const int c0 = range_at(chunks, blockIdx.x), c1 = range_at(chunks, blockIdx.x + 1);
+  // from the range's end: the last of its tensors is found while the sums are under way
+  int i = table.start[blockIdx.x];
+  while (i + 1 < n && table.e[i + 1].first < c1) ++i;
   pdl_wait();
   pdl_launch_dependents();
-  const double norm = norm_of(partial, n_partials, red);
-  const float coef = coef_of(norm, max_norm);
+  const Norm r = norm_of(partial, n_partials, max_norm, sh);
   if (blockIdx.x == 0 && threadIdx.x == 0 && norm_out != nullptr) {
-    norm_out[0] = static_cast<float>(norm);
-    norm_out[1] = coef;
+    norm_out[0] = r.norm;
+    norm_out[1] = r.coef;
   }
-  const int c0 = range_at(chunks, blockIdx.x), c1 = range_at(chunks, blockIdx.x + 1);
-  for (int c = c0, i = find(table, n, c0); c < c1; ++c) {
-    while (i + 1 < n && table.e[i + 1].first <= c) ++i;
+  for (int c = c1 - 1; c >= c0; --c) {
+    while (table.e[i].first > c) --i;
     const Entry& e = table.e[i];
-    if (coef == 1.f && e.dst == e.src) continue;  // nothing changes
-    if (e.bf16) scale_chunk<__nv_bfloat16>(e, c, coef); else scale_chunk<float>(e, c, coef);
+    if (r.coef == 1.f && e.dst == e.src) continue;  // nothing changes
+    if (e.bf16) scale_chunk<__nv_bfloat16>(e, c, r.coef); else scale_chunk<float>(e, c, r.coef);
   }
 }
 
 __global__ void __launch_bounds__(kThreads)
-    grad_norm_kernel(const double* __restrict__ partial, int n, float max_norm, float* __restrict__ norm_out) {
-  __shared__ double red[kThreads / 32];
+    grad_norm_kernel(const Partial* __restrict__ partial, int n, float max_norm, float* __restrict__ norm_out) {
+  __shared__ BlockShared sh;
   pdl_wait();
   pdl_launch_dependents();
-  const double norm = norm_of(partial, n, red);
+  const Norm r = norm_of(partial, n, max_norm, sh);
   if (threadIdx.x == 0) {
-    norm_out[0] = static_cast<float>(norm);
-    norm_out[1] = coef_of(norm, max_norm);
+    norm_out[0] = r.norm;
+    norm_out[1] = r.coef;
   }
 }
 
 int grid_of(int64_t chunks) {
-  const int64_t most = std::min(kGradMaxBlocks, std::max(1, 4 * sm_count()));
+  const int64_t most = std::min(kGradMaxBlocks, kCtasPerSm * std::max(1, sm_count()));
   return static_cast<int>(std::min(std::max<int64_t>(chunks, 1), most));
 }
 
 // One launch's part of the list: up to kTableMax tensors from `i` on, and under 2^31 chunks.
-struct Part {
+struct ListPart {
   Table<kTableMax> table;
   int n = 0, chunks = 0;
   int64_t next;
-  Part(const GradTensor* t, int64_t count, int64_t i) {
+  ListPart(const GradTensor* t, int64_t count, int64_t i) {
     for (; i < count && n < kTableMax; ++i) {
-      if (t[i].numel == 0) continue;
       const int64_t elems = kChunkBytes / (t[i].bf16 ? 2 : 4);
       const int64_t c = (t[i].numel + elems - 1) / elems;
       if (chunks + c >= (1LL << 31)) break;
@@ -266,41 +353,64 @@ struct Part {
   }
 };
 
+// The part as the parameters of `grid` CTAs. Table<kCap>'s layout is the front of every larger one's.
+template <int kCap>
+const Table<kCap>& parameters(ListPart& p, int grid) {
+  int i = 0;
+  for (int b = 0; b < grid; ++b) {
+    const int c = static_cast<int>(static_cast<long long>(p.chunks) * b / grid);  // as range_at
+    while (i + 1 < p.n && p.table.e[i + 1].first <= c) ++i;
+    p.table.start[b] = static_cast<uint16_t>(i);
+  }
+  return *reinterpret_cast<const Table<kCap>*>(&p.table);
+}
+
+template <int kCap>
+cudaError_t launch_square(ListPart& p, int grid, bool add, Partial* partial, cudaStream_t st) {
+  return launch_pdl(grad_square_kernel<kCap>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+                    p.chunks, static_cast<int>(add), partial);
+}
+template <int kCap>
+cudaError_t launch_scale(ListPart& p, const Partial* partial, int n_partials, float max_norm, float* norm_out,
+                         cudaStream_t st) {
+  const int grid = grid_of(p.chunks);
+  return launch_pdl(grad_scale_kernel<kCap>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+                    p.chunks, partial, n_partials, max_norm, norm_out);
+}
+// A launch carries a table of 32, 224 or 880 tensors.
+constexpr int kTableSmall = 32, kTableMiddle = 224;
+
 }  // namespace
 
-size_t grad_norm_workspace_bytes() { return sizeof(double) * kGradMaxBlocks; }
+size_t grad_norm_workspace_bytes() { return sizeof(Partial) * kGradMaxBlocks; }
 
 int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm_out, bool scale, void* ws,
                      cudaStream_t st) {
-  double* partial = static_cast<double*>(ws);
+  Partial* partial = static_cast<Partial*>(ws);
   int n_partials = 0;
   for (int64_t i = 0; i < n;) {
-    const Part p(t, n, i);
-    const bool only = i == 0 && p.next == n;
-    i = p.next;
-    if (p.n == 0) break;
+    ListPart p(t, n, i);
     // a list of several launches: each adds to the partials of the one before it
-    const int grid = grid_of(only ? p.chunks : INT64_MAX);
-    if (launch_pdl(grad_square_kernel<kTableMax>, dim3(grid), dim3(kThreads), 0, st, p.table, p.n, p.chunks,
-                   static_cast<int>(n_partials != 0), partial) != cudaSuccess)
-      return -3;
+    const int grid = grid_of(i == 0 && p.next == n ? p.chunks : INT64_MAX);
+    const auto launch = p.n <= kTableSmall    ? launch_square<kTableSmall>
+                        : p.n <= kTableMiddle ? launch_square<kTableMiddle>
+                                              : launch_square<kTableMax>;
+    if (launch(p, grid, i > 0, partial, st) != cudaSuccess) return -3;
     n_partials = grid;
+    i = p.next;
   }
-  if (!scale || n_partials == 0)
-    return launch_pdl(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, static_cast<const double*>(partial),
+  if (!scale || n == 0)
+    return launch_pdl(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, static_cast<const Partial*>(partial),
                       n_partials, max_norm, norm_out) == cudaSuccess
                ? 0
                : -3;
-  bool first = true;
   for (int64_t i = 0; i < n;) {
-    const Part p(t, n, i);
+    ListPart p(t, n, i);
+    const auto launch = p.n <= kTableSmall    ? launch_scale<kTableSmall>
+                        : p.n <= kTableMiddle ? launch_scale<kTableMiddle>
+                                              : launch_scale<kTableMax>;
+    if (launch(p, partial, n_partials, max_norm, i == 0 ? norm_out : nullptr, st) != cudaSuccess) return -3;
     i = p.next;
-    if (p.n == 0) break;
-    if (launch_pdl(grad_scale_kernel<kTableMax>, dim3(grid_of(p.chunks)), dim3(kThreads), 0, st, p.table, p.n,
-                   p.chunks, static_cast<const double*>(partial), n_partials, max_norm,
-                   first ? norm_out : static_cast<float*>(nullptr)) != cudaSuccess)
-      return -3;
-    first = false;
   }
   return 0;
 }

@@ -183,11 +183,11 @@ struct TokenStatsGradArgs {
   int64_t ld_d;
   int* err;
 };
-// CTAs a row takes: S * L * tiles must stay below 2^31
+// tiles of a row: S * L * tiles must stay below 2^32
 int64_t token_stats_grad_tiles(int64_t V);
 int launch_token_stats_grad(const TokenStatsGradArgs& a, cudaStream_t stream);
 
-// Global norm of a list of tensors and clipping (grad_clip.cu); ws holds one fp64 partial a CTA.
+// Global norm of a list of tensors and clipping (grad_clip.cu); ws holds one partial sum a CTA.
 struct GradTensor {
   const void* grad;
   void* out;
@@ -196,7 +196,7 @@ struct GradTensor {
 };
 constexpr int kGradMaxBlocks = 1216;
 size_t grad_norm_workspace_bytes();
-// norm_out [2] = (norm, coefficient); scale: out = grad * coefficient as well
+// norm_out [2] = (norm, coefficient); scale: out = grad * coefficient as well. No tensor is empty.
 int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm_out, bool scale, void* ws,
                      cudaStream_t st);
 

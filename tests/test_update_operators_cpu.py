@@ -115,7 +115,7 @@ def test_token_stats_grad_argument_errors(lib):
     assert _grad(lib, dt=2) == 4 and _grad(lib, gdt=5) == 4
     assert _grad(lib, S=-1) == 2 and _grad(lib, ld=99) == 2 and _grad(lib, ld_d=99) == 2
     assert _grad(lib, V=0, ld=0, ld_d=0) == 2
-    assert _grad(lib, S=1 << 15, L=1 << 14, V=32000, ld=32000, ld_d=32000) == 2  # more than 2^31 blocks
+    assert _grad(lib, S=1 << 15, L=1 << 14, V=32000, ld=32000, ld_d=32000) == 2  # more than 2^32 tiles
     assert _grad(lib, z=None) == 1 and _grad(lib, norm=None) == 1 and _grad(lib, d=None) == 1
     assert _grad(lib, gl=None, gh=None) == 1
     assert _grad(lib, ids=None) == 1 and _grad(lib, ent=None) == 1
