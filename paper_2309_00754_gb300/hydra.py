@@ -223,21 +223,40 @@ def _req(t, dtype, name):
 
 def _on_device(*tensors):
     """Refuse tensors of another device than the current one, whose stream the call would not order."""
-    now = torch.cuda.current_device() if _raw_device is None else _raw_device()
+    now = _current_device()
     for t in tensors:
         if t is not None and t.device.index != now:
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{now}")
 
 
+def _current_device():
+    return torch.cuda.current_device() if _raw_device is None else _raw_device()
+
+
+def _arg(t, dtype, n, device, name):
+    """The pointer of an optional contiguous tensor of n elements on the current device. One condition
+    where all is well: a check after another took most of a small call's time."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    _req(t, dtype, name)
+    _on_device(t)
+    raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+
+
 def _rows_of(t, rows, name):
-    """Row stride of [rows, V] logits or their gradient: rows may stand apart, elements may not."""
+    """(pointer, dtype code, row stride) of [rows, V] logits or their gradient: rows may stand apart,
+    elements may not."""
+    code = HYDRA_F32 if t.dtype is torch.float32 else _out_dtype(t, name)
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dim() != 2 or t.shape[0] != rows:
         raise ValueError(f"{name} must have {rows} rows, got shape {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and t.shape[1] > 1:
         raise ValueError(f"{name} rows must be unit-stride")
-    return t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), code, ld if rows > 1 else max(ld, t.shape[1])
 
 
 def device_error(clear: bool = True) -> int:
@@ -452,35 +471,24 @@ def hydra_token_logprobs_kl(logits_actor, logits_ref, ids, lengths, seq_score, b
         _p(reward_tok), _p(lse_actor), _p(lse_ref), _stream(stream)))
 
 
-def _per_row(rows, *named):
-    for t, n in named:
-        _req(t, torch.float32, n)
-        if t is not None and t.numel() != (2 * rows if n == "norm" else rows):
-            raise ValueError(f"{n} must have {'[rows, 2]' if n == 'norm' else 'one'} element(s) per row of {rows}")
-
-
 def hydra_token_logprobs_entropy(logits, ids, lengths, S, L, logp=None, entropy=None, norm=None,
                                  top_ids=None, top_logp=None, stream=None):
     """Per row of logits [S*L, V] (fp32 or bf16, rows may stand apart): log-probability of ids (int32
-    [S*L]), entropy, norm = (max, log-sum) [S*L, 2], and the top_ids.shape[1] likeliest tokens
+    [S*L]), entropy, norm = (max, log-sum) [S*L, 2], and the top_ids.shape[-1] likeliest tokens
     (int32 ids and fp32 log-probabilities [S*L, k]). Outputs are preallocated, any may be None."""
     rows = S * L
-    dt = _out_dtype(logits, "logits")
-    ld = _rows_of(logits, rows, "logits")
-    _req(ids, torch.int32, "ids")
-    _req(lengths, torch.int32, "lengths")
-    _req(top_ids, torch.int32, "top_ids")
-    _req(top_logp, torch.float32, "top_logp")
-    _per_row(rows, (logp, "logp"), (entropy, "entropy"), (norm, "norm"))
+    z, code, ld = _rows_of(logits, rows, "logits")
+    dev = _current_device()
+    if logits.get_device() != dev:
+        _on_device(logits)
     k = 0 if top_ids is None else top_ids.shape[-1]
-    for t, n, size in ((ids, "ids", rows), (lengths, "lengths", S), (top_ids, "top_ids", rows * k),
-                       (top_logp, "top_logp", rows * k)):
-        if t is not None and t.numel() != size:
-            raise ValueError(f"{n} must have {size} elements, got {t.numel()}")
-    _on_device(logits, ids, lengths, logp, entropy, norm, top_ids, top_logp)
+    f32, i32 = torch.float32, torch.int32
     _check("hydra_token_logprobs_entropy", load().hydra_token_logprobs_entropy(
-        _p(logits), dt, S, L, logits.shape[1], ld, _p(ids), _p(lengths), k, _p(logp), _p(entropy),
-        _p(norm), _p(top_ids), _p(top_logp), _stream(stream)))
+        z, code, S, L, logits.shape[1], ld, _arg(ids, i32, rows, dev, "ids"),
+        _arg(lengths, i32, S, dev, "lengths"), k, _arg(logp, f32, rows, dev, "logp"),
+        _arg(entropy, f32, rows, dev, "entropy"), _arg(norm, f32, 2 * rows, dev, "norm"),
+        _arg(top_ids, i32, rows * k, dev, "top_ids"), _arg(top_logp, f32, rows * k, dev, "top_logp"),
+        _stream(stream)))
 
 
 def hydra_token_logprobs_entropy_grad(logits, ids, lengths, S, L, norm, entropy, grad_logp,
@@ -489,21 +497,19 @@ def hydra_token_logprobs_entropy_grad(logits, ids, lengths, S, L, norm, entropy,
     respect to hydra_token_logprobs_entropy's logp and entropy (either None: 0), whose norm and
     entropy outputs it takes."""
     rows = S * L
-    dt, dt_d = _out_dtype(logits, "logits"), _out_dtype(dlogits, "dlogits")
-    ld, ld_d = _rows_of(logits, rows, "logits"), _rows_of(dlogits, rows, "dlogits")
+    z, code, ld = _rows_of(logits, rows, "logits")
+    d, code_d, ld_d = _rows_of(dlogits, rows, "dlogits")
     if dlogits.shape[1] != logits.shape[1]:
         raise ValueError("dlogits and logits must have the same columns")
-    _req(ids, torch.int32, "ids")
-    _req(lengths, torch.int32, "lengths")
-    _per_row(rows, (norm, "norm"), (entropy, "entropy"), (grad_logp, "grad_logp"),
-             (grad_entropy, "grad_entropy"))
-    for t, n, size in ((ids, "ids", rows), (lengths, "lengths", S)):
-        if t is not None and t.numel() != size:
-            raise ValueError(f"{n} must have {size} elements, got {t.numel()}")
-    _on_device(logits, ids, lengths, norm, entropy, grad_logp, grad_entropy, dlogits)
+    dev = _current_device()
+    if logits.get_device() != dev or dlogits.get_device() != dev:
+        _on_device(logits, dlogits)
+    f32, i32 = torch.float32, torch.int32
     _check("hydra_token_logprobs_entropy_grad", load().hydra_token_logprobs_entropy_grad(
-        _p(logits), dt, S, L, logits.shape[1], ld, _p(ids), _p(lengths), _p(norm), _p(entropy),
-        _p(grad_logp), _p(grad_entropy), _p(dlogits), dt_d, ld_d, _stream(stream)))
+        z, code, S, L, logits.shape[1], ld, _arg(ids, i32, rows, dev, "ids"),
+        _arg(lengths, i32, S, dev, "lengths"), _arg(norm, f32, 2 * rows, dev, "norm"),
+        _arg(entropy, f32, rows, dev, "entropy"), _arg(grad_logp, f32, rows, dev, "grad_logp"),
+        _arg(grad_entropy, f32, rows, dev, "grad_entropy"), d, code_d, ld_d, _stream(stream)))
 
 
 def ppo_gae(rewards, values, lengths, gamma, lam, advantages, returns, stream=None):
@@ -609,13 +615,13 @@ def grad_norm_workspace_size():
 
 
 def _grad_norm(fn, tensors, max_norm, norm_out, workspace, stream):
-    _req(norm_out, torch.float32, "norm_out")
-    if norm_out.numel() != 2:
-        raise ValueError("norm_out must have two elements")
-    _on_device(norm_out, workspace)
-    if not tensors.devices <= {norm_out.device.index}:
-        raise ValueError(f"gradients on devices {sorted(tensors.devices)}, norm_out on {norm_out.device}")
-    _check(fn, getattr(load(), fn)(tensors.c, len(tensors), float(max_norm), _p(norm_out), _p(workspace),
+    dev = _current_device()
+    out = _arg(norm_out, torch.float32, 2, dev, "norm_out")
+    if workspace.get_device() != dev:
+        _on_device(workspace)
+    if tensors.devices and tensors.devices != {dev}:
+        raise ValueError(f"gradients on devices {sorted(tensors.devices)}, but the current one is cuda:{dev}")
+    _check(fn, getattr(load(), fn)(tensors.c, len(tensors), float(max_norm), out, _p(workspace),
                                    workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
