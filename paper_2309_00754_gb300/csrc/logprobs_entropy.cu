@@ -34,7 +34,6 @@ constexpr int kSummers = 256;  // threads of a CTA that sum a row; one more warp
 constexpr int kWarps = kSummers / 32;
 constexpr int kSlotsEach = 4;  // slots a thread takes of a stage
 constexpr int kStageSlots = kSummers * kSlotsEach;
-constexpr int kStages = 3;
 constexpr int kClusterMax = 8;
 constexpr int kEvenMax = 128;     // sequences whose live rows are counted
 constexpr int kEnders = 3;        // warps of a CTA that finish rows where tokens are selected
@@ -389,7 +388,12 @@ struct alignas(16) Stage {
 // beside n: the row's first and last stage in this CTA, the last of a segment, and which one
 constexpr int kFirst = 1 << 16, kLast = 1 << 17, kSegmentEnd = 1 << 18, kSegmentShift = 20;
 
+template <bool kTop>
+constexpr int stages_of() { return kTop ? 4 : 3; }
+
+template <bool kTop>
 struct Shared {
+  static constexpr int kStages = stages_of<kTop>();
   unsigned char ring[kStages][kStageSlots * 16];
   Stage stage[kStages];
   uint64_t full[kStages], drained[kStages], others;
@@ -421,14 +425,14 @@ struct SharedTop {
   }
 };
 static_assert(kClusterMax * 32 * sizeof(uint64_t) <= sizeof(End::segment), "the keys of a cluster");
-static_assert(4 * (sizeof(Shared) + 1024) <= 228 * 1024 && 2 * (sizeof(Shared) + sizeof(SharedTop) + 1024) <= 228 * 1024,
-              "CTAs an SM");
 template <bool kTop>
-constexpr size_t shared_bytes() { return sizeof(Shared) + (kTop ? sizeof(SharedTop) : 0); }
+constexpr size_t shared_bytes() { return sizeof(Shared<kTop>) + (kTop ? sizeof(SharedTop) : 0); }
 template <bool kTop>
 constexpr int block_threads() { return kSummers + 32 + (kTop ? kEnders * 32 : 0); }
 template <bool kTop>
 constexpr int ctas_per_sm() { return kTop ? 2 : 4; }
+static_assert(2 * (shared_bytes<true>() + 1024) <= 228 * 1024 && 4 * (shared_bytes<false>() + 1024) <= 228 * 1024,
+              "CTAs an SM");
 
 // A row's slots in this CTA of a cluster of 1 << bits.
 struct Part {
@@ -641,7 +645,7 @@ struct Outputs {
 
 // A CTA's part of a row, by a warp: written out, or in a cluster sent to its first CTA, which writes the whole.
 template <bool kTop>
-__device__ __forceinline__ void finish(Shared& sh, SharedTop& top, const Outputs& out, unsigned row, Stats st, float z_id,
+__device__ __forceinline__ void finish(Shared<kTop>& sh, SharedTop& top, const Outputs& out, unsigned row, Stats st, float z_id,
                                        uint64_t best, unsigned rank, unsigned cs, int lane, int* err) {
   if (cs > 1) {
     if (rank != 0) {
@@ -689,8 +693,9 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
                        const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, unsigned bits,
                        const Outputs out, int* err) {
   extern __shared__ __align__(16) unsigned char raw[];
-  Shared& sh = *reinterpret_cast<Shared*>(raw);
-  SharedTop& top = *reinterpret_cast<SharedTop*>(raw + sizeof(Shared));  // with kTop
+  constexpr int kStages = stages_of<kTop>();
+  Shared<kTop>& sh = *reinterpret_cast<Shared<kTop>*>(raw);
+  SharedTop& top = *reinterpret_cast<SharedTop*>(raw + sizeof(Shared<kTop>));  // with kTop
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const unsigned cs = 1u << bits, rank = bits > 0 ? cluster_rank() : 0;
   if (tid == 0) {
@@ -873,11 +878,13 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
     }
     const uint4* src = reinterpret_cast<const uint4*>(sh.ring[q]) + tid;
     float cm = -kInf;
-    if (n == kStageSlots) {
+    if (n > kStageSlots / 2) {  // a stage that is not full with -inf behind its slots
       uint32_t v[4 * kSlotsEach];
 #pragma unroll
       for (int u = 0; u < kSlotsEach; ++u) {
-        const uint4 x = src[u * kSummers];
+        const uint32_t fill = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+        uint4 x = make_uint4(fill, fill, fill, fill);
+        if (u < kSlotsEach / 2 || tid + u * kSummers < n) x = src[u * kSummers];
         v[4 * u] = x.x;
         v[4 * u + 1] = x.y;
         v[4 * u + 2] = x.z;
