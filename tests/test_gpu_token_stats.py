@@ -160,6 +160,48 @@ def test_top_of_rows_with_ties_and_clusters(rows):
         assert np.array_equal(o["top_ids"].cpu().numpy(), r["top_ids"])
 
 
+@pytest.mark.parametrize("S,L,k", [(1, 700, 3), (5, 300, 0), (32, 41, 5), (127, 13, 0), (128, 11, 8), (129, 11, 8), (700, 2, 0),
+                                   (900, 3, 2)])
+def test_ragged_batches_of_more_rows_than_ctas(S, L, k):
+    """Few sequences have their live rows dealt by number, many by row: empty ones, full ones and one token."""
+    V = 600
+    z, values, ids, lengths, _ = make(S + L, S, L, V, torch.bfloat16, ld=603, shift=1)
+    lengths[1::4], lengths[2::7] = 0, 1
+    check_stats(run_stats(z, ids, lengths, S, L, k), values, ids, lengths, S, L, k)
+    lengths[:] = 0
+    check_stats(run_stats(z, ids, lengths, S, L, k), values, ids, lengths, S, L, k)
+
+
+@pytest.mark.parametrize("rows,V,k", [(20000, 37, 9), (5000, 1, 1), (3000, 300, 32)])
+def test_many_short_rows(rows, V, k):
+    z, values, ids, _, _ = make(V, rows, 1, V, torch.float32)
+    check_stats(run_stats(z, ids, None, rows, 1, k), values, ids, None, rows, 1, k)
+
+
+@pytest.mark.parametrize("rows", [2, 500])
+def test_more_candidates_than_are_ranked_at_once(rows):
+    """Values above the bound, equal to it and NaN, each in more places than fit: 32 lanes of a group share
+    slots that hold them all."""
+    V, k = 66000, 32
+    i = np.arange(V)
+    group = (i // 8) % 256 < 4  # four threads' slots of every 256
+    kinds = [np.where(group, 1.0 + (i % 977) * 2.0 ** -6, 0.0),             # hundreds above any bound
+             np.where(group, 2.0, np.where(i % 50 == 0, 1.0, 0.0)),         # thousands equal at the top
+             np.where(i % 7 == 0, np.nan, 1.0),                             # thousands of NaN
+             np.where(i > V - 400, 3.0, np.where(i % 9 == 0, 2.0, 1.0)),    # equal ones at the very end
+             np.where(i < 10, 5.0, -np.inf)]                                # fewer than k, then -inf by index
+    base = np.stack([kinds[n % len(kinds)] for n in range(rows)])
+    z, _ = rows_of(base, torch.bfloat16, V + 1, 1)
+    ids = torch.full((rows, k), -7, dtype=torch.int32, device="cuda")
+    logp = torch.zeros(rows, k, device="cuda")
+    H.hydra_token_logprobs_entropy(z, None, None, rows, 1, top_ids=ids, top_logp=logp)
+    values = np.where(np.isnan(base), np.inf, host_f64(z))  # NaN first, by index
+    want = np.argsort(-values[:5], axis=1, kind="stable")[:, :k]
+    got = ids.cpu().numpy()
+    for n in range(rows):
+        assert np.array_equal(got[n], want[n % 5]), n
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_stats_of_large_and_infinite_logits(dtype):
     """Large magnitudes cancel exactly; NaN and +inf make the row NaN and come first among the top."""
@@ -378,6 +420,57 @@ def test_captured_graph_and_other_stream():
         _update(z, ids, lengths, S, L, o, g)
     side.synchronize()
     assert all(torch.equal(o[k], want[k]) for k in want)
+
+
+def test_calls_on_two_streams_at_once():
+    """Neither keeps anything that the other uses."""
+    a, b = (_update_state(6, 40, 32000, torch.bfloat16, seed) for seed in (51, 52))
+    want = []
+    for z, _, ids, lengths, o, g in (a, b):
+        _update(z, dev_i32(ids), dev_i32(lengths), 6, 40, o, g)
+        want.append({k: o[k].clone() for k in ("logp", "entropy", "norm", "gl", "d")})
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    args = [(dev_i32(x[2]), dev_i32(x[3])) for x in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, (z, _, _, _, o, g), (ids, lengths) in zip(streams, (a, b), args):
+            with torch.cuda.stream(st):
+                _update(z, ids, lengths, 6, 40, o, g)
+    torch.cuda.synchronize()
+    for w, x in zip(want, (a, b)):
+        assert all(torch.equal(x[4][k], w[k]) for k in w)
+
+
+def test_update_from_logits_to_clipped_lora_gradients():
+    """An update of the head's LoRA set as it would be made: statistics, losses, the gradient in the logits, the
+    gradients of A and B (z = x W^T + (x A^T) B^T), and these clipped."""
+    S, L, V, d, r = 4, 25, 2000, 64, 8
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, W, A, B = (torch.randn(*s, device="cuda", generator=g) * c for s, c in
+                  (((S * L, d), 1.0), ((V, d), 0.2), ((r, d), 0.2), ((V, r), 0.2)))
+    z = x @ W.T + (x @ A.T) @ B.T
+    _, _, ids, lengths, o, gr = _update_state(S, L, V, torch.float32)
+    values = host_f64(z)
+    gr["old"] = dev_f32(O.token_stats(values, ids, None, S, L)["logp"].reshape(S, L) + 0.05)
+    _update(z, dev_i32(ids), dev_i32(lengths), S, L, o, gr)
+    dA, dB = (o["d"] @ B).T @ x, o["d"].T @ (x @ A.T)
+    n2, ws = torch.zeros(2, device="cuda"), torch.empty(H.grad_norm_workspace_size(), dtype=torch.uint8, device="cuda")
+    grads = [dA.contiguous(), dB.to(torch.bfloat16).contiguous()]
+    before = [host_f64(t) for t in grads]
+    H.hydra_clip_grad_norm(H.GradList(grads), 1e-3, n2, ws)
+    norm, coef, want = O.clip_grad_norm(before, 1e-3)
+    assert coef < 1 and abs(n2[0].item() - norm) <= 20 * U * norm
+    for t, w in zip(grads, want):
+        assert np.all(np.abs(host_f64(t) - w) <= (24 * U + torch.finfo(t.dtype).eps / 2 * 1.02) * np.abs(w) + 2.0 ** -133)
+    # and the whole chain: the gradient of the fp64 loss in A, whose fp32 products are off by their sums of 100 and 2000
+    lp = O.token_stats(values, ids, lengths, S, L)
+    loss = O.ppo_loss(lp["logp"].reshape(S, L), host_f64(gr["old"]), host_f64(gr["adv"]), host_f64(gr["ret"]),
+                      host_f64(gr["val"]), lengths)
+    dz = O.token_stats_grad(values, ids, lengths, S, L, loss["grad_logp"].reshape(-1), host_f64(gr["gh"]))
+    exact = (dz @ host_f64(B)).T @ host_f64(x)
+    size = (np.abs(dz) @ np.abs(host_f64(B))).T @ np.abs(host_f64(x))
+    assert np.all(np.abs(before[0] - exact) <= 1e-3 * size)  # TF32 products, if they are on, are off by 2^-11 a factor
 
 
 def test_rows_far_into_a_large_buffer():
