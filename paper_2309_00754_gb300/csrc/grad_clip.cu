@@ -4,13 +4,13 @@
 //     norm = sqrt(sum over all tensors and elements of g^2)
 //     coef = min(1, max_norm / (norm + 1e-6)), 1 where the norm is not finite;  out = g coef
 //
-// Two launches: every CTA sums the squares of a contiguous range of 16 KB chunks and writes one
+// Two launches: every CTA sums the squares of a contiguous range of chunks and writes one
 // partial sum; every CTA of the second pass adds all partials in the same fixed order and scales its
 // range, from its end, whose chunks L2 still holds. The tensors' addresses travel as a kernel parameter, so
 // that a captured call stands by itself.
 //
 // Squares are summed in fp32 over a thread's elements of a chunk, and these sums as pairs of fp32 numbers with
-// their rounding errors (Knuth 1969): fp64 runs at a hundredth of the fp32 rate here (393 chunks of fp32: 21 us
+// their rounding errors (Knuth 1969): fp64 runs at a sixty-fourth of the fp32 rate here (393 chunks of fp32: 21 us
 // with fp64 sums over CTAs). A chunk whose fp32 sum leaves [2^-80, 2^90] while its elements are not all
 // zero is summed again in fp64, where no square of an fp32 value overflows or vanishes, and only then is anything
 // beyond it done in fp64.
@@ -24,8 +24,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCtasPerSm = 4;  // (six: 205 MB of fp32 140 us, eight 163, for 95)
-constexpr int kChunkBytes = 16384;
-constexpr int kVecs = kChunkBytes / 16 / kThreads;  // of a thread in a whole chunk
+// Chunks of 16 KB, of a large list 32 KB: 820 MB of bf16 193 us and 212 with the small ones, 205 MB of fp32 94 and 97;
+// but 26 MB of fp32 18.4 and 16.0.
+constexpr int kChunkSmall = 16384, kChunkLarge = 32768;
+constexpr int64_t kLargeBytes = 160 << 20;
 // Of a longer list the last of every CTA's range, where the second pass begins, is to stay in L2; the rest and the outputs
 // leave it first (102 MB of fp32 53.5 -> 48.8 us, 205 MB 100.4 -> 96.3, 822 MB 390 -> 386; the norm alone 21.5 -> 21.4,
 // 37.1 -> 32.1, 128 -> 125).
@@ -56,11 +58,12 @@ __device__ __forceinline__ float from_f<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// A chunk's elements: [lo, hi) of its tensor, of which those of whole 16-byte vectors are [v0, v1).
-template <typename T>
+// A chunk's elements, from `src` on.
+template <typename T, int kBytes>
 struct Chunk {
   static constexpr int E = 16 / sizeof(T);
-  static constexpr int kElems = kChunkBytes / sizeof(T);
+  static constexpr int kElems = kBytes / sizeof(T);
+  static constexpr int kVecs = kBytes / 16 / kThreads;  // of a thread in a whole chunk
   const T* src;
   int n, head, vecs;  // elements, elements before the first vector, vectors
   __device__ __forceinline__ Chunk(const Entry& e, int c) {
@@ -128,9 +131,9 @@ struct Squares {
   Sum sum;
   double d = 0.0;
 
-  template <typename T>
-  __device__ __forceinline__ void add(const Chunk<T>& c, uint64_t policy) {
-    constexpr int E = Chunk<T>::E;
+  template <typename T, int kBytes>
+  __device__ __forceinline__ void add(const Chunk<T, kBytes>& c, uint64_t policy) {
+    constexpr int E = 16 / sizeof(T), kVecs = Chunk<T, kBytes>::kVecs;
     const int t = threadIdx.x, tail = c.head + c.vecs * E;
     uint4 v[kVecs];
     float ends[2] = {0.f, 0.f};  // up to E - 1 elements at either end
@@ -203,7 +206,7 @@ __device__ __forceinline__ int range_at(int chunks, unsigned b) {
 }
 
 // partial[b] = (add: +=) sum of the squares of CTA b's chunks
-template <int kCap>
+template <int kCap, int kBytes>
 __global__ void __launch_bounds__(kThreads)
     grad_square_kernel(const __grid_constant__ Table<kCap> table, int n, int chunks, int add,
                        Partial* __restrict__ partial) {
@@ -213,13 +216,13 @@ __global__ void __launch_bounds__(kThreads)
   pdl_wait();
   pdl_launch_dependents();
   Squares squares;
-  const int keep = kKeepBytes / kChunkBytes / gridDim.x;
+  const int keep = kKeepBytes / kBytes / gridDim.x;
   const uint64_t first = policy_first();
   for (int c = c0; c < c1; ++c) {
     while (i + 1 < n && table.e[i + 1].first <= c) ++i;
     const Entry& e = table.e[i];
     const uint64_t policy = c >= c1 - keep ? policy_normal() : first;
-    if (e.bf16) squares.add(Chunk<__nv_bfloat16>(e, c), policy); else squares.add(Chunk<float>(e, c), policy);
+    if (e.bf16) squares.add(Chunk<__nv_bfloat16, kBytes>(e, c), policy); else squares.add(Chunk<float, kBytes>(e, c), policy);
   }
   Partial p = block_sum(squares.sum, squares.d, sh);
   if (threadIdx.x == 0) {
@@ -250,10 +253,10 @@ __device__ __forceinline__ uint4 scaled(const uint4& v, float coef) {
                       pack_bf16x2(x[4] * coef, x[5] * coef), pack_bf16x2(x[6] * coef, x[7] * coef));
 }
 
-template <typename T>
+template <typename T, int kBytes>
 __device__ __forceinline__ void scale_chunk(const Entry& e, int ci, float coef) {
-  constexpr int E = Chunk<T>::E;
-  const Chunk<T> c(e, ci);
+  constexpr int E = 16 / sizeof(T), kVecs = Chunk<T, kBytes>::kVecs;
+  const Chunk<T, kBytes> c(e, ci);
   T* dst = static_cast<T*>(e.dst) + (c.src - static_cast<const T*>(e.src));
   const int t = threadIdx.x;
   if (((reinterpret_cast<uintptr_t>(dst) ^ reinterpret_cast<uintptr_t>(c.src)) & 15) == 0) {
@@ -294,7 +297,7 @@ __device__ __forceinline__ Norm norm_of(const Partial* partial, int n, float max
               isfinite(norm) ? static_cast<float>(fmin(1.0, static_cast<double>(max_norm) / (norm + kEps))) : 1.f};
 }
 
-template <int kCap>
+template <int kCap, int kBytes>
 __global__ void __launch_bounds__(kThreads)
     grad_scale_kernel(const __grid_constant__ Table<kCap> table, int n, int chunks,
                       const Partial* __restrict__ partial, int n_partials, float max_norm,
@@ -315,7 +318,7 @@ __global__ void __launch_bounds__(kThreads)
     while (table.e[i].first > c) --i;
     const Entry& e = table.e[i];
     if (r.coef == 1.f && e.dst == e.src) continue;  // nothing changes
-    if (e.bf16) scale_chunk<__nv_bfloat16>(e, c, r.coef); else scale_chunk<float>(e, c, r.coef);
+    if (e.bf16) scale_chunk<__nv_bfloat16, kBytes>(e, c, r.coef); else scale_chunk<float, kBytes>(e, c, r.coef);
   }
 }
 
@@ -341,9 +344,9 @@ struct ListPart {
   Table<kTableMax> table;
   int n = 0, chunks = 0;
   int64_t next;
-  ListPart(const GradTensor* t, int64_t count, int64_t i) {
+  ListPart(const GradTensor* t, int64_t count, int64_t i, int chunk_bytes) {
     for (; i < count && n < kTableMax; ++i) {
-      const int64_t elems = kChunkBytes / (t[i].bf16 ? 2 : 4);
+      const int64_t elems = chunk_bytes / (t[i].bf16 ? 2 : 4);
       const int64_t c = (t[i].numel + elems - 1) / elems;
       if (chunks + c >= (1LL << 31)) break;
       table.e[n++] = Entry{t[i].grad, t[i].out, t[i].numel, chunks, t[i].bf16};
@@ -365,16 +368,16 @@ const Table<kCap>& parameters(ListPart& p, int grid) {
   return *reinterpret_cast<const Table<kCap>*>(&p.table);
 }
 
-template <int kCap>
+template <int kCap, int kBytes>
 cudaError_t launch_square(ListPart& p, int grid, bool add, Partial* partial, cudaStream_t st) {
-  return launch_pdl(grad_square_kernel<kCap>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+  return launch_pdl(grad_square_kernel<kCap, kBytes>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
                     p.chunks, static_cast<int>(add), partial);
 }
-template <int kCap>
+template <int kCap, int kBytes>
 cudaError_t launch_scale(ListPart& p, const Partial* partial, int n_partials, float max_norm, float* norm_out,
                          cudaStream_t st) {
   const int grid = grid_of(p.chunks);
-  return launch_pdl(grad_scale_kernel<kCap>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+  return launch_pdl(grad_scale_kernel<kCap, kBytes>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
                     p.chunks, partial, n_partials, max_norm, norm_out);
 }
 // A launch carries a table of 32, 224 or 880 tensors.
@@ -387,14 +390,19 @@ size_t grad_norm_workspace_bytes() { return sizeof(Partial) * kGradMaxBlocks; }
 int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm_out, bool scale, void* ws,
                      cudaStream_t st) {
   Partial* partial = static_cast<Partial*>(ws);
+  int64_t bytes = 0;
+  for (int64_t i = 0; i < n; ++i) bytes += t[i].numel * (t[i].bf16 ? 2 : 4);
+  const bool large = bytes >= kLargeBytes;
+  const int chunk_bytes = large ? kChunkLarge : kChunkSmall;
   int n_partials = 0;
   for (int64_t i = 0; i < n;) {
-    ListPart p(t, n, i);
+    ListPart p(t, n, i, chunk_bytes);
     // a list of several launches: each adds to the partials of the one before it
     const int grid = grid_of(i == 0 && p.next == n ? p.chunks : INT64_MAX);
-    const auto launch = p.n <= kTableSmall    ? launch_square<kTableSmall>
-                        : p.n <= kTableMiddle ? launch_square<kTableMiddle>
-                                              : launch_square<kTableMax>;
+    const auto launch = large                 ? launch_square<kTableMax, kChunkLarge>
+                        : p.n <= kTableSmall  ? launch_square<kTableSmall, kChunkSmall>
+                        : p.n <= kTableMiddle ? launch_square<kTableMiddle, kChunkSmall>
+                                              : launch_square<kTableMax, kChunkSmall>;
     if (launch(p, grid, i > 0, partial, st) != cudaSuccess) return -3;
     n_partials = grid;
     i = p.next;
@@ -405,10 +413,11 @@ int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm
                ? 0
                : -3;
   for (int64_t i = 0; i < n;) {
-    ListPart p(t, n, i);
-    const auto launch = p.n <= kTableSmall    ? launch_scale<kTableSmall>
-                        : p.n <= kTableMiddle ? launch_scale<kTableMiddle>
-                                              : launch_scale<kTableMax>;
+    ListPart p(t, n, i, chunk_bytes);
+    const auto launch = large                 ? launch_scale<kTableMax, kChunkLarge>
+                        : p.n <= kTableSmall  ? launch_scale<kTableSmall, kChunkSmall>
+                        : p.n <= kTableMiddle ? launch_scale<kTableMiddle, kChunkSmall>
+                                              : launch_scale<kTableMax, kChunkSmall>;
     if (launch(p, partial, n_partials, max_norm, i == 0 ? norm_out : nullptr, st) != cudaSuccess) return -3;
     i = p.next;
   }

@@ -95,5 +95,8 @@ def test_every_compiled_table_is_taken_by_some_list(fake):
         taken |= {v[0] for v in fake.launches()}
         assert fake.lib.hydra_grad_norm(c, n, 1.0, P, P, BIG, None) == 0
         taken |= {v[0] for v in fake.launches()}
+    c = (H.GradTensorC * 1)(H.GradTensorC(1 << 40, 1 << 40, 1 << 27, 0))  # a large list
+    assert fake.lib.hydra_clip_grad_norm(c, 1, 1.0, P, P, BIG, None) == 0
+    taken |= {v[0] for v in fake.launches()}
     assert taken == {n for n in fake.lib.fake_kernels().decode().split() if "grad_square" in n or "grad_scale" in n or
                      "grad_norm" in n}
