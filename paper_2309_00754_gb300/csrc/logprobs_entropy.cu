@@ -107,6 +107,15 @@ __device__ __forceinline__ float order_value(uint32_t k) {
   if (k == kNanKey) return kNan;
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
+// Whether a value's order_key is not below `least`, without working the key out.
+struct AtLeast {
+  float value;    // not below it
+  bool nan_only;  // least is beyond +inf
+  __device__ __forceinline__ explicit AtLeast(uint32_t least)
+      : value(order_value(least)), nan_only(least > order_key(kInf)) {}
+  __device__ __forceinline__ bool operator()(float v) const { return nan_only ? v != v : !(v < value); }
+};
+
 // A row's elements in slots of 16 bytes on the address grid: slot j holds elements
 // [j E - a, j E - a + E), the first and the last of them possibly in part.
 template <typename T>
@@ -147,13 +156,13 @@ struct Row {
       }
     }
   }
-  // a bit for each element of slot j whose order_key is not below `least`
-  __device__ __forceinline__ uint32_t at_least(const uint4& v, int j, uint32_t least) const {
+  // a bit for each element of slot j that is `enough`
+  __device__ __forceinline__ uint32_t which(const uint4& v, int j, const AtLeast& enough) const {
     float f[E];
     unpack(v, f);
     uint32_t mask = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) mask |= (order_key(f[e]) >= least ? 1u : 0u) << e;
+    for (int e = 0; e < E; ++e) mask |= (enough(f[e]) ? 1u : 0u) << e;
     const int i = first(j);
     if (i < 0) mask &= ~0u << -i;
     if (i + E > V) mask &= (1u << (V - i)) - 1;
@@ -448,8 +457,13 @@ __device__ __forceinline__ int segment_stages(const Part& part) {
   return ((part.hi - part.lo + kStageSlots - 1) / kStageSlots + kSegments - 1) / kSegments;
 }
 
-// The sum of v over the lanes below, and over all of them.
+// The sum of v over the lanes below, and over all of them. Mostly no lane has more than one.
 __device__ __forceinline__ int scan(int v, int lane, int& total) {
+  const uint32_t some = __ballot_sync(0xffffffffu, v != 0);
+  if (!__any_sync(0xffffffffu, v > 1)) {
+    total = __popc(some);
+    return __popc(some & ((1u << lane) - 1));
+  }
   int sum = v;
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
@@ -478,6 +492,7 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
   for (;;) {
     const bool none = above && bound == kNanKey;  // is above it
     const uint32_t least = above ? bound + 1 : max(bound, 1u);
+    const AtLeast enough(least);
     e.best[lane] = 0;
     int asked, found = 0;
     uint32_t is = 0;  // a bit for each warp's summer of this lane
@@ -493,7 +508,7 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
 #pragma unroll
       for (int q = 0; q < kSegments; ++q)
         if (part.lo + q * stages * kStageSlots + summer < part.hi)
-          is |= (order_key(__bfloat162float(e.segment[q][summer])) >= least ? 1u : 0u) << q;
+          is |= (enough(__bfloat162float(e.segment[q][summer])) ? 1u : 0u) << q;
       if (x0 + lane >= asked) is = 0;
       int owners;
       for (int at = scan(__popc(is), lane, owners); is != 0; is &= is - 1)
@@ -525,7 +540,7 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
           int hits = 0;
 #pragma unroll
           for (int g = 0; g < G; ++g)
-            if (j[g] >= part.hi || order_key(Row<T>::max_of(v[g])) < least) j[g] = -1; else ++hits;
+            if (j[g] >= part.hi || !enough(Row<T>::max_of(v[g]))) j[g] = -1; else ++hits;
           int slots;
           int at = scan(hits, lane, slots);
 #pragma unroll
@@ -538,7 +553,7 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
           for (int h0 = 0; h0 < slots; h0 += 32) {
             const int slot = h0 + lane < slots ? e.hit_slot[h0 + lane] : 0;
             uint32_t mask = 0;
-            if (h0 + lane < slots) mask = r.at_least(e.hit[h0 + lane], slot, least);
+            if (h0 + lane < slots) mask = r.which(e.hit[h0 + lane], slot, enough);
             int more;
             int c = found + scan(__popc(mask), lane, more);
             found += more;
@@ -584,15 +599,16 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
   }
   // the first values that equal the bound, in the segments that may hold some
   int place = __popc(__ballot_sync(0xffffffffu, e.best[lane] != 0));
+  const AtLeast equal(bound);  // or above, where no more are
   for (int j0 = part.lo; j0 < part.hi && place < k; j0 += 32) {
     const int j = j0 + lane, in = j - part.lo;
-    const bool may = j < part.hi && order_key(__bfloat162float(e.segment[in / (stages * kStageSlots)][in % kSummers])) >= bound;
+    const bool may = j < part.hi && equal(__bfloat162float(e.segment[in / (stages * kStageSlots)][in % kSummers]));
     if (!__any_sync(0xffffffffu, may)) continue;
     uint32_t mask = 0;
     if (may) {
       const uint4 v = r.load(j);
-      mask = r.at_least(v, j, bound);
-      if (bound != kNanKey) mask &= ~r.at_least(v, j, bound + 1);
+      mask = r.which(v, j, equal);
+      if (bound != kNanKey) mask &= ~r.which(v, j, AtLeast(bound + 1));
     }
     int more;
     int at = place + scan(__popc(mask), lane, more);
@@ -844,7 +860,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
         if (e.id < 0 || e.id >= V) record_error(err, kDevBadTokenId); else z_id = to_f(r.p[e.id]);
       }
       Stats st = lane < kWarps ? Stats{sh.red[f][0][lane], sh.red[f][1][lane], sh.red[f][2][lane]} : Stats{-kInf, 0.f, 0.f};
-      st.merge_lanes(32);
+      st.merge_lanes(kWarps);
       const uint64_t best = select_top<T>(e, r, Part(r.n_slots, rank, bits), out.k, lane);
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&e.free));
@@ -941,7 +957,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
       summers_sync();
       if (warp == 0) {
         st = lane < kWarps ? Stats{sh.red[buf][0][lane], sh.red[buf][1][lane], sh.red[buf][2][lane]} : Stats{-kInf, 0.f, 0.f};
-        st.merge_lanes(32);
+        st.merge_lanes(kWarps);
         finish<kTop>(sh, top, out, in.row, st, z_id, 0, rank, cs, lane, err);
       }
     }
