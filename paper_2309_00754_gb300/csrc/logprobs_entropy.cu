@@ -10,15 +10,15 @@
 // The rows come through a ring of 16 KB stages that one warp fills with bulk copies, rows ahead of the
 // eight warps that sum them: 256 threads with a maximum and two sums each, whose parts one warp puts
 // together. Four CTAs an SM take every 608th row. 2 % of the threads' time is waiting where the row is
-// fp32 (4096 x 32000: 76.5 us, all of the measured HBM rate); bf16 needs 8.4 instructions an element
-// (8192 x 32000: 83 us, 93 %). Few rows are shared by clusters, which meet in the first CTA's memory.
+// fp32 (4096 x 32000: 76.5 to 79.5 us, 97 to 101 % of the measured HBM rate); bf16 needs 8.4 instructions an element
+// (8192 x 32000: 82.7 us, 94 %). Few rows are shared by clusters, which meet in the first CTA's memory.
 //
 // The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps its best
 // value of each eighth of the row. A bound that k of the 256 threads reach holds for the k-th best element,
 // too; the eighths that reach it, about k, are read again, and the few elements not behind it are ranked by
 // counting. Three warps of a CTA do that, a row each, while the others are in the next rows, as it takes
-// 3 to 8 us, most of it one step waiting for the one before. Two such CTAs fit an SM (8192 x 32000 bf16,
-// k = 8: 103 us; in the summing threads themselves 130, with one such warp a CTA 160).
+// 3 to 8 us, most of it one step waiting for the one before. Two such CTAs fit an SM (4096 x 32000 fp32, k = 8:
+// 81 us; 8192 x 32000 bf16 101, three CTAs of fewer registers 113; selected by the summing threads themselves 130).
 //
 // Backward, with p = exp((z - m) - log s):
 //     dz[v] = g_logp (1[v = id] - p_v) - g_entropy p_v (log p_v + entropy)
@@ -64,6 +64,12 @@ __device__ __forceinline__ float exp2_fast(float x) {  // 2 ulp
 __device__ __forceinline__ uint64_t pack2(float a, float b) {
   uint64_t r;
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+// v twice, kept: the compiler would build it again for every pair
+__device__ __forceinline__ uint64_t twice(float v) {
+  uint64_t r;
+  asm volatile("mov.b64 %0, {%1, %1};" : "=l"(r) : "f"(v));
   return r;
 }
 __device__ __forceinline__ float2 unpack2(uint64_t v) {
@@ -872,8 +878,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
   int q = 0, buf = 0;
   uint32_t parity = 0, used = 0;  // used: bit 0 of how often both buffers were filled, bit 1 whether they were
   float z_id = 0.f;
-  uint64_t log2e;  // twice; kept, as it is not built again for every pair
-  asm volatile("mov.b64 %0, {%1, %1};" : "=l"(log2e) : "f"(kLog2e));
+  const uint64_t log2e = twice(kLog2e);
   Running<T> run;
   float segment = -kInf;  // the thread's maximum of the segment so far
   bool holds = false;     // whether it has any slot
@@ -982,7 +987,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
 }
 
 constexpr int kUnit = 8;  // elements a lane turns at once
-constexpr int kTileUnits = 8;  // units a lane takes of a tile, four under way at once
+constexpr int kTileUnits = 8;  // units a lane takes of a tile
 constexpr int kTile = 32 * kUnit * kTileUnits;
 constexpr int kGradWarps = 8;
 
@@ -1031,8 +1036,8 @@ struct RowGrad {
 
 // A warp takes a tile of a row. Units lie on the 16-byte grid of both arrays where their rows start alike on it
 // (`a` elements before the row); else every element goes by itself.
-// Memory bounds it: 2048 x 32000 fp32 80 us (97 % of measured HBM), fp32 to bf16 59.5 (97 %), bf16 44.6 (87 %; 62.8
-// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 11.6 now).
+// Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 60 (96 %), bf16 42 (92 %; 62.8
+// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.7 now).
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(kGradWarps * 32, 4)
     token_stats_grad_kernel(const TI* logits, long long ld, unsigned L, int V, unsigned tiles, unsigned items,
@@ -1040,7 +1045,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
                             const float* __restrict__ norm, const float* __restrict__ entropy,
                             const float* __restrict__ grad_logp, const float* __restrict__ grad_entropy,
                             TO* dlogits, long long ld_d, int* err) {
-  constexpr int G = 4;
+  constexpr int G = sizeof(TI) + sizeof(TO) == 4 ? 8 : 4;  // units under way at once (bf16 to bf16: 44.3 us with four)
   pdl_wait();
   pdl_launch_dependents();
   const unsigned item = blockIdx.x * (blockDim.x / 32) + (threadIdx.x >> 5);
@@ -1091,9 +1096,10 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
   const float mref = g.m * kLog2e;
   const float rest = fmaf(g.m, kLog2e, -mref) + g.c * kLog2e;
   const float low = g.m + kFloor - 0x1p-6f * fabsf(g.m);  // values below it count as it: p = 0
-  const uint64_t log2e = pack2(kLog2e, kLog2e), nref = pack2(-mref, -mref), nrest = pack2(-rest, -rest);
-  const float slope = -g.gh * kLn2, base = -(g.gl + g.gh * g.h);
-  const uint64_t slope2 = pack2(slope, slope), base2 = pack2(base, base);
+  const uint32_t low2 = pack_bf16x2(low, low);
+  const uint64_t log2e = twice(kLog2e), nref = twice(-mref), nrest = twice(-rest);
+  const uint64_t slope = twice(-g.gh * kLn2), base = twice(-(g.gl + g.gh * g.h));
+  const int unit = g.logp ? g.id - i0 : -1;  // the token's place in the tile
 #pragma unroll 1
   for (int u0 = 0; u0 < kTileUnits; u0 += G) {
     if (i0 + u0 * 32 * kUnit >= V) return;
@@ -1106,6 +1112,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
 #pragma unroll
     for (int u = 0; u < G; ++u) {
       const int i = i0 + ((u0 + u) * 32 + lane) * kUnit;
+      if (i0 + (u0 + u) * 32 * kUnit >= V) return;
       if (i >= 0 && i <= V - kUnit) {
         uint64_t o[kUnit / 2] = {};
         if (live) {
@@ -1117,14 +1124,14 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
               z2 = pack2(max_nan(__uint_as_float(q % 2 ? x.z : x.x), low), max_nan(__uint_as_float(q % 2 ? x.w : x.y), low));
             } else {
               const uint4& x = v[u][0];
-              const uint32_t c = max_nan_bf16x2(q == 0 ? x.x : q == 1 ? x.y : q == 2 ? x.z : x.w, pack_bf16x2(low, low));
+              const uint32_t c = max_nan_bf16x2(q == 0 ? x.x : q == 1 ? x.y : q == 2 ? x.z : x.w, low2);
               z2 = pack2(__uint_as_float(c << 16), __uint_as_float(c & 0xffff0000u));
             }
             const uint64_t x2 = add2(fma2(z2, log2e, nref), nrest);
             const float2 x = unpack2(x2);
-            o[q] = mul2(pack2(exp2_fast(x.x), exp2_fast(x.y)), fma2(x2, slope2, base2));
+            o[q] = mul2(pack2(exp2_fast(x.x), exp2_fast(x.y)), fma2(x2, slope, base));
           }
-          if (static_cast<unsigned>(g.id - i) < kUnit && g.logp) {
+          if (unit >= 0 && unit / kUnit == (u0 + u) * 32 + lane) {
 #pragma unroll
             for (int q = 0; q < kUnit / 2; ++q) {
               float2 x = unpack2(o[q]);
@@ -1135,7 +1142,7 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
           }
         }
         store_unit(d + i, o);
-      } else {
+      } else if (i < V) {
         for (int e = max(i, 0); e < min(i + kUnit, V); ++e) d[e] = from_f<TO>(live ? g.value(to_f(z[e]), e) : 0.f);
       }
     }
