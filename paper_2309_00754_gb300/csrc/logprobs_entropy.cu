@@ -260,6 +260,14 @@ struct Running {
     }
   }
 
+  __device__ __forceinline__ static bool all_are(const uint32_t* r, int n, float v) {
+    const uint32_t want = sizeof(T) == 4 ? __float_as_uint(v) : pack_bf16x2(v, v);
+    uint32_t other = 0;
+#pragma unroll
+    for (int i = 0; i < 4 * n; ++i) other |= r[i] ^ want;
+    return other == 0;
+  }
+
   __device__ __forceinline__ void add_pair(uint64_t z2, uint64_t log2e) {
     const uint64_t x2 = fma2(z2, log2e, nref);
     const float2 x = unpack2(x2);
@@ -286,6 +294,11 @@ struct Running {
           add_pair(pack2(__uint_as_float(c << 16), __uint_as_float(c & 0xffff0000u)), log2e);
         }
       }
+    } else if (from < kInf && all_are(r, n, from)) {
+      // masked with the type's lowest value, and nothing above it yet: x = 0 (420 x 32000 bf16, k = 20: 17 us, 104
+      // with the terms below and all elements of a row collected before the top is found to be too many)
+      const float count = n * (Row<T>::E / 2);
+      s = add2(s, pack2(count, count));
     } else {
       const float base = -unpack2(nref).x;
 #pragma unroll 1
@@ -507,7 +520,7 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
     for (int at = scan(__popc(is), lane, asked); is != 0; is &= is - 1)
       e.asked[at++] = static_cast<uint16_t>((__ffs(is) - 1) * 32 + lane);
     __syncwarp();
-    for (int x0 = 0; x0 < asked; x0 += 32) {
+    for (int x0 = 0; x0 < asked && found <= kCandidates; x0 += 32) {
       // their segments that hold candidates: up to kSegments a lane
       const int summer = x0 + lane < asked ? e.asked[x0 + lane] : 0;
       is = 0;
@@ -521,10 +534,10 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
         e.owner[at++] = static_cast<uint16_t>((__ffs(is) - 1) << 10 | summer);
       __syncwarp();
 #pragma unroll 1
-      for (int i0 = 0; i0 < each; i0 += 1 << bits) {
+      for (int i0 = 0; i0 < each && found <= kCandidates; i0 += 1 << bits) {
         const int i = i0 + (lane & ((1 << bits) - 1));
 #pragma unroll 1
-        for (int g0 = 0; g0 < owners; g0 += G * at_once) {
+        for (int g0 = 0; g0 < owners && found <= kCandidates; g0 += G * at_once) {  // more than fit: enough is known
           uint4 v[G];
           int j[G];
           bool in_part = false;
@@ -1026,6 +1039,11 @@ struct RowGrad {
   int id;
   bool logp;
 
+  // an element that is not the token's, for any m
+  __device__ __forceinline__ float other(float z) const {
+    const float lp = max_nan((z - m) - c, kFloor);
+    return -exp2_fast(lp * kLog2e) * ((gl + gh * h) + gh * lp);
+  }
   // one element: 1 - p of a token that is nearly certain, and any m
   __device__ __forceinline__ float value(float z, int i) const {
     const float lp = max_nan((z - m) - c, kFloor);
@@ -1038,6 +1056,33 @@ struct RowGrad {
 // (`a` elements before the row); else every element goes by itself.
 // Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 60 (96 %), bf16 42 (92 %; 62.8
 // when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.7 now).
+// A tile of a row whose x would be rounded apart, or of rows that do not lie alike on the grid: a call, as its registers
+// would slow the kernel down (2048 x 32000 bf16: 42.3 us, 44.9 with it in line).
+template <typename TI, typename TO>
+__device__ __noinline__ void tile_apart(const TI* z, TO* d, int i0, int V, bool together, bool live, const RowGrad& g,
+                                        int lane) {
+  const int hi = min(i0 + kTile, V);
+  if (together) {  // mostly a row of which a mask of the type's lowest value leaves nothing (7092 x 1736, a third of the
+                   // rows such: 43 us an element at a time, 21 so)
+#pragma unroll 2
+    for (int i = i0 + lane * kUnit; i < hi; i += 32 * kUnit) {
+      if (i >= 0 && i <= V - kUnit && (!g.logp || g.id < i || g.id >= i + kUnit)) {
+        uint4 v[sizeof(TI) / 2];
+        uint64_t o[kUnit / 2];
+        load_unit(z + i, v);
+#pragma unroll
+        for (int q = 0; q < kUnit / 2; ++q)
+          o[q] = pack2(g.other(element<TI>(v, 2 * q)), g.other(element<TI>(v, 2 * q + 1)));
+        store_unit(d + i, o);
+      } else {
+        for (int e = max(i, 0); e < min(i + kUnit, V); ++e) d[e] = from_f<TO>(g.value(to_f(z[e]), e));
+      }
+    }
+  } else {
+    for (int i = max(i0, 0) + lane; i < hi; i += 32) d[i] = from_f<TO>(live ? g.value(to_f(z[i]), i) : 0.f);
+  }
+}
+
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(kGradWarps * 32, 4)
     token_stats_grad_kernel(const TI* logits, long long ld, unsigned L, int V, unsigned tiles, unsigned items,
@@ -1088,9 +1133,9 @@ __global__ void __launch_bounds__(kGradWarps * 32, 4)
                         (phase_o - a) % static_cast<int>(16 / sizeof(TO)) == 0;
   const int i0 = tile * kTile - a;  // the tile's first element (below 0 in a first one)
   // beyond, z log2 e and the rest of x are rounded apart
-  if (!together || (live && !(fabsf(g.m) < 0x1p20f))) {
-    const int hi = min(i0 + kTile, V);
-    for (int i = max(i0, 0) + lane; i < hi; i += 32) d[i] = from_f<TO>(live ? g.value(to_f(z[i]), i) : 0.f);
+  const bool huge = live && !(fabsf(g.m) < 0x1p20f);
+  if (!together || huge) {
+    tile_apart<TI, TO>(z, d, i0, V, together, live, g, lane);
     return;
   }
   const float mref = g.m * kLog2e;

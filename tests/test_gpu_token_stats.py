@@ -226,6 +226,44 @@ def test_stats_of_large_and_infinite_logits(dtype):
     assert o["top_ids"][4, 0] == 77 and o["top_ids"][5, :2].tolist() == [55, 99]
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(1, 32000), (40, 32001), (700, 4100)])
+def test_masks_of_the_lowest_value_that_leave_few_tokens(rows, V, dtype):
+    """None, one, fewer than k, just k or a few more tokens left, -inf beside the lowest value, all -inf but one and
+    another row of the largest value: the statistics, the top and the gradient."""
+    k, t = 20, DTYPES[dtype]
+    rng = np.random.default_rng(V)
+    low, high = float(torch.finfo(t).min), float(torch.finfo(t).max)
+    z = np.full((rows, V), low)
+    for n in range(rows):
+        left = [0, 1, 7, 0, 20, 23, 300, 0][n % 8]
+        at = rng.choice(V, left, replace=False)
+        if n % 8 == 3:
+            z[n, rng.random(V) < 0.5] = -INF  # equal weights on the rest
+        elif n % 8 == 7:
+            z[n] = high if n % 16 == 7 else -INF
+            z[n, V // 3] = low if n % 16 == 15 else high
+        z[n, at] = rng.normal(0, 3, left)
+    dev, _ = rows_of(z, t)
+    values, ids = host_f64(dev), rng.integers(0, V, rows)
+    check_stats(run_stats(dev, ids, None, rows, 1, k), values, ids, None, rows, 1, k)
+    gl, gh = (rng.normal(size=rows).astype(np.float32) for _ in range(2))
+    r = O.token_stats(values, None, None, rows, 1)
+    for t_out in DTYPES.values():
+        d, _ = run_grad(dev, ids, None, rows, 1, r["norm"], r["entropy"], gl, gh, t_out)
+        check_grad(d, values, ids, None, rows, 1, r, gl.astype(float), gh.astype(float))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_of_nothing_but_positive_infinity(dtype):
+    z, _ = rows_of(np.full((2, 5000), INF), DTYPES[dtype])
+    o = run_stats(z, np.zeros(2, np.int64), None, 2, 1, 3)
+    for key in ("logp", "entropy", "top_logp"):
+        assert torch.isnan(o[key]).all(), key
+    assert torch.isnan(o["norm"][:, 1]).all()
+    assert o["top_ids"].tolist() == [[0, 1, 2]] * 2
+
+
 def test_stats_outputs_one_by_one_and_dead_rows():
     """Each output alone equals it among all; rows behind a sequence's end are not read (NaN there)."""
     S, L, V, k = 3, 4, 5001, 6
