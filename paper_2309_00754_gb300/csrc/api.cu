@@ -142,18 +142,24 @@ bool token_rows_ok(int64_t S, int64_t L, int64_t V, int64_t ld) {
 // A tensor's memory range in a list of gradients.
 struct Span {
   uintptr_t lo, hi;
-  bool written;
 };
 
-// Whether a range that is written overlaps any other one.
-bool spans_clash(std::vector<Span>& v) {
+// Whether a range of `out` overlaps another of it or one of `in`. Each in ascending order is the usual list; a sort of
+// the two together costs twice the checks of the arguments.
+bool spans_clash(std::vector<Span>& out, std::vector<Span>& in) {
   const auto before = [](const Span& a, const Span& b) { return a.lo < b.lo; };
-  if (!std::is_sorted(v.begin(), v.end(), before)) std::sort(v.begin(), v.end(), before);
-  uintptr_t end = 0, end_written = 0;
-  for (const Span& s : v) {
-    if (s.lo < (s.written ? end : end_written)) return true;
-    end = std::max(end, s.hi);
-    if (s.written) end_written = std::max(end_written, s.hi);
+  for (std::vector<Span>* v : {&out, &in})
+    if (!std::is_sorted(v->begin(), v->end(), before)) std::sort(v->begin(), v->end(), before);
+  uintptr_t end = 0, end_out = 0;  // of all ranges so far, and of those of `out`
+  for (size_t i = 0, j = 0; i < out.size() || j < in.size();) {
+    if (j == in.size() || (i < out.size() && out[i].lo <= in[j].lo)) {
+      if (out[i].lo < end) return true;
+      end_out = out[i++].hi;
+      end = std::max(end, end_out);
+    } else {
+      if (in[j].lo < end_out) return true;
+      end = std::max(end, in[j++].hi);
+    }
   }
   return false;
 }
@@ -169,9 +175,12 @@ hydra_status grad_norm_impl(const hydra_grad_tensor* tensors, int64_t n, float m
     return HYDRA_ERR_WORKSPACE;
   std::vector<hydra::GradTensor> list;
   try {
-    std::vector<Span> spans;
+    std::vector<Span> out, in;
     list.reserve(static_cast<size_t>(n));
-    if (clip) spans.reserve(2 * static_cast<size_t>(n));
+    if (clip) {
+      out.reserve(static_cast<size_t>(n));
+      in.reserve(static_cast<size_t>(n));
+    }
     for (int64_t i = 0; i < n; ++i) {
       const hydra_grad_tensor& t = tensors[i];
       if (t.dtype != HYDRA_F32 && t.dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
@@ -183,11 +192,11 @@ hydra_status grad_norm_impl(const hydra_grad_tensor* tensors, int64_t n, float m
       if (src % size != 0 || (clip && dst % size != 0)) return HYDRA_ERR_ALIGN;
       list.push_back({t.grad, t.out, t.numel, t.dtype == HYDRA_BF16});
       if (clip) {
-        spans.push_back({dst, dst + bytes, true});
-        if (src != dst) spans.push_back({src, src + bytes, false});
+        out.push_back({dst, dst + bytes});
+        if (src != dst) in.push_back({src, src + bytes});
       }
     }
-    if (clip && spans_clash(spans)) return HYDRA_ERR_RANGE;
+    if (clip && spans_clash(out, in)) return HYDRA_ERR_RANGE;
   } catch (const std::bad_alloc&) {
     return HYDRA_ERR_SHAPE;  // no host memory for a list of this length
   }

@@ -339,10 +339,10 @@ int grid_of(int64_t chunks) {
   return static_cast<int>(std::min(std::max<int64_t>(chunks, 1), most));
 }
 
-// One launch's part of the list: up to kTableMax tensors from `i` on, and under 2^31 chunks.
+// One launch's part of the list: up to kTableMax tensors from `i` on, and under 2^31 chunks, for a grid of CTAs.
 struct ListPart {
   Table<kTableMax> table;
-  int n = 0, chunks = 0;
+  int n = 0, chunks = 0, grid = 0;
   int64_t next;
   ListPart(const GradTensor* t, int64_t count, int64_t i, int chunk_bytes) {
     for (; i < count && n < kTableMax; ++i) {
@@ -354,30 +354,35 @@ struct ListPart {
     }
     next = i;
   }
+  // the first tensor of each CTA's range; range_at without a division a CTA
+  void deal(int ctas) {
+    grid = ctas;
+    const int each = chunks / grid, rest = chunks % grid;
+    for (int b = 0, c = 0, part = 0, i = 0; b < grid; ++b) {
+      while (i + 1 < n && table.e[i + 1].first <= c) ++i;
+      table.start[b] = static_cast<uint16_t>(i);
+      c += each;
+      part += rest;
+      if (part >= grid) {
+        part -= grid;
+        ++c;
+      }
+    }
+  }
+  // Table<kCap>'s layout is the front of every larger one's
+  template <int kCap>
+  const Table<kCap>& parameters() const { return *reinterpret_cast<const Table<kCap>*>(&table); }
 };
 
-// The part as the parameters of `grid` CTAs. Table<kCap>'s layout is the front of every larger one's.
-template <int kCap>
-const Table<kCap>& parameters(ListPart& p, int grid) {
-  int i = 0;
-  for (int b = 0; b < grid; ++b) {
-    const int c = static_cast<int>(static_cast<long long>(p.chunks) * b / grid);  // as range_at
-    while (i + 1 < p.n && p.table.e[i + 1].first <= c) ++i;
-    p.table.start[b] = static_cast<uint16_t>(i);
-  }
-  return *reinterpret_cast<const Table<kCap>*>(&p.table);
-}
-
 template <int kCap, int kBytes>
-cudaError_t launch_square(ListPart& p, int grid, bool add, Partial* partial, cudaStream_t st) {
-  return launch_pdl(grad_square_kernel<kCap, kBytes>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+cudaError_t launch_square(const ListPart& p, bool add, Partial* partial, cudaStream_t st) {
+  return launch_pdl(grad_square_kernel<kCap, kBytes>, dim3(p.grid), dim3(kThreads), 0, st, p.parameters<kCap>(), p.n,
                     p.chunks, static_cast<int>(add), partial);
 }
 template <int kCap, int kBytes>
-cudaError_t launch_scale(ListPart& p, const Partial* partial, int n_partials, float max_norm, float* norm_out,
+cudaError_t launch_scale(const ListPart& p, const Partial* partial, int n_partials, float max_norm, float* norm_out,
                          cudaStream_t st) {
-  const int grid = grid_of(p.chunks);
-  return launch_pdl(grad_scale_kernel<kCap, kBytes>, dim3(grid), dim3(kThreads), 0, st, parameters<kCap>(p, grid), p.n,
+  return launch_pdl(grad_scale_kernel<kCap, kBytes>, dim3(p.grid), dim3(kThreads), 0, st, p.parameters<kCap>(), p.n,
                     p.chunks, partial, n_partials, max_norm, norm_out);
 }
 // A launch carries a table of 32, 224 or 880 tensors.
@@ -395,31 +400,36 @@ int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm
   const bool large = bytes >= kLargeBytes;
   const int chunk_bytes = large ? kChunkLarge : kChunkSmall;
   int n_partials = 0;
-  for (int64_t i = 0; i < n;) {
-    ListPart p(t, n, i, chunk_bytes);
+  ListPart p(t, n, 0, chunk_bytes);
+  const bool whole = p.next == n;  // then both launches take the same part
+  for (int64_t i = 0; i < n; i = p.next) {
+    if (i > 0) p = ListPart(t, n, i, chunk_bytes);
     // a list of several launches: each adds to the partials of the one before it
-    const int grid = grid_of(i == 0 && p.next == n ? p.chunks : INT64_MAX);
-    const auto launch = large                 ? launch_square<kTableMax, kChunkLarge>
+    p.deal(grid_of(whole ? p.chunks : INT64_MAX));
+    const auto launch = large ? (p.n <= kTableMiddle ? launch_square<kTableMiddle, kChunkLarge>
+                                                     : launch_square<kTableMax, kChunkLarge>)
                         : p.n <= kTableSmall  ? launch_square<kTableSmall, kChunkSmall>
                         : p.n <= kTableMiddle ? launch_square<kTableMiddle, kChunkSmall>
                                               : launch_square<kTableMax, kChunkSmall>;
-    if (launch(p, grid, i > 0, partial, st) != cudaSuccess) return -3;
-    n_partials = grid;
-    i = p.next;
+    if (launch(p, i > 0, partial, st) != cudaSuccess) return -3;
+    n_partials = p.grid;
   }
   if (!scale || n == 0)
     return launch_pdl(grad_norm_kernel, dim3(1), dim3(kThreads), 0, st, static_cast<const Partial*>(partial),
                       n_partials, max_norm, norm_out) == cudaSuccess
                ? 0
                : -3;
-  for (int64_t i = 0; i < n;) {
-    ListPart p(t, n, i, chunk_bytes);
-    const auto launch = large                 ? launch_scale<kTableMax, kChunkLarge>
+  for (int64_t i = 0; i < n; i = p.next) {
+    if (!whole) {
+      p = ListPart(t, n, i, chunk_bytes);
+      p.deal(grid_of(p.chunks));
+    }
+    const auto launch = large ? (p.n <= kTableMiddle ? launch_scale<kTableMiddle, kChunkLarge>
+                                                     : launch_scale<kTableMax, kChunkLarge>)
                         : p.n <= kTableSmall  ? launch_scale<kTableSmall, kChunkSmall>
                         : p.n <= kTableMiddle ? launch_scale<kTableMiddle, kChunkSmall>
                                               : launch_scale<kTableMax, kChunkSmall>;
     if (launch(p, partial, n_partials, max_norm, i == 0 ? norm_out : nullptr, st) != cudaSuccess) return -3;
-    i = p.next;
   }
   return 0;
 }

@@ -2,6 +2,7 @@
 the fake CUDA runtime of tests/test_dispatch_cpu.py, which dereferences no device pointer."""
 import shutil
 
+import numpy as np
 import pytest
 
 from paper_2309_00754_gb300 import hydra as H
@@ -95,8 +96,28 @@ def test_every_compiled_table_is_taken_by_some_list(fake):
         taken |= {v[0] for v in fake.launches()}
         assert fake.lib.hydra_grad_norm(c, n, 1.0, P, P, BIG, None) == 0
         taken |= {v[0] for v in fake.launches()}
-    c = (H.GradTensorC * 1)(H.GradTensorC(1 << 40, 1 << 40, 1 << 27, 0))  # a large list
-    assert fake.lib.hydra_clip_grad_norm(c, 1, 1.0, P, P, BIG, None) == 0
-    taken |= {v[0] for v in fake.launches()}
+    for n in (1, 225):  # large lists
+        c = (H.GradTensorC * n)(*[H.GradTensorC((i + 1) << 40, (i + 1) << 40, 1 << 27, 0) for i in range(n)])
+        assert fake.lib.hydra_clip_grad_norm(c, n, 1.0, P, P, BIG, None) == 0
+        taken |= {v[0] for v in fake.launches()}
     assert taken == {n for n in fake.lib.fake_kernels().decode().split() if "grad_square" in n or "grad_scale" in n or
                      "grad_norm" in n}
+
+
+def test_overlaps_are_found_in_lists_of_any_order(fake):
+    """Against every pair of ranges: an output may overlap nothing but the gradient it replaces."""
+    rng, seen = np.random.default_rng(5), set()
+    for _ in range(400):
+        n = int(rng.integers(1, 7))
+        src, dst, numel = rng.integers(1, 60, n) * 16, rng.integers(1, 60, n) * 16, rng.integers(0, 13, n)
+        inside = rng.random(n) < 0.5
+        dst[inside] = src[inside]
+        rows = [(int(a), int(b), int(m)) for a, b, m in zip(src, dst, numel) if m > 0]
+        meet = lambda a, b, m, o: a < b + 4 * o and b < a + 4 * m  # noqa: E731
+        clash = any(meet(b, a2, m, m2) and not (i == j and b == a2) or (i != j and meet(b, b2, m, m2))
+                    for i, (a, b, m) in enumerate(rows) for j, (a2, b2, m2) in enumerate(rows))
+        c = (H.GradTensorC * n)(*[H.GradTensorC(int(a), int(b), int(m), 1) for a, b, m in zip(src, dst, numel)])
+        assert fake.lib.hydra_clip_grad_norm(c, n, 1.0, P, P, BIG, None) == (4 if clash else 0), rows
+        fake.launches()
+        seen.add(clash)
+    assert seen == {True, False}
