@@ -1079,7 +1079,24 @@ __device__ __noinline__ void tile_apart(const TI* z, TO* d, int i0, int V, bool 
       }
     }
   } else {
-    for (int i = max(i0, 0) + lane; i < hi; i += 32) d[i] = from_f<TO>(live ? g.value(to_f(z[i]), i) : 0.f);
+    // eight elements a lane under way (2048 x 32001 into rows of 32008: fp32 104 us, 230 one after another; bf16 77, 180)
+    constexpr int G = 8;
+    const int lo = max(i0, 0);
+    int i = lo + lane;
+#pragma unroll 1
+    for (; i + 32 * (G - 1) < hi; i += 32 * G) {
+      TI x[G];
+      if (live) {
+#pragma unroll
+        for (int q = 0; q < G; ++q) x[q] = z[i + 32 * q];
+      }
+#pragma unroll
+      for (int q = 0; q < G; ++q) d[i + 32 * q] = from_f<TO>(live ? g.other(to_f(x[q])) : 0.f);
+    }
+#pragma unroll 1
+    for (; i < hi; i += 32) d[i] = from_f<TO>(live ? g.other(to_f(z[i])) : 0.f);
+    if (live && g.logp && g.id >= lo && g.id < hi && (g.id - lo) % 32 == lane)  // by the lane that wrote it
+      d[g.id] = from_f<TO>(g.value(to_f(z[g.id]), g.id));
   }
 }
 
