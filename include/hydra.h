@@ -326,7 +326,7 @@ hydra_status hydra_token_logprobs_kl(const void* logits_actor, const void* logit
  *             ld >= V elements; any row may start at any element (16-byte rows are not needed).
  *   ids     : int32 [S*L] token ids in [0, V) for logp; may be NULL without logp.
  *   lengths : int32 [S] valid tokens per sequence, 0..L; NULL means all L.
- *   top_k   : 0..32, at most V.
+ *   top_k   : 0..32, at most V; with top_k > 0 V is at most 2^20.
  *   logp, entropy fp32 [S*L], norm fp32 [S*L, 2]: outputs, each may be NULL; top_ids int32 and
  *             top_logp fp32 [S*L, top_k], ignored with top_k == 0. At least one output is wanted.
  * Rows t >= len: not read; logp, entropy, norm and top_logp 0, top_ids -1.
@@ -336,8 +336,9 @@ hydra_status hydra_token_logprobs_kl(const void* logits_actor, const void* logit
  * logp, entropy, norm[1] and top_logp NaN; top_ids then counts NaN as the largest.
  * Bits: sums are fp32 and depend on nothing but the row's values, V, top_k > 0, its start modulo 16
  * bytes and the number of rows S*L.
- * Errors: logits_dtype or top_k -> HYDRA_ERR_RANGE; S, L < 0, S*L >= 2^31, V < 1, V > 2^30 or
- * ld < V -> HYDRA_ERR_SHAPE; a needed pointer or every output NULL -> HYDRA_ERR_NULL; logits not
+ * Outputs overlap neither each other nor an input.
+ * Errors: logits_dtype or top_k -> HYDRA_ERR_RANGE; S, L < 0, S*L >= 2^31, V < 1, V > 2^30 (2^20
+ * with top_k) or ld < V -> HYDRA_ERR_SHAPE; a needed pointer or every output NULL -> HYDRA_ERR_NULL; logits not
  * aligned to its element -> HYDRA_ERR_ALIGN; id out of range -> device error 0x201 and logp NaN;
  * length out of range -> device error 0x202, clamped. S*L == 0 is a no-op.
  */
@@ -496,10 +497,11 @@ typedef struct hydra_grad_tensor {
  *   norm_out : device fp32 [2] = (norm, coef).
  *   workspace: device, 16-byte aligned, >= hydra_grad_norm_workspace_size() bytes, caller-owned; no
  *              initial contents required; calls sharing a workspace must be stream-ordered.
- * A tensor's squares are summed in fp32 over runs of some dozens of elements and in fp64 beyond, in an
- * order that depends on nothing but the list and the device: equal calls give equal bits. No fp32
- * element is too large or too small for its square.
- * An out range may not overlap any other range of the list, read or written (the same tensor twice
+ * Squares are summed in fp32 over runs of some dozens of elements and beyond that in pairs of fp32
+ * numbers that carry their rounding errors (in fp64 where a run's squares would overflow or vanish in
+ * fp32), in an order that depends on nothing but the list and the device: equal calls give equal bits.
+ * No fp32 element is too large or too small for its square.
+ * norm_out and the workspace overlap none of the tensors. An out range may not overlap any other range of the list, read or written (the same tensor twice
  * among them); hydra_grad_norm, which only reads, counts a tensor listed twice twice.
  * Errors: n < 0, n >= 2^31, a numel < 0 or >= 2^40 -> HYDRA_ERR_SHAPE; max_norm or a dtype, or
  * overlapping ranges -> HYDRA_ERR_RANGE; NULL norm_out, list or (numel > 0) tensor -> HYDRA_ERR_NULL;

@@ -548,6 +548,7 @@ hydra_status hydra_token_logprobs_entropy(const void* logits, int logits_dtype, 
   if (logits_dtype != HYDRA_F32 && logits_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
   if (!token_rows_ok(S, L, V, ld)) return HYDRA_ERR_SHAPE;
   if (top_k < 0 || top_k > hydra::kTokenTopMax || top_k > V) return HYDRA_ERR_RANGE;
+  if (top_k > 0 && V > hydra::kTokenTopMaxV) return HYDRA_ERR_SHAPE;
   if (S == 0 || L == 0) return HYDRA_OK;
   if (logits == nullptr || (logp != nullptr && ids == nullptr)) return HYDRA_ERR_NULL;
   if (top_k > 0 && (top_ids == nullptr || top_logp == nullptr)) return HYDRA_ERR_NULL;

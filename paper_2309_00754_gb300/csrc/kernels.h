@@ -167,6 +167,9 @@ struct TokenStatsArgs {
   int* err;
 };
 constexpr int kTokenTopMax = 32;
+// With top_k the values beyond a bound may come in the order that raises it most slowly: time that grows with V^2, 2.5 ms
+// a row at 65536 logits. At this V that stays below the limit of the waits for it.
+constexpr int64_t kTokenTopMaxV = 1 << 20;
 int launch_token_stats(const TokenStatsArgs& a, cudaStream_t stream);
 struct TokenStatsGradArgs {
   const void* logits;

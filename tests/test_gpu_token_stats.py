@@ -203,6 +203,28 @@ def test_more_candidates_than_are_ranked_at_once(rows):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,V", [(1, 600000), (40, 262147), (4, 1 << 20)])
+def test_large_logits_in_the_same_places_of_every_run(rows, V, dtype):
+    """Ascending, descending and shuffled values that recur in a few slots of every 256, tens of thousands beyond
+    any bound, with ties among the best."""
+    k, t = 32, DTYPES[dtype]
+    per = 4 if t is torch.float32 else 8
+    rng = np.random.default_rng(V)
+    i = np.arange(V)
+    at = i[(i // per) % 256 < 12]
+    z = np.zeros((rows, V))
+    for n in range(rows):
+        value = np.linspace(1, 200, len(at))
+        z[n, at] = [value, value[::-1], rng.permutation(value), np.round(value / 16)][n % 4]
+    dev, _ = rows_of(z, t, V + 3, 1)
+    values = host_f64(dev)
+    ids = torch.full((rows, k), -7, dtype=torch.int32, device="cuda")
+    H.hydra_token_logprobs_entropy(dev, None, None, rows, 1, top_ids=ids, top_logp=torch.zeros(rows, k, device="cuda"))
+    want = np.argsort(-values, axis=1, kind="stable")[:, :k]
+    assert np.array_equal(ids.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_stats_of_large_and_infinite_logits(dtype):
     """Large magnitudes cancel exactly; NaN and +inf make the row NaN and come first among the top."""
     V = 3001

@@ -89,6 +89,13 @@ def _stats(lib, **kw):
                                             a["k"], a["logp"], a["ent"], a["norm"], a["top_ids"], a["top_logp"], None)
 
 
+def test_token_stats_vocabulary_with_alternatives_is_bounded(lib):
+    top = dict(top_ids=FAKE, top_logp=FAKE, k=5)
+    assert _stats(lib, V=(1 << 20) + 1, ld=1 << 21, **top) == 2
+    assert _stats(lib, V=1 << 20, ld=1 << 20, **top) not in (2, 4)
+    assert _stats(lib, V=(1 << 20) + 1, ld=1 << 21) not in (2, 4)
+
+
 def test_token_stats_argument_errors(lib):
     assert _stats(lib, dt=2) == 4
     assert _stats(lib, S=-1) == 2 and _stats(lib, L=-1) == 2 and _stats(lib, S=1 << 16, L=1 << 15) == 2
