@@ -23,14 +23,14 @@ namespace hydra {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kCtasPerSm = 4;  // (six: 205 MB of fp32 140 us, eight 163, for 95)
-// Chunks of 16 KB, of a large list 32 KB: 820 MB of bf16 193 us and 212 with the small ones, 205 MB of fp32 94 and 97;
-// but 26 MB of fp32 18.4 and 16.0.
+constexpr int kCtasPerSm = 4;  // (two: 205 MB of fp32 103 us, six 140, eight 163, for 94)
+// Chunks of 16 KB, of a large list 32 KB: 410 MB of bf16 193 us and 212 with the small ones, 205 MB of fp32 94 and 97;
+// but 26 MB of fp32 18.4 and 16.0. The large ones are scaled by two CTAs an SM at a time (registers; held to 64 of them
+// 126 us).
 constexpr int kChunkSmall = 16384, kChunkLarge = 32768;
 constexpr int64_t kLargeBytes = 160 << 20;
 // Of a longer list the last of every CTA's range, where the second pass begins, is to stay in L2; the rest and the outputs
-// leave it first (102 MB of fp32 53.5 -> 48.8 us, 205 MB 100.4 -> 96.3, 822 MB 390 -> 386; the norm alone 21.5 -> 21.4,
-// 37.1 -> 32.1, 128 -> 125).
+// leave it first (102 MB of fp32 53 -> 49 us, 205 MB 110 -> 94, 822 MB 411 -> 376; 16 or 32 MB of it 53, 99 and 96, 376).
 constexpr int kKeepBytes = 64 << 20;
 constexpr int kTableMax = 880;  // tensors of one launch: 30 KB of parameters
 constexpr float kEps = 1e-6f;

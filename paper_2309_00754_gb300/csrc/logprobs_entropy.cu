@@ -9,9 +9,9 @@
 //
 // The rows come through a ring of 16 KB stages that one warp fills with bulk copies, rows ahead of the
 // eight warps that sum them: 256 threads with a maximum and two sums each, whose parts one warp puts
-// together. Four CTAs an SM take every 608th row. 2 % of the threads' time is waiting where the row is
-// fp32 (4096 x 32000: 76.5 to 79.5 us, 97 to 101 % of the measured HBM rate); bf16 needs 8.4 instructions an element
-// (8192 x 32000: 82.7 us, 94 %). Few rows are shared by clusters, which meet in the first CTA's memory.
+// together. Four CTAs an SM take every 608th row. HBM bounds it where the logits are fp32 (4096 x 32000: 77 to 80 us,
+// 97 to 101 % of the measured rate), and nearly so the 8.6 instructions an element of bf16 (8192 x 32000: 82.7 us,
+// 94 %). Few rows are shared by clusters, which meet in the first CTA's memory.
 //
 // The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps its best
 // value of each eighth of the row. A bound that k of the 256 threads reach holds for the k-th best element,
@@ -1054,8 +1054,8 @@ struct RowGrad {
 
 // A warp takes a tile of a row. Units lie on the 16-byte grid of both arrays where their rows start alike on it
 // (`a` elements before the row); else every element goes by itself.
-// Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 60 (96 %), bf16 42 (92 %; 62.8
-// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.7 now).
+// Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 58 (99 %), bf16 42 (92 %; 62.8
+// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.4 now).
 // A tile of a row whose x would be rounded apart, or of rows that do not lie alike on the grid: a call, as its registers
 // would slow the kernel down (2048 x 32000 bf16: 42.3 us, 44.9 with it in line).
 template <typename TI, typename TO>
