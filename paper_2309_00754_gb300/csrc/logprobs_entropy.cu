@@ -1052,10 +1052,6 @@ struct RowGrad {
   }
 };
 
-// A warp takes a tile of a row. Units lie on the 16-byte grid of both arrays where their rows start alike on it
-// (`a` elements before the row); else every element goes by itself.
-// Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 58 (99 %), bf16 42 (92 %; 62.8
-// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.4 now).
 // A tile of a row whose x would be rounded apart, or of rows that do not lie alike on the grid: a call, as its registers
 // would slow the kernel down (2048 x 32000 bf16: 42.3 us, 44.9 with it in line).
 template <typename TI, typename TO>
@@ -1100,6 +1096,10 @@ __device__ __noinline__ void tile_apart(const TI* z, TO* d, int i0, int V, bool 
   }
 }
 
+// A warp takes a tile of a row. Units lie on the 16-byte grid of both arrays where their rows start alike on it
+// (`a` elements before the row); else every element goes by itself.
+// Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 58 (99 %), bf16 42 (92 %; 62.8
+// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.4 now).
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(kGradWarps * 32, 4)
     token_stats_grad_kernel(const TI* logits, long long ld, unsigned L, int V, unsigned tiles, unsigned items,

@@ -390,6 +390,18 @@ def test_grad_in_place_has_the_same_bits(dtype, ld, shift):
     assert torch.equal(z, d)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("ld,shift", [(4100, 0), (4103, 3)])
+def test_grad_in_place_where_the_lowest_value_masks(dtype, ld, shift):
+    S, L, V = 3, 5, 4099
+    z, values, ids, lengths, _ = make(22, S, L, V, DTYPES[dtype], "lowest", ld=ld, shift=shift)
+    gl, gh = np.linspace(-1, 1, S * L), np.full(S * L, -0.01)
+    r = O.token_stats(values, None, None, S, L)
+    d, _ = run_grad(z, ids, lengths, S, L, r["norm"], r["entropy"], gl, gh, DTYPES[dtype], ld, shift)
+    run_grad(z, ids, lengths, S, L, r["norm"], r["entropy"], gl, gh, None, into=z)
+    assert torch.equal(z, d)
+
+
 def test_grad_against_differences():
     """The kernel's gradient against central differences of the oracle's loss: with steps of 1e-4
     the differences are off by 1e-8 / 6 times a third derivative under 10, the kernel by fp32."""
