@@ -295,7 +295,7 @@ struct Running {
         }
       }
     } else if (from < kInf && all_are(r, n, from)) {
-      // masked with the type's lowest value, and nothing above it yet: x = 0 (420 x 32000 bf16, k = 20: 17 us, 104
+      // masked with the type's lowest value, and nothing above it yet: x = 0 (420 x 32000 bf16, k = 20: 14 us, 104
       // with the terms below and all elements of a row collected before the top is found to be too many)
       const float count = n * (Row<T>::E / 2);
       s = add2(s, pack2(count, count));
@@ -439,7 +439,7 @@ struct End {
   uint32_t key[kWarps][32];               // order_key of its best value of all, 0 where it has none
   int hit_slot[128];
   uint16_t asked[kSummers];               // summers that hold candidates
-  uint16_t owner[kSegments * 32];         // segments that do, of 32 of them
+  uint16_t owner[kSegments * kSummers];   // segments that do
   unsigned row;
   int id;                                 // the row's token
   bool end;                               // no row is left
@@ -520,8 +520,10 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
     for (int at = scan(__popc(is), lane, asked); is != 0; is &= is - 1)
       e.asked[at++] = static_cast<uint16_t>((__ffs(is) - 1) * 32 + lane);
     __syncwarp();
-    for (int x0 = 0; x0 < asked && found <= kCandidates; x0 += 32) {
-      // their segments that hold candidates: up to kSegments a lane
+    // their segments that hold candidates, up to kSegments a lane; all of them first, or batches of the loads below
+    // would go half empty (8192 x 32000 bf16, k = 32: 131 us, 125 so)
+    int owners = 0;
+    for (int x0 = 0; x0 < asked && (above || owners <= kCandidates); x0 += 32) {
       const int summer = x0 + lane < asked ? e.asked[x0 + lane] : 0;
       is = 0;
 #pragma unroll
@@ -529,61 +531,66 @@ __device__ __forceinline__ uint64_t select_top(End& e, const Row<T>& r, const Pa
         if (part.lo + q * stages * kStageSlots + summer < part.hi)
           is |= (enough(__bfloat162float(e.segment[q][summer])) ? 1u : 0u) << q;
       if (x0 + lane >= asked) is = 0;
-      int owners;
-      for (int at = scan(__popc(is), lane, owners); is != 0; is &= is - 1)
-        e.owner[at++] = static_cast<uint16_t>((__ffs(is) - 1) << 10 | summer);
-      __syncwarp();
+      int more;
+      int at = owners + scan(__popc(is), lane, more);
+      for (; is != 0; is &= is - 1) e.owner[at++] = static_cast<uint16_t>((__ffs(is) - 1) << 10 | summer);
+      owners += more;
+    }
+    if (!above && owners > kCandidates) {  // with a candidate each, too many of them
+      above = true;
+      continue;
+    }
+    __syncwarp();
 #pragma unroll 1
-      for (int i0 = 0; i0 < each && found <= kCandidates; i0 += 1 << bits) {
-        const int i = i0 + (lane & ((1 << bits) - 1));
+    for (int i0 = 0; i0 < each && found <= kCandidates; i0 += 1 << bits) {
+      const int i = i0 + (lane & ((1 << bits) - 1));
 #pragma unroll 1
-        for (int g0 = 0; g0 < owners && found <= kCandidates; g0 += G * at_once) {  // more than fit: enough is known
-          uint4 v[G];
-          int j[G];
-          bool in_part = false;
+      for (int g0 = 0; g0 < owners && found <= kCandidates; g0 += G * at_once) {  // more than fit: enough is known
+        uint4 v[G];
+        int j[G];
+        bool in_part = false;
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const int o = g0 + g * at_once + (lane >> bits);
-            j[g] = part.hi;
-            if (o < owners && i < each)
-              j[g] = part.lo + (e.owner[o] >> 10) * stages * kStageSlots + (e.owner[o] & 1023) + i * kSummers;
-            if (j[g] >= r.full_lo && j[g] < full_hi) v[g] = r.load_full(j[g]); else in_part |= j[g] < part.hi;
-          }
-          // the row's first and last slot, where it has them in part
-          if (__any_sync(0xffffffffu, in_part)) {
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-              if (j[g] < part.hi && (j[g] < r.full_lo || j[g] >= full_hi)) v[g] = r.load(j[g]);
-          }
-          // the slots that hold some, in a row; then their elements, a slot a lane
-          int hits = 0;
+        for (int g = 0; g < G; ++g) {
+          const int o = g0 + g * at_once + (lane >> bits);
+          j[g] = part.hi;
+          if (o < owners && i < each)
+            j[g] = part.lo + (e.owner[o] >> 10) * stages * kStageSlots + (e.owner[o] & 1023) + i * kSummers;
+          if (j[g] >= r.full_lo && j[g] < full_hi) v[g] = r.load_full(j[g]); else in_part |= j[g] < part.hi;
+        }
+        // the row's first and last slot, where it has them in part
+        if (__any_sync(0xffffffffu, in_part)) {
 #pragma unroll
           for (int g = 0; g < G; ++g)
-            if (j[g] >= part.hi || !enough(Row<T>::max_of(v[g]))) j[g] = -1; else ++hits;
-          int slots;
-          int at = scan(hits, lane, slots);
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            if (j[g] < 0) continue;
-            e.hit[at] = v[g];
-            e.hit_slot[at++] = j[g];
-          }
-          __syncwarp();
-          for (int h0 = 0; h0 < slots; h0 += 32) {
-            const int slot = h0 + lane < slots ? e.hit_slot[h0 + lane] : 0;
-            uint32_t mask = 0;
-            if (h0 + lane < slots) mask = r.which(e.hit[h0 + lane], slot, enough);
-            int more;
-            int c = found + scan(__popc(mask), lane, more);
-            found += more;
-            for (; mask != 0; mask &= mask - 1, ++c) {
-              const int q = __ffs(mask) - 1;
-              if (c < kCandidates)
-                e.cand[c] = rank_key(order_key(to_f(reinterpret_cast<const T*>(&e.hit[h0 + lane])[q])), r.first(slot) + q);
-            }
-          }
-          __syncwarp();
+            if (j[g] < part.hi && (j[g] < r.full_lo || j[g] >= full_hi)) v[g] = r.load(j[g]);
         }
+        // the slots that hold some, in a row; then their elements, a slot a lane
+        int hits = 0;
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+          if (j[g] >= part.hi || !enough(Row<T>::max_of(v[g]))) j[g] = -1; else ++hits;
+        int slots;
+        int at = scan(hits, lane, slots);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if (j[g] < 0) continue;
+          e.hit[at] = v[g];
+          e.hit_slot[at++] = j[g];
+        }
+        __syncwarp();
+        for (int h0 = 0; h0 < slots; h0 += 32) {
+          const int slot = h0 + lane < slots ? e.hit_slot[h0 + lane] : 0;
+          uint32_t mask = 0;
+          if (h0 + lane < slots) mask = r.which(e.hit[h0 + lane], slot, enough);
+          int more;
+          int c = found + scan(__popc(mask), lane, more);
+          found += more;
+          for (; mask != 0; mask &= mask - 1, ++c) {
+            const int q = __ffs(mask) - 1;
+            if (c < kCandidates)
+              e.cand[c] = rank_key(order_key(to_f(reinterpret_cast<const T*>(&e.hit[h0 + lane])[q])), r.first(slot) + q);
+          }
+        }
+        __syncwarp();
       }
     }
     if (found > kCandidates && !above) {
