@@ -395,11 +395,18 @@ __device__ __forceinline__ uint32_t kth_bound(const uint32_t (*list)[32], int k,
   return shfl(a, k - 1);
 }
 
-__device__ __forceinline__ void st_cluster_f32(const float* local, uint32_t rank, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(map_to_rank(smem_u32(local), rank)), "f"(v) : "memory");
+// A value to the address of `local` in another CTA of the cluster; its bytes arrive on that CTA's `bar`
+__device__ __forceinline__ void send(const float* local, const uint64_t* bar, uint32_t rank, float v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(
+                   map_to_rank(smem_u32(local), rank)),
+               "f"(v), "r"(map_to_rank(smem_u32(bar), rank))
+               : "memory");
 }
-__device__ __forceinline__ void st_cluster_u64(const uint64_t* local, uint32_t rank, uint64_t v) {
-  asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_rank(smem_u32(local), rank)), "l"(v) : "memory");
+__device__ __forceinline__ void send(const uint64_t* local, const uint64_t* bar, uint32_t rank, uint64_t v) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(
+                   map_to_rank(smem_u32(local), rank)),
+               "l"(v), "r"(map_to_rank(smem_u32(bar), rank))
+               : "memory");
 }
 // [p, p + bytes) to shared memory at dst, all on 16-byte boundaries; its bytes arrive on `bar`
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* p, uint32_t bytes, uint32_t bar) {
@@ -447,7 +454,7 @@ struct End {
 };
 struct SharedTop {
   End end[kEnders];
-  // a cluster has one row, for the first ender: the other's segments hold what its CTAs send
+  // a cluster has one row, for the first ender: another's segments hold what its CTAs send
   __device__ __forceinline__ uint64_t* cluster_best(unsigned rank) {
     return reinterpret_cast<uint64_t*>(end[1].segment) + rank * 32;
   }
@@ -685,21 +692,19 @@ struct Outputs {
   }
 };
 
+// What a CTA sends to the first of its cluster.
+template <bool kTop>
+constexpr uint32_t sent_bytes() { return 3 * sizeof(float) + (kTop ? 32 * sizeof(uint64_t) : 0); }
+
 // A CTA's part of a row, by a warp: written out, or in a cluster sent to its first CTA, which writes the whole.
+// (Bytes that arrive by themselves: plain stores, a fence and an arrival took 0.5 us more.)
 template <bool kTop>
 __device__ __forceinline__ void finish(Shared<kTop>& sh, SharedTop& top, const Outputs& out, unsigned row, Stats st, float z_id,
                                        uint64_t best, unsigned rank, unsigned cs, int lane, int* err) {
   if (cs > 1) {
     if (rank != 0) {
-      if (lane == 0) {
-        st_cluster_f32(&sh.cluster_stats[rank][0], 0, st.m);
-        st_cluster_f32(&sh.cluster_stats[rank][1], 0, st.s);
-        st_cluster_f32(&sh.cluster_stats[rank][2], 0, st.w);
-      }
-      if constexpr (kTop) st_cluster_u64(top.cluster_best(rank) + lane, 0, best);
-      asm volatile("fence.acq_rel.cluster;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&sh.others), 0));
+      if (lane < 3) send(&sh.cluster_stats[rank][lane], &sh.others, 0, lane == 0 ? st.m : lane == 1 ? st.s : st.w);
+      if constexpr (kTop) send(top.cluster_best(rank) + lane, &sh.others, 0, best);
       return;
     }
     if (!warp_wait_cluster_bounded(smem_u32(&sh.others), 0, &sh.abort_flag, err, kDevTimeoutEpilogue)) st.m = kNan;
@@ -714,6 +719,7 @@ __device__ __forceinline__ void finish(Shared<kTop>& sh, SharedTop& top, const O
       for (int c = 1; c < kClusterMax; ++c) list[c] = c < static_cast<int>(cs) ? top.cluster_best(c)[c % 2 ? 31 - lane : lane] : 0;
 #pragma unroll
       for (int half = kClusterMax / 2; half > 0; half >>= 1) {
+        if (half >= static_cast<int>(cs)) continue;
 #pragma unroll
         for (int c = 0; c < half; ++c) {
           // the second of a pair backwards
@@ -729,23 +735,23 @@ __device__ __forceinline__ void finish(Shared<kTop>& sh, SharedTop& top, const O
 
 // Clusters of one CTA take every gridDim.x-th row in turn, larger ones one row that their CTAs share. The last
 // warp of a CTA fetches the slots of its rows, stage by stage, and the others sum them.
-template <typename T, bool kTop>
+template <typename T, bool kTop, bool kCluster>
 __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
     token_stats_kernel(const T* __restrict__ logits, long long ld, unsigned rows, unsigned L, int V,
-                       const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, unsigned bits,
+                       const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, unsigned cluster_bits,
                        const Outputs out, int* err) {
   extern __shared__ __align__(16) unsigned char raw[];
   constexpr int kStages = stages_of<kTop>();
   Shared<kTop>& sh = *reinterpret_cast<Shared<kTop>*>(raw);
   SharedTop& top = *reinterpret_cast<SharedTop*>(raw + sizeof(Shared<kTop>));  // with kTop
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const unsigned cs = 1u << bits, rank = bits > 0 ? cluster_rank() : 0;
+  const unsigned bits = kCluster ? cluster_bits : 0, cs = 1u << bits, rank = kCluster ? cluster_rank() : 0;
   if (tid == 0) {
     for (int q = 0; q < kStages; ++q) {
       mbar_init(smem_u32(&sh.full[q]), 1);
       mbar_init(smem_u32(&sh.drained[q]), kWarps);
     }
-    mbar_init(smem_u32(&sh.others), cs > 1 ? cs - 1 : 1);
+    mbar_init(smem_u32(&sh.others), 1);
     if constexpr (kTop)
       for (int f = 0; f < kEnders; ++f) {
         mbar_init(smem_u32(&top.end[f].done), kWarps);
@@ -753,6 +759,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
       }
     sh.abort_flag = 0;
     fence_mbar_init();
+    if (cs > 1 && rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.others), (cs - 1) * sent_bytes<kTop>());
   }
   if (cs > 1) cluster_sync_all(); else __syncthreads();
   pdl_wait();
@@ -1246,7 +1253,7 @@ int clusters_held(int dev, int bits) {
   cudaLaunchConfig_t cfg = stats_config<T, kTop>(1, 1 << bits, nullptr, attr);
   cfg.numAttrs = 1;
   int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, token_stats_kernel<T, kTop>, &cfg) != cudaSuccess) {
+  if (cudaOccupancyMaxActiveClusters(&n, token_stats_kernel<T, kTop, true>, &cfg) != cudaSuccess) {
     cudaGetLastError();
     return 0;
   }
@@ -1274,9 +1281,10 @@ int launch_stats(const TokenStatsArgs& a, cudaStream_t stream) {
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
   if (!attr_set[dev]) {
-    if (cudaFuncSetAttribute(token_stats_kernel<T, kTop>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             static_cast<int>(shared_bytes<kTop>())) != cudaSuccess)
-      return -1;
+    for (auto* kernel : {token_stats_kernel<T, kTop, false>, token_stats_kernel<T, kTop, true>})
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared_bytes<kTop>())) !=
+          cudaSuccess)
+        return -1;
     attr_set[dev] = true;
   }
   const int64_t rows = a.S * a.L;
@@ -1285,7 +1293,8 @@ int launch_stats(const TokenStatsArgs& a, cudaStream_t stream) {
   cudaLaunchAttribute attr[2];
   const cudaLaunchConfig_t cfg =
       stats_config<T, kTop>(static_cast<unsigned>(bits > 0 ? rows : std::min(rows, resident)), 1 << bits, stream, attr);
-  return cudaLaunchKernelEx(&cfg, token_stats_kernel<T, kTop>, static_cast<const T*>(a.logits),
+  const auto kernel = bits > 0 ? token_stats_kernel<T, kTop, true> : token_stats_kernel<T, kTop, false>;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<const T*>(a.logits),
                             static_cast<long long>(a.ld), static_cast<unsigned>(rows), static_cast<unsigned>(a.L),
                             static_cast<int>(a.V), a.ids, a.lengths, static_cast<unsigned>(bits),
                             Outputs{a.logp, a.entropy, a.norm, a.top_ids, a.top_logp, static_cast<int>(a.top_k)},

@@ -24,9 +24,10 @@ def stats(fake, rows, v, k, bf16=False, lengths=None, seqs=None):
 
 
 def test_statistics_are_one_launch_of_a_kernel_by_type_and_selection(fake):
-    names = {stats(fake, 64, 32000, k, bf16)[0] for k in (0, 1, 32) for bf16 in (False, True)}
+    names = [{stats(fake, rows, 32000, k, bf16)[0] for k in (0, 1, 32) for bf16 in (False, True)} for rows in (1, 1000)]
     compiled = {n for n in fake.lib.fake_kernels().decode().split() if "token_stats_kernel" in n}
-    assert len(names) == 4 and names == compiled
+    assert [len(n) for n in names] == [4, 4] and names[0] | names[1] == compiled  # of clusters, and of single CTAs
+    assert not names[0] & names[1]
 
 
 def test_few_long_rows_are_shared_by_clusters_that_fit(fake):
