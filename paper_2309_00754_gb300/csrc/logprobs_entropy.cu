@@ -1261,17 +1261,16 @@ int clusters_held(int dev, int bits) {
   return n;
 }
 
-// How many CTAs share a row (as a power of two): the most of which the device holds a cluster for every row,
-// where a row is long enough. A cluster costs 0.6 us (1.3 where tokens are selected, whose lists are merged), and
-// one CTA reads 128 KB in about 2. Of eight / four / two / one CTAs, us in a graph: 1 x 32000 fp32 3.9 / 4.3 /
-// 5.1 / 5.8, 64 x 128001 bf16 8.4 / 8.2 / 8.9 / 12.4, 1 x 8000 fp32 3.5 / 3.7 / 3.9 / 3.4; with eight tokens 32 x
-// 32000 bf16 9.1 / 7.9 / 8.4 / 7.6, 19 x 128001 bf16 9.6 / 10.3 / 12.3 / 14.6, 64 x 128001 20.8 / 11.9 / 12.8 / 14.9.
+// How many CTAs share a row (as a power of two): the most of which the device holds a cluster for every row, where a row
+// is long enough. Of one / two / four / eight CTAs, us in a graph, 32 KB a row: 1 x 8000 fp32 3.3 / 3.3 / 3.3 / 3.1,
+// 75 rows 3.4 / 3.3 / 3.9 / -; 64 KB: 1 x 32000 bf16 4.5 / 3.9 / 3.4 / 3.3, 75 rows 5.8 / 5.0 / 5.3 / -; 512 KB: 37 x
+// 128001 fp32 18.0 / 11.5 / 8.5 / 7.6. With eight tokens, whose lists are merged: 32 KB 5.8 / 6.1 / 6.1 / 6.3, 64 KB 7.2 /
+// 6.9 / 6.4 / 6.7, 125 KB 8.2 / 7.4 / 6.6 / 6.4; 75 rows of 64 KB (fp32) 7.5 / 7.7 / -, of 125 KB 9.2 / 8.9 / -.
 template <typename T, bool kTop>
 int cluster_bits(int64_t rows, int64_t V, int dev) {
-  for (int bits = 3; bits > 0; --bits) {
-    const int64_t least = 48 * 1024 * (kTop ? kClusterMax >> bits : 1);
-    if (V * static_cast<int64_t>(sizeof(T)) >= least && rows <= clusters_held<T, kTop>(dev, bits)) return bits;
-  }
+  constexpr int64_t kLeast[] = {0, (kTop ? 120 : 48) * 1024, 48 * 1024, (kTop ? 96 : 31) * 1024};
+  for (int bits = 3; bits > 0; --bits)
+    if (V * static_cast<int64_t>(sizeof(T)) >= kLeast[bits] && rows <= clusters_held<T, kTop>(dev, bits)) return bits;
   return 0;
 }
 

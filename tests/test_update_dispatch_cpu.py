@@ -36,11 +36,12 @@ def test_few_long_rows_are_shared_by_clusters_that_fit(fake):
         for rows, cs in ((1, 8), (36, 8), (37, 2), (76, 2), (77, 1), (1000, 1)):
             name, x, y, z, cluster, _ = stats(fake, rows, v, 0, bf16)
             assert (cluster, x) == (cs, rows * cs if cs > 1 else min(rows, 4 * 152)), (v, rows)
-    # selection: two and four share rows of 192 and 96 KB, and fewer CTAs are resident
-    for rows, v, cs in ((20, 32000, 8), (40, 32000, 1), (40, 128001, 2), (400, 32000, 1)):
+    # selection: two, four and eight share rows of 120, 48 and 96 KB, and fewer CTAs are resident
+    for rows, v, cs in ((20, 32000, 8), (20, 20000, 4), (40, 20000, 1), (40, 32000, 2), (40, 128001, 2), (400, 32000, 1)):
         name, x, *_, cluster, _ = stats(fake, rows, v, 5)
         assert (cluster, x) == (cs, rows * cs if cs > 1 else min(rows, 2 * 152))
-    assert stats(fake, 1, 8000, 0)[4] == 1  # short rows are not shared
+    assert stats(fake, 1, 7900, 0)[4] == 1  # short rows are not shared
+    assert stats(fake, 1, 8000, 0)[4] == 8 and stats(fake, 40, 8000, 0)[4] == 1
 
 
 def test_a_device_without_clusters_takes_rows_one_by_one(fake):
