@@ -1013,6 +1013,56 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
   }
 }
 
+// Short rows without alternatives, a warp each: nothing passes between warps, where a row of the kernel above
+// takes the summing threads' meeting and one of their warps' end, about 2 us a row for a CTA.
+constexpr int kShortWarps = 8, kShortSlots = 8;  // of a CTA; of a lane under way
+template <typename T>
+__global__ void __launch_bounds__(kShortWarps * 32)
+    token_stats_short_kernel(const T* __restrict__ logits, long long ld, unsigned rows, unsigned L, int V,
+                             const int32_t* __restrict__ ids, const int32_t* __restrict__ lengths, const Outputs out,
+                             int* err) {
+  pdl_wait();
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const unsigned row = blockIdx.x * kShortWarps + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  if (lengths != nullptr) {
+    const unsigned sq = row / L;
+    const int n = lengths[sq];
+    if ((n < 0 || n > static_cast<int>(L)) && lane == 0) record_error(err, kDevBadLength);
+    if (static_cast<int>(row - sq * L) >= n) {
+      if (lane == 0) out.dead(row);
+      return;
+    }
+  }
+  const Row<T> r(logits + row * ld, V);
+  float z_id = kNan;
+  if (lane == 0 && out.logp) {
+    const int id = ids[row];
+    if (id < 0 || id >= V) record_error(err, kDevBadTokenId); else z_id = to_f(r.p[id]);
+  }
+  const uint64_t log2e = twice(kLog2e);
+  Running<T> run;
+  for (int j0 = lane; j0 < r.n_slots; j0 += 32 * kShortSlots) {
+    uint32_t v[4 * kShortSlots];
+#pragma unroll
+    for (int u = 0; u < kShortSlots; ++u) {
+      const int j = j0 + u * 32;
+      const uint32_t fill = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
+      uint4 x = make_uint4(fill, fill, fill, fill);
+      if (j < r.n_slots) x = r.load(j);
+      v[4 * u] = x.x;
+      v[4 * u + 1] = x.y;
+      v[4 * u + 2] = x.z;
+      v[4 * u + 3] = x.w;
+    }
+    run.template add<kShortSlots>(v, run.max_of(v, kShortSlots), log2e);
+  }
+  Stats st = run.rebase();
+  st.merge_lanes(32);
+  out.live<false>(row, st, z_id, 0, lane);
+}
+
 constexpr int kUnit = 8;  // elements a lane turns at once
 constexpr int kTileUnits = 8;  // units a lane takes of a tile
 constexpr int kTile = 32 * kUnit * kTileUnits;
@@ -1274,6 +1324,28 @@ int cluster_bits(int64_t rows, int64_t V, int dev) {
   return 0;
 }
 
+template <typename T>
+int launch_short(const TokenStatsArgs& a, cudaStream_t stream) {
+  const int64_t rows = a.S * a.L;
+  return launch_pdl(token_stats_short_kernel<T>, dim3(static_cast<unsigned>((rows + kShortWarps - 1) / kShortWarps)),
+                    dim3(kShortWarps * 32), 0, stream, static_cast<const T*>(a.logits), static_cast<long long>(a.ld),
+                    static_cast<unsigned>(rows), static_cast<unsigned>(a.L), static_cast<int>(a.V), a.ids, a.lengths,
+                    Outputs{a.logp, a.entropy, a.norm, nullptr, nullptr, 0}, a.err) == cudaSuccess
+             ? 0
+             : -3;
+}
+
+// Whether rows go to a warp each: those that it has under way at once (600 x 1000 fp32 3.4 -> 2.5 us, 8000 x 1000
+// 20.0 -> 9.9, 30000 x 500 bf16 69 -> 30), and of many rows longer ones (2000 x 4000 fp32 10.5 -> 9.1 us, 30000 x 2000
+// 79 -> 41, 2000 x 6000 13.5 -> 11.9; but 2000 x 12000 19.3 and 20.4, 600 x 4000 5.3 and 7.0).
+template <typename T>
+bool rows_are_short(int64_t rows, int64_t V) {
+  const int64_t bytes = V * static_cast<int64_t>(sizeof(T));
+  if (bytes <= 32 * kShortSlots * 16) return true;
+  // (and no lane adds more than 128 terms one after another)
+  return bytes <= 24 * 1024 && V <= 8192 && rows > 2 * static_cast<int64_t>(ctas_per_sm<false>()) * std::max(1, sm_count());
+}
+
 template <typename T, bool kTop>
 int launch_stats(const TokenStatsArgs& a, cudaStream_t stream) {
   static bool attr_set[64] = {false};  // the shared-memory limit is a per-device attribute
@@ -1320,7 +1392,11 @@ int launch_grad(const TokenStatsGradArgs& a, cudaStream_t stream) {
 
 int launch_token_stats(const TokenStatsArgs& a, cudaStream_t stream) {
   if (a.top_k > 0) return a.bf16 ? launch_stats<__nv_bfloat16, true>(a, stream) : launch_stats<float, true>(a, stream);
-  return a.bf16 ? launch_stats<__nv_bfloat16, false>(a, stream) : launch_stats<float, false>(a, stream);
+  const int64_t rows = a.S * a.L;
+  if (a.bf16)
+    return rows_are_short<__nv_bfloat16>(rows, a.V) ? launch_short<__nv_bfloat16>(a, stream)
+                                                    : launch_stats<__nv_bfloat16, false>(a, stream);
+  return rows_are_short<float>(rows, a.V) ? launch_short<float>(a, stream) : launch_stats<float, false>(a, stream);
 }
 
 // the row's first unit may start up to kUnit - 1 elements before it

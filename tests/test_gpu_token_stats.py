@@ -178,6 +178,35 @@ def test_many_short_rows(rows, V, k):
     check_stats(run_stats(z, ids, None, rows, 1, k), values, ids, None, rows, 1, k)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("mask", [None, "inf", "lowest"])
+@pytest.mark.parametrize("S,L,V,ld,shift", [(5, 3, 1, 1, 0), (700, 3, 33, 35, 1), (3, 7, 1000, 1003, 3), (7, 3, 2047, 2051, 5),
+                                            (30, 60, 6100, 6101, 1), (9, 170, 9001, 9001, 7), (5, 300, 13001, 13003, 1)])
+def test_stats_without_alternatives(S, L, V, ld, shift, mask, dtype):
+    """A warp a row, up to where the rows are long or few, and beyond: ragged, with rows that start anywhere. Of 6100
+    logits a lane adds 96 terms to each of its two sums, and six steps join them: with the terms' own 8 fewer
+    than the 125 that the tolerance counts."""
+    z, values, ids, lengths, _ = make(V + S, S, L, V, DTYPES[dtype], mask, ld=ld, shift=shift)
+    check_stats(run_stats(z, ids, lengths, S, L, 0), values, ids, lengths, S, L, 0)
+    only = torch.full((S * L,), float("nan"), device="cuda")
+    H.hydra_token_logprobs_entropy(z, None, dev_i32(lengths), S, L, entropy=only)
+    assert torch.equal(only, run_stats(z, ids, lengths, S, L, 0)["entropy"])
+
+
+def test_short_rows_report_bad_ids_and_lengths():
+    z, values, _, _, _ = make(3, 4, 3, 200, torch.float32)
+    ids = np.full(12, 7)
+    ids[5] = 200
+    o = run_stats(z, ids, None, 4, 3, 0)
+    assert H.device_error(clear=True) == 0x201 and torch.isnan(o["logp"][5]) and int(torch.isnan(o["logp"]).sum()) == 1
+    for bad in (-1, 4):
+        lengths = np.array([3, bad, 0, 2])
+        o = run_stats(z, np.full(12, 7), lengths, 4, 3, 0)
+        assert H.device_error(clear=True) == 0x202
+        lengths[1] = 0 if bad < 0 else 3
+        check_stats(o, values, np.full(12, 7), lengths, 4, 3, 0)
+
+
 @pytest.mark.parametrize("rows", [2, 500])
 def test_more_candidates_than_are_ranked_at_once(rows):
     """Values above the bound, equal to it and NaN, each in more places than fit: 32 lanes of a group share

@@ -44,6 +44,16 @@ def test_few_long_rows_are_shared_by_clusters_that_fit(fake):
     assert stats(fake, 1, 8000, 0)[4] == 8 and stats(fake, 40, 8000, 0)[4] == 1
 
 
+def test_short_rows_take_a_warp_each(fake):
+    for rows, v, bf16, short in ((1, 1, False, True), (3, 1024, False, True), (3, 1025, False, False), (8, 2048, True, True),
+                                 (1216, 6144, False, False), (1217, 6144, False, True), (1217, 6145, False, False),
+                                 (20000, 8192, True, True), (20000, 8193, True, False)):
+        name, x, *_ = stats(fake, rows, v, 0, bf16)
+        assert ("token_stats_short_kernel" in name) == short, (rows, v, bf16)
+        assert x == ((rows + 7) // 8 if short else min(rows, 608))
+    assert "short" not in stats(fake, 3, 500, 1)[0]  # with alternatives
+
+
 def test_a_device_without_clusters_takes_rows_one_by_one(fake):
     fake.device(device=1, pairs=0, quads=0)
     assert stats(fake, 1, 128001, 0)[4] == 1 and stats(fake, 1, 128001, 8)[4] == 1
