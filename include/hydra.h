@@ -335,7 +335,7 @@ hydra_status hydra_token_logprobs_kl(const void* logits_actor, const void* logit
  * -inf. The type's lowest value is a number like any other. A NaN or +inf logit makes the row's
  * logp, entropy, norm[1] and top_logp NaN; top_ids then counts NaN as the largest.
  * Bits: sums are fp32 and depend on nothing but the row's values, V, top_k > 0, its start modulo 16
- * bytes and the number of rows S*L.
+ * bytes, the number of rows S*L and the device.
  * Outputs overlap neither each other nor an input.
  * Errors: logits_dtype or top_k -> HYDRA_ERR_RANGE; S, L < 0, S*L >= 2^31, V < 1, V > 2^30 (2^20
  * with top_k) or ld < V -> HYDRA_ERR_SHAPE; a needed pointer or every output NULL -> HYDRA_ERR_NULL; logits not

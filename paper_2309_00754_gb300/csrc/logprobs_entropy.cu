@@ -11,14 +11,14 @@
 // eight warps that sum them: 256 threads with a maximum and two sums each, whose parts one warp puts
 // together. Four CTAs an SM take every 608th row. HBM bounds it where the logits are fp32 (4096 x 32000: 77 to 80 us,
 // 97 to 101 % of the measured rate), and nearly so the 8.6 instructions an element of bf16 (8192 x 32000: 82.7 us,
-// 94 %). Few rows are shared by clusters, which meet in the first CTA's memory.
+// 94 %). Few rows are shared by clusters, which meet in the first CTA's memory; short ones take a warp each.
 //
 // The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps its best
 // value of each eighth of the row. A bound that k of the 256 threads reach holds for the k-th best element,
 // too; the eighths that reach it, about k, are read again, and the few elements not behind it are ranked by
 // counting. Three warps of a CTA do that, a row each, while the others are in the next rows, as it takes
 // 3 to 8 us, most of it one step waiting for the one before. Two such CTAs fit an SM (4096 x 32000 fp32, k = 8:
-// 81 us; 8192 x 32000 bf16 101, three CTAs of fewer registers 113; selected by the summing threads themselves 130).
+// 81 us; 8192 x 32000 bf16 97, three CTAs of fewer registers 113; selected by the summing threads themselves 130).
 //
 // Backward, with p = exp((z - m) - log s):
 //     dz[v] = g_logp (1[v = id] - p_v) - g_entropy p_v (log p_v + entropy)
