@@ -408,6 +408,8 @@ __device__ __forceinline__ void send(const uint64_t* local, const uint64_t* bar,
                "l"(v), "r"(map_to_rank(smem_u32(bar), rank))
                : "memory");
 }
+// This thread's stores to shared memory before the bulk copies that it issues from here on
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 // [p, p + bytes) to shared memory at dst, all on 16-byte boundaries; its bytes arrive on `bar`
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* p, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
@@ -849,9 +851,12 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
           if (lane == 0) {
             const int j1 = min(j0 + kStageSlots, part.hi), lo = max(j0, r.full_lo), hi = min(j1, r.full_hi);
             unsigned char* dst = sh.ring[q];
-            // the row's first and last slot, where it has them in part
-            if (j0 < min(lo, j1)) *reinterpret_cast<uint4*>(dst) = r.load(j0);
-            if (hi < j1 && j1 > lo) *reinterpret_cast<uint4*>(dst + (j1 - 1 - j0) * 16) = r.load(j1 - 1);
+            // The row's first and last slot, where it has them in part. Whole stages that lie there later are written by
+            // bulk copies: a proxy of their own, before which these stores have to be done.
+            const bool head = j0 < min(lo, j1), tail = hi < j1 && j1 > lo;
+            if (head) *reinterpret_cast<uint4*>(dst) = r.load(j0);
+            if (tail) *reinterpret_cast<uint4*>(dst + (j1 - 1 - j0) * 16) = r.load(j1 - 1);
+            if (head || tail) fence_proxy_async();
             sh.stage[q] = Stage{row, j0,
                                 (j1 - j0) | (j0 == part.lo ? kFirst : 0) | (j1 == part.hi ? kLast : 0) |
                                     (left <= 1 || j1 == part.hi ? kSegmentEnd : 0) | segment << kSegmentShift,
