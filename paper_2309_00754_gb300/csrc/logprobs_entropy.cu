@@ -377,8 +377,10 @@ __device__ __forceinline__ uint32_t sort_warp(uint32_t v, int lane) {
   }
   return v;
 }
-// A barrier of the summing threads.
+// A barrier of the summing threads. A warp that leaves early is excused from the next one: it arrives there without
+// waiting, so that a wait that has run out in one warp keeps none of the others.
 __device__ __forceinline__ void summers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kSummers) : "memory"); }
+__device__ __forceinline__ void summers_excuse() { asm volatile("bar.arrive 1, %0;" ::"n"(kSummers) : "memory"); }
 
 // A bound that at least k of 256 keys reach, or 0 where fewer than k are not 0: the k-th largest of the best of 64
 // groups of four. list[w] holds a key a lane.
@@ -698,6 +700,16 @@ struct Outputs {
 template <bool kTop>
 constexpr uint32_t sent_bytes() { return 3 * sizeof(float) + (kTop ? 32 * sizeof(uint64_t) : 0); }
 
+// A warp of a cluster's first CTA that has given up a wait stays until nothing more can arrive in its memory: until
+// the peers' threads have ended (the barrier counts those as arrived) and what they sent has come, or cannot come any
+// more. Without an expiry none is needed: the CTA that ends a row has waited for all of it.
+// (A call: in line it makes the kernels of clusters 0.1 to 0.2 us longer.)
+__device__ __noinline__ void outlive_peers(uint32_t others, int* err) {
+  cluster_sync_all();
+  int never = 0;
+  warp_wait_cluster_bounded(others, 0, &never, err, kDevTimeoutEpilogue);
+}
+
 // A CTA's part of a row, by a warp: written out, or in a cluster sent to its first CTA, which writes the whole.
 // (Bytes that arrive by themselves: plain stores, a fence and an arrival took 0.5 us more.)
 template <bool kTop>
@@ -709,7 +721,10 @@ __device__ __forceinline__ void finish(Shared<kTop>& sh, SharedTop& top, const O
       if constexpr (kTop) send(top.cluster_best(rank) + lane, &sh.others, 0, best);
       return;
     }
-    if (!warp_wait_cluster_bounded(smem_u32(&sh.others), 0, &sh.abort_flag, err, kDevTimeoutEpilogue)) st.m = kNan;
+    if (!warp_wait_cluster_bounded(smem_u32(&sh.others), 0, &sh.abort_flag, err, kDevTimeoutEpilogue)) {
+      outlive_peers(smem_u32(&sh.others), err);
+      st.m = kNan;
+    }
     if (lane > 0) {
       st = Stats{-kInf, 0.f, 0.f};
       if (lane < static_cast<int>(cs)) st = Stats{sh.cluster_stats[lane][0], sh.cluster_stats[lane][1], sh.cluster_stats[lane][2]};
@@ -767,6 +782,9 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
   pdl_wait();
   pdl_launch_dependents();
 
+  auto give_up = [&]() {
+    if (kCluster && rank == 0) outlive_peers(smem_u32(&sh.others), err);
+  };
   if (warp == kWarps) {
     // ------------------------------------------------------------------ fetch
     const unsigned step = gridDim.x >> bits;
@@ -819,65 +837,76 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
       return n > static_cast<int>(L) || static_cast<int>(t) < n;
     };
     // 32 of the rows at a time, one a lane: whether it holds a token, and which
-    for (unsigned long long base = blockIdx.x >> bits; base < items; base += 32ull * step) {
-      const unsigned long long item = base + static_cast<unsigned long long>(lane) * step;
-      unsigned row_l = static_cast<unsigned>(item);
-      bool live = item < items;
-      int id = 0;
-      if (live) {
-        if (even) {  // the last sequence with no more rows before it
-          int lo = 0, hi = kEvenMax;
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (sh.before[mid] <= static_cast<int>(item)) lo = mid; else hi = mid;
+    auto fetch = [&]() {  // false where a wait has run out
+      for (unsigned long long base = blockIdx.x >> bits; base < items; base += 32ull * step) {
+        const unsigned long long item = base + static_cast<unsigned long long>(lane) * step;
+        unsigned row_l = static_cast<unsigned>(item);
+        bool live = item < items;
+        int id = 0;
+        if (live) {
+          if (even) {  // the last sequence with no more rows before it
+            int lo = 0, hi = kEvenMax;
+            while (hi - lo > 1) {
+              const int mid = (lo + hi) / 2;
+              if (sh.before[mid] <= static_cast<int>(item)) lo = mid; else hi = mid;
+            }
+            row_l = lo * L + static_cast<unsigned>(item) - sh.before[lo];
           }
-          row_l = lo * L + static_cast<unsigned>(item) - sh.before[lo];
+          if (out.logp) id = ids[row_l];
+          if (!even) {
+            live = live_row(row_l, rank == 0);
+            if (!live && rank == 0) out.dead(row_l);
+          }
         }
-        if (out.logp) id = ids[row_l];
-        if (!even) {
-          live = live_row(row_l, rank == 0);
-          if (!live && rank == 0) out.dead(row_l);
+        for (uint32_t todo = __ballot_sync(0xffffffffu, live); todo != 0; todo &= todo - 1) {
+          const int l = __ffs(todo) - 1;
+          const unsigned row = __shfl_sync(0xffffffffu, row_l, l);
+          const int row_id = __shfl_sync(0xffffffffu, id, l);
+          const Row<T> r(logits + row * ld, V);
+          const Part part(r.n_slots, rank, bits);
+          int j0 = part.lo, segment = 0, left = segment_stages(part);
+          do {  // a part without slots has a stage, too
+            if (!acquire()) return false;
+            if (lane == 0) {
+              const int j1 = min(j0 + kStageSlots, part.hi), lo = max(j0, r.full_lo), hi = min(j1, r.full_hi);
+              unsigned char* dst = sh.ring[q];
+              // The row's first and last slot, where it has them in part. Whole stages that lie there later are written by
+              // bulk copies: a proxy of their own, before which these stores have to be done.
+              const bool head = j0 < min(lo, j1), tail = hi < j1 && j1 > lo;
+              if (head) *reinterpret_cast<uint4*>(dst) = r.load(j0);
+              if (tail) *reinterpret_cast<uint4*>(dst + (j1 - 1 - j0) * 16) = r.load(j1 - 1);
+              if (head || tail) fence_proxy_async();
+              sh.stage[q] = Stage{row, j0,
+                                  (j1 - j0) | (j0 == part.lo ? kFirst : 0) | (j1 == part.hi ? kLast : 0) |
+                                      (left <= 1 || j1 == part.hi ? kSegmentEnd : 0) | segment << kSegmentShift,
+                                  row_id};
+              const uint32_t bytes = hi > lo ? static_cast<uint32_t>(hi - lo) * 16 : 0;
+              mbar_arrive_expect_tx(smem_u32(&sh.full[q]), bytes);
+              if (bytes > 0) bulk_load(smem_u32(dst + (lo - j0) * 16), r.p + r.first(lo), bytes, smem_u32(&sh.full[q]));
+            }
+            advance();
+            j0 += kStageSlots;
+            if (--left == 0) {
+              left = segment_stages(part);
+              ++segment;
+            }
+          } while (j0 < part.hi);
         }
       }
-      for (uint32_t todo = __ballot_sync(0xffffffffu, live); todo != 0; todo &= todo - 1) {
-        const int l = __ffs(todo) - 1;
-        const unsigned row = __shfl_sync(0xffffffffu, row_l, l);
-        const int row_id = __shfl_sync(0xffffffffu, id, l);
-        const Row<T> r(logits + row * ld, V);
-        const Part part(r.n_slots, rank, bits);
-        int j0 = part.lo, segment = 0, left = segment_stages(part);
-        do {  // a part without slots has a stage, too
-          if (!acquire()) return;
-          if (lane == 0) {
-            const int j1 = min(j0 + kStageSlots, part.hi), lo = max(j0, r.full_lo), hi = min(j1, r.full_hi);
-            unsigned char* dst = sh.ring[q];
-            // The row's first and last slot, where it has them in part. Whole stages that lie there later are written by
-            // bulk copies: a proxy of their own, before which these stores have to be done.
-            const bool head = j0 < min(lo, j1), tail = hi < j1 && j1 > lo;
-            if (head) *reinterpret_cast<uint4*>(dst) = r.load(j0);
-            if (tail) *reinterpret_cast<uint4*>(dst + (j1 - 1 - j0) * 16) = r.load(j1 - 1);
-            if (head || tail) fence_proxy_async();
-            sh.stage[q] = Stage{row, j0,
-                                (j1 - j0) | (j0 == part.lo ? kFirst : 0) | (j1 == part.hi ? kLast : 0) |
-                                    (left <= 1 || j1 == part.hi ? kSegmentEnd : 0) | segment << kSegmentShift,
-                                row_id};
-            const uint32_t bytes = hi > lo ? static_cast<uint32_t>(hi - lo) * 16 : 0;
-            mbar_arrive_expect_tx(smem_u32(&sh.full[q]), bytes);
-            if (bytes > 0) bulk_load(smem_u32(dst + (lo - j0) * 16), r.p + r.first(lo), bytes, smem_u32(&sh.full[q]));
-          }
-          advance();
-          j0 += kStageSlots;
-          if (--left == 0) {
-            left = segment_stages(part);
-            ++segment;
-          }
-        } while (j0 < part.hi);
+      if (!acquire()) return false;
+      if (lane == 0) {
+        sh.stage[q] = Stage{0, 0, -1, 0};
+        mbar_arrive(smem_u32(&sh.full[q]));
       }
-    }
-    if (!acquire()) return;
-    if (lane == 0) {
-      sh.stage[q] = Stage{0, 0, -1, 0};
-      mbar_arrive(smem_u32(&sh.full[q]));
+      return true;
+    };
+    if (!fetch()) {  // the copies under way come before this CTA's memory goes
+      int never = 0;
+      for (int x = 0; x < kStages; ++x)
+        if (x < q || wrapped)
+          warp_wait_bounded(smem_u32(&sh.full[x]), x < q ? parity ^ 1 : parity, &never, err, kDevTimeoutProducer);
+      give_up();
+      return;
     }
     if (even)
       for (unsigned long long row = blockIdx.x + static_cast<unsigned long long>(lane) * step; row < rows; row += 32ull * step)
@@ -890,7 +919,11 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
     const int f = warp - kWarps - 1;
     End& e = top.end[f];
     for (uint32_t parity = 0;; parity ^= 1) {
-      if (!warp_wait_bounded(smem_u32(&e.done), parity, &sh.abort_flag, err, kDevTimeoutEpilogue) || e.end) return;
+      if (!warp_wait_bounded(smem_u32(&e.done), parity, &sh.abort_flag, err, kDevTimeoutEpilogue)) {
+        give_up();
+        return;
+      }
+      if (e.end) return;
       const unsigned row = e.row;
       const Row<T> r(logits + row * ld, V);
       float z_id = kNan;
@@ -915,7 +948,11 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
   float segment = -kInf;  // the thread's maximum of the segment so far
   bool holds = false;     // whether it has any slot
   for (;;) {
-    if (!mbar_wait_bounded(smem_u32(&sh.full[q]), parity, &sh.abort_flag, err, kDevTimeoutEpilogue)) return;
+    if (!warp_wait_bounded(smem_u32(&sh.full[q]), parity, &sh.abort_flag, err, kDevTimeoutEpilogue)) {
+      if constexpr (!kTop) summers_excuse();
+      give_up();
+      return;
+    }
     const Stage in = sh.stage[q];
     if (in.n_flags < 0) break;
     const int n = in.n_flags & (kFirst - 1);
@@ -923,7 +960,7 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
       run = Running<T>();
       holds = tid < n;  // a summer without a slot in the first stage has none
       if (kTop && (used & 2) && !warp_wait_bounded(smem_u32(&top.end[buf].free), used & 1, &sh.abort_flag, err, kDevTimeoutDrain))
-        return;
+        return;  // (not in a cluster: it has one row)
       if (!kTop && tid == 0 && rank == 0 && out.logp) {
         z_id = kNan;
         if (in.id < 0 || in.id >= V) record_error(err, kDevBadTokenId); else z_id = to_f(logits[in.row * ld + in.id]);
@@ -996,6 +1033,11 @@ __global__ void __launch_bounds__(block_threads<kTop>(), ctas_per_sm<kTop>())
         st = lane < kWarps ? Stats{sh.red[buf][0][lane], sh.red[buf][1][lane], sh.red[buf][2][lane]} : Stats{-kInf, 0.f, 0.f};
         st.merge_lanes(kWarps);
         finish<kTop>(sh, top, out, in.row, st, z_id, 0, rank, cs, lane, err);
+      }
+      // one that missed this barrier has raised the flag before it; all the others see that here or at the next
+      if (!kCluster && *static_cast<volatile int*>(&sh.abort_flag)) {
+        summers_excuse();
+        return;
       }
     }
     if (++buf == kEnders) {

@@ -37,3 +37,17 @@ def test_rows_that_fill_a_stage_of_the_ring_in_part_and_whole(k, dtype):
     for _ in range(20):
         again = run_stats(z, ids, None, rows, 1, k)
         assert all(torch.equal(first[name], again[name]) for name in first)
+
+
+@pytest.mark.parametrize("k", [0, 5])
+@pytest.mark.parametrize("rows", [1, 30, 70])
+def test_clusters_whose_row_holds_no_token_end_at_once(rows, k):
+    """The first CTA of a cluster waits for what the others send, which they do for a row that holds a token only: no
+    wait may run out (the device error would say so), call after call."""
+    V = 32000
+    z, _ = rows_of(np.random.default_rng(rows).normal(0, 3, (rows, V)), torch.float32)
+    ids, values = np.arange(rows), host_f64(z)
+    for live in (np.zeros(rows, np.int64), np.ones(rows, np.int64), np.arange(rows) % 2):
+        for _ in range(3):
+            check_stats(run_stats(z, ids, live, rows, 1, k), values, ids, live, rows, 1, k)
+            assert H.device_error() == 0
