@@ -167,8 +167,8 @@ struct TokenStatsArgs {
   int* err;
 };
 constexpr int kTokenTopMax = 32;
-// With top_k the values beyond a bound may come in the order that raises it most slowly: time that grows with V^2, 2.5 ms
-// a row at 65536 logits. At this V that stays below the limit of the waits for it.
+// With top_k one warp selects from a row, in at most 36 passes over what may be among its best. At this V the slowest order
+// that was found takes 3.7 ms (400 rows of fp32); the others of its CTA wait for about 1 s at most.
 constexpr int64_t kTokenTopMaxV = 1 << 20;
 int launch_token_stats(const TokenStatsArgs& a, cudaStream_t stream);
 struct TokenStatsGradArgs {
