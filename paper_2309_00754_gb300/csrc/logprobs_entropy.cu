@@ -233,7 +233,11 @@ struct Running {
   __device__ __forceinline__ void raise(float nm) {  // m' to nm, NaN if there is a NaN
     const bool h = fabsf(nm) >= 0x1p20f;
     const float ref = h ? nm : nm * kLog2e;
-    const float d = max_nan(h || huge ? (from - nm) * kLog2e : -unpack2(nref).x - ref, kFloor * kLog2e);
+    // From the old reference to the new one, each with its own rounding, which may be 2^-4 near 2^20 and is in every term
+    // so far: (of a huge one: none) one fma takes the other from it.
+    const float old = -unpack2(nref).x;
+    const float d = max_nan(huge ? (h ? (from - nm) * kLog2e : fmaf(from, kLog2e, -ref))
+                                 : (h ? fmaf(-nm, kLog2e, old) : old - ref), kFloor * kLog2e);
     const float c = exp2_fast(d);
     w = fma2(s, pack2(d, d), w);
     s = fma2(s, pack2(c, c), 0);

@@ -54,6 +54,25 @@ def test_clusters_whose_row_holds_no_token_end_at_once(rows, k):
             assert H.device_error() == 0
 
 
+@pytest.mark.parametrize("rows,V", [(1300, 6000), (40, 20000), (400, 20000)])
+@pytest.mark.parametrize("base", [2.0 ** 20, -(2.0 ** 20)])
+def test_maximum_that_passes_2_to_the_20(rows, V, base):
+    """A thread's terms are summed in another way from there on: nearly all of the row just below, later a
+    little of it just above, more than the reference may trail. All values are multiples of 1/4, exact in fp32; what is
+    below has 1 % to 10 % of the sum."""
+    rng = np.random.default_rng(V + rows)
+    z = base - rng.integers(28, 40, (rows, V)) / 4.0
+    late = np.arange(V) >= V // 2
+    z[:, late] = np.where(rng.random((rows, int(late.sum()))) < 0.01, base + rng.integers(0, 8, (rows, int(late.sum()))) / 4.0,
+                          z[:, late])
+    dev, _ = rows_of(z, torch.float32)
+    values, ids = host_f64(dev), rng.integers(0, V, rows)
+    assert np.array_equal(values, z)
+    check_stats(run_stats(dev, ids, None, rows, 1, 0), values, ids, None, rows, 1, 0)
+    if V == 20000:
+        check_stats(run_stats(dev, ids, None, rows, 1, 5), values, ids, None, rows, 1, 5)
+
+
 def slow_order(rows, V, dtype):
     """Rows whose 31 times 4 of 256 threads hold values that ascend in about the order in which a selection collects them:
     every bound of it is passed by the most values that there can be."""
