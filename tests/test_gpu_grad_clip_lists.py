@@ -1,0 +1,38 @@
+"""Gradient norm and clipping: the three operations behind the sum, and lists of every size that takes a way of its own.
+
+u = 2^-24, half a step of fp32."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2309_00754_gb300 import build as B
+from paper_2309_00754_gb300 import hydra as H
+from tests.test_gpu_grad_clip import BF16, F32, U, workspace
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    assert torch.cuda.is_available(), "GPU tests need a CUDA device"
+    B.build()
+    H.load()
+    H.device_error(clear=True)
+    yield
+    assert H.device_error(clear=True) == 0
+
+
+def test_norm_and_coefficient_are_rounded_once():
+    """Squares of whole numbers add up exactly, so nothing but root, sum and quotient can be off: half a step, and
+    2^-40 for what the correction of each leaves out. Norms far below 1e-6 and in the range of the fp64 sums, too."""
+    rng = np.random.default_rng(1)
+    n2, ws = torch.zeros(2, device="cuda"), workspace()
+    for _ in range(300):
+        g = rng.integers(-999, 1000, rng.integers(1, 700)) * 2.0 ** rng.integers(-60, 50)
+        max_norm = float(np.float32(np.sqrt((g * g).sum() + 1e-14) * 10 ** rng.uniform(-5, 1)))
+        H.hydra_grad_norm(H.GradList([torch.from_numpy(g.astype(np.float32)).cuda()]), max_norm, n2, ws)
+        norm = np.sqrt((g * g).sum())
+        want = np.array([norm, min(1.0, max_norm / (norm + 1e-6))])
+        got = n2.cpu().numpy()
+        half = np.spacing(want.astype(np.float32)).astype(np.float64) / 2
+        assert np.all(np.abs(got.astype(np.float64) - want) <= half + 2.0 ** -40 * want), (got, want, g)
