@@ -489,7 +489,10 @@ typedef struct hydra_grad_tensor {
  *     norm = sqrt(sum of g^2 over all elements of all tensors)
  *     coef = min(1, max_norm / (norm + 1e-6)), and 1 where the norm is not finite
  * and hydra_clip_grad_norm also writes out = g coef to every tensor (fp32 product, rounded once to
- * dtype). A norm that is not finite leaves the values as they were: the caller sees it in norm_out.
+ * dtype). A norm that is not finite (an element is an infinity or NaN) leaves the values as they were.
+ * A norm that is finite but beyond fp32 is written as +inf, and its values are clipped all the same, with
+ * a coefficient below 1 that is rounded to fp32 (below 2^-126 to fewer bits, at last to 0). So norm_out[0]
+ * alone does not tell whether values were touched; norm_out[1] does: they were where it is not 1.
  *   tensors  : HOST array of n entries (device pointers inside), read during the call only: a
  *              captured call keeps the addresses. Types may be mixed, pointers need no more than
  *              their element's alignment, empty tensors (numel 0) are skipped.
@@ -501,8 +504,9 @@ typedef struct hydra_grad_tensor {
  * numbers that carry their rounding errors (in fp64 where a run's squares would overflow or vanish in
  * fp32), in an order that depends on nothing but the list and the device: equal calls give equal bits.
  * No fp32 element is too large or too small for its square.
- * norm_out and the workspace overlap none of the tensors. An out range may not overlap any other range of the list, read or written (the same tensor twice
- * among them); hydra_grad_norm, which only reads, counts a tensor listed twice twice.
+ * norm_out and the workspace overlap neither each other nor any of the tensors. An out range may not overlap
+ * any other range of the list, read or written (the same tensor twice among them); hydra_grad_norm,
+ * which only reads, counts a tensor listed twice twice.
  * Errors: n < 0, n >= 2^31, a numel < 0 or >= 2^40 -> HYDRA_ERR_SHAPE; max_norm or a dtype, or
  * overlapping ranges -> HYDRA_ERR_RANGE; NULL norm_out, list or (numel > 0) tensor -> HYDRA_ERR_NULL;
  * a pointer not aligned to its element -> HYDRA_ERR_ALIGN; small or misaligned workspace ->

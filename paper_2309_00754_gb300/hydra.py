@@ -631,7 +631,9 @@ def hydra_grad_norm(tensors, max_norm, norm_out, workspace, stream=None):
 
 
 def hydra_clip_grad_norm(tensors, max_norm, norm_out, workspace, stream=None):
-    """hydra_grad_norm, and every gradient times that coefficient into its output."""
+    """hydra_grad_norm, and every gradient times that coefficient into its output. The values are left as they
+    were where norm_out[1] is 1: for a small norm, and for one that is not finite (an infinity or NaN among
+    them). A finite norm beyond fp32 reads +inf, too, but its coefficient is below 1 and its values are clipped."""
     _grad_norm("hydra_clip_grad_norm", tensors, max_norm, norm_out, workspace, stream)
 
 

@@ -11,6 +11,8 @@ from tests.test_gpu_grad_clip import BF16, F32, U, workspace
 
 pytestmark = pytest.mark.gpu
 
+INF = float("inf")
+
 
 @pytest.fixture(scope="module", autouse=True)
 def lib():
@@ -36,3 +38,18 @@ def test_norm_and_coefficient_are_rounded_once():
         got = n2.cpu().numpy()
         half = np.spacing(want.astype(np.float32)).astype(np.float64) / 2
         assert np.all(np.abs(got.astype(np.float64) - want) <= half + 2.0 ** -40 * want), (got, want, g)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("size,touched", [(1e38, True), (3e38, True), (INF, False)])
+def test_the_coefficient_tells_whether_values_were_touched(size, touched, in_place):
+    """A norm of +inf may be a finite one beyond fp32: then the coefficient is below 1 and every value clipped."""
+    g = torch.full((100_000,), size, device="cuda")
+    out, n2 = g if in_place else torch.zeros_like(g), torch.zeros(2, device="cuda")
+    H.hydra_clip_grad_norm(H.GradList([g], [out]), 1.0, n2, workspace())
+    norm, coef = n2.tolist()
+    assert norm == INF and (coef < 1) == touched
+    want = 1 / np.sqrt(1e5) if touched else size
+    # a coefficient of about 1e-41 is a multiple of 2^-149: half a step of it
+    tol = want * (2.0 ** -150 / coef + 4 * U) if touched else 0
+    assert (out.double() == want).all() if not touched else ((out.double() - want).abs() <= tol).all()
