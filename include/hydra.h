@@ -510,7 +510,7 @@ typedef struct hydra_grad_tensor {
  * Errors: n < 0, n >= 2^31, a numel < 0 or >= 2^40 -> HYDRA_ERR_SHAPE; max_norm or a dtype, or
  * overlapping ranges -> HYDRA_ERR_RANGE; NULL norm_out, list or (numel > 0) tensor -> HYDRA_ERR_NULL;
  * a pointer not aligned to its element -> HYDRA_ERR_ALIGN; small or misaligned workspace ->
- * HYDRA_ERR_WORKSPACE. n == 0 writes (0, 1).
+ * HYDRA_ERR_WORKSPACE. n == 0 is a norm of 0: (0, 1), or (0, max_norm / 1e-6) for a max_norm below 1e-6.
  */
 size_t hydra_grad_norm_workspace_size(void);
 hydra_status hydra_grad_norm(const hydra_grad_tensor* tensors, int64_t n, float max_norm, float* norm_out,

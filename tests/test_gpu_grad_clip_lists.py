@@ -53,3 +53,11 @@ def test_the_coefficient_tells_whether_values_were_touched(size, touched, in_pla
     # a coefficient of about 1e-41 is a multiple of 2^-149: half a step of it
     tol = want * (2.0 ** -150 / coef + 4 * U) if touched else 0
     assert (out.double() == want).all() if not touched else ((out.double() - want).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("fn", [H.hydra_grad_norm, H.hydra_clip_grad_norm])
+def test_empty_lists_have_a_norm_of_zero(fn):
+    n2 = torch.full((2,), 5.0, device="cuda")
+    for max_norm, coef in ((1.0, 1.0), (1e-6, 1.0), (2.5e-7, 0.25), (INF, 1.0)):
+        fn(H.GradList([]), max_norm, n2, workspace())
+        assert n2[0] == 0 and abs(n2[1].item() - min(1.0, float(np.float32(max_norm)) / 1e-6)) <= U * coef
