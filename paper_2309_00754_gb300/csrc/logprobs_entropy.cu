@@ -23,6 +23,7 @@
 // Backward, with p = exp((z - m) - log s):
 //     dz[v] = g_logp (1[v = id] - p_v) - g_entropy p_v (log p_v + entropy)
 #include <algorithm>
+#include <atomic>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -1378,9 +1379,8 @@ cudaLaunchConfig_t stats_config(unsigned clusters, int cs, cudaStream_t stream, 
 // Clusters of 1 << bits CTAs that the device holds at once (0: none, or it does not say, which is not kept).
 template <typename T, bool kTop>
 int clusters_held(int dev, int bits) {
-  static int held[64][4];  // and one more
-  int& h = held[dev][bits];
-  if (h > 0) return h - 1;
+  static std::atomic<int> held[64][4];  // and one more; host threads may ask at once
+  if (const int known = held[dev][bits]; known > 0) return known - 1;
   cudaLaunchAttribute attr[2];
   cudaLaunchConfig_t cfg = stats_config<T, kTop>(1, 1 << bits, nullptr, attr);
   cfg.numAttrs = 1;
@@ -1389,7 +1389,7 @@ int clusters_held(int dev, int bits) {
     cudaGetLastError();
     return 0;
   }
-  h = n + 1;
+  held[dev][bits] = n + 1;
   return n;
 }
 
@@ -1430,7 +1430,7 @@ bool rows_are_short(int64_t rows, int64_t V) {
 
 template <typename T, bool kTop>
 int launch_stats(const TokenStatsArgs& a, cudaStream_t stream) {
-  static bool attr_set[64] = {false};  // the shared-memory limit is a per-device attribute
+  static std::atomic<bool> attr_set[64];  // the shared-memory limit is a per-device attribute
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
   if (!attr_set[dev]) {

@@ -24,6 +24,8 @@
 //    adjacent in the schedule, so each W tile comes from HBM once and again from L2.
 #include <float.h>
 
+#include <atomic>
+
 #include "common.cuh"
 #include "kernels.h"
 
@@ -980,15 +982,15 @@ static bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t c
 }
 
 int sm_count() {
-  static int cached[64] = {0};
+  static std::atomic<int> cached[64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  if (cached[dev] == 0) {
-    int n = 0;
+  int n = cached[dev];
+  if (n == 0) {
     if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
     cached[dev] = n;
   }
-  return cached[dev];
+  return n;
 }
 
 // Tile width of the CTA-pair kernel: the candidate with the least waves x (width + 224)
