@@ -590,7 +590,10 @@ def all_reduce_adv_moments(moments, group=None):
 class GradList:
     """The gradient tensors of an update (fp32 or bf16, contiguous) as hydra_grad_norm and
     hydra_clip_grad_norm take them, with the tensors that receive the clipped values (None: in
-    place). Built once and kept as long as the buffers: it holds references to them."""
+    place). Built once and kept as long as the buffers: it stands for the memory that the tensors have now
+    and keeps that alive. Gradients that a step replaces (`p.grad = ...`, `p.grad.data = ...`, a backward
+    pass after zero_grad(set_to_none=True)) want a new list, as the old one goes on with the old memory;
+    their storages must not be resized meanwhile."""
 
     def __init__(self, grads, outs=None):
         self.grads = list(grads)
@@ -605,6 +608,8 @@ class GradList:
                 raise ValueError(f"outs[{i}] has shape {tuple(o.shape)}, its gradient {tuple(g.shape)}")
             self.c[i] = GradTensorC(_p(g), _p(o), g.numel(), _out_dtype(g, f"grads[{i}]"))
         self.devices = {t.device.index for t in (*self.grads, *self.outs)}
+        # a tensor that is given other memory lets go of this one
+        self.storages = [t.untyped_storage() for t in (self.grads if outs is None else (*self.grads, *self.outs))]
 
     def __len__(self):
         return len(self.grads)

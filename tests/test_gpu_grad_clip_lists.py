@@ -61,3 +61,18 @@ def test_empty_lists_have_a_norm_of_zero(fn):
     for max_norm, coef in ((1.0, 1.0), (1e-6, 1.0), (2.5e-7, 0.25), (INF, 1.0)):
         fn(H.GradList([]), max_norm, n2, workspace())
         assert n2[0] == 0 and abs(n2[1].item() - min(1.0, float(np.float32(max_norm)) / 1e-6)) <= U * coef
+
+
+def test_a_list_keeps_the_memory_that_its_tensors_had():
+    """Memory that a gradient has let go of is not given to another tensor while a list writes there."""
+    n2, ws = torch.zeros(2, device="cuda"), workspace()
+    g = torch.full((3_000_000,), 2.0, device="cuda")
+    out = torch.zeros_like(g)
+    plans = [H.GradList([g]), H.GradList([g], [out])]
+    g.data, out.data = torch.ones(5, device="cuda"), torch.ones(5, device="cuda")
+    others = [torch.full((3_000_000,), 7.0, device="cuda") for _ in range(4)]
+    for plan in plans:
+        H.hydra_clip_grad_norm(plan, 1.0, n2, ws)
+    assert all((x == 7).all() for x in others)
+    H.hydra_grad_norm(plans[0], 1.0, n2, ws)
+    assert abs(n2[0].item() - 1) <= 1e-6
