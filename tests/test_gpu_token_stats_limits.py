@@ -6,7 +6,7 @@ import torch
 
 from paper_2309_00754_gb300 import build as B
 from paper_2309_00754_gb300 import hydra as H
-from tests.test_gpu_token_stats import DTYPES, check_stats, rows_of, run_stats
+from tests.test_gpu_token_stats import DTYPES, check_stats, make, rows_of, run_stats
 from tests.helpers import host_f64
 
 pytestmark = pytest.mark.gpu
@@ -155,3 +155,15 @@ def test_selection_takes_a_time_that_grows_with_the_vocabulary():
             best = min(best, a.elapsed_time(b))
         took.append(best)
     assert took[1] < 8 * took[0], took
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 6200), ("bf16", 8200)])
+@pytest.mark.parametrize("S,L", [(1, 700), (127, 8), (128, 7), (129, 7), (700, 2)])
+def test_ragged_batches_without_alternatives_that_go_through_the_ring(S, L, dtype, V):
+    """Rows too long for a warp each, more of them than CTAs: up to 128 sequences have their live rows dealt by number, more
+    of them by row. Full and empty sequences and those of one token, and a batch of none."""
+    z, values, ids, lengths, _ = make(S + L, S, L, V, DTYPES[dtype], ld=V + 3, shift=1)
+    lengths[1::4], lengths[2::7] = 0, 1
+    check_stats(run_stats(z, ids, lengths, S, L, 0), values, ids, lengths, S, L, 0)
+    lengths[:] = 0
+    check_stats(run_stats(z, ids, lengths, S, L, 0), values, ids, lengths, S, L, 0)
