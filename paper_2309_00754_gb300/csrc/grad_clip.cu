@@ -24,11 +24,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kCtasPerSm = 4;  // (two: 205 MB of fp32 103 us, six 140, eight 163, for 94)
-// Chunks of 16 KB, of a large list 32 KB: 410 MB of bf16 193 us and 212 with the small ones, 205 MB of fp32 94 and 97;
-// but 26 MB of fp32 18.4 and 16.0. The large ones are scaled by two CTAs an SM at a time (registers; held to 64 of them
-// 126 us).
+// Chunks of 16 KB, of a large list 32 KB. Small / large, us in a graph, 20 tensors, fp32 and bf16: 50 MB 24.6 / 25.8 and
+// 25.5 / 28.1, 100 MB 47.8 / 48.6 and 49.5 / 51.3, 130 MB 62.1 / 61.9 and 65.5 / 64.4, 155 MB 74.5 / 72.8 and 78.9 / 76.1,
+// 205 MB 97.9 / 96.9 and 104.4 / 99.6; 400 tensors cross at the same size. The large ones are scaled by two CTAs an SM at a
+// time (registers; held to 64 of them 126 us for 205 MB).
 constexpr int kChunkSmall = 16384, kChunkLarge = 32768;
-constexpr int64_t kLargeBytes = 160 << 20;
+constexpr int64_t kLargeBytes = 120 << 20;
 // Of a longer list the last of every CTA's range, where the second pass begins, is to stay in L2; the rest and the outputs
 // leave it first (102 MB of fp32 53 -> 49 us, 205 MB 110 -> 94, 822 MB 411 -> 376; 16 or 32 MB of it 53, 99 and 96, 376).
 constexpr int kKeepBytes = 64 << 20;
@@ -397,7 +398,9 @@ cudaError_t launch_scale(const ListPart& p, const Partial* partial, int n_partia
   return launch_pdl(grad_scale_kernel<kCap, kBytes>, dim3(p.grid), dim3(kThreads), 0, st, p.parameters<kCap>(), p.n,
                     p.chunks, partial, n_partials, max_norm, norm_out);
 }
-// A launch carries a table of 32, 224 or 880 tensors.
+// A launch carries a table of 32, 224 or 880 tensors: it is copied twice on its way, in full. A call's enqueueing of 20 / 100
+// / 194 tensors takes 7.5 / 9.3 / 10.7 us so, 9.5 / 10.7 / 12.3 with the table of 880 alone; the kernels take the same.
+// 224 hold the LoRA gradients of 32 layers (six a layer) and some more.
 constexpr int kTableSmall = 32, kTableMiddle = 224;
 
 }  // namespace

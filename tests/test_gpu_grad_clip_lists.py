@@ -1,7 +1,7 @@
 """Gradient norm and clipping: the three operations behind the sum, and lists of every size that takes a way of its own.
 
 u = 2^-24, half a step of fp32. A thread adds the squares of its elements of a chunk in fp32, one rounding each: of 32 KB (lists
-of 160 MB on) up to 64 of bf16 and one or two at its ends, 66 roundings of sums that only grow, so 66 u relative; of 16 KB
+of 120 MB on) up to 64 of bf16 and one or two at its ends, 66 roundings of sums that only grow, so 66 u relative; of 16 KB
 34 u. These sums are added in pairs of fp32 numbers, whose own errors (2^-46 each, 2^11 in a row at most) vanish beside
 that, and root and quotient are rounded once. So the norm is off by (66 / 2 + 1) u, the coefficient by 35 u, a clipped
 value by 36 u with its product's rounding and by the rounding to its type (half a step, eps / 2)."""
@@ -122,7 +122,7 @@ def check_all(grads, max_norm, out_shifts):
     assert int(bad) == 0
 
 
-LARGE = {  # 32 KB chunks, in tables of 224 and 880 and several launches; all over 160 MB
+LARGE = {  # 32 KB chunks, in tables of 224 and 880 and several launches
     "few": ([20_000_003, 33_000_001, 5, 7_000_009, 8191, 16385, 1], [F32, BF16, F32, F32, BF16]),
     "bf16": ([60_000_007, 25_000_000, 333], [BF16]),
     "300": ([180_001 + 7 * i for i in range(300)], [F32, F32, BF16]),
