@@ -10,7 +10,7 @@
 // The rows come through a ring of 16 KB stages that one warp fills with bulk copies, rows ahead of the
 // eight warps that sum them: 256 threads with a maximum and two sums each, whose parts one warp puts
 // together. Four CTAs an SM take every 608th row. HBM bounds it where the logits are fp32 (4096 x 32000: 77 to 80 us,
-// 97 to 101 % of the measured rate), and nearly so the 8.6 instructions an element of bf16 (8192 x 32000: 82.7 us,
+// 97 to 101 % of the measured rate), and nearly so the 8.4 instructions an element of bf16 (8192 x 32000: 82.3 us,
 // 94 %). Few rows are shared by clusters, which meet in the first CTA's memory; short ones take a warp each.
 //
 // The k likeliest tokens, in the order (logit descending, index ascending): every thread keeps its best
@@ -18,7 +18,8 @@
 // too; the eighths that reach it, about k, are read again, and the few elements not behind it are ranked by
 // counting. Three warps of a CTA do that, a row each, while the others are in the next rows, as it takes
 // 3 to 8 us, most of it one step waiting for the one before. Two such CTAs fit an SM (4096 x 32000 fp32, k = 8:
-// 81 us; 8192 x 32000 bf16 97, three CTAs of fewer registers 113; selected by the summing threads themselves 130).
+// 81 us; 8192 x 32000 bf16 99; when that was 97, three CTAs of fewer registers took 113, and selection by the summing
+// threads themselves 130).
 //
 // Backward, with p = exp((z - m) - log s):
 //     dz[v] = g_logp (1[v = id] - p_v) - g_entropy p_v (log p_v + entropy)
@@ -382,8 +383,8 @@ __device__ __forceinline__ uint32_t sort_warp(uint32_t v, int lane) {
   }
   return v;
 }
-// warp_wait_bounded whose loop the whole warp takes together, without lanes that branch off (8192 x 32000 bf16, k = 8: 66.8
-// us, 67.8 with that)
+// warp_wait_bounded whose loop the whole warp takes together, without lanes that branch off (8 x 1024 ragged rows of 32000
+// bf16, k = 8: 66.8 us, 67.8 with that)
 __device__ __forceinline__ bool warp_wait_converged(uint32_t bar, uint32_t parity, volatile int* abort, int* err, int code) {
   if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
   const long long t0 = clock64();
@@ -1246,7 +1247,8 @@ __device__ __noinline__ void tile_apart(const TI* z, TO* d, int i0, int V, bool 
 // A warp takes a tile of a row. Units lie on the 16-byte grid of both arrays where their rows start alike on it
 // (`a` elements before the row); else every element goes by itself.
 // Memory bounds it: 2048 x 32000 fp32 80 us (96 % of measured HBM), fp32 to bf16 58 (99 %), bf16 42 (92 %; 62.8
-// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.4 now).
+// when every element was turned by itself, with a CTA a tile of 4096; so were 8000 x 1001, 22 us, 12.4 now), bf16 to fp32
+// 65 (89 %).
 template <typename TI, typename TO>
 __global__ void __launch_bounds__(kGradWarps * 32, 4)
     token_stats_grad_kernel(const TI* logits, long long ld, unsigned L, int V, unsigned tiles, unsigned items,
