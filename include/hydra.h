@@ -61,7 +61,8 @@ int hydra_abi_version(void);
  * Read (and optionally clear) the device error word of the current CUDA device.
  * Synchronises the device. *code_out receives 0 when no kernel has reported an error,
  * otherwise the first code recorded (0x1xx: bounded wait expired, 0x201: token id out of
- * range, 0x202: sequence length out of range). Returns HYDRA_OK, HYDRA_ERR_NULL or
+ * range, 0x202: sequence length out of range, 0x203: page number outside a paged cache, 0x204:
+ * position outside a page table or rotation table). Returns HYDRA_OK, HYDRA_ERR_NULL or
  * HYDRA_ERR_CUDA.
  */
 hydra_status hydra_device_error(int32_t* code_out, int clear);
@@ -552,6 +553,135 @@ hydra_status hydra_rope(void* qkv, int64_t R, int64_t ld, int64_t d, int64_t hea
 hydra_status hydra_causal_attention(const void* qkv, int64_t nseq, int64_t P, int64_t ld,
                                     int64_t n_heads, int64_t head_dim, void* out, int64_t ld_out,
                                     void* stream);
+
+/* ----- Keys and values of generation in a paged cache, and drafted tokens ------------------------
+ *
+ * The actor's generation (Algorithms 1 and 2) with a cache that the caller keeps: pages of 16 to 128 tokens that
+ * sequences share a pool of, held in bf16 or in 4 bits, and several new tokens a sequence and step. A step with
+ * drafted tokens is hydra_kv_append and hydra_paged_attention in every layer, the LM head, and
+ * hydra_verify_drafts; tokens that it refuses are dropped by adding only the kept ones to `cached`, and the next step
+ * writes over them.
+ */
+typedef enum hydra_kv_kind { HYDRA_KV_BF16 = 0, HYDRA_KV_INT4 = 1 } hydra_kv_kind;
+
+/* A pool of pages. The struct is HOST memory and read during the call only. */
+typedef struct hydra_kv_cache {
+  void* data;         /* device, 16-byte aligned, n_pages * hydra_kv_page_bytes(...) bytes */
+  int64_t n_pages;    /* 1 .. 2^31 - 1 */
+  int64_t page;       /* tokens of a page: 16, 32, 64 or 128 */
+  int64_t n_kv_heads; /* 1 .. 4096 */
+  int64_t head_dim;   /* 64 or 128 */
+  int64_t kind;       /* hydra_kv_kind */
+} hydra_kv_cache;
+
+/* Bytes of a page: page * n_kv_heads * (4 head_dim in bf16, 9/8 head_dim in 4 bits); 0 where a parameter is not
+ * supported. Pages of a cache may be copied and moved whole. */
+size_t hydra_kv_page_bytes(int kind, int64_t page, int64_t n_kv_heads, int64_t head_dim);
+
+/*
+ * Appends the keys and values of up to L new tokens of each of S sequences to the cache, with the rotary position
+ * embedding (Su et al. 2021, rotate-half pairing as hydra_rope) applied to keys and queries on the way.
+ * Slot t of sequence s (row s*L + t) holds a token if t < lengths[s]; its position is cached[s] + t, and it lies in
+ * page table[s][position / page] at position % page.
+ *   table   : int32 rows of max_pages page numbers at stride ld_table. Entries that no token needs are not read.
+ *             Pages that two sequences share are read only (a prefix); two new tokens never have one place.
+ *   cached  : int32 [S] tokens already in the cache, >= 0; NULL means none.
+ *   lengths : int32 [S] new tokens, 0..L; NULL means all L.
+ *   q       : bf16 rows [S*L] of n_heads heads of head_dim at stride ld_q (e.g. the first columns of a fused q/k/v).
+ *   k, v    : bf16 rows of n_kv_heads heads at stride ld_kv.
+ *   rope_table : fp32 [rope_len, head_dim/2, 2], as hydra_rope_table writes it, or a table of the caller's own;
+ *             NULL: nothing is rotated. Products and sums are rounded as hydra_rope rounds them.
+ *   q_out   : bf16 rows at ld_q_out: the rotated queries, 0 in empty slots. q_out == q with the same stride works in
+ *             place. n_heads == 0: no queries (q, q_out ignored).
+ * A bf16 cache holds the rotated keys and the values rounded once. A cache in 4 bits holds each group of 64 channels of a
+ * token and head as scale (code - zero): with lo and hi the least and largest fp32 value of the group and 0,
+ *   scale = bf16((hi/2 - lo/2) 2/15), zero = clamp(rint(-lo / scale), 0, 15),
+ *   code = clamp(rint(x / scale) + zero, 0, 15)  (rint: ties to even; scale 0: the group is 0),
+ * so that it errs by about half a scale, at the ends of the range by up to one (scale and zero point are rounded; finite
+ * values over 3.3e38 may be held as an infinity). An infinity or NaN makes its group NaN.
+ * Pages that no token is written to, and a page's other tokens, keep their bytes.
+ * Errors: kind, page, head_dim, or q_out == q with another stride -> HYDRA_ERR_RANGE; S, L < 0, S*L >= 2^31, n_pages,
+ * n_heads or n_kv_heads outside their range, max_pages < 1 or max_pages * page >= 2^31, ld_table < max_pages, a row
+ * stride below its heads, rope_len < 1 with a table -> HYDRA_ERR_SHAPE; NULL cache, data, table, k, v (with n_heads:
+ * q, q_out) -> HYDRA_ERR_NULL; pointers not 16-byte aligned or row strides not multiples of 8 -> HYDRA_ERR_ALIGN.
+ * On the device: a length out of range -> 0x202, clamped; a page number outside [0, n_pages) -> 0x203, the token is not
+ * written; cached < 0, or new tokens past max_pages * page or rope_len -> 0x204, none of the sequence's tokens is
+ * written and its q_out rows are NaN. S*L == 0 is a no-op.
+ */
+hydra_status hydra_kv_append(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                             const int32_t* cached, const int32_t* lengths, int64_t S, int64_t L, const void* q,
+                             int64_t n_heads, int64_t ld_q, const void* k, const void* v, int64_t ld_kv,
+                             const float* rope_table, int64_t rope_len, void* q_out, int64_t ld_q_out, void* stream);
+
+/*
+ * Reads cached tokens back into dense rows: row s*L + t of k_out and v_out gets the keys and values of position
+ * first[s] + t (t < lengths[s]; other rows 0), as the cache holds them (keys rotated): in fp32 exactly, in bf16 rounded once.
+ *   first, lengths, table, cache : as cached, lengths, table and cache of hydra_kv_append.
+ *   k_out, v_out : rows [S*L] of n_kv_heads heads of out_dtype (HYDRA_BF16 or HYDRA_F32) at stride ld; either may be NULL.
+ * Errors as hydra_kv_append; out_dtype -> HYDRA_ERR_RANGE; both outputs NULL -> HYDRA_ERR_NULL. A token in a bad page
+ * (0x203), and a sequence's tokens where they pass the table (0x204), are NaN.
+ */
+hydra_status hydra_kv_read(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                           const int32_t* first, const int32_t* lengths, int64_t S, int64_t L, void* k_out, void* v_out,
+                           int out_dtype, int64_t ld, void* stream);
+
+/*
+ * Attention of the new tokens that hydra_kv_append has put in the cache, over all that the cache holds of their
+ * sequences up to themselves: for slot t < lengths[s] and query head h, with kv head h / (n_heads / n_kv_heads),
+ *     out = softmax_j(scale q.k_j) v_j,   j = 0 .. cached[s] + t
+ *   q     : bf16 rows [S*L] of n_heads heads at stride ld_q, rotated (q_out of hydra_kv_append).
+ *   out   : bf16 rows at stride ld_out, 0 in empty slots; out does not overlap q. n_heads % n_kv_heads == 0.
+ *   table, cached, lengths, S, L, cache : as the append of the same step.
+ *   workspace : device, 16-byte aligned, >= hydra_paged_attention_workspace_size(...) bytes, caller-owned; no
+ *             initial contents required; calls sharing a workspace must be stream-ordered.
+ * It is made for decoding, where L is a few tokens and the cache's bytes are all that counts; any L works, but every 32
+ * query rows (tokens times n_heads / n_kv_heads) of a kv head read the cache again.
+ * Bytes behind a sequence's last token may be anything, NaN among them, and what one query must not see does not
+ * change it. Scores, their maximum and sums are fp32.
+ * Bits: equal calls on one device give equal bits; a sequence's depend on the others' lengths (where work is cut).
+ * Errors as hydra_kv_append; n_heads not a multiple of n_kv_heads -> HYDRA_ERR_SHAPE; scale not finite ->
+ * HYDRA_ERR_RANGE; NULL q or out -> HYDRA_ERR_NULL; small, NULL or misaligned workspace -> HYDRA_ERR_WORKSPACE. A bad page
+ * makes the rows that read it NaN (0x203); positions past the table, or cached < 0, a sequence's rows (0x204).
+ */
+size_t hydra_paged_attention_workspace_size(int64_t S, int64_t L, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim);
+hydra_status hydra_paged_attention(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                                   const int32_t* cached, const int32_t* lengths, int64_t S, int64_t L, const void* q,
+                                   int64_t n_heads, int64_t ld_q, float scale, void* out, int64_t ld_out, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities from given random numbers (speculative sampling,
+ * Leviathan et al. 2023), so that what is kept is distributed as the target alone would draw it. With p_i the softmax of
+ * target row i, q_i that of draft row i, x_i the drafted token and n = n_draft[s]:
+ *     accept_i = min(1, p_i(x_i) / q_i(x_i))   (0 where p_i(x_i) = 0; 1 where only q_i(x_i) = 0)
+ *     x_i is kept while uniform_i < accept_i, up to the first refusal j;
+ *     the token after them: argmax_v(log max(p_j(v) - q_j(v), 0) + gumbel_v) at a refusal,
+ *                           argmax_v(target row n [v] + gumbel_v) where all n were kept; ties to the lowest v.
+ * Where p_j - q_j is nowhere positive the token comes from target row j, as with no draft. Without draft_logits the drafts
+ * are certain (copied text): accept_i = p_i(x_i), and a refusal draws from p_j without x_j. With uniform and gumbel
+ * both NULL verification is greedy: x_i is kept if it is row i's argmax, and the token after is the argmax.
+ * Arguments:
+ *   target_logits : rows of V logits of logits_dtype (HYDRA_F32 or HYDRA_BF16) at stride ld >= V; row s*(D+1) + i is
+ *             what the target says after i drafts. Any row may start at any element.
+ *   draft_logits : rows s*D + i at stride ld_draft >= V of the same type, or NULL; NULL in greedy verification.
+ *   draft_ids : int32 [S, D] in [0, V).   n_draft : int32 [S] in 0..D, NULL means D.   0 <= D <= 32.
+ *   uniform : fp32 [S, D] in [0, 1).   gumbel : fp32 rows [S] of V standard Gumbel numbers at stride ld_gumbel >= V.
+ * Outputs:
+ *   tokens   : int32 [S, D+1] the kept drafts, the token after them, then -1.   accepted : int32 [S] drafts kept.
+ *   logp     : fp32 [S, D+1] log-probability of each of these tokens under the target, then 0; may be NULL.
+ *   accept   : fp32 [S, D] of every draft i < n (greedy: 1 or 0), then 0; may be NULL.
+ * Rows past n are not read. Masked logits: -inf cannot be drawn; a target row of nothing but -inf gives token 0 with
+ * logp -inf. A NaN or +inf logit makes its row's accept and logp NaN and refuses its draft; the token after is then some
+ * token in [0, V). Sums are fp32 and depend on nothing but the rows, S, V and the device.
+ * Errors: logits_dtype, D, or draft_logits without gumbel -> HYDRA_ERR_RANGE; S < 0, S > 2^24, V < 1, V > 2^30 or a stride below
+ * V -> HYDRA_ERR_SHAPE; a needed pointer NULL, or (D > 0) one of uniform and gumbel alone -> HYDRA_ERR_NULL; logits not
+ * aligned to their element -> HYDRA_ERR_ALIGN. On the device: a drafted id out of range -> 0x201, accept NaN, refused; n_draft
+ * out of range -> 0x202, clamped. S == 0 is a no-op. Outputs overlap neither each other nor an input.
+ */
+hydra_status hydra_verify_drafts(const void* target_logits, const void* draft_logits, int logits_dtype, int64_t S, int64_t D,
+                                 int64_t V, int64_t ld, int64_t ld_draft, const int32_t* draft_ids, const int32_t* n_draft,
+                                 const float* uniform, const float* gumbel, int64_t ld_gumbel, int32_t* tokens,
+                                 int32_t* accepted, float* logp, float* accept, void* stream);
 
 /* SwiGLU (Shazeer 2020): m = bf16(silu(g) * u), gu bf16 [R, 2F] = [gate | up], m [R, F]. */
 hydra_status hydra_swiglu(const void* gu, int64_t R, int64_t F, void* m, void* stream);

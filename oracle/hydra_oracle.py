@@ -612,3 +612,106 @@ def llama_generate(weights, prompt_ids, n_steps, cfg, gumbel=None, n_layers=None
     out["tokens"] = tokens
     out["prompt_len"] = P
     return out
+
+
+# ------------------------------------------------------------------ paged cache and drafted tokens
+
+
+def rope_by_table(x, table_rows):
+    """Rotate-half rotation of x [..., heads, D] (fp32 values) by table rows [..., D/2, 2] of (cos, sin), each product
+    and sum rounded to fp32."""
+    x = np.asarray(x, dtype=np.float32)
+    a, b = np.split(x, 2, axis=-1)
+    c, s = (np.asarray(table_rows, dtype=np.float32)[..., None, :, i] for i in (0, 1))
+    return np.concatenate([a * c - b * s, a * s + b * c], axis=-1)
+
+
+def kv_quantise(x, group=64):
+    """(codes, scales, zeros) of fp32 values [..., D] in 4 bits: per group of channels scale = bf16((hi/2 - lo/2) 2/15)
+    and zero = rint(-lo / scale), lo and hi the least and largest value and 0; every operation in fp32. A group
+    with an infinity or NaN has scale NaN."""
+    f = np.float32
+    x = np.asarray(x, dtype=f)
+    x = x.reshape(*x.shape[:-1], -1, group)
+    sick = ~np.isfinite(x).all(axis=-1, keepdims=True)
+    y = np.where(sick, f(0), x)
+    lo, hi = np.minimum(y.min(axis=-1, keepdims=True), f(0)), np.maximum(y.max(axis=-1, keepdims=True), f(0))
+    scale = round_bf16(((hi * f(0.5) - lo * f(0.5)) * f(2.0 / 15.0)).astype(np.float64)).astype(f)
+    by = np.where(scale > 0, scale, f(1))
+    zero = np.where(scale > 0, np.clip(np.rint(-lo / by), 0, 15), f(0))
+    codes = np.where(scale > 0, np.clip(np.rint(y / by) + zero, 0, 15), f(0))
+    return codes, np.where(sick, f(np.nan), scale), zero
+
+
+def kv_held(x, int4):
+    """The fp32 values that a cache in 4 bits (else bf16) holds for fp32 values [..., D]."""
+    if not int4:
+        return round_bf16(np.asarray(x, dtype=np.float64)).astype(np.float32)
+    codes, scale, zero = kv_quantise(x)
+    with np.errstate(over="ignore"):
+        return (scale * (codes - zero)).reshape(np.shape(x)).astype(np.float32)
+
+
+def cached_attention(q, k, v, cached, scale):
+    """One sequence's n new tokens q [n, heads, D] over k, v [cached + n, kv heads, D] up to themselves: (out, for each
+    row sum_j p_j |v_j|, for each row the largest sum_d |q_d k_jd| scale)."""
+    q, k, v = (np.asarray(x, dtype=np.float64) for x in (q, k, v))
+    n, heads, _ = q.shape
+    by = heads // k.shape[1]
+    out, size, reach = np.zeros_like(q), np.zeros_like(q), np.zeros((n, heads))
+    for t in range(n):
+        for h in range(heads):
+            kk, vv = k[:cached + t + 1, h // by], v[:cached + t + 1, h // by]
+            z = kk @ q[t, h] * scale
+            p = np.exp(z - z.max())
+            p /= p.sum()
+            out[t, h], size[t, h] = p @ vv, p @ np.abs(vv)
+            reach[t, h] = (np.abs(kk) @ np.abs(q[t, h])).max() * abs(scale)
+    return out, size, reach
+
+
+def verify_drafts(z, w, ids, n_draft, uniform, gumbel, S, D):
+    """Speculative sampling of S sequences with up to D drafts: target rows z [S*(D+1), V], draft rows w [S*D, V] or
+    None (certain drafts), uniform and gumbel both None: greedy. Returns tokens, accepted, logp, accept."""
+    z = np.asarray(z, dtype=np.float64).reshape(S, D + 1, -1)
+
+    def log_p(row):
+        m = row.max()
+        if m == -np.inf:
+            return np.full_like(row, -np.inf)
+        return row - m - np.log(np.exp(row - m).sum())
+
+    out = {"tokens": np.full((S, D + 1), -1), "accepted": np.zeros(S, dtype=np.int64), "logp": np.zeros((S, D + 1)),
+           "accept": np.zeros((S, D))}
+    with np.errstate(invalid="ignore", divide="ignore"):
+        for s in range(S):
+            n = D if n_draft is None else int(n_draft[s])
+            lp = [log_p(z[s, i]) for i in range(n + 1)]
+            lq = None if w is None else [log_p(np.asarray(w, dtype=np.float64).reshape(S, D, -1)[s, i]) for i in range(n)]
+            kept = 0
+            for i in range(n):
+                x = int(ids[s][i])
+                if gumbel is None:
+                    a = float(np.argmax(z[s, i]) == x)
+                elif lp[i][x] == -np.inf:
+                    a = 0.0
+                else:
+                    a = min(1.0, np.exp(min(0.0, lp[i][x] - (0.0 if lq is None else lq[i][x]))))
+                out["accept"][s, i] = a
+                if kept == i and (a == 1.0 if gumbel is None else uniform[s][i] < a):
+                    kept += 1
+            score = z[s, kept]
+            if gumbel is not None:
+                if kept < n:
+                    if lq is None:
+                        rest = score.copy()
+                        rest[int(ids[s][kept])] = -np.inf
+                    else:
+                        rest = np.log(np.maximum(np.exp(lp[kept]) - np.exp(lq[kept]), 0.0))
+                    score = rest if rest.max() > -np.inf else score
+                score = score + np.asarray(gumbel[s], dtype=np.float64)
+            row = [int(x) for x in ids[s][:kept]] + [int(np.argmax(score))]
+            out["accepted"][s] = kept
+            for i, x in enumerate(row):
+                out["tokens"][s, i], out["logp"][s, i] = x, lp[i][x]
+    return out

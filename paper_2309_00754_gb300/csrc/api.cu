@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -627,6 +628,176 @@ hydra_status hydra_clip_grad_norm(const hydra_grad_tensor* tensors, int64_t n, f
                                   float* norm_out, void* workspace, size_t workspace_bytes,
                                   void* stream) {
   return grad_norm_impl(tensors, n, max_norm, norm_out, true, workspace, workspace_bytes, stream);
+}
+
+// A paged cache and the sequences of a call. Positions stay in 32 bits.
+static hydra_status kv_args(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                            const int32_t* cached, const int32_t* lengths, int64_t S, int64_t L, hydra::KvCache* c,
+                            hydra::KvBatch* b) {
+  if (cache == nullptr) return HYDRA_ERR_NULL;
+  if (hydra_kv_page_bytes(static_cast<int>(cache->kind), cache->page, 1, cache->head_dim) == 0) return HYDRA_ERR_RANGE;
+  if (cache->n_pages < 1 || cache->n_pages >= (1LL << 31) || cache->n_kv_heads < 1 || cache->n_kv_heads > hydra::kKvMaxHeads)
+    return HYDRA_ERR_SHAPE;
+  if (S < 0 || L < 0 || S >= (1LL << 31) || L >= (1LL << 31) || S * L >= (1LL << 31)) return HYDRA_ERR_SHAPE;
+  if (max_pages < 1 || max_pages > ((1LL << 31) - 1) / cache->page || ld_table < max_pages || ld_table >= (1LL << 31))
+    return HYDRA_ERR_SHAPE;
+  if (S > 0 && L > 0 && (cache->data == nullptr || table == nullptr)) return HYDRA_ERR_NULL;
+  if (!aligned16(cache->data)) return HYDRA_ERR_ALIGN;
+  int bits = 4;
+  while ((1 << bits) < cache->page) ++bits;
+  *c = hydra::KvCache{cache->data, cache->n_pages, bits, static_cast<int>(cache->n_kv_heads),
+                      static_cast<int>(cache->head_dim), cache->kind == HYDRA_KV_INT4};
+  *b = hydra::KvBatch{table, ld_table, max_pages, cached, lengths, S, L};
+  return HYDRA_OK;
+}
+
+// Rows of `heads` heads at stride ld, in whole 16 bytes.
+static hydra_status head_rows(const void* p, int64_t heads, int64_t head_dim, int64_t ld) {
+  if (ld < heads * head_dim || ld >= (1LL << 31)) return HYDRA_ERR_SHAPE;
+  return ld % 8 != 0 || !aligned16(p) ? HYDRA_ERR_ALIGN : HYDRA_OK;
+}
+
+size_t hydra_kv_page_bytes(int kind, int64_t page, int64_t n_kv_heads, int64_t head_dim) {
+  if (kind != HYDRA_KV_BF16 && kind != HYDRA_KV_INT4) return 0;
+  if (page != 16 && page != 32 && page != 64 && page != 128) return 0;
+  if ((head_dim != 64 && head_dim != 128) || n_kv_heads < 1 || n_kv_heads > hydra::kKvMaxHeads) return 0;
+  return static_cast<size_t>(page * n_kv_heads * (kind == HYDRA_KV_BF16 ? 4 * head_dim : head_dim + head_dim / 8));
+}
+
+hydra_status hydra_kv_append(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                             const int32_t* cached, const int32_t* lengths, int64_t S, int64_t L, const void* q,
+                             int64_t n_heads, int64_t ld_q, const void* k, const void* v, int64_t ld_kv,
+                             const float* rope_table, int64_t rope_len, void* q_out, int64_t ld_q_out, void* stream) {
+  hydra::KvAppendArgs a;
+  if (const hydra_status e = kv_args(cache, table, ld_table, max_pages, cached, lengths, S, L, &a.cache, &a.batch); e != HYDRA_OK)
+    return e;
+  const int64_t dh = cache->head_dim;
+  if (n_heads < 0 || n_heads > hydra::kKvMaxHeads) return HYDRA_ERR_SHAPE;
+  if (rope_table != nullptr && rope_len < 1) return HYDRA_ERR_SHAPE;
+  if (!aligned16(rope_table)) return HYDRA_ERR_ALIGN;
+  for (const void* p : {k, v})
+    if (const hydra_status e = head_rows(p, cache->n_kv_heads, dh, ld_kv); e != HYDRA_OK) return e;
+  if (n_heads > 0) {
+    if (const hydra_status e = head_rows(q, n_heads, dh, ld_q); e != HYDRA_OK) return e;
+    if (const hydra_status e = head_rows(q_out, n_heads, dh, ld_q_out); e != HYDRA_OK) return e;
+    // in place every element is read and written by one thread; with another stride they would race
+    if (q == q_out && q != nullptr && ld_q != ld_q_out) return HYDRA_ERR_RANGE;
+  }
+  if (S == 0 || L == 0) return HYDRA_OK;
+  if (k == nullptr || v == nullptr || (n_heads > 0 && (q == nullptr || q_out == nullptr))) return HYDRA_ERR_NULL;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.n_heads = n_heads;
+  a.ld_q = ld_q;
+  a.ld_kv = ld_kv;
+  a.rope = rope_table;
+  a.rope_len = rope_len;
+  a.q_out = q_out;
+  a.ld_q_out = ld_q_out;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_kv_append(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+hydra_status hydra_kv_read(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                           const int32_t* first, const int32_t* lengths, int64_t S, int64_t L, void* k_out, void* v_out,
+                           int out_dtype, int64_t ld, void* stream) {
+  hydra::KvReadArgs a;
+  if (const hydra_status e = kv_args(cache, table, ld_table, max_pages, first, lengths, S, L, &a.cache, &a.batch); e != HYDRA_OK)
+    return e;
+  if (out_dtype != HYDRA_BF16 && out_dtype != HYDRA_F32) return HYDRA_ERR_RANGE;
+  for (const void* p : {k_out, v_out})
+    if (const hydra_status e = head_rows(p, cache->n_kv_heads, cache->head_dim, ld); e != HYDRA_OK) return e;
+  if (S == 0 || L == 0) return HYDRA_OK;
+  if (k_out == nullptr && v_out == nullptr) return HYDRA_ERR_NULL;
+  a.k = k_out;
+  a.v = v_out;
+  a.f32 = out_dtype == HYDRA_F32;
+  a.ld = ld;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_kv_read(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+static bool paged_heads_ok(int64_t S, int64_t L, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim) {
+  return S >= 0 && L >= 0 && S < (1LL << 31) && L < (1LL << 31) && S * L < (1LL << 31) && n_kv_heads >= 1 &&
+         n_kv_heads <= hydra::kKvMaxHeads && n_heads >= 1 && n_heads <= hydra::kKvMaxHeads && n_heads % n_kv_heads == 0 &&
+         (head_dim == 64 || head_dim == 128);
+}
+
+size_t hydra_paged_attention_workspace_size(int64_t S, int64_t L, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim) {
+  return paged_heads_ok(S, L, n_heads, n_kv_heads, head_dim)
+             ? hydra::paged_attention_workspace_bytes(S, L, n_heads, n_kv_heads, head_dim)
+             : 0;
+}
+
+hydra_status hydra_paged_attention(const hydra_kv_cache* cache, const int32_t* table, int64_t ld_table, int64_t max_pages,
+                                   const int32_t* cached, const int32_t* lengths, int64_t S, int64_t L, const void* q,
+                                   int64_t n_heads, int64_t ld_q, float scale, void* out, int64_t ld_out, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  hydra::PagedAttentionArgs a;
+  if (const hydra_status e = kv_args(cache, table, ld_table, max_pages, cached, lengths, S, L, &a.cache, &a.batch); e != HYDRA_OK)
+    return e;
+  if (!paged_heads_ok(S, L, n_heads, cache->n_kv_heads, cache->head_dim)) return HYDRA_ERR_SHAPE;
+  if (!std::isfinite(scale)) return HYDRA_ERR_RANGE;
+  if (const hydra_status e = head_rows(q, n_heads, cache->head_dim, ld_q); e != HYDRA_OK) return e;
+  if (const hydra_status e = head_rows(out, n_heads, cache->head_dim, ld_out); e != HYDRA_OK) return e;
+  if (S == 0 || L == 0) return HYDRA_OK;
+  if (q == nullptr || out == nullptr) return HYDRA_ERR_NULL;
+  if (workspace == nullptr || !aligned16(workspace) ||
+      workspace_bytes < hydra_paged_attention_workspace_size(S, L, n_heads, cache->n_kv_heads, cache->head_dim))
+    return HYDRA_ERR_WORKSPACE;
+  a.q = q;
+  a.n_heads = n_heads;
+  a.ld_q = ld_q;
+  a.scale = scale;
+  a.out = out;
+  a.ld_out = ld_out;
+  a.ws = workspace;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_paged_attention(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
+}
+
+hydra_status hydra_verify_drafts(const void* target_logits, const void* draft_logits, int logits_dtype, int64_t S, int64_t D,
+                                 int64_t V, int64_t ld, int64_t ld_draft, const int32_t* draft_ids, const int32_t* n_draft,
+                                 const float* uniform, const float* gumbel, int64_t ld_gumbel, int32_t* tokens,
+                                 int32_t* accepted, float* logp, float* accept, void* stream) {
+  if (logits_dtype != HYDRA_F32 && logits_dtype != HYDRA_BF16) return HYDRA_ERR_RANGE;
+  if (D < 0 || D > hydra::kVerifyMaxDrafts) return HYDRA_ERR_RANGE;
+  if (!token_rows_ok(S, D + 1, V, ld) || S > hydra::kVerifyMaxSequences) return HYDRA_ERR_SHAPE;
+  if ((draft_logits != nullptr && ld_draft < V) || (gumbel != nullptr && ld_gumbel < V)) return HYDRA_ERR_SHAPE;
+  if (S == 0) return HYDRA_OK;
+  if (target_logits == nullptr || tokens == nullptr || accepted == nullptr || (D > 0 && draft_ids == nullptr))
+    return HYDRA_ERR_NULL;
+  // random numbers for both or for neither; greedy verification knows no draft distribution
+  if (D > 0 && (uniform == nullptr) != (gumbel == nullptr)) return HYDRA_ERR_NULL;
+  if (gumbel == nullptr && draft_logits != nullptr) return HYDRA_ERR_RANGE;
+  const size_t size = logits_dtype == HYDRA_BF16 ? 2 : 4;
+  if (reinterpret_cast<uintptr_t>(target_logits) % size != 0 || reinterpret_cast<uintptr_t>(draft_logits) % size != 0)
+    return HYDRA_ERR_ALIGN;
+  hydra::VerifyArgs a;
+  a.target = target_logits;
+  a.draft = D > 0 ? draft_logits : nullptr;
+  a.bf16 = logits_dtype == HYDRA_BF16;
+  a.S = S;
+  a.D = D;
+  a.V = V;
+  a.ld = ld;
+  a.ld_draft = ld_draft;
+  a.ids = draft_ids;
+  a.n_draft = n_draft;
+  a.uniform = uniform;
+  a.gumbel = gumbel;
+  a.ld_gumbel = ld_gumbel;
+  a.tokens = tokens;
+  a.accepted = accepted;
+  a.logp = logp;
+  a.accept = accept;
+  a.err = hydra::device_error_word();
+  if (a.err == nullptr) return HYDRA_ERR_CUDA;
+  return hydra::launch_verify_drafts(a, static_cast<cudaStream_t>(stream)) == 0 ? HYDRA_OK : HYDRA_ERR_CUDA;
 }
 
 hydra_status ppo_gae(const float* rewards, const float* values, const int32_t* lengths, int64_t S,

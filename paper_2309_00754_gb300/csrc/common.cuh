@@ -21,6 +21,8 @@ enum DeviceError : int {
   kDevTimeoutSelftest = 0x105,  // hydra_selftest_wait_timeout: the expected expiry
   kDevBadTokenId = 0x201,
   kDevBadLength = 0x202,
+  kDevBadPage = 0x203,
+  kDevBadPosition = 0x204,
 };
 
 // Spin budget of every mbarrier wait, in SM clock cycles (~1 s at 2 GHz). A correct

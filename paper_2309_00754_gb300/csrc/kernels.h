@@ -203,6 +203,76 @@ size_t grad_norm_workspace_bytes();
 int launch_grad_norm(const GradTensor* t, int64_t n, float max_norm, float* norm_out, bool scale, void* ws,
                      cudaStream_t st);
 
+// A paged key/value cache (kv_cache.cuh), and a call's sequences: S slots of L new tokens each behind `cached` ones.
+struct KvCache {
+  void* data;
+  long long n_pages;
+  int page_bits, kv_heads, head_dim;  // pages of 1 << page_bits tokens
+  bool int4;
+};
+struct KvBatch {
+  const int32_t* table;  // [S] rows of max_pages at ld_table
+  int64_t ld_table, max_pages;
+  const int32_t* cached;   // or NULL: none
+  const int32_t* lengths;  // or NULL: L
+  int64_t S, L;
+};
+constexpr int64_t kKvMaxHeads = 4096;
+struct KvAppendArgs {
+  KvCache cache;
+  KvBatch batch;
+  const void *q, *k, *v;  // bf16 rows [S * L] at ld_q (n_heads of head_dim) and ld_kv
+  int64_t n_heads, ld_q, ld_kv;
+  const float* rope;  // [rope_len][head_dim / 2][2] (cos, sin), or NULL
+  int64_t rope_len;
+  void* q_out;  // bf16 rows at ld_q_out, or NULL
+  int64_t ld_q_out;
+  int* err;
+};
+int launch_kv_append(const KvAppendArgs& a, cudaStream_t stream);
+struct KvReadArgs {
+  KvCache cache;
+  KvBatch batch;
+  void *k, *v;  // rows [S * L] at ld, bf16 or (f32) fp32; either may be NULL
+  bool f32;
+  int64_t ld;
+  int* err;
+};
+int launch_kv_read(const KvReadArgs& a, cudaStream_t stream);
+struct PagedAttentionArgs {
+  KvCache cache;
+  KvBatch batch;
+  const void* q;  // bf16 rows [S * L] at ld_q
+  int64_t n_heads, ld_q;
+  float scale;
+  void* out;  // bf16 rows at ld_out
+  int64_t ld_out;
+  void* ws;
+  int* err;
+};
+size_t paged_attention_workspace_bytes(int64_t S, int64_t L, int64_t n_heads, int64_t kv_heads, int64_t head_dim);
+int launch_paged_attention(const PagedAttentionArgs& a, cudaStream_t stream);
+// Verification of drafted tokens (verify_drafts.cu).
+struct VerifyArgs {
+  const void* target;  // rows [S * (D + 1)] of V logits at ld
+  const void* draft;   // rows [S * D] at ld_draft, or NULL
+  bool bf16;
+  int64_t S, D, V, ld, ld_draft;
+  const int32_t* ids;
+  const int32_t* n_draft;  // or NULL: D
+  const float* uniform;    // [S * D], NULL: greedy
+  const float* gumbel;     // [S] rows of V at ld_gumbel, NULL: greedy
+  int64_t ld_gumbel;
+  int32_t* tokens;    // [S * (D + 1)]
+  int32_t* accepted;  // [S]
+  float* logp;        // [S * (D + 1)] or NULL
+  float* accept;      // [S * D] or NULL
+  int* err;
+};
+constexpr int kVerifyMaxDrafts = 32;
+constexpr int64_t kVerifyMaxSequences = 1 << 24;
+int launch_verify_drafts(const VerifyArgs& a, cudaStream_t stream);
+
 // The full pass's stacked linear over ns row-stacked streams (score_llama.cu): rows [0, T)
 // of x are the LoRA-off stream, [T, 2T) the LoRA-on stream (LoRA set A, B; u receives its
 // down-projection) and, for ns == 3, [2T, 3T) a third stream with the set A2, B2 (u2). epi:

@@ -16,6 +16,8 @@ HEADER = os.path.join(os.path.dirname(_PKG), "include", "hydra.h")
 
 HYDRA_BF16 = 0
 HYDRA_F32 = 1
+HYDRA_KV_BF16 = 0
+HYDRA_KV_INT4 = 1
 
 _c_i64 = ctypes.c_int64
 _vp = ctypes.c_void_p
@@ -77,6 +79,24 @@ _SIGNATURES = {
                                              _vp]),
     "hydra_ppo_merge_moments": (ctypes.c_int, [_vp, _c_i64, _vp]),
 }
+
+
+class KvCacheC(ctypes.Structure):
+    _fields_ = [("data", _vp)] + [(n, _c_i64) for n in ("n_pages", "page", "n_kv_heads", "head_dim", "kind")]
+
+
+_kv = [ctypes.POINTER(KvCacheC), _vp, _c_i64, _c_i64, _vp, _vp, _c_i64, _c_i64]  # cache, table, batch
+_SIGNATURES.update({
+    "hydra_kv_page_bytes": (ctypes.c_size_t, [ctypes.c_int, _c_i64, _c_i64, _c_i64]),
+    "hydra_kv_append": (ctypes.c_int, _kv + [_vp, _c_i64, _c_i64, _vp, _vp, _c_i64, _vp, _c_i64, _vp,
+                                             _c_i64, _vp]),
+    "hydra_kv_read": (ctypes.c_int, _kv + [_vp, _vp, ctypes.c_int, _c_i64, _vp]),
+    "hydra_paged_attention_workspace_size": (ctypes.c_size_t, [_c_i64] * 5),
+    "hydra_paged_attention": (ctypes.c_int, _kv + [_vp, _c_i64, _c_i64, ctypes.c_float, _vp, _c_i64, _vp,
+                                                   ctypes.c_size_t, _vp]),
+    "hydra_verify_drafts": (ctypes.c_int, [_vp, _vp, ctypes.c_int, _c_i64, _c_i64, _c_i64, _c_i64, _c_i64,
+                                           _vp, _vp, _vp, _vp, _c_i64, _vp, _vp, _vp, _vp, _vp]),
+})
 
 
 class GradTensorC(ctypes.Structure):
@@ -680,6 +700,160 @@ def hydra_causal_attention(qkv, nseq, P, n_heads, head_dim, out, stream=None):
     _check("hydra_causal_attention", load().hydra_causal_attention(
         _p(qkv), nseq, P, qkv.shape[1], n_heads, head_dim, _p(out), out.shape[1],
         _stream(stream)))
+
+
+# ----------------------------------------------------------------------------- paged cache
+
+
+def kv_page_bytes(kind, page, n_kv_heads, head_dim):
+    """Bytes of a page of a paged cache; 0 for a kind, page or head size that is not supported."""
+    return int(load().hydra_kv_page_bytes(kind, page, n_kv_heads, head_dim))
+
+
+class KvCache:
+    """A pool of n_pages pages of `page` tokens for n_kv_heads heads of head_dim: HYDRA_KV_BF16 or HYDRA_KV_INT4.
+    `data` is its memory, uint8 [n_pages, ...] (None: made here, on `device`); it wants no initial contents."""
+
+    def __init__(self, kind, n_pages, page, n_kv_heads, head_dim, data=None, device="cuda"):
+        size = kv_page_bytes(kind, page, n_kv_heads, head_dim)
+        if size == 0:
+            raise ValueError(f"no cache of kind {kind} has pages of {page} tokens for {n_kv_heads} heads of {head_dim}")
+        if data is None:
+            data = torch.empty(n_pages, size, dtype=torch.uint8, device=device)
+        _req(data, torch.uint8, "data")
+        if data.numel() != n_pages * size:
+            raise ValueError(f"data must have {n_pages} pages of {size} bytes, got {data.numel()} bytes")
+        self.data, self.kind, self.n_pages, self.page = data, kind, n_pages, page
+        self.n_kv_heads, self.head_dim, self.page_bytes = n_kv_heads, head_dim, size
+        self.c = KvCacheC(data.data_ptr(), n_pages, page, n_kv_heads, head_dim, kind)
+
+
+def _kv_args(cache, table, cached, lengths, S, L, dev):
+    """What every call with a cache begins with."""
+    if cache.data.get_device() != dev:
+        _on_device(cache.data)
+    if table.dtype is not torch.int32 or table.get_device() != dev:
+        if table.dtype is not torch.int32 or not table.is_cuda:
+            raise ValueError(f"table must be an int32 CUDA tensor, got {table.dtype} on {table.device}")
+        _on_device(table)
+    if table.dim() != 2 or table.shape[0] != S:
+        raise ValueError(f"table must have {S} rows, got shape {tuple(table.shape)}")
+    ld, step = table.stride()
+    if step != 1 and table.shape[1] > 1:
+        raise ValueError("table rows must be unit-stride")
+    i32 = torch.int32
+    return (ctypes.byref(cache.c), table.data_ptr(), ld if S > 1 else max(ld, table.shape[1]), table.shape[1],
+            _arg(cached, i32, S, dev, "cached"), _arg(lengths, i32, S, dev, "lengths"), S, L)
+
+
+def _heads(t, rows, head_dim, dtype, dev, name):
+    """(pointer, heads, row stride) of rows of heads, which may be columns of a wider matrix."""
+    if t.dtype is not dtype or t.get_device() != dev:
+        if t.dtype is not dtype or not t.is_cuda:
+            raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
+        _on_device(t)
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] % head_dim != 0:
+        raise ValueError(f"{name} must have {rows} rows of heads of {head_dim}, got shape {tuple(t.shape)}")
+    ld, step = t.stride()
+    if step != 1:
+        raise ValueError(f"{name} rows must be unit-stride")
+    return t.data_ptr(), t.shape[1] // head_dim, ld if rows > 1 else t.shape[1]
+
+
+def _kv_pair(k, v, rows, cache, dtype, dev, names):
+    """(k, v, row stride) of two outputs or inputs of the cache's heads with one stride; either may be None."""
+    got = [None if t is None else _heads(t, rows, cache.head_dim, dtype, dev, n) for t, n in zip((k, v), names)]
+    for g, n in zip(got, names):
+        if g is not None and g[1] != cache.n_kv_heads:
+            raise ValueError(f"{n} must have {cache.n_kv_heads} heads, got {g[1]}")
+    strides = {g[2] for g in got if g is not None}
+    if len(strides) > 1:
+        raise ValueError(f"{names[0]} and {names[1]} must have one row stride")
+    return (*(None if g is None else g[0] for g in got), strides.pop() if strides else cache.n_kv_heads * cache.head_dim)
+
+
+def hydra_kv_append(cache, table, cached, lengths, S, L, q, k, v, rope_table=None, q_out=None, stream=None):
+    """Rotates the new tokens' queries into q_out (q itself: in place) and their keys, and puts keys and values
+    into the cache. q [S*L, heads * D], k and v [S*L, kv heads * D] bf16, rows may stand apart (columns of a fused
+    q/k/v); table int32 [S, pages]; cached and lengths int32 [S] or None; rope_table fp32 [P, D/2, 2] or None; q
+    and q_out None: keys and values alone."""
+    dev, rows, bf16 = _current_device(), S * L, torch.bfloat16
+    head = _kv_args(cache, table, cached, lengths, S, L, dev)
+    if k is None or v is None or (q is None) != (q_out is None):
+        raise ValueError("k and v, and q with q_out, must be given")
+    pk, pv, ld_kv = _kv_pair(k, v, rows, cache, bf16, dev, ("k", "v"))
+    pq, heads, ld_q = (None, 0, 0) if q is None else _heads(q, rows, cache.head_dim, bf16, dev, "q")
+    po, heads_out, ld_o = (None, 0, 0) if q is None else _heads(q_out, rows, cache.head_dim, bf16, dev, "q_out")
+    if heads != heads_out:
+        raise ValueError(f"q has {heads} heads, q_out {heads_out}")
+    P = 0 if rope_table is None else rope_table.shape[0]
+    _check("hydra_kv_append", load().hydra_kv_append(
+        *head, pq, heads, ld_q, pk, pv, ld_kv,
+        _arg(rope_table, torch.float32, P * cache.head_dim, dev, "rope_table"), P, po, ld_o, _stream(stream)))
+
+
+def hydra_kv_read(cache, table, first, lengths, S, L, k_out, v_out, stream=None):
+    """Positions first .. first + lengths - 1 of every sequence back into rows of k_out and v_out ([S*L, kv heads * D],
+    bf16 or fp32; either may be None)."""
+    dev = _current_device()
+    some = k_out if k_out is not None else v_out
+    if some is None:
+        raise ValueError("k_out or v_out must be given")
+    code = _out_dtype(some, "k_out")
+    head = _kv_args(cache, table, first, lengths, S, L, dev)
+    pk, pv, ld = _kv_pair(k_out, v_out, S * L, cache, some.dtype, dev, ("k_out", "v_out"))
+    _check("hydra_kv_read", load().hydra_kv_read(*head, pk, pv, code, ld, _stream(stream)))
+
+
+def paged_attention_workspace_size(S, L, n_heads, n_kv_heads, head_dim):
+    return int(load().hydra_paged_attention_workspace_size(S, L, n_heads, n_kv_heads, head_dim))
+
+
+def hydra_paged_attention(cache, table, cached, lengths, S, L, q, out, scale, workspace, stream=None):
+    """out [S*L, heads * D] = attention of the tokens that hydra_kv_append has just put behind `cached` ones, over the
+    cache up to themselves; q and out bf16, rows may stand apart."""
+    dev, rows, bf16 = _current_device(), S * L, torch.bfloat16
+    head = _kv_args(cache, table, cached, lengths, S, L, dev)
+    pq, heads, ld_q = _heads(q, rows, cache.head_dim, bf16, dev, "q")
+    po, heads_out, ld_o = _heads(out, rows, cache.head_dim, bf16, dev, "out")
+    if heads != heads_out:
+        raise ValueError(f"q has {heads} heads, out {heads_out}")
+    if workspace.get_device() != dev:
+        _on_device(workspace)
+    _check("hydra_paged_attention", load().hydra_paged_attention(
+        *head, pq, heads, ld_q, float(scale), po, ld_o, _p(workspace),
+        workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def hydra_verify_drafts(target, draft, ids, n_draft, uniform, gumbel, S, D, tokens, accepted, logp=None, accept=None,
+                        stream=None):
+    """Keeps drafted ids (int32 [S, D]) by the target's logits [S*(D+1), V] and the draft model's [S*D, V] (fp32 or bf16; None:
+    the drafts are certain), from uniform [S, D] and gumbel [S, V] (both None: greedy), and draws the token after
+    them. Outputs: tokens int32 [S, D+1], accepted int32 [S], logp fp32 [S, D+1] and accept fp32 [S, D] (or None)."""
+    f32, i32 = torch.float32, torch.int32
+    z, code, ld = _rows_of(target, S * (D + 1), "target")
+    V, dev = target.shape[1], _current_device()
+    w, ld_w = None, V
+    if draft is not None:
+        w, code_w, ld_w = _rows_of(draft, S * D, "draft")
+        if code_w != code or draft.shape[1] != V:
+            raise ValueError("target and draft must have one dtype and the same columns")
+        if draft.get_device() != dev:
+            _on_device(draft)
+    g, ld_g = None, V
+    if gumbel is not None:
+        g, code_g, ld_g = _rows_of(gumbel, S, "gumbel")
+        if code_g != HYDRA_F32 or gumbel.shape[1] != V:
+            raise ValueError("gumbel must be float32 with the target's columns")
+        if gumbel.get_device() != dev:
+            _on_device(gumbel)
+    if target.get_device() != dev:
+        _on_device(target)
+    _check("hydra_verify_drafts", load().hydra_verify_drafts(
+        z, w, code, S, D, V, ld, ld_w, _arg(ids, i32, S * D, dev, "ids"), _arg(n_draft, i32, S, dev, "n_draft"),
+        _arg(uniform, f32, S * D, dev, "uniform"), g, ld_g, _arg(tokens, i32, S * (D + 1), dev, "tokens"),
+        _arg(accepted, i32, S, dev, "accepted"), _arg(logp, f32, S * (D + 1), dev, "logp"),
+        _arg(accept, f32, S * D, dev, "accept"), _stream(stream)))
 
 
 def hydra_swiglu(gu, m, stream=None):
