@@ -2,10 +2,12 @@
 
 Tolerances, with u = 2^-24. A score is a sum of D products in fp32, off by at most (D + 16) u of the sum of their
 magnitudes (`reach`), so a weight is off by (D + 16) u reach relative, and the quotient of two sums of weights twice
-that. Weights enter the second product rounded to 11 bits (half a step 2^-12 up to the next power of two: 2^-11
-relative) or as two bf16 (2^-16), and weights under 2^-24 of the largest at an absolute 2^-33 of it. The sums themselves are
-fp32 over N terms: at most N u, with 64 for the order. So an output is off by
-    (2^-11 + 2 (D + 16) u reach + (N + 64) u) sum_j p_j |v_j| + N 2^-32 max |v|,
+that. Weights enter the second product rounded to fp16 (half a step: 2^-11 relative) together with their value's scale, the
+largest such product of a row at 2^6 or more: below 2^-14 fp16 has steps of 2^-24, so a weight is off by 2^-25 at most, 2^-31
+of the largest product w sv. Times a code of up to 15, and sv <= max |v| / 7.5 (a scale is a fifteenth of its range),
+that is N 2^-30 max |v| over N tokens. (Two bf16, 2^-16 relative, in a bf16 cache.) The sums themselves are fp32 over N terms:
+at most N u, with 64 for the order and the logarithms of sums that are added up. So an output is off by
+    (2^-11 + 2 (D + 16) u reach + (N + 64) u) sum_j p_j |v_j| + N 2^-30 max |v|,
 and rounded to bf16: half a step, 2^-8 of its value (and of what it is off by)."""
 import numpy as np
 import pytest
@@ -92,7 +94,7 @@ def check(c, got, scale=None, sick=None):
             continue
         N = int(c["cached"][s]) + n
         ref, size, reach = O.cached_attention(q[s, :n], c["k"][s, :N], c["v"][s, :N], int(c["cached"][s]), scale)
-        tol = (2.0 ** -11 + 2 * (D + 16) * U * reach[..., None] + (N + 64) * U) * size + N * 2.0 ** -32 * np.abs(c["v"][s, :N]).max()
+        tol = (2.0 ** -11 + 2 * (D + 16) * U * reach[..., None] + (N + 64) * U) * size + N * 2.0 ** -30 * np.abs(c["v"][s, :N]).max()
         tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
         off = np.abs(got[s, :n] - ref)
         assert np.isfinite(got[s, :n]).all(), f"sequence {s}: not finite"
