@@ -32,9 +32,9 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
 constexpr int kMaxRowTiles = 4;   // of 8 query rows that share a pass
-constexpr int kMinUnits = 4;      // tiles of a warp, where there are more warps than that fills
+constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
 constexpr float kFar = -1e30f;    // a maximum of nothing
-// Exponents relative to m. bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
+// Exponents relative to m (exact for scales of values up to 2^100: above that small probabilities are flushed). bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
 // 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108.
 constexpr float kSlack = 8.f, kTop = 6.f, kMost = 14.f, kAlone = 100.f;
 
@@ -61,11 +61,13 @@ struct Config {
   static constexpr int kCtasPerSm = kInt4 && kR == 1 ? 2 : 1;
   static constexpr bool kQShared = kR > 2;  // the queries' fragments: shared memory, else registers
   static constexpr int kPair = kInt4 && kR <= 2 ? 2 : 1;  // tiles that are taken together
+  static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that share a wait
+  static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
   // a warp's ring also takes its last part at the end
-  static constexpr int kLeast = (8 * kR * kDh * 4 + Tile::kBytes - 1) / Tile::kBytes;
-  static constexpr int kWant = kInt4 ? 6 : kDh == 64 ? 4 : kR <= 2 ? 3 : 2;
-  static constexpr int kStages = kWant > kLeast ? kWant : kLeast;
-  static constexpr int kRing = kWarps * kStages * Tile::kBytes;
+  static constexpr int kLeast = (8 * kR * kDh * 4 + kStageBytes - 1) / kStageBytes;
+  static constexpr int kStages = kLeast > 2 || (!kInt4 && kDh == 64) ? 4 : 2;
+  static_assert(kLeast <= kStages, "a part fits the ring");
+  static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kQ = kQShared ? kWarps * kR * kMTiles * 32 * 8 : 0;
   static constexpr int kSmem = kRing + kQ + kWarps * kStages * 8;
 };
@@ -81,30 +83,30 @@ struct WarpEnd {
   bool tail;        // the last segment begins an item and does not end it
 };
 
+// (not volatile: the compiler interleaves them)
+__device__ __forceinline__ void first_mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <bool kInt4>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (kInt4) mma_f16(d, a, b0, b1); else mma_bf16(d, a, b0, b1);
-}
 __device__ __forceinline__ uint32_t turned(uint32_t a) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));  // (with subnormals: m may lie far above the scores)
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ float lg2(float x) {
@@ -140,12 +142,25 @@ __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v 
 // 2^e, e in [-126, 127]
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
 
-// code - zero of the low nibbles of the bytes 0 and 2 (16 (code - zero) of the high ones), as fp16.
-__device__ __forceinline__ uint32_t low_nibbles(uint32_t w, uint32_t minus) { return add_f16((w & 0x000f000fu) | 0x64006400u, minus); }
-__device__ __forceinline__ uint32_t high_nibbles(uint32_t w, uint32_t minus) { return add_f16((w & 0x00f000f0u) | 0x64006400u, minus); }
-// -(1024 + zero), -(1024 + 16 zero) from two zero points as the cache holds them
-__device__ __forceinline__ uint32_t minus_low(uint32_t z) { return (z & 0x000f000fu) | 0xe400e400u; }
-__device__ __forceinline__ uint32_t minus_high(uint32_t z) { return (z & 0x00f000f0u) | 0xe400e400u; }
+// (w & mask) | bits in one instruction: `bits` comes from a register, as two constants in one would take two instructions
+template <uint32_t kMask>
+__device__ __forceinline__ uint32_t merged(uint32_t w, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(w), "n"(kMask), "r"(bits));
+  return r;
+}
+__device__ __forceinline__ uint32_t held(uint32_t constant) {
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(constant));
+  return r;
+}
+constexpr uint32_t kFp16Of1024 = 0x64006400u, kFp16OfMinus1024 = 0xe400e400u;
+// code - zero of the low nibbles of the bytes 0 and 2 (16 (code - zero) of the high ones), as fp16; `of`: kFp16Of1024
+__device__ __forceinline__ uint32_t low_nibbles(uint32_t w, uint32_t minus, uint32_t of) { return add_f16(merged<0x000f000fu>(w, of), minus); }
+__device__ __forceinline__ uint32_t high_nibbles(uint32_t w, uint32_t minus, uint32_t of) { return add_f16(merged<0x00f000f0u>(w, of), minus); }
+// -(1024 + zero), -(1024 + 16 zero) from two zero points as the cache holds them; `of`: kFp16OfMinus1024
+__device__ __forceinline__ uint32_t minus_low(uint32_t z, uint32_t of) { return merged<0x000f000fu>(z, of); }
+__device__ __forceinline__ uint32_t minus_high(uint32_t z, uint32_t of) { return merged<0x00f000f0u>(z, of); }
 
 // ---------------------------------------------------------------- what is whose
 
@@ -226,7 +241,10 @@ __device__ __forceinline__ Scan block_scan(long long v, long long* sh) {
 
 // Where the warp's part of the units begins, and how many they are. As few warps as have kMinUnits each, over all CTAs;
 // `active` is how many of a CTA's warps these are.
+template <int kR>
 struct Shared {
+  Place<kR> load[kWarps], take[kWarps];  // items that a warp copies and computes
+  int load_left[kWarps];
   long long scan[kWarps];
   long long offset[kWarps];
   int s[kWarps];
@@ -235,7 +253,7 @@ struct Shared {
   int abort;
 };
 template <int kR>
-__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& c, int& active, Shared& sh) {
+__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& c, int& active, Shared<kR>& sh) {
   const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5;
   int* const err = blockIdx.x == 0 ? p.err : nullptr;
   long long mine = 0, total = 0;
@@ -247,10 +265,14 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     total += scan.total;
   }
   const long long want = (total + kMinUnits - 1) / kMinUnits;
-  active = static_cast<int>(min(static_cast<long long>(kWarps), (want + gridDim.x - 1) / gridDim.x));
-  const long long warps = min(want, static_cast<long long>(gridDim.x) * active);
-  const long long first_warp = static_cast<long long>(blockIdx.x) * active;
-  auto from = [&](long long w) { return w >= warps ? total : total * w / warps; };
+  const int all = static_cast<int>(min(want, static_cast<long long>(gridDim.x * kWarps)));
+  active = (all + gridDim.x - 1) / gridDim.x;
+  const int warps = min(all, static_cast<int>(gridDim.x) * active), first_warp = blockIdx.x * active;
+  // (a division of 64 bits takes as long as a read of memory)
+  long long each;
+  if (total < (1LL << 31)) each = static_cast<unsigned>(total) / static_cast<unsigned>(warps); else each = total / warps;
+  const int over = static_cast<int>(total - each * warps);
+  auto from = [&](int w) { return w >= warps ? total : each * w + min(w, over); };
   // the sequence that a warp's first unit is in
   long long before = 0;
   for (int at = 0; at < S; at += kThreads) {
@@ -276,72 +298,91 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   c.seq = seq_of(p, c.s, nullptr);
   for (c.rt = 0;; ++c.rt) {
     c.tiles = tiles_of<kR>(g, c.seq, c.rt);
-    const long long units = max(1, c.tiles);
-    if (rest < units * g.kv_heads) {
-      c.h = static_cast<int>(rest / units);
-      c.tile = static_cast<int>(rest % units);
+    const long long units = static_cast<long long>(max(1, c.tiles)) * g.kv_heads;
+    if (rest < units) {
+      c.h = rest < (1LL << 31) ? static_cast<unsigned>(rest) / static_cast<unsigned>(max(1, c.tiles)) : static_cast<int>(rest / max(1, c.tiles));
+      c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * max(1, c.tiles));
       break;
     }
-    rest -= units * g.kv_heads;
+    rest -= units;
   }
   return static_cast<int>(from(first_warp + warp + 1) - from(first_warp + warp));
 }
 
 // ---------------------------------------------------------------- a warp's copies
 
+// Tiles of a stage, the first at `tile`: two from an even one on, so that they lie in one page or in two neighbours of a
+// batch (below).
+template <typename C>
+__device__ __forceinline__ int stage_tiles(int tile, int end) {
+  return C::kStageTiles == 1 || (tile & 1) != 0 ? 1 : min(2, end - tile);
+}
+
+// What a warp copies next. Every lane holds where one of 32 neighbouring tiles lies (a batch; without the head's offset, as
+// the heads of a sequence lie in the same pages), and copies it when its turn comes.
 template <int kDh, bool kInt4, int kR>
 struct Loader {
   using C = Config<kDh, kInt4, kR>;
-  Place<kR> at;
-  int left;                  // units not copied yet
-  const int32_t* row;        // of the page table
-  int page;                  // of the next tile, loaded a tile ahead
-  const uint8_t* src;        // of the next tile, unless a page begins with it
-  bool turn;                 // a page begins with it
-  int stage = 0, issued = 0;
-  uint32_t bad = 0;          // stages whose page is none of the cache's
+  const uint8_t* mine;   // the lane's tile, for head 0
+  long long head;        // offset of the item's head
+  int s, tile, end;      // sequence, next tile to copy, end of the warp's part of the item
+  int issued = 0;        // stages
+  bool bad = false;      // a page was none of the cache's
 
-  __device__ __forceinline__ void find(const PagedAttentionArgs& p, const Geometry& g) {
-    while (left > 0 && at.tiles == 0)
-      if (--left > 0) at.next_item(p, g);
-    if (left <= 0) return;
-    row = p.batch.table + static_cast<long long>(at.s) * p.batch.ld_table;
-    page = row[(at.tile * kKvTile) >> p.cache.page_bits];
-    turn = true;
+  __device__ __forceinline__ void batch(const PagedAttentionArgs& p, int lane) {
+    const int at = (tile & ~31) + lane;
+    int page = 0;
+    if (at < end) page = p.batch.table[static_cast<long long>(s) * p.batch.ld_table + ((at * kKvTile) >> p.cache.page_bits)];
+    const bool ok = page >= 0 && page < p.cache.n_pages;
+    if (__any_sync(0xffffffffu, !ok)) {
+      bad = true;
+      if (lane == 0) record_error(p.err, kDevBadPage);
+    }
+    mine = kv_tile<typename C::Tile>(p.cache, ok ? page : 0, 0, at * kKvTile);
   }
-  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, int lane, uint8_t* ring, uint32_t bars) {
-    if (left <= 0) return;
-    if (turn) {
-      const bool ok = page >= 0 && page < p.cache.n_pages;
-      if (!ok && lane == 0) record_error(p.err, kDevBadPage);
-      src = kv_tile<typename C::Tile>(p.cache, ok ? page : 0, at.h, at.tile * kKvTile);
-      page = ok ? page : -1;
-      turn = false;
+  // The item that `at` says, `left` units from its tile on; those without tiles are passed over. `at` goes on to the next.
+  // (The lanes read the shared copies, compute the same, and write them again.)
+  __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane, bool same) {
+    Place<kR> now = at;
+    int n = left;
+    while (n > 0 && now.tiles == 0)
+      if (--n > 0) {
+        now.next_item(p, g);
+        same = false;
+      }
+    tile = now.tile;
+    end = min(now.tiles, tile + n);
+    s = now.s;
+    if (n > 0) {
+      head = static_cast<long long>(now.h) * ((1 << (p.cache.page_bits - 4)) * C::Tile::kBytes);
+      // (the same sequence's next head, in the batch that is there)
+      if (!same || now.h == 0 || now.tiles > 32) batch(p, lane);
+      n -= end - tile;
+      if (n > 0) now.next_item(p, g);
     }
-    bad = page >= 0 ? bad & ~(1u << stage) : bad | (1u << stage);
-    if (lane == 0) {
-      const uint32_t bar = bars + 8 * stage;
-      mbar_arrive_expect_tx(bar, C::Tile::kBytes);
+    __syncwarp();
+    at = now;
+    left = n;
+    __syncwarp();
+  }
+  // The next stage: a wait's tiles.
+  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
+                                        uint32_t dst, uint32_t bar) {
+    if (tile >= end) {
+      if (left <= 0) return;
+      item(p, g, at, left, lane, true);
+      if (tile >= end) return;
+    }
+    const int n = stage_tiles<C>(tile, end), which = lane - (tile & 31);
+    if (which == 0) mbar_arrive_expect_tx(bar, n * C::Tile::kBytes);
+    if (which >= 0 && which < n)
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                       smem_u32(ring + stage * C::Tile::kBytes)),
-                   "l"(reinterpret_cast<uint64_t>(src)), "r"(C::Tile::kBytes), "r"(bar)
+                       dst + which * C::Tile::kBytes),
+                   "l"(reinterpret_cast<uint64_t>(mine + head)), "n"(C::Tile::kBytes), "r"(bar)
                    : "memory");
-    }
-    stage = stage + 1 == C::kStages ? 0 : stage + 1;
     ++issued;
-    --left;
-    if (++at.tile == at.tiles) {
-      if (left > 0) {
-        at.next_item(p, g);
-        find(p, g);
-      }
-    } else {
-      src += C::Tile::kBytes;
-      if ((at.tile & ((1 << (p.cache.page_bits - 4)) - 1)) == 0 && left > 0) {
-        page = row[(at.tile * kKvTile) >> p.cache.page_bits];
-        turn = true;
-      }
-    }
+    tile += n;
+    if ((tile & 31) == 0 && tile < end) batch(p, lane);
   }
 };
 
@@ -354,16 +395,19 @@ struct Rows {
   float factor[kR][2];
   int limit[kR][2];             // last position that rows 2t and 2t + 1 of each eight see
   int first_limit, last_limit;  // the least and the largest of the rows'
+  // fragments of 16 channels; in 4 bits fp16, of which the second word is a sixteenth
   uint2 q[C::kQShared ? 1 : kR][C::kQShared ? 1 : kDh / 16];
   const uint2* q_shared;
   float o[C::kMTiles][kR][4], m[kR][2], l[kR][2];
+  uint32_t plus1024, minus1024;  // kFp16Of1024, kFp16OfMinus1024 in registers
 
   __device__ __forceinline__ uint2 query(int n, int step, int lane) const {
     if constexpr (C::kQShared) return q_shared[(n * C::kMTiles + step) * 32 + lane];
     else return q[n][step];
   }
 
-  // The queries' fragments; in 4 bits (fp16) each row times a power of two that makes its largest 2^7.
+  // The queries' fragments; in 4 bits each row times a power of two that makes its largest 2^7 to 2^8 (fp16 holds all bits
+  // of a bf16 down to 2^-21 of that; a row with an infinity or NaN is NaN).
   __device__ __forceinline__ void begin(const PagedAttentionArgs& p, const Geometry& geo, const Place<kR>& c, int live, int lane,
                                         uint2* to_shared) {
     const int g = lane >> 2, t = lane & 3;
@@ -402,8 +446,8 @@ struct Rows {
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int exponent = (__float_as_int(top) >> 23) - 127;  // -127 for 0 and what is below 2^-126
-        const int by = exponent > 127 ? 0 : min(126, 7 - exponent);
-        by_row *= pow2(max(-by, -126));
+        const int by = min(126, 7 - exponent);
+        by_row = exponent > 127 ? __int_as_float(0x7fffffff) : by_row * pow2(max(-by, -126));
         const float up = pow2(by);
 #pragma unroll
         for (int i = 0; i < kDh / 32; ++i)
@@ -437,7 +481,7 @@ struct Rows {
 
   // kN neighbouring tiles, the first at position `pos`; kMasked: some of their tokens may lie behind what some rows see.
   template <int kN, bool kMasked>
-  __device__ __forceinline__ void take(const uint8_t* const (&tiles)[kN], int pos, int lane) {
+  __device__ __forceinline__ void take(const uint8_t* first_tile, int pos, int lane) {
     using Tile = typename C::Tile;
     constexpr int kGroups = kInt4 ? kDh / kKvGroup : 1;  // that have a scale of their own
     constexpr int kWords = kDh / 32;
@@ -446,14 +490,8 @@ struct Rows {
     float sc[kN][kR][4], sv[kN][2][kGroups];  // values' scales of tokens g and g + 8
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const uint8_t* tp = tiles[i];
+      const uint8_t* tp = first_tile + i * Tile::kBytes;
       float part[kGroups][kR][4];
-#pragma unroll
-      for (int gr = 0; gr < kGroups; ++gr)
-#pragma unroll
-        for (int n = 0; n < kR; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) part[gr][n][e] = 0.f;
       if constexpr (kInt4) {
         float sk[2][kGroups];
         uint32_t zk[2][kGroups], kw[2][kWords];
@@ -489,21 +527,28 @@ struct Rows {
             kw[h][1] = w.y;
           }
         }
+        uint32_t minus[2][kGroups][2];
 #pragma unroll
-        for (int w = 0; w < kWords; ++w) {
-          const int gr = w / 2;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
+          for (int gr = 0; gr < kGroups; ++gr) {
+            minus[h][gr][0] = minus_low(zk[h][gr], minus1024);
+            minus[h][gr][1] = minus_high(zk[h][gr], minus1024);
+          }
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+#pragma unroll
+          for (int gr = 0; gr < kGroups; ++gr) {  // (groups in turn: their sums are chains)
+            const int w = 2 * gr + step / 2, x = step % 2;
             const uint32_t w0 = x == 0 ? kw[0][w] : kw[0][w] >> 8, w1 = x == 0 ? kw[1][w] : kw[1][w] >> 8;
-            const uint32_t a[4] = {low_nibbles(w0, minus_low(zk[0][gr])), low_nibbles(w1, minus_low(zk[1][gr])),
-                                   high_nibbles(w0, minus_high(zk[0][gr])), high_nibbles(w1, minus_high(zk[1][gr]))};
+            const uint32_t a[4] = {low_nibbles(w0, minus[0][gr][0], plus1024), low_nibbles(w1, minus[1][gr][0], plus1024),
+                                   high_nibbles(w0, minus[0][gr][1], plus1024), high_nibbles(w1, minus[1][gr][1], plus1024)};
 #pragma unroll
             for (int n = 0; n < kR; ++n) {
               const uint2 f = query(n, 2 * w + x, lane);
-              mma<true>(part[gr][n], a, f.x, f.y);
+              if (step == 0) first_mma_f16(part[gr][n], a, f.x, f.y); else mma_f16(part[gr][n], a, f.x, f.y);
             }
           }
-        }
 #pragma unroll
         for (int n = 0; n < kR; ++n)
 #pragma unroll
@@ -512,6 +557,10 @@ struct Rows {
             if constexpr (kGroups == 2) sc[i][n][e] = fmaf(part[1][n][e], sk[e >> 1][1], sc[i][n][e]);
           }
       } else {
+#pragma unroll
+        for (int n = 0; n < kR; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) part[0][n][e] = 0.f;
 #pragma unroll
         for (int w = 0; w < kWords; ++w) {
           const uint4 k0 = *reinterpret_cast<const uint4*>(tp + (w * kKvTile + g) * 64 + t * 16);
@@ -522,7 +571,7 @@ struct Rows {
 #pragma unroll
             for (int n = 0; n < kR; ++n) {
               const uint2 f = query(n, 2 * w + x, lane);
-              mma<false>(part[0][n], a, f.x, f.y);
+              mma_bf16(part[0][n], a, f.x, f.y);
             }
           }
         }
@@ -625,7 +674,7 @@ struct Rows {
     // ---- O^T += V^T P^T
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
-      const uint8_t* tp = tiles[i];
+      const uint8_t* tp = first_tile + i * Tile::kBytes;
       if constexpr (kInt4) {
         uint32_t zv[2][kGroups], vw[2][kWords];
         if constexpr (kDh == 128) {
@@ -653,14 +702,22 @@ struct Rows {
             vw[h][1] = w.y;
           }
         }
+        uint32_t minus[2][kGroups][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int gr = 0; gr < kGroups; ++gr) {
+            minus[h][gr][0] = minus_low(zv[h][gr], minus1024);
+            minus[h][gr][1] = minus_high(zv[h][gr], minus1024);
+          }
 #pragma unroll
         for (int j = 0; j < C::kMTiles; ++j) {
           const int w = j / 2, gr = w / 2;
           const uint32_t w0 = j % 2 == 0 ? vw[0][w] : vw[0][w] >> 8, w1 = j % 2 == 0 ? vw[1][w] : vw[1][w] >> 8;
-          const uint32_t a[4] = {low_nibbles(w0, minus_low(zv[0][gr])), high_nibbles(w0, minus_high(zv[0][gr])),
-                                 low_nibbles(w1, minus_low(zv[1][gr])), high_nibbles(w1, minus_high(zv[1][gr]))};
+          const uint32_t a[4] = {low_nibbles(w0, minus[0][gr][0], plus1024), high_nibbles(w0, minus[0][gr][1], plus1024),
+                                 low_nibbles(w1, minus[1][gr][0], plus1024), high_nibbles(w1, minus[1][gr][1], plus1024)};
 #pragma unroll
-          for (int n = 0; n < kR; ++n) mma<true>(o[j][n], a, pf[i][gr][n][0], pf[i][gr][n][1]);
+          for (int n = 0; n < kR; ++n) mma_f16(o[j][n], a, pf[i][gr][n][0], pf[i][gr][n][1]);
         }
       } else {
         // bytes behind the last token count as zeros, an infinity or NaN that some rows may see too, at first
@@ -698,8 +755,8 @@ struct Rows {
             const uint32_t a[4] = {v[0][2 * x], v[0][2 * x + 1], v[1][2 * x], v[1][2 * x + 1]};
 #pragma unroll
             for (int n = 0; n < kR; ++n) {
-              mma<false>(o[j][n], a, pf[i][0][n][0], pf[i][0][n][1]);
-              mma<false>(o[j][n], a, pf[i][1][n][0], pf[i][1][n][1]);
+              mma_bf16(o[j][n], a, pf[i][0][n][0], pf[i][0][n][1]);
+              mma_bf16(o[j][n], a, pf[i][1][n][0], pf[i][1][n][1]);
             }
             if constexpr (kMasked) {
               if (any) {  // a token at a time, for the rows that see it
@@ -715,7 +772,7 @@ struct Rows {
 #pragma unroll
                   for (int n = 0; n < kR; ++n) {
                     float d[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma<false>(d, b, pf[i][0][n][0], pf[i][0][n][1]);
+                    mma_bf16(d, b, pf[i][0][n][0], pf[i][0][n][1]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                       if (pos + kKvTile * i + tok <= limit[n][e & 1]) o[j][n][e] += d[e];
@@ -767,9 +824,9 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
   using Tile = typename C::Tile;
   using Parts = Part<kDh, kR>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ Shared sh;
+  __shared__ Shared<kR> sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  uint8_t* const ring = smem + warp * (C::kStages * Tile::kBytes);
+  uint8_t* const ring = smem + warp * (C::kStages * C::kStageBytes);
   const uint32_t bars = smem_u32(smem + C::kRing + C::kQ) + warp * C::kStages * 8;
   if (lane == 0)
     for (int i = 0; i < C::kStages; ++i) mbar_init(bars + 8 * i, 1);
@@ -783,17 +840,26 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
   int left = begin(p, geo, c, active, sh);  // (synchronises the block)
   WarpEnd end{0, 0, 0, 0, false, false, false, false};
   if (left > 0) {
+    Place<kR>& load = sh.load[warp];
+    Place<kR>& take = sh.take[warp];
+    int& load_left = sh.load_left[warp];
+    const uint32_t ring_at = smem_u32(ring);
     Loader<kDh, kInt4, kR> loader;
-    loader.at = c;
-    loader.left = left;
-    loader.find(p, geo);
+    load = c;
+    take = c;
+    load_left = left;
+    __syncwarp();
+    loader.item(p, geo, load, load_left, lane, false);
 #pragma unroll 1
-    for (int i = 0; i < C::kStages; ++i) loader.issue(p, geo, lane, ring, bars);
-    int stage = 0, used = 0;  // of the ring
-    uint32_t phase = 0;
+    for (int i = 0; i < C::kStages; ++i)
+      loader.issue(p, geo, load, load_left, lane, ring_at + i * C::kStageBytes, bars + 8 * i);
+    int used = 0;  // stages; a stage that has been used is the next to be filled
     Rows<kDh, kInt4, kR> rows;
+    rows.plus1024 = held(kFp16Of1024);
+    rows.minus1024 = held(kFp16OfMinus1024);
 #pragma unroll 1
     while (left > 0) {
+      c = take;
       const int lo = c.tile, units = max(1, c.tiles), hi = min(units, lo + left);
       left -= hi - lo;
       const bool whole = lo == 0 && hi == units;
@@ -802,52 +868,43 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
       bool poison = false;
       if (c.tiles > 0) {
         rows.begin(p, geo, c, live, lane, reinterpret_cast<uint2*>(smem + C::kRing) + warp * (C::kQ / kWarps / 8));
-        auto wait = [&]() {
-          const bool there = warp_wait_bounded(bars + 8 * stage, phase, &sh.abort, p.err, kDevTimeoutProducer);
-          poison |= !there || ((loader.bad >> stage) & 1) != 0;
-          const uint8_t* at = ring + stage * Tile::kBytes;
-          if (there) {
-            ++used;
-            if (++stage == C::kStages) {
-              stage = 0;
-              phase ^= 1;
-            }
-          }
-          return at;
-        };
 #pragma unroll 1
         for (int tile = lo; tile < hi;) {
-          const int pos = tile * kKvTile;
-          int taken = 1;
-          if (C::kPair == 2 && tile + 2 <= hi && pos + 2 * kKvTile - 1 <= rows.first_limit) {
-            const uint8_t* const at0 = wait();
-            const uint8_t* const at[2] = {at0, wait()};
-            rows.template take<2, false>(at, pos, lane);
-            taken = 2;
-          } else if (C::kPair == 1 && pos + kKvTile - 1 <= rows.first_limit) {
-            const uint8_t* const at[1] = {wait()};
-            rows.template take<1, false>(at, pos, lane);
-          } else {
-            const uint8_t* const at[1] = {wait()};
-            rows.template take<1, true>(at, pos, lane);
+          const int stage = used & (C::kStages - 1), n = stage_tiles<C>(tile, hi);
+          const uint32_t bar = bars + 8 * stage;
+          const uint8_t* const at = ring + stage * C::kStageBytes;
+          if (!warp_wait_bounded(bar, used / C::kStages & 1, &sh.abort, p.err, kDevTimeoutProducer)) {
+            poison = true;
+            tile += n;
+            continue;
           }
-          tile += taken;
+          ++used;
+          if (loader.bad)  // rare: whether it is these tiles' pages
+            for (int i = tile; i < tile + n; ++i) poison |= kv_page(p.batch, p.cache, c.s, i * kKvTile, nullptr) < 0;
+          const int pos = tile * kKvTile;
+          const bool clear = pos + n * kKvTile - 1 <= rows.first_limit;
+          if (C::kPair == 2 && n == 2 && clear) {
+            rows.template take<C::kPair, false>(at, pos, lane);
+          } else if (C::kPair == 1 && clear) {
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) rows.template take<1, false>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+          } else {
+#pragma unroll 1
+            for (int i = 0; i < n; ++i) rows.template take<1, true>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+          }
+          tile += n;
           __syncwarp();
-          if (sh.abort == 0)
-            for (; taken > 0; --taken) loader.issue(p, geo, lane, ring, bars);
+          loader.issue(p, geo, load, load_left, lane, smem_u32(at), bar);
         }
       }
 
       // ---- an item as a whole goes out, a part of one waits: the last segment's in the ring, an earlier one's in memory
       const bool last = left == 0;
+      c = take;
       if (last) {
         for (; used < loader.issued; ++used) {  // copies that a wait has given up are not left behind
           int alone = 0;
-          mbar_wait_bounded(bars + 8 * stage, phase, &alone, p.err, kDevTimeoutDrain);
-          if (++stage == C::kStages) {
-            stage = 0;
-            phase ^= 1;
-          }
+          mbar_wait_bounded(bars + 8 * (used & (C::kStages - 1)), used / C::kStages & 1, &alone, p.err, kDevTimeoutDrain);
         }
         __syncwarp();
       }
@@ -898,61 +955,73 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
       end.s = c.s;
       end.rt = c.rt;
       end.h = c.h;
-      c.tile = hi;
-      if (left > 0) c.next_item(p, geo);
+      if (!last) {
+        c.next_item(p, geo);
+        __syncwarp();
+        take = c;
+        __syncwarp();
+      }
     }
   }
   if (lane == 0) sh.end[warp] = end;
   __syncthreads();
 
   // ---- chains of parts of one item: from what an earlier CTA began, or from a warp's tail, over the following warps' first
-  // parts to the one that ends it. A warp a row of a chain.
-  int chain = 0, tail_warp = -1, ends = 0;
-  for (int start = -1; start < active; ++start) {
-    const bool from_before = start < 0;
-    if (from_before ? !sh.end[0].first : !sh.end[start].tail) continue;
-    const WarpEnd& item = sh.end[from_before ? 0 : start];
-    int stop = from_before ? 0 : start + 1;  // one past its last warp
-    bool done = false;
-    while (stop < active && sh.end[stop].first && !done) done = sh.end[stop++].first_ends;
-    if (from_before) ends = done;
-    if (!from_before && !done) tail_warp = start;
-    const int rt = from_before ? item.first_rt : item.rt;
-    const int shown = min(8 * kR, geo.rows - rt * 8 * kR);
-    Parts* to = cta_part<kDh, kR>(p, blockIdx.x, from_before ? 0 : 1);
-    const int base = from_before ? 0 : start;
+  // parts to the one that ends it. A warp a row of a chain; a lane holds a part's mass, and all parts are read at once.
+  const WarpEnd& my_end = sh.end[lane & (kWarps - 1)];
+  const unsigned have = (1u << active) - 1;
+  const unsigned firsts = __ballot_sync(0xffffffffu, my_end.first) & have, enders = __ballot_sync(0xffffffffu, my_end.first_ends) & have;
+  const unsigned tails = __ballot_sync(0xffffffffu, my_end.tail) & have, ringed = __ballot_sync(0xffffffffu, my_end.first_last) & have;
+  int turn = 0, tail_warp = -1;
+  bool ends = false;
+  for (unsigned starts = (firsts & 1u) | tails << 1; starts != 0; starts &= starts - 1) {
+    const int start = __ffs(starts) - 2, next = start + 1;  // start -1: an earlier CTA's
+    // the run of first parts from `next` on, up to the one that ends the item
+    const unsigned run = ~(firsts >> next), stop_at = enders >> next;
+    const int length = __ffs(run) - 1, end_at = __ffs(stop_at);
+    const bool done = end_at > 0 && end_at <= length;
+    const int stop = next + (done ? end_at : length);
+    if (start < 0) ends = done;
+    else if (!done) tail_warp = start;
+    const WarpEnd& item = sh.end[max(start, 0)];
+    const int rt = start < 0 ? item.first_rt : item.rt, shown = min(8 * kR, geo.rows - rt * 8 * kR);
     constexpr int kE = kDh / 32;
     // (rows past the last token hold nothing; what is made of them is not read)
-    for (int row = (warp + kWarps - chain % kWarps) % kWarps; row < shown; row += kWarps) {
-      float mass[kWarps], top = kFar, sum = 0.f, out[kE];
-      const float* part[kWarps];
+    for (int row = (warp - turn) & (kWarps - 1); row < shown; row += kWarps) {
+      float mass = kFar;
+      if (lane < stop && lane >= max(start, 0))
+        mass = lane == start || (ringed >> lane & 1) != 0 ? sh.mass[lane][row] : warp_part<kDh, kR>(p, lane)->mass[row];
+      float in[kWarps][kE];
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        mass[w] = kFar;
-        part[w] = nullptr;
-        if (w >= base && w < stop) {
-          const bool ringed = w == start || sh.end[w].first_last;
-          const Parts* kept = warp_part<kDh, kR>(p, w);
-          part[w] = ringed ? reinterpret_cast<const float*>(smem + w * (C::kStages * Tile::kBytes)) + row * kDh : kept->o[row];
-          mass[w] = ringed ? sh.mass[w][row] : kept->mass[row];
+        const float* ring_part = reinterpret_cast<const float*>(smem + w * (C::kStages * C::kStageBytes)) + row * kDh + lane * kE;
+        const float* far_part = &warp_part<kDh, kR>(p, w)->o[row][lane * kE];
+        const bool there = w < stop && w >= max(start, 0), near = w == start || (ringed >> w & 1) != 0;
+#pragma unroll
+        for (int i = 0; i < kE; ++i) {
+          in[w][i] = 0.f;
+          if (there && near) in[w][i] = ring_part[i];
+          if (there && !near) in[w][i] = far_part[i];
         }
-        top = fmaxf(top, mass[w]);
       }
+      float top = mass;
+#pragma unroll
+      for (int off = 4; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const float weight = mass == kFar ? 0.f : ex2(mass - top);
+      float sum = weight;
+#pragma unroll
+      for (int off = 4; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      const float share = sum == 0.f ? 0.f : weight / sum;
+      float out[kE];
 #pragma unroll
       for (int i = 0; i < kE; ++i) out[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        mass[w] = mass[w] == kFar ? 0.f : ex2(mass[w] - top);
-        sum += mass[w];
+        const float by = __shfl_sync(0xffffffffu, share, w);
+#pragma unroll
+        for (int i = 0; i < kE; ++i) out[i] = by == 0.f ? out[i] : fmaf(in[w][i], by, out[i]);
       }
-      const float norm = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w)
-        if (mass[w] != 0.f) {
-#pragma unroll
-          for (int i = 0; i < kE; ++i) out[i] = fmaf(part[w][lane * kE + i], mass[w] * norm, out[i]);
-        }
-      if (!from_before && done) {
+      if (start >= 0 && done) {
         const KvSeq seq = seq_of(p, item.s, nullptr);
         const int q_row = rt * 8 * kR + row;
         __nv_bfloat16* dst = out_row<kR>(p, geo, item.s, q_row, item.h, kDh) + lane * kE;
@@ -960,12 +1029,14 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
         for (int i = 0; i < kE; i += 2)
           *reinterpret_cast<uint32_t*>(dst + i) = q_row < seq.n * geo.group ? pack_bf16x2(out[i], out[i + 1]) : 0u;
       } else {
+        Parts* to = cta_part<kDh, kR>(p, blockIdx.x, start < 0 ? 0 : 1);
 #pragma unroll
         for (int i = 0; i < kE; ++i) to->o[row][lane * kE + i] = out[i];
-        if (lane == 0) to->mass[row] = sum == 0.f ? kFar : top + log2f(sum);
+        const float total = __shfl_sync(0xffffffffu, sum, 0), highest = __shfl_sync(0xffffffffu, top, 0);
+        if (lane == 0) to->mass[row] = total == 0.f ? kFar : highest + log2f(total);
       }
     }
-    chain += shown;
+    turn += shown;
   }
   if (threadIdx.x == 0) {
     Desc d{0, 0, 0, -1, ends, {0, 0, 0}};

@@ -1,13 +1,14 @@
 """Attention over a paged cache against the fp64 oracle on the values that the cache holds.
 
 Tolerances, with u = 2^-24. A score is a sum of D products in fp32, off by at most (D + 16) u of the sum of their
-magnitudes (`reach`), so a weight is off by (D + 16) u reach relative, and the quotient of two sums of weights twice
-that. Weights enter the second product rounded to fp16 (half a step: 2^-11 relative) together with their value's scale, the
+magnitudes (`reach`); in 4 bits a query is two e4m3, relative to its row's largest, between 2^7 and 2^8 then, of which the
+second has steps of 2^-9 at least: an element is off by 2^-10, 2^-17 of the largest, and a score by that times sum_d |k_jd|
+(`coarse`). So a weight is off by e = (D + 16) u reach + 2^-17 coarse relative, and the quotient of two sums of weights twice that. Weights enter the second product rounded to fp16 (half a step: 2^-11 relative) together with their value's scale, the
 largest such product of a row at 2^6 or more: below 2^-14 fp16 has steps of 2^-24, so a weight is off by 2^-25 at most, 2^-31
 of the largest product w sv. Times a code of up to 15, and sv <= max |v| / 7.5 (a scale is a fifteenth of its range),
 that is N 2^-30 max |v| over N tokens. (Two bf16, 2^-16 relative, in a bf16 cache.) The sums themselves are fp32 over N terms:
-at most N u, with 64 for the order and the logarithms of sums that are added up. So an output is off by
-    (2^-11 + 2 (D + 16) u reach + (N + 64) u) sum_j p_j |v_j| + N 2^-30 max |v|,
+at most N u, with 128 for the order and for logarithms of up to 128, rounded, by which parts are added up. So an output is off by
+    (2^-11 + 2 e + (N + 128) u) sum_j p_j |v_j| + N 2^-30 max |v|,
 and rounded to bf16: half a step, 2^-8 of its value (and of what it is off by)."""
 import numpy as np
 import pytest
@@ -94,7 +95,10 @@ def check(c, got, scale=None, sick=None):
             continue
         N = int(c["cached"][s]) + n
         ref, size, reach = O.cached_attention(q[s, :n], c["k"][s, :N], c["v"][s, :N], int(c["cached"][s]), scale)
-        tol = (2.0 ** -11 + 2 * (D + 16) * U * reach[..., None] + (N + 64) * U) * size + N * 2.0 ** -30 * np.abs(c["v"][s, :N]).max()
+        by = c["heads"] // c["kv"]
+        coarse = np.abs(q[s, :n]).max(-1) * np.abs(c["k"][s, :N].astype(np.float64)).sum(-1).max(0).repeat(by)[None] * abs(scale)
+        e = ((D + 16) * U * reach + 2.0 ** -17 * coarse)[..., None]
+        tol = (2.0 ** -11 + 2 * e + (N + 128) * U) * size + N * 2.0 ** -30 * np.abs(c["v"][s, :N]).max()
         tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
         off = np.abs(got[s, :n] - ref)
         assert np.isfinite(got[s, :n]).all(), f"sequence {s}: not finite"
