@@ -22,6 +22,7 @@
 // CTA's warps are added up, and what CTAs share a second kernel adds up, both in the order of the parts.
 #include <algorithm>
 #include <climits>
+#include <type_traits>
 
 #include "kv_cache.cuh"
 
@@ -33,6 +34,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
 constexpr int kMaxRowTiles = 4;   // of 8 query rows that share a pass
 constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
+constexpr int kItemUnits = 2;     // what an item costs beside its tiles, in tiles
 constexpr float kFar = -1e30f;    // a maximum of nothing
 // Exponents relative to m (exact for scales of values up to 2^100: above that small probabilities are flushed). bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
 // 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108.
@@ -43,7 +45,8 @@ struct Desc {
   int s, rt, h;   // the item that its last segment begins and does not end, if slot >= 0
   int slot;       // where that segment's part lies, or -1
   int ends;       // its first segment (slot 0) ends an item that an earlier CTA began
-  int pad[3];
+  int live;       // rows of the item that have a token
+  int pad[2];
 };
 
 // Part of an item's rows, normalised, with log2 of the sum of exp2(s) that it stands for (NaN: unusable).
@@ -57,6 +60,7 @@ template <int kDh, bool kInt4, int kR>
 struct Config {
   using Tile = KvTile<kDh, kInt4>;
   using Parts = Part<kDh, kR>;
+  using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
   static constexpr int kCtasPerSm = kInt4 && kR == 1 ? 2 : 1;
   static constexpr bool kQShared = kR > 2;  // the queries' fragments: shared memory, else registers
@@ -81,6 +85,7 @@ struct WarpEnd {
   bool first_last;  // it is the last segment as well, and lies in the ring
   bool first_ends;  // it ends its item
   bool tail;        // the last segment begins an item and does not end it
+  int live;         // rows with a token of that item
 };
 
 // (not volatile: the compiler interleaves them)
@@ -180,16 +185,19 @@ __device__ __forceinline__ Geometry geometry(const PagedAttentionArgs& p) {
 // Tiles of cached tokens that rows [8 kR rt, ...) of a sequence see; 0 where there is nothing to compute.
 template <int kR>
 __device__ __forceinline__ int tiles_of(const Geometry& g, const KvSeq& seq, int rt) {
+  if (!seq.ok || seq.n == 0) return 0;
+  if (g.row_tiles == 1) return (seq.cached + seq.n - 1) / kKvTile + 1;
   const int live = g.group * seq.n, first = rt * 8 * kR;
-  if (!seq.ok || first >= live) return 0;
+  if (first >= live) return 0;
   const int last = (min(first + 8 * kR, live) - 1) / g.group;
   return (seq.cached + last) / kKvTile + 1;
 }
-// Units of a sequence's items of one head, at least one each: an item without tiles has rows to fill.
+// Units of an item: its tiles, at least one (an item without tiles has rows to fill), and behind them what it costs besides.
+__device__ __forceinline__ int units_of_item(int tiles) { return max(1, tiles) + kItemUnits; }
 template <int kR>
 __device__ __forceinline__ long long units_of(const Geometry& g, const KvSeq& seq) {
   long long n = 0;
-  for (int rt = 0; rt < g.row_tiles; ++rt) n += max(1, tiles_of<kR>(g, seq, rt));
+  for (int rt = 0; rt < g.row_tiles; ++rt) n += units_of_item(tiles_of<kR>(g, seq, rt));
   return n;
 }
 
@@ -298,15 +306,21 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   c.seq = seq_of(p, c.s, nullptr);
   for (c.rt = 0;; ++c.rt) {
     c.tiles = tiles_of<kR>(g, c.seq, c.rt);
-    const long long units = static_cast<long long>(max(1, c.tiles)) * g.kv_heads;
+    const int each_item = units_of_item(c.tiles);
+    const long long units = static_cast<long long>(each_item) * g.kv_heads;
     if (rest < units) {
-      c.h = rest < (1LL << 31) ? static_cast<unsigned>(rest) / static_cast<unsigned>(max(1, c.tiles)) : static_cast<int>(rest / max(1, c.tiles));
-      c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * max(1, c.tiles));
+      c.h = rest < (1LL << 31) ? static_cast<unsigned>(rest) / static_cast<unsigned>(each_item) : static_cast<int>(rest / each_item);
+      c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * each_item);
       break;
     }
     rest -= units;
   }
-  return static_cast<int>(from(first_warp + warp + 1) - from(first_warp + warp));
+  int left = static_cast<int>(from(first_warp + warp + 1) - from(first_warp + warp));
+  if (c.tile >= max(1, c.tiles)) {  // behind an item's tiles
+    left -= units_of_item(c.tiles) - c.tile;
+    if (left > 0) c.next_item(p, g);
+  }
+  return left;
 }
 
 // ---------------------------------------------------------------- a warp's copies
@@ -325,7 +339,7 @@ struct Loader {
   using C = Config<kDh, kInt4, kR>;
   const uint8_t* mine;   // the lane's tile, for head 0
   long long head;        // offset of the item's head
-  int s, tile, end;      // sequence, next tile to copy, end of the warp's part of the item
+  int s = 0, tile = 0, end = 0;  // sequence, next tile to copy, end of the warp's part of the item
   int issued = 0;        // stages
   bool bad = false;      // a page was none of the cache's
 
@@ -345,11 +359,11 @@ struct Loader {
   __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane, bool same) {
     Place<kR> now = at;
     int n = left;
-    while (n > 0 && now.tiles == 0)
-      if (--n > 0) {
-        now.next_item(p, g);
-        same = false;
-      }
+    while (n > 0 && now.tiles == 0) {
+      n -= units_of_item(0);
+      if (n > 0) now.next_item(p, g);
+      same = false;
+    }
     tile = now.tile;
     end = min(now.tiles, tile + n);
     s = now.s;
@@ -357,7 +371,7 @@ struct Loader {
       head = static_cast<long long>(now.h) * ((1 << (p.cache.page_bits - 4)) * C::Tile::kBytes);
       // (the same sequence's next head, in the batch that is there)
       if (!same || now.h == 0 || now.tiles > 32) batch(p, lane);
-      n -= end - tile;
+      n -= units_of_item(now.tiles) - tile;
       if (n > 0) now.next_item(p, g);
     }
     __syncwarp();
@@ -365,14 +379,16 @@ struct Loader {
     left = n;
     __syncwarp();
   }
-  // The next stage: a wait's tiles.
-  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
-                                        uint32_t dst, uint32_t bar) {
+  // The next stage, one wait's tiles; false where there are none.
+  __device__ __forceinline__ bool issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
+                                        uint32_t ring, uint32_t bars) {
     if (tile >= end) {
-      if (left <= 0) return;
-      item(p, g, at, left, lane, true);
-      if (tile >= end) return;
+      if (left <= 0) return false;
+      item(p, g, at, left, lane, issued > 0);
+      if (tile >= end) return false;
     }
+    const int stage = issued & (C::kStages - 1);
+    const uint32_t dst = ring + stage * C::kStageBytes, bar = bars + 8 * stage;
     const int n = stage_tiles<C>(tile, end), which = lane - (tile & 31);
     if (which == 0) mbar_arrive_expect_tx(bar, n * C::Tile::kBytes);
     if (which >= 0 && which < n)
@@ -383,6 +399,7 @@ struct Loader {
     ++issued;
     tile += n;
     if ((tile & 31) == 0 && tile < end) batch(p, lane);
+    return true;
   }
 };
 
@@ -838,7 +855,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
   Place<kR> c;
   int active;
   int left = begin(p, geo, c, active, sh);  // (synchronises the block)
-  WarpEnd end{0, 0, 0, 0, false, false, false, false};
+  WarpEnd end{0, 0, 0, 0, false, false, false, false, 0};
   if (left > 0) {
     Place<kR>& load = sh.load[warp];
     Place<kR>& take = sh.take[warp];
@@ -849,118 +866,113 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
     take = c;
     load_left = left;
     __syncwarp();
-    loader.item(p, geo, load, load_left, lane, false);
-#pragma unroll 1
-    for (int i = 0; i < C::kStages; ++i)
-      loader.issue(p, geo, load, load_left, lane, ring_at + i * C::kStageBytes, bars + 8 * i);
-    int used = 0;  // stages; a stage that has been used is the next to be filled
     Rows<kDh, kInt4, kR> rows;
     rows.plus1024 = held(kFp16Of1024);
     rows.minus1024 = held(kFp16OfMinus1024);
+    int used = 0;  // stages
+    int lo = 0, tile = 0, hi = 0, live = 0;  // the warp's part of the present item, the next tile; rows with a token
+    bool open = false, poison = false;
+    // (one place each where a stage is filled, an item begun and ended: what runs rarely runs from a cold instruction cache)
 #pragma unroll 1
-    while (left > 0) {
-      c = take;
-      const int lo = c.tile, units = max(1, c.tiles), hi = min(units, lo + left);
-      left -= hi - lo;
-      const bool whole = lo == 0 && hi == units;
-      const int row0 = c.rt * 8 * kR;
-      const int live = c.tiles == 0 ? 0 : min(8 * kR, c.seq.n * geo.group - row0);  // rows with a token
-      bool poison = false;
-      if (c.tiles > 0) {
-        rows.begin(p, geo, c, live, lane, reinterpret_cast<uint2*>(smem + C::kRing) + warp * (C::kQ / kWarps / 8));
-#pragma unroll 1
-        for (int tile = lo; tile < hi;) {
-          const int stage = used & (C::kStages - 1), n = stage_tiles<C>(tile, hi);
-          const uint32_t bar = bars + 8 * stage;
-          const uint8_t* const at = ring + stage * C::kStageBytes;
-          if (!warp_wait_bounded(bar, used / C::kStages & 1, &sh.abort, p.err, kDevTimeoutProducer)) {
-            poison = true;
-            tile += n;
-            continue;
+    for (;;) {
+      if (loader.issued - used < C::kStages && loader.issue(p, geo, load, load_left, lane, ring_at, bars) &&
+          loader.issued - used < C::kStages)
+        continue;
+      if (tile >= hi) {
+        c = take;
+        const int row0 = c.rt * 8 * kR;
+        if (open) {
+          // ---- an item as a whole goes out, a part of one waits: the last segment's in the ring, an earlier one's in memory
+          const bool last = left <= 0, ended = hi == max(1, c.tiles), whole = lo == 0 && ended;
+          if (last) {
+            for (; used < loader.issued; ++used) {  // copies that a wait has given up are not left behind
+              int alone = 0;
+              mbar_wait_bounded(bars + 8 * (used & (C::kStages - 1)), used / C::kStages & 1, &alone, p.err, kDevTimeoutDrain);
+            }
+            __syncwarp();
           }
-          ++used;
-          if (loader.bad)  // rare: whether it is these tiles' pages
-            for (int i = tile; i < tile + n; ++i) poison |= kv_page(p.batch, p.cache, c.s, i * kKvTile, nullptr) < 0;
-          const int pos = tile * kKvTile;
-          const bool clear = pos + n * kKvTile - 1 <= rows.first_limit;
-          if (C::kPair == 2 && n == 2 && clear) {
-            rows.template take<C::kPair, false>(at, pos, lane);
-          } else if (C::kPair == 1 && clear) {
-#pragma unroll 1
-            for (int i = 0; i < n; ++i) rows.template take<1, false>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
-          } else {
-#pragma unroll 1
-            for (int i = 0; i < n; ++i) rows.template take<1, true>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
-          }
-          tile += n;
-          __syncwarp();
-          loader.issue(p, geo, load, load_left, lane, smem_u32(at), bar);
-        }
-      }
-
-      // ---- an item as a whole goes out, a part of one waits: the last segment's in the ring, an earlier one's in memory
-      const bool last = left == 0;
-      c = take;
-      if (last) {
-        for (; used < loader.issued; ++used) {  // copies that a wait has given up are not left behind
-          int alone = 0;
-          mbar_wait_bounded(bars + 8 * (used & (C::kStages - 1)), used / C::kStages & 1, &alone, p.err, kDevTimeoutDrain);
-        }
-        __syncwarp();
-      }
-      float* part_o = last ? reinterpret_cast<float*>(ring) : &warp_part<kDh, kR>(p, warp)->o[0][0];
-      float* part_mass = last ? sh.mass[warp] : warp_part<kDh, kR>(p, warp)->mass;
-      const int slots = min(8 * kR, geo.rows - row0);
+          float* part_o = last ? reinterpret_cast<float*>(ring) : &warp_part<kDh, kR>(p, warp)->o[0][0];
+          float* part_mass = last ? sh.mass[warp] : warp_part<kDh, kR>(p, warp)->mass;
+          const int slots = min(8 * kR, geo.rows - row0);
 #pragma unroll
-      for (int n = 0; n < kR; ++n)
+          for (int n = 0; n < kR; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int row = n * 8 + 2 * t + e;
-          float sum = 0.f, by = 0.f;
-          if (c.tiles > 0) {
-            sum = rows.l[n][e];
+            for (int e = 0; e < 2; ++e) {
+              const int row = n * 8 + 2 * t + e;
+              float sum = rows.l[n][e];
 #pragma unroll
-            for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
-          }
-          if (whole) {
-            if (row < slots) {
-              __nv_bfloat16* dst = out_row<kR>(p, geo, c.s, row0 + row, c.h, kDh);
-              if (row < live) {
-                rows.each(n, e, by, lane, [&](int d, const float4& v) {
-                  *reinterpret_cast<uint2*>(dst + d) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
-                });
-              } else {
-                // an empty slot, or positions that cannot be (NaN)
-                const uint32_t fill = !c.seq.ok && row0 + row < c.seq.n * geo.group ? 0x7fff7fffu : 0u;
-                for (int d = 4 * g; d < kDh; d += 32) *reinterpret_cast<uint2*>(dst + d) = make_uint2(fill, fill);
+              for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+              const float by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
+              if (whole) {
+                if (row < slots) {
+                  __nv_bfloat16* dst = out_row<kR>(p, geo, c.s, row0 + row, c.h, kDh);
+                  // an empty slot, or positions that cannot be (NaN)
+                  const uint32_t fill = !c.seq.ok && row0 + row < c.seq.n * geo.group ? 0x7fff7fffu : 0u;
+                  rows.each(n, e, by, lane, [&](int d, const float4& v) {
+                    *reinterpret_cast<uint2*>(dst + d) =
+                        row < live ? make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)) : make_uint2(fill, fill);
+                  });
+                }
+              } else if (row < live) {
+                rows.each(n, e, by, lane, [&](int d, const float4& v) { *reinterpret_cast<float4*>(part_o + row * kDh + d) = v; });
+                if (g == 0)
+                  part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kFar : rows.m[n][e] + log2f(sum);
               }
             }
-          } else if (row < live) {
-            rows.each(n, e, by, lane, [&](int d, const float4& v) { *reinterpret_cast<float4*>(part_o + row * kDh + d) = v; });
-            if (g == 0)
-              part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kFar : rows.m[n][e] + log2f(sum);
+          if (!whole) {
+            if (lo > 0) {
+              end.first = true;
+              end.first_rt = c.rt;
+              end.first_last = last;
+              end.first_ends = ended;
+            } else {
+              end.tail = true;
+              end.live = live;
+            }
           }
+          end.s = c.s;
+          end.rt = c.rt;
+          end.h = c.h;
+          if (last) break;
+          c.next_item(p, geo);
+          __syncwarp();
+          take = c;
+          __syncwarp();
         }
-      if (!whole) {
-        if (lo > 0) {
-          end.first = true;
-          end.first_rt = c.rt;
-          end.first_last = last;
-          end.first_ends = hi == units;
-        } else {
-          end.tail = true;
+        // ---- the next item
+        lo = tile = c.tile;
+        hi = min(max(1, c.tiles), lo + left);
+        left -= units_of_item(c.tiles) - lo;
+        live = c.tiles == 0 ? 0 : min(8 * kR, c.seq.n * geo.group - c.rt * 8 * kR);
+        open = true;
+        poison = false;
+        rows.begin(p, geo, c, live, lane, reinterpret_cast<uint2*>(smem + C::kRing) + warp * (C::kQ / kWarps / 8));
+        if (c.tiles == 0) {
+          tile = hi;
+          continue;
         }
       }
-      end.s = c.s;
-      end.rt = c.rt;
-      end.h = c.h;
-      if (!last) {
-        c.next_item(p, geo);
-        __syncwarp();
-        take = c;
-        __syncwarp();
+      const int stage = used & (C::kStages - 1), n = stage_tiles<C>(tile, hi), pos = tile * kKvTile;
+      const uint8_t* const at = ring + stage * C::kStageBytes;
+      tile += n;
+      if (!warp_wait_bounded(bars + 8 * stage, used / C::kStages & 1, &sh.abort, p.err, kDevTimeoutProducer)) {
+        poison = true;
+        continue;
       }
+      if (loader.bad)  // rare: whether it is these tiles' pages
+        for (int i = 0; i < n; ++i) poison |= kv_page(p.batch, p.cache, take.s, pos + i * kKvTile, nullptr) < 0;
+      const bool clear = pos + n * kKvTile - 1 <= rows.first_limit;
+      if (C::kPair == 2 && n == 2 && clear) {
+        rows.template take<C::kPair, false>(at, pos, lane);
+      } else if (C::kPair == 1 && clear) {
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) rows.template take<1, false>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) rows.template take<1, true>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+      }
+      __syncwarp();
+      ++used;
     }
   }
   if (lane == 0) sh.end[warp] = end;
@@ -988,22 +1000,17 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
     constexpr int kE = kDh / 32;
     // (rows past the last token hold nothing; what is made of them is not read)
     for (int row = (warp - turn) & (kWarps - 1); row < shown; row += kWarps) {
-      float mass = kFar;
-      if (lane < stop && lane >= max(start, 0))
-        mass = lane == start || (ringed >> lane & 1) != 0 ? sh.mass[lane][row] : warp_part<kDh, kR>(p, lane)->mass[row];
-      float in[kWarps][kE];
+      using Vec = typename C::Vec;
+      const bool there = lane < stop && lane >= max(start, 0), near = lane == start || (ringed >> (lane & 31) & 1) != 0;
+      const int w0 = there ? lane : 0;
+      const Parts* far_part = warp_part<kDh, kR>(p, w0);
+      const float* row_at = there && !near ? far_part->o[row]
+                                           : reinterpret_cast<const float*>(smem + w0 * (C::kStages * C::kStageBytes)) + row * kDh;
+      const float mass = !there ? kFar : near ? sh.mass[w0][row] : far_part->mass[row];
+      Vec in[kWarps];
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float* ring_part = reinterpret_cast<const float*>(smem + w * (C::kStages * C::kStageBytes)) + row * kDh + lane * kE;
-        const float* far_part = &warp_part<kDh, kR>(p, w)->o[row][lane * kE];
-        const bool there = w < stop && w >= max(start, 0), near = w == start || (ringed >> w & 1) != 0;
-#pragma unroll
-        for (int i = 0; i < kE; ++i) {
-          in[w][i] = 0.f;
-          if (there && near) in[w][i] = ring_part[i];
-          if (there && !near) in[w][i] = far_part[i];
-        }
-      }
+      for (int w = 0; w < kWarps; ++w)
+        in[w] = reinterpret_cast<const Vec*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row_at), w))[lane];
       float top = mass;
 #pragma unroll
       for (int off = 4; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -1018,16 +1025,15 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
         const float by = __shfl_sync(0xffffffffu, share, w);
+        if (by == 0.f) continue;
+        const float* x = reinterpret_cast<const float*>(&in[w]);
 #pragma unroll
-        for (int i = 0; i < kE; ++i) out[i] = by == 0.f ? out[i] : fmaf(in[w][i], by, out[i]);
+        for (int i = 0; i < kE; ++i) out[i] = fmaf(x[i], by, out[i]);
       }
       if (start >= 0 && done) {
-        const KvSeq seq = seq_of(p, item.s, nullptr);
-        const int q_row = rt * 8 * kR + row;
-        __nv_bfloat16* dst = out_row<kR>(p, geo, item.s, q_row, item.h, kDh) + lane * kE;
+        __nv_bfloat16* dst = out_row<kR>(p, geo, item.s, rt * 8 * kR + row, item.h, kDh) + lane * kE;
 #pragma unroll
-        for (int i = 0; i < kE; i += 2)
-          *reinterpret_cast<uint32_t*>(dst + i) = q_row < seq.n * geo.group ? pack_bf16x2(out[i], out[i + 1]) : 0u;
+        for (int i = 0; i < kE; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = row < item.live ? pack_bf16x2(out[i], out[i + 1]) : 0u;
       } else {
         Parts* to = cta_part<kDh, kR>(p, blockIdx.x, start < 0 ? 0 : 1);
 #pragma unroll
@@ -1039,11 +1045,12 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
     turn += shown;
   }
   if (threadIdx.x == 0) {
-    Desc d{0, 0, 0, -1, ends, {0, 0, 0}};
+    Desc d{0, 0, 0, -1, ends, 0, {0, 0}};
     if (tail_warp >= 0) {
       d.s = sh.end[tail_warp].s;
       d.rt = sh.end[tail_warp].rt;
       d.h = sh.end[tail_warp].h;
+      d.live = sh.end[tail_warp].live;
       d.slot = 1;
     }
     static_cast<Desc*>(p.ws)[blockIdx.x] = d;
@@ -1060,17 +1067,19 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   const Desc* desc = static_cast<const Desc*>(p.ws);
   const int b = blockIdx.x, row = blockIdx.y;
   const Desc mine = desc[b];
+  int more = b + 1 + lane < ctas && desc[b + 1 + lane].ends != 0;  // (read beside it)
   if (mine.slot < 0) return;
   const Geometry geo = geometry<kR>(p);
   const int q_row = mine.rt * 8 * kR + row;
   if (q_row >= geo.rows) return;
   int end = ctas;  // parts: this CTA's, then slot 0 of those up to the first that ends the item
   for (int at = b + 1; at < ctas; at += 32) {
-    const unsigned found = __ballot_sync(0xffffffffu, at + lane < ctas && desc[at + lane].ends != 0);
+    const unsigned found = __ballot_sync(0xffffffffu, more);
     if (found != 0) {
       end = at + __ffs(found);
       break;
     }
+    more = at + 32 + lane < ctas && desc[at + 32 + lane].ends != 0;
   }
   constexpr int kE = kDh / 32;
   float top = kFar, sum = 0.f, out[kE];
@@ -1102,9 +1111,8 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
       total += sh_sum[w] * by;
       acc += sh_o[w][threadIdx.x] * by;
     }
-    const KvSeq seq = seq_of(p, mine.s, nullptr);
     __nv_bfloat16* dst = out_row<kR>(p, geo, mine.s, q_row, mine.h, kDh);
-    dst[threadIdx.x] = __float2bfloat16_rn(q_row >= seq.n * geo.group ? 0.f : acc / total);
+    dst[threadIdx.x] = __float2bfloat16_rn(row >= mine.live ? 0.f : acc / total);
   }
 }
 
