@@ -34,7 +34,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
 constexpr int kMaxRowTiles = 4;   // of 8 query rows that share a pass
 constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
-constexpr int kItemUnits = 2;     // what an item costs beside its tiles, in tiles
+constexpr int kItemUnits = 3;     // what an item costs beside its tiles, in tiles
 constexpr float kFar = -1e30f;    // a maximum of nothing
 // Exponents relative to m (exact for scales of values up to 2^100: above that small probabilities are flushed). bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
 // 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108.
@@ -63,7 +63,7 @@ struct Config {
   using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
   static constexpr int kCtasPerSm = kInt4 && kR == 1 ? 2 : 1;
-  static constexpr bool kQShared = kR > 2;  // the queries' fragments: shared memory, else registers
+  static constexpr bool kQShared = kInt4 ? kR != 2 : kR > 2;  // the queries' fragments: shared memory, else registers
   static constexpr int kPair = kInt4 && kR <= 2 ? 2 : 1;  // tiles that are taken together
   static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that share a wait
   static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
@@ -223,21 +223,26 @@ struct Place {
   }
 };
 
-// The exclusive prefix of a value over the block's threads, and its sum.
+// The exclusive prefix of a value over the warp's or the block's threads, and its sum.
 struct Scan {
   long long before, total;
 };
-__device__ __forceinline__ Scan block_scan(long long v, long long* sh) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ Scan warp_scan(long long v) {
+  const int lane = threadIdx.x & 31;
   long long x = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const long long y = __shfl_up_sync(0xffffffffu, x, o);
     if (lane >= o) x += y;
   }
-  if (lane == 31) sh[warp] = x;
+  return Scan{x - v, __shfl_sync(0xffffffffu, x, 31)};
+}
+__device__ __forceinline__ Scan block_scan(long long v, long long* sh) {
+  const int warp = threadIdx.x >> 5;
+  const Scan own = warp_scan(v);
+  if ((threadIdx.x & 31) == 31) sh[warp] = own.total;
   __syncthreads();
-  Scan r{x - v, 0};
+  Scan r{own.before, 0};
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
     if (w < warp) r.before += sh[w];
@@ -262,14 +267,15 @@ struct Shared {
 };
 template <int kR>
 __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& c, int& active, Shared<kR>& sh) {
-  const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5;
+  const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* const err = blockIdx.x == 0 ? p.err : nullptr;
+  const bool few = S <= 32;  // each warp looks for itself, a lane a sequence
   long long mine = 0, total = 0;
   Scan scan{0, 0};
   for (int at = 0; at < S; at += kThreads) {
-    const int s = at + static_cast<int>(threadIdx.x);
+    const int s = few ? lane : at + static_cast<int>(threadIdx.x);
     mine = s < S ? units_of<kR>(g, seq_of(p, s, err)) * g.kv_heads : 0;
-    scan = block_scan(mine, sh.scan);
+    scan = few ? warp_scan(mine) : block_scan(mine, sh.scan);
     total += scan.total;
   }
   const long long want = (total + kMinUnits - 1) / kMinUnits;
@@ -290,6 +296,17 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
       scan = block_scan(mine, sh.scan);
     }
     const long long start = before + scan.before;
+    if (few) {
+      const long long first = from(first_warp + warp);
+      const unsigned found = __ballot_sync(0xffffffffu, first >= start && first < start + mine);
+      const int s = found == 0 ? 0 : __ffs(found) - 1;
+      const long long offset = first - __shfl_sync(0xffffffffu, start, s);
+      if (lane == 0) {
+        sh.s[warp] = s;
+        sh.offset[warp] = offset;
+      }
+      break;
+    }
     for (int w = 0; w < active; ++w) {
       const long long first = from(first_warp + w);
       if (first >= start && first < start + mine) {
@@ -299,7 +316,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     }
     before += scan.total;
   }
-  __syncthreads();
+  if (few) __syncwarp(); else __syncthreads();
   if (warp >= active || first_warp + warp >= warps) return 0;
   c.s = sh.s[warp];
   long long rest = sh.offset[warp];
@@ -1060,7 +1077,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
 // Items that several CTAs have parts of: the CTA that holds an item's first part adds up all of them, a row in y.
 template <int kDh, int kR>
 __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const PagedAttentionArgs p, int ctas) {
-  __shared__ float sh_o[kWarps][kDh], sh_top[kWarps], sh_sum[kWarps];
+  __shared__ float sh_o[kWarps][kDh], sh_sum[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_launch_dependents();
@@ -1081,35 +1098,37 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
     }
     more = at + 32 + lane < ctas && desc[at + 32 + lane].ends != 0;
   }
+  // a lane a part's mass; a warp adds up every eighth part, its loads independent of each other
+  using Vec = std::conditional_t<kDh == 128, float4, float2>;
   constexpr int kE = kDh / 32;
-  float top = kFar, sum = 0.f, out[kE];
+  const int n = end - b;
+  float mass = kFar, top, sum = 0.f, out[kE];
+  for (int i = lane; i < n; i += 32) mass = fmaxf(mass, cta_part<kDh, kR>(p, b + i, i == 0 ? mine.slot : 0)->mass[row]);
+  top = mass;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
 #pragma unroll
   for (int i = 0; i < kE; ++i) out[i] = 0.f;
-  for (int at = b + warp; at < end; at += kWarps) {
-    const Part<kDh, kR>& part = *cta_part<kDh, kR>(p, at, at == b ? mine.slot : 0);
-    const float mass = part.mass[row];
-    const float now = fmaxf(top, mass), by = ex2(top - now), weight = mass == kFar ? 0.f : ex2(mass - now);
-    top = now;
-    sum = sum * by + weight;
+#pragma unroll 4
+  for (int i = warp; i < n; i += kWarps) {
+    const Part<kDh, kR>* part = cta_part<kDh, kR>(p, b + i, i == 0 ? mine.slot : 0);
+    const Vec x = reinterpret_cast<const Vec*>(part->o[row])[lane];
+    const float m = part->mass[row], weight = m == kFar ? 0.f : ex2(m - top);
+    sum += weight;
 #pragma unroll
-    for (int i = 0; i < kE; ++i) out[i] = out[i] * by + (weight == 0.f ? 0.f : weight * part.o[row][lane * kE + i]);
+    for (int e = 0; e < kE; ++e)
+      if (weight != 0.f) out[e] = fmaf(reinterpret_cast<const float*>(&x)[e], weight, out[e]);
   }
 #pragma unroll
   for (int i = 0; i < kE; ++i) sh_o[warp][lane * kE + i] = out[i];
-  if (lane == 0) {
-    sh_top[warp] = top;
-    sh_sum[warp] = sum;
-  }
+  if (lane == 0) sh_sum[warp] = sum;
   __syncthreads();
   if (threadIdx.x < kDh) {
-    float all = kFar, total = 0.f, acc = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) all = fmaxf(all, sh_top[w]);
+    float total = 0.f, acc = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float by = ex2(sh_top[w] - all);
-      total += sh_sum[w] * by;
-      acc += sh_o[w][threadIdx.x] * by;
+      total += sh_sum[w];
+      acc += sh_o[w][threadIdx.x];
     }
     __nv_bfloat16* dst = out_row<kR>(p, geo, mine.s, q_row, mine.h, kDh);
     dst[threadIdx.x] = __float2bfloat16_rn(row >= mine.live ? 0.f : acc / total);
