@@ -17,8 +17,8 @@
 // maxima else. A bf16 cache takes the probability as two bf16.
 //
 // Bound by the cache's bytes. Work is cut evenly: the tiles of all (sequence, rows, head) items in a row, a contiguous part for
-// each warp, which copies its tiles into a ring of its own (cp.async.bulk) and needs no other warp on the way: it writes the
-// items that it has whole. What it has of an item that others share it leaves until the CTA's end, where the parts of the
+// each warp, which copies its tiles into a ring of its own (cp.async: a bulk copy and its barrier cost a warp some hundred
+// clocks a stage) and needs no other warp on the way: it writes the items that it has whole. What it has of an item that others share it leaves until the CTA's end, where the parts of the
 // CTA's warps are added up, and what CTAs share a second kernel adds up, both in the order of the parts.
 #include <algorithm>
 #include <climits>
@@ -34,6 +34,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
 constexpr int kMaxRowTiles = 4;   // of 8 query rows that share a pass
 constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
+constexpr int64_t kAlignedTokens = 1280;  // of a table, up to which a CTA takes an item alone where there are CTAs for all
 constexpr int kItemUnits = 3;     // what an item costs beside its tiles, in tiles
 constexpr float kFar = -1e30f;    // a maximum of nothing
 // Exponents relative to m (exact for scales of values up to 2^100: above that small probabilities are flushed). bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
@@ -63,17 +64,16 @@ struct Config {
   using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
   static constexpr int kCtasPerSm = kInt4 && kR == 1 ? 2 : 1;
-  static constexpr bool kQShared = kInt4 ? kR != 2 : kR > 2;  // the queries' fragments: shared memory, else registers
   static constexpr int kPair = kInt4 && kR <= 2 ? 2 : 1;  // tiles that are taken together
-  static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that share a wait
+  static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that are copied together
   static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
   // a warp's ring also takes its last part at the end
   static constexpr int kLeast = (8 * kR * kDh * 4 + kStageBytes - 1) / kStageBytes;
   static constexpr int kStages = kLeast > 2 || (!kInt4 && kDh == 64) ? 4 : 2;
   static_assert(kLeast <= kStages, "a part fits the ring");
   static constexpr int kRing = kWarps * kStages * kStageBytes;
-  static constexpr int kQ = kQShared ? kWarps * kR * kMTiles * 32 * 8 : 0;
-  static constexpr int kSmem = kRing + kQ + kWarps * kStages * 8;
+  static constexpr int kQ = kR * 8 * kDh * 2;  // a warp's queries, as rows and then as fragments
+  static constexpr int kSmem = kRing + kWarps * kQ;
 };
 
 // A warp's last part (in its ring) and the one before it that does not begin its item (in the workspace), by what becomes
@@ -252,8 +252,6 @@ __device__ __forceinline__ Scan block_scan(long long v, long long* sh) {
   return r;
 }
 
-// Where the warp's part of the units begins, and how many they are. As few warps as have kMinUnits each, over all CTAs;
-// `active` is how many of a CTA's warps these are.
 template <int kR>
 struct Shared {
   Place<kR> load[kWarps], take[kWarps];  // items that a warp copies and computes
@@ -263,12 +261,27 @@ struct Shared {
   int s[kWarps];
   WarpEnd end[kWarps];
   float mass[kWarps][8 * kMaxRowTiles];  // of the parts in the rings
-  int abort;
 };
+// Where the warp's part begins, and how many units it has; `active` is how many of a CTA's warps have one. Three ways:
+//  - aligned (the host knows that there are no more items than CTAs, and short ones): a CTA an item, which is joined there.
+//  - few items for many warps: each in equal parts of at most `chunk` tiles, so that a warp has one part of one item.
+//  - else the units in a row, a contiguous part for each warp.
 template <int kR>
-__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& c, int& active, Shared<kR>& sh) {
+__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, bool aligned, Place<kR>& c, int& active, Shared<kR>& sh) {
   const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* const err = blockIdx.x == 0 ? p.err : nullptr;
+  if (aligned) {
+    const int items_of_s = g.kv_heads * g.row_tiles;
+    c.s = static_cast<int>(blockIdx.x) / items_of_s;
+    const int i = static_cast<int>(blockIdx.x) - c.s * items_of_s;
+    c.rt = i / g.kv_heads;
+    c.h = i - c.rt * g.kv_heads;
+    c.seq = seq_of(p, c.s, i == 0 ? p.err : nullptr);
+    c.tiles = tiles_of<kR>(g, c.seq, c.rt);
+    active = min(kWarps, max(1, (c.tiles + kMinUnits - 1) / kMinUnits));
+    c.tile = c.tiles * warp / active;
+    return warp >= active ? 0 : max(1, c.tiles) * (warp + 1) / active - c.tile;
+  }
   const bool few = S <= 32;  // each warp looks for itself, a lane a sequence
   long long mine = 0, total = 0;
   Scan scan{0, 0};
@@ -278,16 +291,38 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     scan = few ? warp_scan(mine) : block_scan(mine, sh.scan);
     total += scan.total;
   }
-  const long long want = (total + kMinUnits - 1) / kMinUnits;
-  const int all = static_cast<int>(min(want, static_cast<long long>(gridDim.x * kWarps)));
+  const int most = gridDim.x * kWarps;
+  const long long items = static_cast<long long>(S) * g.row_tiles * g.kv_heads;
+  const bool cut = items <= most / 8 && S <= kThreads;  // (the chunk is an eighth longer than an even share at most)
+  auto ratio = [](long long x, int y) -> long long {  // (a division of 64 bits takes as long as a read of memory)
+    if (x < (1LL << 31)) return static_cast<unsigned>(x) / static_cast<unsigned>(y);
+    return x / y;
+  };
+  int chunk = 0;
+  if (cut) {
+    // parts: at most total / chunk + items
+    chunk = static_cast<int>(max(static_cast<long long>(kMinUnits), ratio(total, most - static_cast<int>(items)) + 1));
+    auto parts_of = [&](int s) {
+      const KvSeq seq = seq_of(p, s, nullptr);
+      int n = 0;
+      for (int rt = 0; rt < g.row_tiles; ++rt) n += (max(1, tiles_of<kR>(g, seq, rt)) + chunk - 1) / chunk;
+      return static_cast<long long>(n) * g.kv_heads;
+    };
+    total = 0;
+    for (int at = 0; at < S; at += kThreads) {
+      const int s = few ? lane : at + static_cast<int>(threadIdx.x);
+      mine = s < S ? parts_of(s) : 0;
+      scan = few ? warp_scan(mine) : block_scan(mine, sh.scan);
+      total += scan.total;
+    }
+  }
+  const int all = static_cast<int>(cut ? total : min((total + kMinUnits - 1) / kMinUnits, static_cast<long long>(most)));
   active = (all + gridDim.x - 1) / gridDim.x;
   const int warps = min(all, static_cast<int>(gridDim.x) * active), first_warp = blockIdx.x * active;
-  // (a division of 64 bits takes as long as a read of memory)
-  long long each;
-  if (total < (1LL << 31)) each = static_cast<unsigned>(total) / static_cast<unsigned>(warps); else each = total / warps;
+  const long long each = cut ? 1 : ratio(total, warps);
   const int over = static_cast<int>(total - each * warps);
   auto from = [&](int w) { return w >= warps ? total : each * w + min(w, over); };
-  // the sequence that a warp's first unit is in
+  // the sequence that a warp's first unit (part) is in
   long long before = 0;
   for (int at = 0; at < S; at += kThreads) {
     if (S > kThreads) {
@@ -321,16 +356,20 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   c.s = sh.s[warp];
   long long rest = sh.offset[warp];
   c.seq = seq_of(p, c.s, nullptr);
+  int each_item;
   for (c.rt = 0;; ++c.rt) {
     c.tiles = tiles_of<kR>(g, c.seq, c.rt);
-    const int each_item = units_of_item(c.tiles);
+    each_item = cut ? (max(1, c.tiles) + chunk - 1) / chunk : units_of_item(c.tiles);
     const long long units = static_cast<long long>(each_item) * g.kv_heads;
-    if (rest < units) {
-      c.h = rest < (1LL << 31) ? static_cast<unsigned>(rest) / static_cast<unsigned>(each_item) : static_cast<int>(rest / each_item);
-      c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * each_item);
-      break;
-    }
+    if (rest < units) break;
     rest -= units;
+  }
+  c.h = static_cast<int>(ratio(rest, each_item));
+  c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * each_item);
+  if (cut) {
+    const int part = c.tile, n = max(1, c.tiles);
+    c.tile = static_cast<int>(static_cast<long long>(n) * part / each_item);
+    return static_cast<int>(static_cast<long long>(n) * (part + 1) / each_item) - c.tile;
   }
   int left = static_cast<int>(from(first_warp + warp + 1) - from(first_warp + warp));
   if (c.tile >= max(1, c.tiles)) {  // behind an item's tiles
@@ -342,6 +381,18 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
 
 // ---------------------------------------------------------------- a warp's copies
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there = true) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(there ? 16 : 0)
+               : "memory");  // (zeros where there is nothing)
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// until at most kGroups of the warp's groups are on their way
+template <int kGroups>
+__device__ __forceinline__ void wait_copies() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(kGroups) : "memory");
+  __syncwarp();
+}
+
 // Tiles of a stage, the first at `tile`: two from an even one on, so that they lie in one page or in two neighbours of a
 // batch (below).
 template <typename C>
@@ -349,19 +400,20 @@ __device__ __forceinline__ int stage_tiles(int tile, int end) {
   return C::kStageTiles == 1 || (tile & 1) != 0 ? 1 : min(2, end - tile);
 }
 
-// What a warp copies next. Every lane holds where one of 32 neighbouring tiles lies (a batch; without the head's offset, as
-// the heads of a sequence lie in the same pages), and copies it when its turn comes.
+// What a warp copies next. Every lane holds where one of 32 neighbouring tiles lies (a batch).
 template <int kDh, bool kInt4, int kR>
 struct Loader {
   using C = Config<kDh, kInt4, kR>;
-  const uint8_t* mine;   // the lane's tile, for head 0
-  long long head;        // offset of the item's head
-  int s = 0, tile = 0, end = 0;  // sequence, next tile to copy, end of the warp's part of the item
-  int issued = 0;        // stages
-  bool bad = false;      // a page was none of the cache's
+  const uint8_t* mine = nullptr;  // the lane's tile
+  long long head = 0;             // offset of the item's head
+  int s = -1, tile = 0, end = 0;  // sequence, next tile to copy, end of the warp's part of the item
+  int base = -1;                  // of the batch
+  int issued = 0;                 // stages
+  bool bad = false;               // a page was none of the cache's
 
   __device__ __forceinline__ void batch(const PagedAttentionArgs& p, int lane) {
-    const int at = (tile & ~31) + lane;
+    base = tile & ~31;
+    const int at = base + lane;
     int page = 0;
     if (at < end) page = p.batch.table[static_cast<long long>(s) * p.batch.ld_table + ((at * kKvTile) >> p.cache.page_bits)];
     const bool ok = page >= 0 && page < p.cache.n_pages;
@@ -369,25 +421,26 @@ struct Loader {
       bad = true;
       if (lane == 0) record_error(p.err, kDevBadPage);
     }
-    mine = kv_tile<typename C::Tile>(p.cache, ok ? page : 0, 0, at * kKvTile);
+    mine = kv_tile<typename C::Tile>(p.cache, ok ? page : 0, 0, at * kKvTile) + head;
   }
   // The item that `at` says, `left` units from its tile on; those without tiles are passed over. `at` goes on to the next.
   // (The lanes read the shared copies, compute the same, and write them again.)
-  __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane, bool same) {
+  __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left) {
     Place<kR> now = at;
     int n = left;
     while (n > 0 && now.tiles == 0) {
       n -= units_of_item(0);
       if (n > 0) now.next_item(p, g);
-      same = false;
     }
-    tile = now.tile;
-    end = min(now.tiles, tile + n);
-    s = now.s;
     if (n > 0) {
-      head = static_cast<long long>(now.h) * ((1 << (p.cache.page_bits - 4)) * C::Tile::kBytes);
-      // (the same sequence's next head, in the batch that is there)
-      if (!same || now.h == 0 || now.tiles > 32) batch(p, lane);
+      // a sequence's next head of up to 32 tiles lies in the batch that is there, the same way on
+      const long long to = static_cast<long long>(now.h) * ((1 << (p.cache.page_bits - 4)) * C::Tile::kBytes);
+      if (now.s != s || now.h == 0 || now.tiles > 32) base = -1;
+      mine += to - head;
+      head = to;
+      s = now.s;
+      tile = now.tile;
+      end = min(now.tiles, tile + n);
       n -= units_of_item(now.tiles) - tile;
       if (n > 0) now.next_item(p, g);
     }
@@ -396,27 +449,37 @@ struct Loader {
     left = n;
     __syncwarp();
   }
-  // The next stage, one wait's tiles; false where there are none.
-  __device__ __forceinline__ bool issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
-                                        uint32_t ring, uint32_t bars) {
-    if (tile >= end) {
-      if (left <= 0) return false;
-      item(p, g, at, left, lane, issued > 0);
-      if (tile >= end) return false;
+  // The next stage: a group of copies, empty where nothing is left.
+  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
+                                        uint32_t ring) {
+    if (tile >= end && left > 0) item(p, g, at, left);
+    int n = 0;
+    if (tile < end) {
+      if ((tile & ~31) != base) batch(p, lane);
+      n = stage_tiles<C>(tile, end);
     }
-    const int stage = issued & (C::kStages - 1);
-    const uint32_t dst = ring + stage * C::kStageBytes, bar = bars + 8 * stage;
-    const int n = stage_tiles<C>(tile, end), which = lane - (tile & 31);
-    if (which == 0) mbar_arrive_expect_tx(bar, n * C::Tile::kBytes);
-    if (which >= 0 && which < n)
-      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                       dst + which * C::Tile::kBytes),
-                   "l"(reinterpret_cast<uint64_t>(mine + head)), "n"(C::Tile::kBytes), "r"(bar)
-                   : "memory");
-    ++issued;
+    fill(p, n, lane, ring);
+  }
+  // n tiles of the batch into the next stage
+  __device__ __forceinline__ void fill(const PagedAttentionArgs& p, int n, int lane, uint32_t ring) {
+    const uint32_t dst = ring + (issued & (C::kStages - 1)) * C::kStageBytes + lane * 16;
+    const uint8_t* src = from_lane(tile & 31) + lane * 16;
+    if (n > 0) copy(dst, src, lane);
+    if (C::kStageTiles == 2 && n == 2)
+      copy(dst + C::Tile::kBytes, p.cache.page_bits == 4 ? from_lane((tile + 1) & 31) + lane * 16 : src + C::Tile::kBytes, lane);
     tile += n;
-    if ((tile & 31) == 0 && tile < end) batch(p, lane);
-    return true;
+    ++issued;
+    commit_copies();
+  }
+  __device__ __forceinline__ const uint8_t* from_lane(int from) const {
+    return reinterpret_cast<const uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(mine), from));
+  }
+  // A tile; dst and src are the lane's first 16 bytes of it.
+  __device__ __forceinline__ static void copy(uint32_t dst, const uint8_t* src, int lane) {
+    constexpr int kWhole = C::Tile::kBytes / 512, kRest = C::Tile::kBytes % 512 / 16;
+#pragma unroll
+    for (int i = 0; i < kWhole; ++i) copy16(dst + i * 512, src + i * 512);
+    if (kRest != 0 && lane < kRest) copy16(dst + kWhole * 512, src + kWhole * 512);
   }
 };
 
@@ -430,40 +493,44 @@ struct Rows {
   int limit[kR][2];             // last position that rows 2t and 2t + 1 of each eight see
   int first_limit, last_limit;  // the least and the largest of the rows'
   // fragments of 16 channels; in 4 bits fp16, of which the second word is a sixteenth
-  uint2 q[C::kQShared ? 1 : kR][C::kQShared ? 1 : kDh / 16];
-  const uint2* q_shared;
+  const uint2* q;
   float o[C::kMTiles][kR][4], m[kR][2], l[kR][2];
   uint32_t plus1024, minus1024;  // kFp16Of1024, kFp16OfMinus1024 in registers
 
-  __device__ __forceinline__ uint2 query(int n, int step, int lane) const {
-    if constexpr (C::kQShared) return q_shared[(n * C::kMTiles + step) * 32 + lane];
-    else return q[n][step];
+  __device__ __forceinline__ uint2 query(int n, int step, int lane) const { return q[(n * C::kMTiles + step) * 32 + lane]; }
+
+  __device__ __forceinline__ static int live_rows(const Geometry& geo, const Place<kR>& c) {
+    return c.tiles == 0 ? 0 : min(8 * kR, c.seq.n * geo.group - c.rt * 8 * kR);
+  }
+  // The queries' rows to where their fragments will be, zeros for rows without a token.
+  __device__ __forceinline__ static void fetch(const PagedAttentionArgs& p, const Geometry& geo, const Place<kR>& c, int lane, uint32_t to) {
+    constexpr int kPieces = kDh / 8, kRowsAtOnce = 32 / kPieces;  // of 16 bytes a row
+    const int live = live_rows(geo, c);
+#pragma unroll
+    for (int i = 0; i < 8 * kR / kRowsAtOnce; ++i) {
+      const int r = i * kRowsAtOnce + lane / kPieces, row = c.rt * 8 * kR + r, tok = geo.group == geo.rows ? 0 : row / geo.group;
+      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q);
+      if (r < live)
+        src += (static_cast<long long>(c.s) * p.batch.L + tok) * p.ld_q + (c.h * geo.group + row - tok * geo.group) * kDh + lane % kPieces * 8;
+      copy16(to + (i * 32 + lane) * 16, src, r < live);
+    }
   }
 
   // The queries' fragments; in 4 bits each row times a power of two that makes its largest 2^7 to 2^8 (fp16 holds all bits
   // of a bf16 down to 2^-21 of that; a row with an infinity or NaN is NaN).
   __device__ __forceinline__ void begin(const PagedAttentionArgs& p, const Geometry& geo, const Place<kR>& c, int live, int lane,
-                                        uint2* to_shared) {
+                                        uint2* shared) {
     const int g = lane >> 2, t = lane & 3;
-    q_shared = to_shared;
+    q = shared;
 #pragma unroll
     for (int n = 0; n < kR; ++n) {
-      const int r = n * 8 + g, row = c.rt * 8 * kR + r;
       uint4 raw[kDh / 32];
 #pragma unroll
-      for (int i = 0; i < kDh / 32; ++i) raw[i] = make_uint4(0, 0, 0, 0);
-      if (r < live) {
-        const int tok = row / geo.group;
-        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q) +
-                                   (static_cast<long long>(c.s) * p.batch.L + tok) * p.ld_q +
-                                   (c.h * geo.group + row - tok * geo.group) * kDh;
-#pragma unroll
-        for (int i = 0; i < kDh / 32; ++i)
-          raw[i] = *reinterpret_cast<const uint4*>(src + (kInt4 ? 64 * (i >> 1) + 16 * t + 8 * (i & 1) : 32 * i + 8 * t));
-      }
-      auto put = [&](int step, uint2 f) {
-        if constexpr (C::kQShared) to_shared[(n * C::kMTiles + step) * 32 + lane] = f; else q[n][step] = f;
-      };
+      for (int i = 0; i < kDh / 32; ++i)
+        raw[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(shared) + (n * 8 + g) * kDh +
+                                                 (kInt4 ? 64 * (i >> 1) + 16 * t + 8 * (i & 1) : 32 * i + 8 * t));
+      __syncwarp();  // (these eight rows' fragments take these eight rows' place)
+      auto put = [&](int step, uint2 f) { shared[(n * C::kMTiles + step) * 32 + lane] = f; };
       float by_row = p.scale * 1.4426950408889634f;
       if constexpr (kInt4) {
         float x[kDh / 32][8], top = 0.f;
@@ -499,7 +566,8 @@ struct Rows {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         factor[n][e] = __shfl_sync(0xffffffffu, by_row, (2 * t + e) * 4);
-        limit[n][e] = c.seq.cached + min((c.rt * 8 * kR + n * 8 + 2 * t + e) / geo.group, c.seq.n - 1);
+        limit[n][e] = c.seq.cached +
+                      (geo.group == geo.rows ? 0 : min((c.rt * 8 * kR + n * 8 + 2 * t + e) / geo.group, c.seq.n - 1));
         m[n][e] = kFar;
         l[n][e] = 0.f;
       }
@@ -510,7 +578,7 @@ struct Rows {
     }
     first_limit = c.seq.cached + c.rt * 8 * kR / geo.group;
     last_limit = c.seq.cached + (min(8 * kR, live) + c.rt * 8 * kR - 1) / geo.group;
-    if constexpr (C::kQShared) __syncwarp();
+    __syncwarp();
   }
 
   // kN neighbouring tiles, the first at position `pos`; kMasked: some of their tokens may lie behind what some rows see.
@@ -853,7 +921,7 @@ __device__ __forceinline__ __nv_bfloat16* out_row(const PagedAttentionArgs& p, c
 
 template <int kDh, bool kInt4, int kR>
 __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
-    paged_attention_kernel(const PagedAttentionArgs p) {
+    paged_attention_kernel(const PagedAttentionArgs p, bool aligned) {
   using C = Config<kDh, kInt4, kR>;
   using Tile = typename C::Tile;
   using Parts = Part<kDh, kR>;
@@ -861,23 +929,21 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
   __shared__ Shared<kR> sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t* const ring = smem + warp * (C::kStages * C::kStageBytes);
-  const uint32_t bars = smem_u32(smem + C::kRing + C::kQ) + warp * C::kStages * 8;
-  if (lane == 0)
-    for (int i = 0; i < C::kStages; ++i) mbar_init(bars + 8 * i, 1);
-  if (threadIdx.x == 0) sh.abort = 0;
-  fence_mbar_init();
   pdl_wait();
   pdl_launch_dependents();
   const Geometry geo = geometry<kR>(p);
   Place<kR> c;
   int active;
-  int left = begin(p, geo, c, active, sh);  // (synchronises the block)
+  int left = begin(p, geo, aligned, c, active, sh);
   WarpEnd end{0, 0, 0, 0, false, false, false, false, 0};
   if (left > 0) {
     Place<kR>& load = sh.load[warp];
     Place<kR>& take = sh.take[warp];
     int& load_left = sh.load_left[warp];
     const uint32_t ring_at = smem_u32(ring);
+    uint2* const queries = reinterpret_cast<uint2*>(smem + C::kRing + warp * C::kQ);
+    using R = Rows<kDh, kInt4, kR>;
+    R::fetch(p, geo, c, lane, smem_u32(queries));
     Loader<kDh, kInt4, kR> loader;
     load = c;
     take = c;
@@ -890,23 +956,25 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
     int lo = 0, tile = 0, hi = 0, live = 0;  // the warp's part of the present item, the next tile; rows with a token
     bool open = false, poison = false;
     // (one place each where a stage is filled, an item begun and ended: what runs rarely runs from a cold instruction cache)
+    int fast = 0;  // stages that need no second look, neither when taken nor (copying) when filled again
+    bool copying = false;
 #pragma unroll 1
     for (;;) {
-      if (loader.issued - used < C::kStages && loader.issue(p, geo, load, load_left, lane, ring_at, bars) &&
-          loader.issued - used < C::kStages)
-        continue;
+      if (fast == 0) {
+      if (loader.issued - used < C::kStages) {
+        loader.issue(p, geo, load, load_left, lane, ring_at);
+        if (loader.issued - used < C::kStages) continue;
+      }
       if (tile >= hi) {
         c = take;
         const int row0 = c.rt * 8 * kR;
         if (open) {
           // ---- an item as a whole goes out, a part of one waits: the last segment's in the ring, an earlier one's in memory
           const bool last = left <= 0, ended = hi == max(1, c.tiles), whole = lo == 0 && ended;
-          if (last) {
-            for (; used < loader.issued; ++used) {  // copies that a wait has given up are not left behind
-              int alone = 0;
-              mbar_wait_bounded(bars + 8 * (used & (C::kStages - 1)), used / C::kStages & 1, &alone, p.err, kDevTimeoutDrain);
-            }
-            __syncwarp();
+          Place<kR> next = c;
+          if (!last) {  // the next item's queries come while this one is finished
+            next.next_item(p, geo);
+            R::fetch(p, geo, next, lane, smem_u32(queries));
           }
           float* part_o = last ? reinterpret_cast<float*>(ring) : &warp_part<kDh, kR>(p, warp)->o[0][0];
           float* part_mass = last ? sh.mass[warp] : warp_part<kDh, kR>(p, warp)->mass;
@@ -951,7 +1019,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
           end.rt = c.rt;
           end.h = c.h;
           if (last) break;
-          c.next_item(p, geo);
+          c = next;
           __syncwarp();
           take = c;
           __syncwarp();
@@ -960,36 +1028,50 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
         lo = tile = c.tile;
         hi = min(max(1, c.tiles), lo + left);
         left -= units_of_item(c.tiles) - lo;
-        live = c.tiles == 0 ? 0 : min(8 * kR, c.seq.n * geo.group - c.rt * 8 * kR);
+        live = R::live_rows(geo, c);
         open = true;
         poison = false;
-        rows.begin(p, geo, c, live, lane, reinterpret_cast<uint2*>(smem + C::kRing) + warp * (C::kQ / kWarps / 8));
+        commit_copies();
+        wait_copies<0>();
+        rows.begin(p, geo, c, live, lane, queries);
         if (c.tiles == 0) {
           tile = hi;
           continue;
         }
       }
-      const int stage = used & (C::kStages - 1), n = stage_tiles<C>(tile, hi), pos = tile * kKvTile;
-      const uint8_t* const at = ring + stage * C::kStageBytes;
-      tile += n;
-      if (!warp_wait_bounded(bars + 8 * stage, used / C::kStages & 1, &sh.abort, p.err, kDevTimeoutProducer)) {
-        poison = true;
-        continue;
-      }
-      if (loader.bad)  // rare: whether it is these tiles' pages
-        for (int i = 0; i < n; ++i) poison |= kv_page(p.batch, p.cache, take.s, pos + i * kKvTile, nullptr) < 0;
-      const bool clear = pos + n * kKvTile - 1 <= rows.first_limit;
-      if (C::kPair == 2 && n == 2 && clear) {
-        rows.template take<C::kPair, false>(at, pos, lane);
-      } else if (C::kPair == 1 && clear) {
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) rows.template take<1, false>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+      constexpr int kT = C::kStageTiles;
+      const int clear = min(hi, (rows.first_limit + 1) / kKvTile) - tile;
+      if (!loader.bad && (tile & (kT - 1)) == 0 && clear >= kT) {
+        const int same = min(loader.end, (loader.tile | 31) + 1) - loader.tile;
+        copying = (loader.tile & (kT - 1)) == 0 && (loader.tile & ~31) == loader.base && same >= kT;
+        fast = copying ? min(clear, same) / kT : 1;
       } else {
+        const int n = stage_tiles<C>(tile, hi), pos = tile * kKvTile;
+        const uint8_t* const at = ring + (used & (C::kStages - 1)) * C::kStageBytes;
+        wait_copies<C::kStages - 1>();
+        if (loader.bad)  // rare: whether it is these tiles' pages
+          for (int i = 0; i < n; ++i) poison |= kv_page(p.batch, p.cache, take.s, pos + i * kKvTile, nullptr) < 0;
 #pragma unroll 1
         for (int i = 0; i < n; ++i) rows.template take<1, true>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
+        __syncwarp();
+        ++used;
+        tile += n;
+        continue;
+      }
+      }
+      --fast;
+      const uint8_t* const at = ring + (used & (C::kStages - 1)) * C::kStageBytes;
+      wait_copies<C::kStages - 1>();
+      if constexpr (C::kPair == C::kStageTiles) {
+        rows.template take<C::kPair, false>(at, tile * kKvTile, lane);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < C::kStageTiles; ++i) rows.template take<1, false>(at + i * Tile::kBytes, (tile + i) * kKvTile, lane);
       }
       __syncwarp();
       ++used;
+      tile += C::kStageTiles;
+      if (copying) loader.fill(p, C::kStageTiles, lane, ring_at);
     }
   }
   if (lane == 0) sh.end[warp] = end;
@@ -1143,8 +1225,15 @@ int launch(const PagedAttentionArgs& a, cudaStream_t st) {
       cudaSuccess)
     return -3;
   const int ctas = std::min(kMaxCtas, std::max(1, sm_count()) * C::kCtasPerSm);
-  if (launch_pdl(paged_attention_kernel<kDh, kInt4, kR>, dim3(ctas), dim3(kThreads), C::kSmem, st, a) != cudaSuccess) return -3;
   const int64_t rows = a.n_heads / a.cache.kv_heads * a.batch.L;
+  const int64_t items = a.batch.S * a.cache.kv_heads * ((rows + 8 * kR - 1) / (8 * kR));
+  const bool aligned = items <= ctas && (a.batch.max_pages << a.cache.page_bits) <= kAlignedTokens;
+  if (aligned)
+    return launch_pdl(paged_attention_kernel<kDh, kInt4, kR>, dim3(static_cast<unsigned>(items)), dim3(kThreads), C::kSmem, st, a, true) ==
+                   cudaSuccess
+               ? 0
+               : -3;
+  if (launch_pdl(paged_attention_kernel<kDh, kInt4, kR>, dim3(ctas), dim3(kThreads), C::kSmem, st, a, false) != cudaSuccess) return -3;
   const dim3 grid(ctas, static_cast<unsigned>(std::min<int64_t>(rows, 8 * kR)));
   return launch_pdl(paged_attention_join_kernel<kDh, kR>, grid, dim3(kThreads), 0, st, a, ctas) == cudaSuccess ? 0 : -3;
 }
