@@ -728,7 +728,7 @@ static bool paged_heads_ok(int64_t S, int64_t L, int64_t n_heads, int64_t n_kv_h
 
 size_t hydra_paged_attention_workspace_size(int64_t S, int64_t L, int64_t n_heads, int64_t n_kv_heads, int64_t head_dim) {
   return paged_heads_ok(S, L, n_heads, n_kv_heads, head_dim)
-             ? hydra::paged_attention_workspace_bytes(S, L, n_heads, n_kv_heads, head_dim)
+             ? hydra::paged_attention_workspace_bytes(head_dim)
              : 0;
 }
 

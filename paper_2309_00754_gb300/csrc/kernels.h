@@ -250,7 +250,7 @@ struct PagedAttentionArgs {
   void* ws;
   int* err;
 };
-size_t paged_attention_workspace_bytes(int64_t S, int64_t L, int64_t n_heads, int64_t kv_heads, int64_t head_dim);
+size_t paged_attention_workspace_bytes(int64_t head_dim);
 int launch_paged_attention(const PagedAttentionArgs& a, cudaStream_t stream);
 // Verification of drafted tokens (verify_drafts.cu).
 struct VerifyArgs {

@@ -16,10 +16,13 @@
 // times scale, and moved only when a row's passes the range, which a vote finds: the pass would spend its time on
 // maxima else. A bf16 cache takes the probability as two bf16.
 //
-// Bound by the cache's bytes. Work is cut evenly: the tiles of all (sequence, rows, head) items in a row, a contiguous part for
-// each warp, which copies its tiles into a ring of its own (cp.async: a bulk copy and its barrier cost a warp some hundred
-// clocks a stage) and needs no other warp on the way: it writes the items that it has whole. What it has of an item that others share it leaves until the CTA's end, where the parts of the
-// CTA's warps are added up, and what CTAs share a second kernel adds up, both in the order of the parts.
+// Bound by the cache's bytes. Work is cut evenly: the tiles of all (sequence, eight rows, head) items in a row, a
+// contiguous part for each warp, which copies its tiles into a ring of its own (cp.async: a bulk copy and its barrier cost a
+// warp some hundred clocks a stage) and needs no other warp on the way: it writes the items that it has whole. What it has of an
+// item that others share it leaves until the CTA's end, where the parts of the CTA's warps are added up, and what CTAs
+// share a second kernel adds up, both in the order of the parts. (Sixteen to 32 rows an item, which unpack a tile once for
+// all of them, want registers: with half or a quarter of the warps they took 43 and 46 us for 16 sequences x 20 rows over
+// 4096 tokens, eight rows 36.)
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -32,13 +35,14 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
-constexpr int kMaxRowTiles = 4;   // of 8 query rows that share a pass
+constexpr int kRows = 8;          // query rows of an item: the columns of a product
 constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
 constexpr int64_t kAlignedTokens = 1280;  // of a table, up to which a CTA takes an item alone where there are CTAs for all
-constexpr int kItemUnits = 3;     // what an item costs beside its tiles, in tiles
+constexpr int kItemUnits = 6;     // what an item costs beside its tiles, in tiles
 constexpr float kFar = -1e30f;    // a maximum of nothing
-// Exponents relative to m (exact for scales of values up to 2^100: above that small probabilities are flushed). bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to
-// 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108.
+// Exponents relative to m. bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to 2^14
+// (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108. (For
+// values' scales above 2^100 probabilities far below the largest are flushed.)
 constexpr float kSlack = 8.f, kTop = 6.f, kMost = 14.f, kAlone = 100.f;
 
 // What a CTA leaves for the second kernel.
@@ -51,28 +55,28 @@ struct Desc {
 };
 
 // Part of an item's rows, normalised, with log2 of the sum of exp2(s) that it stands for (NaN: unusable).
-template <int kDh, int kR>
+template <int kDh>
 struct Part {
-  float o[8 * kR][kDh];
-  float mass[8 * kR];
+  float o[kRows][kDh];
+  float mass[kRows];
 };
 
-template <int kDh, bool kInt4, int kR>
+template <int kDh, bool kInt4>
 struct Config {
   using Tile = KvTile<kDh, kInt4>;
-  using Parts = Part<kDh, kR>;
+  using Parts = Part<kDh>;
   using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
-  static constexpr int kCtasPerSm = kInt4 && kR == 1 ? 2 : 1;
-  static constexpr int kPair = kInt4 && kR <= 2 ? 2 : 1;  // tiles that are taken together
+  static constexpr int kCtasPerSm = kInt4 ? 2 : 1;
+  static constexpr int kPair = kInt4 ? 2 : 1;  // tiles that are taken together
   static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that are copied together
   static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
   // a warp's ring also takes its last part at the end
-  static constexpr int kLeast = (8 * kR * kDh * 4 + kStageBytes - 1) / kStageBytes;
+  static constexpr int kLeast = (kRows * kDh * 4 + kStageBytes - 1) / kStageBytes;
   static constexpr int kStages = kLeast > 2 || (!kInt4 && kDh == 64) ? 4 : 2;
   static_assert(kLeast <= kStages, "a part fits the ring");
   static constexpr int kRing = kWarps * kStages * kStageBytes;
-  static constexpr int kQ = kR * 8 * kDh * 2;  // a warp's queries, as rows and then as fragments
+  static constexpr int kQ = kRows * kDh * 2;  // a warp's queries, as rows and then as fragments
   static constexpr int kSmem = kRing + kWarps * kQ;
 };
 
@@ -165,39 +169,41 @@ __device__ __forceinline__ uint32_t low_nibbles(uint32_t w, uint32_t minus, uint
 __device__ __forceinline__ uint32_t high_nibbles(uint32_t w, uint32_t minus, uint32_t of) { return add_f16(merged<0x00f000f0u>(w, of), minus); }
 // -(1024 + zero), -(1024 + 16 zero) from two zero points as the cache holds them; `of`: kFp16OfMinus1024
 __device__ __forceinline__ uint32_t minus_low(uint32_t z, uint32_t of) { return merged<0x000f000fu>(z, of); }
-__device__ __forceinline__ uint32_t minus_high(uint32_t z, uint32_t of) { return merged<0x00f000f0u>(z, of); }
+// (the second from the first, exactly, as a multiplication and addition: logic has half the rate, and is what a tile waits for)
+__device__ __forceinline__ uint32_t minus_high(uint32_t low) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(low), "r"(0x4c004c00u), "r"(0x73807380u));  // 16 low + 15360
+  return r;
+}
 
 // ---------------------------------------------------------------- what is whose
 
 struct Geometry {
   int group, rows, row_tiles, kv_heads;  // query heads of a kv head; rows of a kv head; passes over its rows
 };
-template <int kR>
 __device__ __forceinline__ Geometry geometry(const PagedAttentionArgs& p) {
   Geometry g;
   g.kv_heads = p.cache.kv_heads;
   g.group = static_cast<int>(p.n_heads) / g.kv_heads;
   g.rows = g.group * static_cast<int>(p.batch.L);
-  g.row_tiles = (g.rows + 8 * kR - 1) / (8 * kR);
+  g.row_tiles = (g.rows + kRows - 1) / kRows;
   return g;
 }
 
-// Tiles of cached tokens that rows [8 kR rt, ...) of a sequence see; 0 where there is nothing to compute.
-template <int kR>
+// Tiles of cached tokens that rows [8 rt, ...) of a sequence see; 0 where there is nothing to compute.
 __device__ __forceinline__ int tiles_of(const Geometry& g, const KvSeq& seq, int rt) {
   if (!seq.ok || seq.n == 0) return 0;
   if (g.row_tiles == 1) return (seq.cached + seq.n - 1) / kKvTile + 1;
-  const int live = g.group * seq.n, first = rt * 8 * kR;
+  const int live = g.group * seq.n, first = rt * kRows;
   if (first >= live) return 0;
-  const int last = (min(first + 8 * kR, live) - 1) / g.group;
+  const int last = (min(first + kRows, live) - 1) / g.group;
   return (seq.cached + last) / kKvTile + 1;
 }
 // Units of an item: its tiles, at least one (an item without tiles has rows to fill), and behind them what it costs besides.
 __device__ __forceinline__ int units_of_item(int tiles) { return max(1, tiles) + kItemUnits; }
-template <int kR>
 __device__ __forceinline__ long long units_of(const Geometry& g, const KvSeq& seq) {
   long long n = 0;
-  for (int rt = 0; rt < g.row_tiles; ++rt) n += units_of_item(tiles_of<kR>(g, seq, rt));
+  for (int rt = 0; rt < g.row_tiles; ++rt) n += units_of_item(tiles_of(g, seq, rt));
   return n;
 }
 
@@ -206,7 +212,6 @@ __device__ __forceinline__ KvSeq seq_of(const PagedAttentionArgs& p, int s, int*
 }
 
 // A place in the units: an item, and a tile of it.
-template <int kR>
 struct Place {
   KvSeq seq;
   int s, rt, h, tile, tiles;
@@ -219,7 +224,7 @@ struct Place {
       ++s;
       seq = seq_of(p, s, nullptr);
     }
-    tiles = tiles_of<kR>(g, seq, rt);
+    tiles = tiles_of(g, seq, rt);
   }
 };
 
@@ -252,22 +257,20 @@ __device__ __forceinline__ Scan block_scan(long long v, long long* sh) {
   return r;
 }
 
-template <int kR>
 struct Shared {
-  Place<kR> load[kWarps], take[kWarps];  // items that a warp copies and computes
+  Place load[kWarps], take[kWarps];  // items that a warp copies and computes
   int load_left[kWarps];
   long long scan[kWarps];
   long long offset[kWarps];
   int s[kWarps];
   WarpEnd end[kWarps];
-  float mass[kWarps][8 * kMaxRowTiles];  // of the parts in the rings
+  float mass[kWarps][kRows];  // of the parts in the rings
 };
 // Where the warp's part begins, and how many units it has; `active` is how many of a CTA's warps have one. Three ways:
 //  - aligned (the host knows that there are no more items than CTAs, and short ones): a CTA an item, which is joined there.
 //  - few items for many warps: each in equal parts of at most `chunk` tiles, so that a warp has one part of one item.
 //  - else the units in a row, a contiguous part for each warp.
-template <int kR>
-__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, bool aligned, Place<kR>& c, int& active, Shared<kR>& sh) {
+__device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, bool aligned, Place& c, int& active, Shared& sh) {
   const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* const err = blockIdx.x == 0 ? p.err : nullptr;
   if (aligned) {
@@ -277,7 +280,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     c.rt = i / g.kv_heads;
     c.h = i - c.rt * g.kv_heads;
     c.seq = seq_of(p, c.s, i == 0 ? p.err : nullptr);
-    c.tiles = tiles_of<kR>(g, c.seq, c.rt);
+    c.tiles = tiles_of(g, c.seq, c.rt);
     active = min(kWarps, max(1, (c.tiles + kMinUnits - 1) / kMinUnits));
     c.tile = c.tiles * warp / active;
     return warp >= active ? 0 : max(1, c.tiles) * (warp + 1) / active - c.tile;
@@ -287,7 +290,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   Scan scan{0, 0};
   for (int at = 0; at < S; at += kThreads) {
     const int s = few ? lane : at + static_cast<int>(threadIdx.x);
-    mine = s < S ? units_of<kR>(g, seq_of(p, s, err)) * g.kv_heads : 0;
+    mine = s < S ? units_of(g, seq_of(p, s, err)) * g.kv_heads : 0;
     scan = few ? warp_scan(mine) : block_scan(mine, sh.scan);
     total += scan.total;
   }
@@ -305,7 +308,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     auto parts_of = [&](int s) {
       const KvSeq seq = seq_of(p, s, nullptr);
       int n = 0;
-      for (int rt = 0; rt < g.row_tiles; ++rt) n += (max(1, tiles_of<kR>(g, seq, rt)) + chunk - 1) / chunk;
+      for (int rt = 0; rt < g.row_tiles; ++rt) n += (max(1, tiles_of(g, seq, rt)) + chunk - 1) / chunk;
       return static_cast<long long>(n) * g.kv_heads;
     };
     total = 0;
@@ -327,7 +330,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   for (int at = 0; at < S; at += kThreads) {
     if (S > kThreads) {
       const int s = at + static_cast<int>(threadIdx.x);
-      mine = s < S ? units_of<kR>(g, seq_of(p, s, nullptr)) * g.kv_heads : 0;
+      mine = s < S ? units_of(g, seq_of(p, s, nullptr)) * g.kv_heads : 0;
       scan = block_scan(mine, sh.scan);
     }
     const long long start = before + scan.before;
@@ -358,7 +361,7 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   c.seq = seq_of(p, c.s, nullptr);
   int each_item;
   for (c.rt = 0;; ++c.rt) {
-    c.tiles = tiles_of<kR>(g, c.seq, c.rt);
+    c.tiles = tiles_of(g, c.seq, c.rt);
     each_item = cut ? (max(1, c.tiles) + chunk - 1) / chunk : units_of_item(c.tiles);
     const long long units = static_cast<long long>(each_item) * g.kv_heads;
     if (rest < units) break;
@@ -385,6 +388,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)), "r"(there ? 16 : 0)
                : "memory");  // (zeros where there is nothing)
 }
+__device__ __forceinline__ void copy16_if(bool there, uint32_t dst, const void* src) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %0, 0;\n\t@p cp.async.cg.shared.global [%1], [%2], 16;\n\t}" ::"r"(
+                   static_cast<uint32_t>(there)),
+               "r"(dst), "l"(reinterpret_cast<uint64_t>(src))
+               : "memory");
+}
 __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 // until at most kGroups of the warp's groups are on their way
 template <int kGroups>
@@ -401,9 +410,9 @@ __device__ __forceinline__ int stage_tiles(int tile, int end) {
 }
 
 // What a warp copies next. Every lane holds where one of 32 neighbouring tiles lies (a batch).
-template <int kDh, bool kInt4, int kR>
+template <int kDh, bool kInt4>
 struct Loader {
-  using C = Config<kDh, kInt4, kR>;
+  using C = Config<kDh, kInt4>;
   const uint8_t* mine = nullptr;  // the lane's tile
   long long head = 0;             // offset of the item's head
   int s = -1, tile = 0, end = 0;  // sequence, next tile to copy, end of the warp's part of the item
@@ -425,8 +434,8 @@ struct Loader {
   }
   // The item that `at` says, `left` units from its tile on; those without tiles are passed over. `at` goes on to the next.
   // (The lanes read the shared copies, compute the same, and write them again.)
-  __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left) {
-    Place<kR> now = at;
+  __device__ __forceinline__ void item(const PagedAttentionArgs& p, const Geometry& g, Place& at, int& left) {
+    Place now = at;
     int n = left;
     while (n > 0 && now.tiles == 0) {
       n -= units_of_item(0);
@@ -450,7 +459,7 @@ struct Loader {
     __syncwarp();
   }
   // The next stage: a group of copies, empty where nothing is left.
-  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, Place<kR>& at, int& left, int lane,
+  __device__ __forceinline__ void issue(const PagedAttentionArgs& p, const Geometry& g, Place& at, int& left, int lane,
                                         uint32_t ring) {
     if (tile >= end && left > 0) item(p, g, at, left);
     int n = 0;
@@ -479,36 +488,36 @@ struct Loader {
     constexpr int kWhole = C::Tile::kBytes / 512, kRest = C::Tile::kBytes % 512 / 16;
 #pragma unroll
     for (int i = 0; i < kWhole; ++i) copy16(dst + i * 512, src + i * 512);
-    if (kRest != 0 && lane < kRest) copy16(dst + kWhole * 512, src + kWhole * 512);
+    if (kRest != 0) copy16_if(lane < kRest, dst + kWhole * 512, src + kWhole * 512);
   }
 };
 
 // ---------------------------------------------------------------- a tile
 
 // What a warp knows of its item's rows, and what it has added up.
-template <int kDh, bool kInt4, int kR>
+template <int kDh, bool kInt4>
 struct Rows {
-  using C = Config<kDh, kInt4, kR>;
-  float factor[kR][2];
-  int limit[kR][2];             // last position that rows 2t and 2t + 1 of each eight see
+  using C = Config<kDh, kInt4>;
+  float factor[2];
+  int limit[2];             // last position that rows 2t and 2t + 1 see
   int first_limit, last_limit;  // the least and the largest of the rows'
   // fragments of 16 channels; in 4 bits fp16, of which the second word is a sixteenth
   const uint2* q;
-  float o[C::kMTiles][kR][4], m[kR][2], l[kR][2];
+  float o[C::kMTiles][4], m[2], l[2];
   uint32_t plus1024, minus1024;  // kFp16Of1024, kFp16OfMinus1024 in registers
 
-  __device__ __forceinline__ uint2 query(int n, int step, int lane) const { return q[(n * C::kMTiles + step) * 32 + lane]; }
+  __device__ __forceinline__ uint2 query(int step, int lane) const { return q[step * 32 + lane]; }
 
-  __device__ __forceinline__ static int live_rows(const Geometry& geo, const Place<kR>& c) {
-    return c.tiles == 0 ? 0 : min(8 * kR, c.seq.n * geo.group - c.rt * 8 * kR);
+  __device__ __forceinline__ static int live_rows(const Geometry& geo, const Place& c) {
+    return c.tiles == 0 ? 0 : min(kRows, c.seq.n * geo.group - c.rt * kRows);
   }
   // The queries' rows to where their fragments will be, zeros for rows without a token.
-  __device__ __forceinline__ static void fetch(const PagedAttentionArgs& p, const Geometry& geo, const Place<kR>& c, int lane, uint32_t to) {
+  __device__ __forceinline__ static void fetch(const PagedAttentionArgs& p, const Geometry& geo, const Place& c, int lane, uint32_t to) {
     constexpr int kPieces = kDh / 8, kRowsAtOnce = 32 / kPieces;  // of 16 bytes a row
     const int live = live_rows(geo, c);
 #pragma unroll
-    for (int i = 0; i < 8 * kR / kRowsAtOnce; ++i) {
-      const int r = i * kRowsAtOnce + lane / kPieces, row = c.rt * 8 * kR + r, tok = geo.group == geo.rows ? 0 : row / geo.group;
+    for (int i = 0; i < kRows / kRowsAtOnce; ++i) {
+      const int r = i * kRowsAtOnce + lane / kPieces, row = c.rt * kRows + r, tok = geo.group == geo.rows ? 0 : row / geo.group;
       const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(p.q);
       if (r < live)
         src += (static_cast<long long>(c.s) * p.batch.L + tok) * p.ld_q + (c.h * geo.group + row - tok * geo.group) * kDh + lane % kPieces * 8;
@@ -518,66 +527,63 @@ struct Rows {
 
   // The queries' fragments; in 4 bits each row times a power of two that makes its largest 2^7 to 2^8 (fp16 holds all bits
   // of a bf16 down to 2^-21 of that; a row with an infinity or NaN is NaN).
-  __device__ __forceinline__ void begin(const PagedAttentionArgs& p, const Geometry& geo, const Place<kR>& c, int live, int lane,
+  __device__ __forceinline__ void begin(const PagedAttentionArgs& p, const Geometry& geo, const Place& c, int live, int lane,
                                         uint2* shared) {
     const int g = lane >> 2, t = lane & 3;
     q = shared;
+    uint4 raw[kDh / 32];
 #pragma unroll
-    for (int n = 0; n < kR; ++n) {
-      uint4 raw[kDh / 32];
+    for (int i = 0; i < kDh / 32; ++i)
+      raw[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(shared) + g * kDh +
+                                               (kInt4 ? 64 * (i >> 1) + 16 * t + 8 * (i & 1) : 32 * i + 8 * t));
+    __syncwarp();  // (these eight rows' fragments take these eight rows' place)
+    auto put = [&](int step, uint2 f) { shared[step * 32 + lane] = f; };
+    float by_row = p.scale * 1.4426950408889634f;
+    if constexpr (kInt4) {
+      float x[kDh / 32][8], top = 0.f;
+#pragma unroll
+      for (int i = 0; i < kDh / 32; ++i) {
+        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[i][2 * e] = bf16_lo(w[e]);
+          x[i][2 * e + 1] = bf16_hi(w[e]);
+          top = fmaxf(top, fmaxf(fabsf(x[i][2 * e]), fabsf(x[i][2 * e + 1])));
+        }
+      }
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const int exponent = (__float_as_int(top) >> 23) - 127;  // -127 for 0 and what is below 2^-126
+      const int by = min(126, 7 - exponent);
+      by_row = exponent > 127 ? __int_as_float(0x7fffffff) : by_row * pow2(max(-by, -126));
+      const float up = pow2(by);
 #pragma unroll
       for (int i = 0; i < kDh / 32; ++i)
-        raw[i] = *reinterpret_cast<const uint4*>(reinterpret_cast<const __nv_bfloat16*>(shared) + (n * 8 + g) * kDh +
-                                                 (kInt4 ? 64 * (i >> 1) + 16 * t + 8 * (i & 1) : 32 * i + 8 * t));
-      __syncwarp();  // (these eight rows' fragments take these eight rows' place)
-      auto put = [&](int step, uint2 f) { shared[(n * C::kMTiles + step) * 32 + lane] = f; };
-      float by_row = p.scale * 1.4426950408889634f;
-      if constexpr (kInt4) {
-        float x[kDh / 32][8], top = 0.f;
 #pragma unroll
-        for (int i = 0; i < kDh / 32; ++i) {
-          const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+        for (int h = 0; h < 2; ++h)
+          put(2 * i + h, make_uint2(pack_f16(x[i][2 * h] * up, x[i][2 * h + 4] * up),
+                                    pack_f16(x[i][2 * h + 1] * (up * 0.0625f), x[i][2 * h + 5] * (up * 0.0625f))));
+    } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            x[i][2 * e] = bf16_lo(w[e]);
-            x[i][2 * e + 1] = bf16_hi(w[e]);
-            top = fmaxf(top, fmaxf(fabsf(x[i][2 * e]), fabsf(x[i][2 * e + 1])));
-          }
-        }
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        const int exponent = (__float_as_int(top) >> 23) - 127;  // -127 for 0 and what is below 2^-126
-        const int by = min(126, 7 - exponent);
-        by_row = exponent > 127 ? __int_as_float(0x7fffffff) : by_row * pow2(max(-by, -126));
-        const float up = pow2(by);
-#pragma unroll
-        for (int i = 0; i < kDh / 32; ++i)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            put(2 * i + h, make_uint2(pack_f16(x[i][2 * h] * up, x[i][2 * h + 4] * up),
-                                      pack_f16(x[i][2 * h + 1] * (up * 0.0625f), x[i][2 * h + 5] * (up * 0.0625f))));
-      } else {
-#pragma unroll
-        for (int i = 0; i < kDh / 32; ++i) {
-          put(2 * i, make_uint2(raw[i].x, raw[i].y));
-          put(2 * i + 1, make_uint2(raw[i].z, raw[i].w));
-        }
+      for (int i = 0; i < kDh / 32; ++i) {
+        put(2 * i, make_uint2(raw[i].x, raw[i].y));
+        put(2 * i + 1, make_uint2(raw[i].z, raw[i].w));
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        factor[n][e] = __shfl_sync(0xffffffffu, by_row, (2 * t + e) * 4);
-        limit[n][e] = c.seq.cached +
-                      (geo.group == geo.rows ? 0 : min((c.rt * 8 * kR + n * 8 + 2 * t + e) / geo.group, c.seq.n - 1));
-        m[n][e] = kFar;
-        l[n][e] = 0.f;
-      }
-#pragma unroll
-      for (int j = 0; j < C::kMTiles; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[j][n][e] = 0.f;
     }
-    first_limit = c.seq.cached + c.rt * 8 * kR / geo.group;
-    last_limit = c.seq.cached + (min(8 * kR, live) + c.rt * 8 * kR - 1) / geo.group;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      factor[e] = __shfl_sync(0xffffffffu, by_row, (2 * t + e) * 4);
+      limit[e] = c.seq.cached +
+                    (geo.group == geo.rows ? 0 : min((c.rt * kRows + 2 * t + e) / geo.group, c.seq.n - 1));
+      m[e] = kFar;
+      l[e] = 0.f;
+    }
+#pragma unroll
+    for (int j = 0; j < C::kMTiles; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
+    first_limit = c.seq.cached + c.rt * kRows / geo.group;
+    last_limit = c.seq.cached + (min(kRows, live) + c.rt * kRows - 1) / geo.group;
     __syncwarp();
   }
 
@@ -589,11 +595,11 @@ struct Rows {
     constexpr int kWords = kDh / 32;
     const int g = lane >> 2, t = lane & 3;
     // ---- scores: S^T = K q^T
-    float sc[kN][kR][4], sv[kN][2][kGroups];  // values' scales of tokens g and g + 8
+    float sc[kN][4], sv[kN][2][kGroups];  // values' scales of tokens g and g + 8
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
       const uint8_t* tp = first_tile + i * Tile::kBytes;
-      float part[kGroups][kR][4];
+      float part[kGroups][4];
       if constexpr (kInt4) {
         float sk[2][kGroups];
         uint32_t zk[2][kGroups], kw[2][kWords];
@@ -635,7 +641,7 @@ struct Rows {
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
             minus[h][gr][0] = minus_low(zk[h][gr], minus1024);
-            minus[h][gr][1] = minus_high(zk[h][gr], minus1024);
+            minus[h][gr][1] = minus_high(minus[h][gr][0]);
           }
 #pragma unroll
         for (int step = 0; step < 4; ++step)
@@ -645,24 +651,17 @@ struct Rows {
             const uint32_t w0 = x == 0 ? kw[0][w] : kw[0][w] >> 8, w1 = x == 0 ? kw[1][w] : kw[1][w] >> 8;
             const uint32_t a[4] = {low_nibbles(w0, minus[0][gr][0], plus1024), low_nibbles(w1, minus[1][gr][0], plus1024),
                                    high_nibbles(w0, minus[0][gr][1], plus1024), high_nibbles(w1, minus[1][gr][1], plus1024)};
-#pragma unroll
-            for (int n = 0; n < kR; ++n) {
-              const uint2 f = query(n, 2 * w + x, lane);
-              if (step == 0) first_mma_f16(part[gr][n], a, f.x, f.y); else mma_f16(part[gr][n], a, f.x, f.y);
-            }
+            const uint2 f = query(2 * w + x, lane);
+            if (step == 0) first_mma_f16(part[gr], a, f.x, f.y); else mma_f16(part[gr], a, f.x, f.y);
           }
 #pragma unroll
-        for (int n = 0; n < kR; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            sc[i][n][e] = part[0][n][e] * sk[e >> 1][0];
-            if constexpr (kGroups == 2) sc[i][n][e] = fmaf(part[1][n][e], sk[e >> 1][1], sc[i][n][e]);
-          }
+        for (int e = 0; e < 4; ++e) {
+          sc[i][e] = part[0][e] * sk[e >> 1][0];
+          if constexpr (kGroups == 2) sc[i][e] = fmaf(part[1][e], sk[e >> 1][1], sc[i][e]);
+        }
       } else {
 #pragma unroll
-        for (int n = 0; n < kR; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) part[0][n][e] = 0.f;
+        for (int e = 0; e < 4; ++e) part[0][e] = 0.f;
 #pragma unroll
         for (int w = 0; w < kWords; ++w) {
           const uint4 k0 = *reinterpret_cast<const uint4*>(tp + (w * kKvTile + g) * 64 + t * 16);
@@ -670,108 +669,97 @@ struct Rows {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             const uint32_t a[4] = {x == 0 ? k0.x : k0.z, x == 0 ? k1.x : k1.z, x == 0 ? k0.y : k0.w, x == 0 ? k1.y : k1.w};
-#pragma unroll
-            for (int n = 0; n < kR; ++n) {
-              const uint2 f = query(n, 2 * w + x, lane);
-              mma_bf16(part[0][n], a, f.x, f.y);
-            }
+            const uint2 f = query(2 * w + x, lane);
+            mma_bf16(part[0], a, f.x, f.y);
           }
         }
 #pragma unroll
-        for (int n = 0; n < kR; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[i][n][e] = part[0][n][e];
+        for (int e = 0; e < 4; ++e) sc[i][e] = part[0][e];
       }
     }
 
     // ---- relative to m: a score's exponent, -inf where the row does not see the token; probabilities, turned into the
     // second product's fragments (4 bits: by group of channels; bf16: the probability and what its rounding left)
-    float pr[kN][kR][4];
-    uint32_t pf[kN][2][kR][2];
-    auto hidden = [&](int i, int n, int e) { return kMasked && pos + kKvTile * i + g + 8 * (e >> 1) > limit[n][e & 1]; };
+    float pr[kN][4];
+    uint32_t pf[kN][2][2];
+    auto hidden = [&](int i, int e) { return kMasked && pos + kKvTile * i + g + 8 * (e >> 1) > limit[e & 1]; };
     auto probabilities = [&]() {
       bool far = false;
       uint32_t most = 0;
 #pragma unroll
-      for (int i = 0; i < kN; ++i)
+      for (int i = 0; i < kN; ++i) {
 #pragma unroll
-        for (int n = 0; n < kR; ++n) {
+        for (int e = 0; e < 4; ++e) {
+          float ex = fmaf(sc[i][e], factor[e & 1], -m[e & 1]);
+          if (hidden(i, e)) ex = -INFINITY;
+          far |= ex > (kInt4 ? kAlone + kSlack : kSlack);
+          pr[i][e] = ex2(ex);
+        }
+        if constexpr (kInt4) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float ex = fmaf(sc[i][n][e], factor[n][e & 1], -m[n][e & 1]);
-            if (hidden(i, n, e)) ex = -INFINITY;
-            far |= ex > (kInt4 ? kAlone + kSlack : kSlack);
-            pr[i][n][e] = ex2(ex);
-          }
-          if constexpr (kInt4) {
+          for (int gr = 0; gr < kGroups; ++gr) {
+            float w[4];
 #pragma unroll
-            for (int gr = 0; gr < kGroups; ++gr) {
-              float w[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                w[e] = pr[i][n][e] * sv[i][e >> 1][gr];
-                if (hidden(i, n, e)) w[e] = 0.f;  // whatever its scale is
-              }
-              pf[i][gr][n][0] = pack_f16(w[0], w[1]);
-              pf[i][gr][n][1] = pack_f16(w[2], w[3]);
-              most = max_f16(most, max_f16(pf[i][gr][n][0], pf[i][gr][n][1]));
+            for (int e = 0; e < 4; ++e) {
+              w[e] = pr[i][e] * sv[i][e >> 1][gr];
+              if (hidden(i, e)) w[e] = 0.f;  // whatever its scale is
             }
+            pf[i][gr][0] = pack_f16(w[0], w[1]);
+            pf[i][gr][1] = pack_f16(w[2], w[3]);
+            most = max_f16(most, max_f16(pf[i][gr][0], pf[i][gr][1]));
           }
         }
+      }
       if constexpr (kInt4) far |= above_f16(most);
       return far;
     };
     if (__any_sync(0xffffffffu, probabilities())) {
 #pragma unroll
-      for (int n = 0; n < kR; ++n)
+      for (int e = 0; e < 2; ++e) {
+        float top = -INFINITY, top_w = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float top = -INFINITY, top_w = -INFINITY;
+        for (int i = 0; i < kN; ++i)
 #pragma unroll
-          for (int i = 0; i < kN; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float x = hidden(i, n, e + 2 * h) ? -INFINITY : sc[i][n][e + 2 * h] * factor[n][e];
-              top = fmaxf(top, x);
-              if constexpr (kInt4) top_w = fmaxf(top_w, x + lg2(fmaxf(sv[i][h][0], sv[i][h][kGroups - 1])));
-            }
-#pragma unroll
-          for (int off = 4; off < 32; off <<= 1) {
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            if constexpr (kInt4) top_w = fmaxf(top_w, __shfl_xor_sync(0xffffffffu, top_w, off));
+          for (int h = 0; h < 2; ++h) {
+            const float x = hidden(i, e + 2 * h) ? -INFINITY : sc[i][e + 2 * h] * factor[e];
+            top = fmaxf(top, x);
+            if constexpr (kInt4) top_w = fmaxf(top_w, x + lg2(fmaxf(sv[i][h][0], sv[i][h][kGroups - 1])));
           }
-          // (the other rows keep theirs: what a row does not see must not change it)
-          if (kInt4 ? top_w - m[n][e] > kMost || top - m[n][e] > kAlone + kSlack : top - m[n][e] > kSlack) {
-            const float now = kInt4 ? fmaxf(top_w - kTop, top - kAlone) : top, by = ex2(m[n][e] - now);
-            m[n][e] = now;
-            l[n][e] *= by;
 #pragma unroll
-            for (int j = 0; j < C::kMTiles; ++j) {
-              o[j][n][e] *= by;
-              o[j][n][e + 2] *= by;
-            }
-          }
+        for (int off = 4; off < 32; off <<= 1) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          if constexpr (kInt4) top_w = fmaxf(top_w, __shfl_xor_sync(0xffffffffu, top_w, off));
         }
-      probabilities();
-    }
+        // (the other rows keep theirs: what a row does not see must not change it)
+        if (kInt4 ? top_w - m[e] > kMost || top - m[e] > kAlone + kSlack : top - m[e] > kSlack) {
+          const float now = kInt4 ? fmaxf(top_w - kTop, top - kAlone) : top, by = ex2(m[e] - now);
+          m[e] = now;
+          l[e] *= by;
 #pragma unroll
-    for (int i = 0; i < kN; ++i)
-#pragma unroll
-      for (int n = 0; n < kR; ++n) {
-        l[n][0] += pr[i][n][0] + pr[i][n][2];
-        l[n][1] += pr[i][n][1] + pr[i][n][3];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if constexpr (kInt4) {
-#pragma unroll
-            for (int gr = 0; gr < kGroups; ++gr) pf[i][gr][n][h] = turned(pf[i][gr][n][h]);
-          } else {
-            const uint32_t top = pack_bf16x2(pr[i][n][2 * h], pr[i][n][2 * h + 1]);
-            pf[i][0][n][h] = turned(top);
-            pf[i][1][n][h] = turned(pack_bf16x2(pr[i][n][2 * h] - bf16_lo(top), pr[i][n][2 * h + 1] - bf16_hi(top)));
+          for (int j = 0; j < C::kMTiles; ++j) {
+            o[j][e] *= by;
+            o[j][e + 2] *= by;
           }
         }
       }
+      probabilities();
+    }
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      l[0] += pr[i][0] + pr[i][2];
+      l[1] += pr[i][1] + pr[i][3];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (kInt4) {
+#pragma unroll
+          for (int gr = 0; gr < kGroups; ++gr) pf[i][gr][h] = turned(pf[i][gr][h]);
+        } else {
+          const uint32_t top = pack_bf16x2(pr[i][2 * h], pr[i][2 * h + 1]);
+          pf[i][0][h] = turned(top);
+          pf[i][1][h] = turned(pack_bf16x2(pr[i][2 * h] - bf16_lo(top), pr[i][2 * h + 1] - bf16_hi(top)));
+        }
+      }
+    }
 
     // ---- O^T += V^T P^T
 #pragma unroll
@@ -810,7 +798,7 @@ struct Rows {
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
             minus[h][gr][0] = minus_low(zv[h][gr], minus1024);
-            minus[h][gr][1] = minus_high(zv[h][gr], minus1024);
+            minus[h][gr][1] = minus_high(minus[h][gr][0]);
           }
 #pragma unroll
         for (int j = 0; j < C::kMTiles; ++j) {
@@ -818,8 +806,7 @@ struct Rows {
           const uint32_t w0 = j % 2 == 0 ? vw[0][w] : vw[0][w] >> 8, w1 = j % 2 == 0 ? vw[1][w] : vw[1][w] >> 8;
           const uint32_t a[4] = {low_nibbles(w0, minus[0][gr][0], plus1024), high_nibbles(w0, minus[0][gr][1], plus1024),
                                  low_nibbles(w1, minus[1][gr][0], plus1024), high_nibbles(w1, minus[1][gr][1], plus1024)};
-#pragma unroll
-          for (int n = 0; n < kR; ++n) mma_f16(o[j][n], a, pf[i][gr][n][0], pf[i][gr][n][1]);
+          mma_f16(o[j], a, pf[i][gr][0], pf[i][gr][1]);
         }
       } else {
         // bytes behind the last token count as zeros, an infinity or NaN that some rows may see too, at first
@@ -855,11 +842,8 @@ struct Rows {
           for (int x = 0; x < 2; ++x) {
             const int j = 2 * w + x;
             const uint32_t a[4] = {v[0][2 * x], v[0][2 * x + 1], v[1][2 * x], v[1][2 * x + 1]};
-#pragma unroll
-            for (int n = 0; n < kR; ++n) {
-              mma_bf16(o[j][n], a, pf[i][0][n][0], pf[i][0][n][1]);
-              mma_bf16(o[j][n], a, pf[i][1][n][0], pf[i][1][n][1]);
-            }
+            mma_bf16(o[j], a, pf[i][0][0], pf[i][0][1]);
+            mma_bf16(o[j], a, pf[i][1][0], pf[i][1][1]);
             if constexpr (kMasked) {
               if (any) {  // a token at a time, for the rows that see it
 #pragma unroll 1
@@ -871,14 +855,11 @@ struct Rows {
                     b[y] = tok < 8 ? sick[0][2 * x + y] & half : 0u;
                     b[2 + y] = tok < 8 ? 0u : sick[1][2 * x + y] & half;
                   }
+                  float d[4] = {0.f, 0.f, 0.f, 0.f};
+                  mma_bf16(d, b, pf[i][0][0], pf[i][0][1]);
 #pragma unroll
-                  for (int n = 0; n < kR; ++n) {
-                    float d[4] = {0.f, 0.f, 0.f, 0.f};
-                    mma_bf16(d, b, pf[i][0][n][0], pf[i][0][n][1]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                      if (pos + kKvTile * i + tok <= limit[n][e & 1]) o[j][n][e] += d[e];
-                  }
+                  for (int e = 0; e < 4; ++e)
+                    if (pos + kKvTile * i + tok <= limit[e & 1]) o[j][e] += d[e];
                 }
               }
             }
@@ -888,68 +869,67 @@ struct Rows {
     }
   }
 
-  // What the lane has of row n * 8 + 2t + e, normalised: f(first channel, values) for every four neighbouring channels.
+  // What the lane has of row 2t + e, normalised: f(first channel, values) for every four neighbouring channels.
   template <typename F>
-  __device__ __forceinline__ void each(int n, int e, float by, int lane, F f) const {
+  __device__ __forceinline__ void each(int e, float by, int lane, F f) const {
     const int g = lane >> 2;
     const float high = kInt4 ? by * 0.0625f : by;
 #pragma unroll
     for (int j = 0; j < C::kMTiles; j += 2)
       f(kInt4 ? 64 * (j >> 2) + 8 * g + 2 * (j & 3) : 32 * (j >> 1) + 4 * g,
-        make_float4(o[j][n][e] * by, o[j][n][e + 2] * high, o[j + 1][n][e] * by, o[j + 1][n][e + 2] * high));
+        make_float4(o[j][e] * by, o[j][e + 2] * high, o[j + 1][e] * by, o[j + 1][e + 2] * high));
   }
 };
 
 // ---------------------------------------------------------------- the kernel
 
 // Parts in the workspace: of each CTA two (what Desc says), then of each warp one.
-template <int kDh, int kR>
-__device__ __forceinline__ Part<kDh, kR>* cta_part(const PagedAttentionArgs& p, int cta, int slot) {
-  return reinterpret_cast<Part<kDh, kR>*>(static_cast<uint8_t*>(p.ws) + sizeof(Desc) * kMaxCtas) + 2 * cta + slot;
+template <int kDh>
+__device__ __forceinline__ Part<kDh>* cta_part(const PagedAttentionArgs& p, int cta, int slot) {
+  return reinterpret_cast<Part<kDh>*>(static_cast<uint8_t*>(p.ws) + sizeof(Desc) * kMaxCtas) + 2 * cta + slot;
 }
-template <int kDh, int kR>
-__device__ __forceinline__ Part<kDh, kR>* warp_part(const PagedAttentionArgs& p, int warp) {
-  return cta_part<kDh, kR>(p, kMaxCtas, 0) + blockIdx.x * kWarps + warp;
+template <int kDh>
+__device__ __forceinline__ Part<kDh>* warp_part(const PagedAttentionArgs& p, int warp) {
+  return cta_part<kDh>(p, kMaxCtas, 0) + blockIdx.x * kWarps + warp;
 }
 
-template <int kR>
 __device__ __forceinline__ __nv_bfloat16* out_row(const PagedAttentionArgs& p, const Geometry& geo, int s, int row, int h, int head_dim) {
   const int tok = row / geo.group;
   return static_cast<__nv_bfloat16*>(p.out) + (static_cast<long long>(s) * p.batch.L + tok) * p.ld_out +
          (h * geo.group + row - tok * geo.group) * head_dim;
 }
 
-template <int kDh, bool kInt4, int kR>
-__global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
+template <int kDh, bool kInt4>
+__global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
     paged_attention_kernel(const PagedAttentionArgs p, bool aligned) {
-  using C = Config<kDh, kInt4, kR>;
+  using C = Config<kDh, kInt4>;
   using Tile = typename C::Tile;
-  using Parts = Part<kDh, kR>;
+  using Parts = Part<kDh>;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ Shared<kR> sh;
+  __shared__ Shared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   uint8_t* const ring = smem + warp * (C::kStages * C::kStageBytes);
   pdl_wait();
   pdl_launch_dependents();
-  const Geometry geo = geometry<kR>(p);
-  Place<kR> c;
+  const Geometry geo = geometry(p);
+  Place c;
   int active;
   int left = begin(p, geo, aligned, c, active, sh);
   WarpEnd end{0, 0, 0, 0, false, false, false, false, 0};
   if (left > 0) {
-    Place<kR>& load = sh.load[warp];
-    Place<kR>& take = sh.take[warp];
+    Place& load = sh.load[warp];
+    Place& take = sh.take[warp];
     int& load_left = sh.load_left[warp];
     const uint32_t ring_at = smem_u32(ring);
     uint2* const queries = reinterpret_cast<uint2*>(smem + C::kRing + warp * C::kQ);
-    using R = Rows<kDh, kInt4, kR>;
+    using R = Rows<kDh, kInt4>;
     R::fetch(p, geo, c, lane, smem_u32(queries));
-    Loader<kDh, kInt4, kR> loader;
+    Loader<kDh, kInt4> loader;
     load = c;
     take = c;
     load_left = left;
     __syncwarp();
-    Rows<kDh, kInt4, kR> rows;
+    Rows<kDh, kInt4> rows;
     rows.plus1024 = held(kFp16Of1024);
     rows.minus1024 = held(kFp16OfMinus1024);
     int used = 0;  // stages
@@ -967,43 +947,41 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
       }
       if (tile >= hi) {
         c = take;
-        const int row0 = c.rt * 8 * kR;
+        const int row0 = c.rt * kRows;
         if (open) {
           // ---- an item as a whole goes out, a part of one waits: the last segment's in the ring, an earlier one's in memory
           const bool last = left <= 0, ended = hi == max(1, c.tiles), whole = lo == 0 && ended;
-          Place<kR> next = c;
+          Place next = c;
           if (!last) {  // the next item's queries come while this one is finished
             next.next_item(p, geo);
             R::fetch(p, geo, next, lane, smem_u32(queries));
           }
-          float* part_o = last ? reinterpret_cast<float*>(ring) : &warp_part<kDh, kR>(p, warp)->o[0][0];
-          float* part_mass = last ? sh.mass[warp] : warp_part<kDh, kR>(p, warp)->mass;
-          const int slots = min(8 * kR, geo.rows - row0);
+          float* part_o = last ? reinterpret_cast<float*>(ring) : &warp_part<kDh>(p, warp)->o[0][0];
+          float* part_mass = last ? sh.mass[warp] : warp_part<kDh>(p, warp)->mass;
+          const int slots = min(kRows, geo.rows - row0);
 #pragma unroll
-          for (int n = 0; n < kR; ++n)
+          for (int e = 0; e < 2; ++e) {
+            const int row = 2 * t + e;
+            float sum = rows.l[e];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const int row = n * 8 + 2 * t + e;
-              float sum = rows.l[n][e];
-#pragma unroll
-              for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-              const float by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
-              if (whole) {
-                if (row < slots) {
-                  __nv_bfloat16* dst = out_row<kR>(p, geo, c.s, row0 + row, c.h, kDh);
-                  // an empty slot, or positions that cannot be (NaN)
-                  const uint32_t fill = !c.seq.ok && row0 + row < c.seq.n * geo.group ? 0x7fff7fffu : 0u;
-                  rows.each(n, e, by, lane, [&](int d, const float4& v) {
-                    *reinterpret_cast<uint2*>(dst + d) =
-                        row < live ? make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)) : make_uint2(fill, fill);
-                  });
-                }
-              } else if (row < live) {
-                rows.each(n, e, by, lane, [&](int d, const float4& v) { *reinterpret_cast<float4*>(part_o + row * kDh + d) = v; });
-                if (g == 0)
-                  part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kFar : rows.m[n][e] + log2f(sum);
+            for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            const float by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
+            if (whole) {
+              if (row < slots) {
+                __nv_bfloat16* dst = out_row(p, geo, c.s, row0 + row, c.h, kDh);
+                // an empty slot, or positions that cannot be (NaN)
+                const uint32_t fill = !c.seq.ok && row0 + row < c.seq.n * geo.group ? 0x7fff7fffu : 0u;
+                rows.each(e, by, lane, [&](int d, const float4& v) {
+                  *reinterpret_cast<uint2*>(dst + d) =
+                      row < live ? make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)) : make_uint2(fill, fill);
+                });
               }
+            } else if (row < live) {
+              rows.each(e, by, lane, [&](int d, const float4& v) { *reinterpret_cast<float4*>(part_o + row * kDh + d) = v; });
+              if (g == 0)
+                part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kFar : rows.m[e] + log2f(sum);
             }
+          }
           if (!whole) {
             if (lo > 0) {
               end.first = true;
@@ -1095,14 +1073,14 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
     if (start < 0) ends = done;
     else if (!done) tail_warp = start;
     const WarpEnd& item = sh.end[max(start, 0)];
-    const int rt = start < 0 ? item.first_rt : item.rt, shown = min(8 * kR, geo.rows - rt * 8 * kR);
+    const int rt = start < 0 ? item.first_rt : item.rt, shown = min(kRows, geo.rows - rt * kRows);
     constexpr int kE = kDh / 32;
     // (rows past the last token hold nothing; what is made of them is not read)
     for (int row = (warp - turn) & (kWarps - 1); row < shown; row += kWarps) {
       using Vec = typename C::Vec;
       const bool there = lane < stop && lane >= max(start, 0), near = lane == start || (ringed >> (lane & 31) & 1) != 0;
       const int w0 = there ? lane : 0;
-      const Parts* far_part = warp_part<kDh, kR>(p, w0);
+      const Parts* far_part = warp_part<kDh>(p, w0);
       const float* row_at = there && !near ? far_part->o[row]
                                            : reinterpret_cast<const float*>(smem + w0 * (C::kStages * C::kStageBytes)) + row * kDh;
       const float mass = !there ? kFar : near ? sh.mass[w0][row] : far_part->mass[row];
@@ -1130,11 +1108,11 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
         for (int i = 0; i < kE; ++i) out[i] = fmaf(x[i], by, out[i]);
       }
       if (start >= 0 && done) {
-        __nv_bfloat16* dst = out_row<kR>(p, geo, item.s, rt * 8 * kR + row, item.h, kDh) + lane * kE;
+        __nv_bfloat16* dst = out_row(p, geo, item.s, rt * kRows + row, item.h, kDh) + lane * kE;
 #pragma unroll
         for (int i = 0; i < kE; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = row < item.live ? pack_bf16x2(out[i], out[i + 1]) : 0u;
       } else {
-        Parts* to = cta_part<kDh, kR>(p, blockIdx.x, start < 0 ? 0 : 1);
+        Parts* to = cta_part<kDh>(p, blockIdx.x, start < 0 ? 0 : 1);
 #pragma unroll
         for (int i = 0; i < kE; ++i) to->o[row][lane * kE + i] = out[i];
         const float total = __shfl_sync(0xffffffffu, sum, 0), highest = __shfl_sync(0xffffffffu, top, 0);
@@ -1157,7 +1135,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4, kR>::kCtasPerSm)
 }
 
 // Items that several CTAs have parts of: the CTA that holds an item's first part adds up all of them, a row in y.
-template <int kDh, int kR>
+template <int kDh>
 __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const PagedAttentionArgs p, int ctas) {
   __shared__ float sh_o[kWarps][kDh], sh_sum[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1168,8 +1146,8 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   const Desc mine = desc[b];
   int more = b + 1 + lane < ctas && desc[b + 1 + lane].ends != 0;  // (read beside it)
   if (mine.slot < 0) return;
-  const Geometry geo = geometry<kR>(p);
-  const int q_row = mine.rt * 8 * kR + row;
+  const Geometry geo = geometry(p);
+  const int q_row = mine.rt * kRows + row;
   if (q_row >= geo.rows) return;
   int end = ctas;  // parts: this CTA's, then slot 0 of those up to the first that ends the item
   for (int at = b + 1; at < ctas; at += 32) {
@@ -1185,7 +1163,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   constexpr int kE = kDh / 32;
   const int n = end - b;
   float mass = kFar, top, sum = 0.f, out[kE];
-  for (int i = lane; i < n; i += 32) mass = fmaxf(mass, cta_part<kDh, kR>(p, b + i, i == 0 ? mine.slot : 0)->mass[row]);
+  for (int i = lane; i < n; i += 32) mass = fmaxf(mass, cta_part<kDh>(p, b + i, i == 0 ? mine.slot : 0)->mass[row]);
   top = mass;
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
@@ -1193,7 +1171,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   for (int i = 0; i < kE; ++i) out[i] = 0.f;
 #pragma unroll 4
   for (int i = warp; i < n; i += kWarps) {
-    const Part<kDh, kR>* part = cta_part<kDh, kR>(p, b + i, i == 0 ? mine.slot : 0);
+    const Part<kDh>* part = cta_part<kDh>(p, b + i, i == 0 ? mine.slot : 0);
     const Vec x = reinterpret_cast<const Vec*>(part->o[row])[lane];
     const float m = part->mass[row], weight = m == kFar ? 0.f : ex2(m - top);
     sum += weight;
@@ -1212,58 +1190,41 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
       total += sh_sum[w];
       acc += sh_o[w][threadIdx.x];
     }
-    __nv_bfloat16* dst = out_row<kR>(p, geo, mine.s, q_row, mine.h, kDh);
+    __nv_bfloat16* dst = out_row(p, geo, mine.s, q_row, mine.h, kDh);
     dst[threadIdx.x] = __float2bfloat16_rn(row >= mine.live ? 0.f : acc / total);
   }
 }
 
-template <int kDh, bool kInt4, int kR>
+template <int kDh, bool kInt4>
 int launch(const PagedAttentionArgs& a, cudaStream_t st) {
-  using C = Config<kDh, kInt4, kR>;
+  using C = Config<kDh, kInt4>;
   static_assert(C::kSmem * C::kCtasPerSm <= 227 * 1024, "shared memory of an SM");
-  if (cudaFuncSetAttribute(paged_attention_kernel<kDh, kInt4, kR>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
+  if (cudaFuncSetAttribute(paged_attention_kernel<kDh, kInt4>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
       cudaSuccess)
     return -3;
   const int ctas = std::min(kMaxCtas, std::max(1, sm_count()) * C::kCtasPerSm);
   const int64_t rows = a.n_heads / a.cache.kv_heads * a.batch.L;
-  const int64_t items = a.batch.S * a.cache.kv_heads * ((rows + 8 * kR - 1) / (8 * kR));
+  const int64_t items = a.batch.S * a.cache.kv_heads * ((rows + kRows - 1) / kRows);
   const bool aligned = items <= ctas && (a.batch.max_pages << a.cache.page_bits) <= kAlignedTokens;
   if (aligned)
-    return launch_pdl(paged_attention_kernel<kDh, kInt4, kR>, dim3(static_cast<unsigned>(items)), dim3(kThreads), C::kSmem, st, a, true) ==
+    return launch_pdl(paged_attention_kernel<kDh, kInt4>, dim3(static_cast<unsigned>(items)), dim3(kThreads), C::kSmem, st, a, true) ==
                    cudaSuccess
                ? 0
                : -3;
-  if (launch_pdl(paged_attention_kernel<kDh, kInt4, kR>, dim3(ctas), dim3(kThreads), C::kSmem, st, a, false) != cudaSuccess) return -3;
-  const dim3 grid(ctas, static_cast<unsigned>(std::min<int64_t>(rows, 8 * kR)));
-  return launch_pdl(paged_attention_join_kernel<kDh, kR>, grid, dim3(kThreads), 0, st, a, ctas) == cudaSuccess ? 0 : -3;
-}
-
-// Passes over the rows of a kv head, 8 to 32 rows each: as few as can be, then the narrowest that do.
-int row_tiles_of(int64_t rows) {
-  const int64_t eights = (rows + 7) / 8, passes = (eights + kMaxRowTiles - 1) / kMaxRowTiles;
-  return static_cast<int>((eights + passes - 1) / passes);
-}
-
-template <int kDh, bool kInt4>
-int launch_rows(const PagedAttentionArgs& a, cudaStream_t st) {
-  switch (row_tiles_of(a.n_heads / a.cache.kv_heads * a.batch.L)) {
-    case 1: return launch<kDh, kInt4, 1>(a, st);
-    case 2: return launch<kDh, kInt4, 2>(a, st);
-    case 3: return launch<kDh, kInt4, 3>(a, st);
-    default: return launch<kDh, kInt4, 4>(a, st);
-  }
+  if (launch_pdl(paged_attention_kernel<kDh, kInt4>, dim3(ctas), dim3(kThreads), C::kSmem, st, a, false) != cudaSuccess) return -3;
+  const dim3 grid(ctas, static_cast<unsigned>(std::min<int64_t>(rows, kRows)));
+  return launch_pdl(paged_attention_join_kernel<kDh>, grid, dim3(kThreads), 0, st, a, ctas) == cudaSuccess ? 0 : -3;
 }
 
 }  // namespace
 
-size_t paged_attention_workspace_bytes(int64_t S, int64_t L, int64_t n_heads, int64_t kv_heads, int64_t head_dim) {
-  const int64_t rows = 8 * row_tiles_of(std::max<int64_t>(1, n_heads / kv_heads * L));
-  return sizeof(Desc) * kMaxCtas + static_cast<size_t>((2 + kWarps) * kMaxCtas * rows * (head_dim + 1) * 4);
+size_t paged_attention_workspace_bytes(int64_t head_dim) {
+  return sizeof(Desc) * kMaxCtas + (2 + kWarps) * kMaxCtas * (head_dim == 128 ? sizeof(Part<128>) : sizeof(Part<64>));
 }
 
 int launch_paged_attention(const PagedAttentionArgs& a, cudaStream_t st) {
-  if (a.cache.head_dim == 128) return a.cache.int4 ? launch_rows<128, true>(a, st) : launch_rows<128, false>(a, st);
-  return a.cache.int4 ? launch_rows<64, true>(a, st) : launch_rows<64, false>(a, st);
+  if (a.cache.head_dim == 128) return a.cache.int4 ? launch<128, true>(a, st) : launch<128, false>(a, st);
+  return a.cache.int4 ? launch<64, true>(a, st) : launch<64, false>(a, st);
 }
 
 }  // namespace hydra
