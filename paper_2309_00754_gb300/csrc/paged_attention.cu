@@ -24,6 +24,7 @@
 // all of them, want registers: with half or a quarter of the warps they took 43 and 46 us for 16 sequences x 20 rows over
 // 4096 tokens, eight rows 36.)
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <type_traits>
 
@@ -1199,9 +1200,15 @@ template <int kDh, bool kInt4>
 int launch(const PagedAttentionArgs& a, cudaStream_t st) {
   using C = Config<kDh, kInt4>;
   static_assert(C::kSmem * C::kCtasPerSm <= 227 * 1024, "shared memory of an SM");
-  if (cudaFuncSetAttribute(paged_attention_kernel<kDh, kInt4>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
-      cudaSuccess)
-    return -3;
+  static std::atomic<bool> attr_set[64];  // the shared-memory limit is a per-device attribute; host threads may ask at once
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -3;
+  if (!attr_set[dev]) {
+    if (cudaFuncSetAttribute(paged_attention_kernel<kDh, kInt4>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmem) !=
+        cudaSuccess)
+      return -3;
+    attr_set[dev] = true;
+  }
   const int ctas = std::min(kMaxCtas, std::max(1, sm_count()) * C::kCtasPerSm);
   const int64_t rows = a.n_heads / a.cache.kv_heads * a.batch.L;
   const int64_t items = a.batch.S * a.cache.kv_heads * ((rows + kRows - 1) / kRows);

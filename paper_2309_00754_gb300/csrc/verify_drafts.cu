@@ -8,10 +8,10 @@
 // draw from the distribution whose logarithm it perturbs. Without random numbers a token is kept while it is the target's
 // argmax.
 //
-// Bound by the reads of the logits. A cluster of CTAs has a sequence: each CTA takes a slice of the vocabulary of all its
-// rows, a warp a share of that, in one pass with a running maximum and sum; the shares' (maximum, sum) pairs are all that
-// the CTAs exchange before every one of them knows where the drafts end. The row that the last token is drawn from is
-// read a second time, from L2 as a rule.
+// Bound by the reads of the logits. A cluster of CTAs has a sequence. Every row is cut in the same number of slices, which its
+// warps take in turn, each in one pass with a running maximum and sum; the slices' (maximum, sum) pairs are all that the CTAs
+// exchange before every one of them knows where the drafts end. (Cut alike, equal rows have equal sums: a draft model that
+// is the target is never refused.) The row that the last token is drawn from is read a second time, from L2 as a rule.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -45,9 +45,12 @@ struct Part {
   Best best;
 };
 
+constexpr int kRounds = 4;  // slices of a warp, where there are not many more warps than rows
+constexpr int kMaxSlices = kMaxRows / kWarps + 1;
+static_assert(kMaxSlices >= kRounds, "a warp's slices");
+
 struct Shared {
-  Part part[kMaxRows][kWarps];
-  Part cta[kMaxRows];              // this CTA's, read by the cluster
+  Part part[kWarps][kMaxSlices];  // read by the cluster
   float m[kMaxRows], c[kMaxRows];  // of whole rows: maximum, log of the sum
   int top[kMaxRows];
   Best best[2][kWarps];
@@ -101,36 +104,8 @@ __device__ __forceinline__ void merge(Part& p, const Part& o) {
   p.m = now;
 }
 
-// [lo, hi) of a row by a warp.
-template <typename T, bool kArg>
-__device__ __forceinline__ Part scan(const T* row, int lo, int hi, int lane) {
-  constexpr int E = 16 / sizeof(T), kDeep = 4;
-  Part p;
-  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row + lo) & 15) / sizeof(T));
-  const int head = min(off == 0 ? 0 : E - off, hi - lo);
-  const int vecs = (hi - lo - head) / E, body = lo + head;
-  if (lane < head) {
-    const float x[1] = {to_f(row[lo + lane])};
-    add<kArg>(p, x, lo + lane);
-  }
-  for (int v = lane; v < vecs; v += 32 * kDeep) {
-    uint4 raw[kDeep];
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d)
-      if (v + 32 * d < vecs) raw[d] = *reinterpret_cast<const uint4*>(row + body + (v + 32 * d) * E);
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d)
-      if (v + 32 * d < vecs) {
-        float x[E];
-        unpack<T>(raw[d], x);
-        add<kArg>(p, x, body + (v + 32 * d) * E);
-      }
-  }
-  const int tail = body + vecs * E + lane;
-  if (tail < hi) {
-    const float x[1] = {to_f(row[tail])};
-    add<kArg>(p, x, tail);
-  }
+template <bool kArg>
+__device__ __forceinline__ Part warp_merge(Part p) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Part other;
@@ -145,6 +120,51 @@ __device__ __forceinline__ Part scan(const T* row, int lo, int hi, int lane) {
   return p;
 }
 
+// [lo, hi) of a row by a warp.
+template <typename T, bool kArg>
+__device__ __forceinline__ Part scan(const T* row, int lo, int hi, int lane) {
+  constexpr int E = 16 / sizeof(T), kDeep = 4;  // vectors of a lane on their way
+  Part p;
+  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row + lo) & 15) / sizeof(T));
+  const int head = min(off == 0 ? 0 : E - off, hi - lo);
+  const int vecs = (hi - lo - head) / E, body = lo + head;
+  if (lane < head) {
+    const float x[1] = {to_f(row[lo + lane])};
+    add<kArg>(p, x, lo + lane);
+  }
+  const uint4* at = reinterpret_cast<const uint4*>(row + body);
+  int v = lane;
+#pragma unroll 1
+  for (; v + 32 * (kDeep - 1) < vecs; v += 32 * kDeep) {
+    uint4 raw[kDeep];
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) raw[d] = at[v + 32 * d];
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      float x[E];
+      unpack<T>(raw[d], x);
+      add<kArg>(p, x, body + (v + 32 * d) * E);
+    }
+  }
+  uint4 raw[kDeep];
+#pragma unroll
+  for (int d = 0; d < kDeep; ++d)
+    if (v + 32 * d < vecs) raw[d] = at[v + 32 * d];
+#pragma unroll
+  for (int d = 0; d < kDeep; ++d)
+    if (v + 32 * d < vecs) {
+      float x[E];
+      unpack<T>(raw[d], x);
+      add<kArg>(p, x, body + (v + 32 * d) * E);
+    }
+  const int tail = body + vecs * E + lane;
+  if (tail < hi) {
+    const float x[1] = {to_f(row[tail])};
+    add<kArg>(p, x, tail);
+  }
+  return warp_merge<kArg>(p);
+}
+
 // (the address of `local` in another CTA)
 __device__ __forceinline__ float ld_cluster(const float* local, unsigned rank) { return ld_cluster_f32(local, rank); }
 __device__ __forceinline__ int ld_cluster(const int* local, unsigned rank) {
@@ -152,7 +172,7 @@ __device__ __forceinline__ int ld_cluster(const int* local, unsigned rank) {
 }
 
 template <typename T, bool kGreedy>
-__global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, int cs) {
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p, int cs) {
   extern __shared__ uint8_t raw_shared[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_shared);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -167,51 +187,62 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, in
   const T* target = static_cast<const T*>(p.target) + s * (D + 1) * p.ld;
   const T* draft = p.draft != nullptr ? static_cast<const T*>(p.draft) + s * D * p.ld_draft : nullptr;
   const int rows = n + 1 + (draft != nullptr ? n : 0);
+  auto row_at = [&](int r) { return r <= n ? target + r * p.ld : draft + (r - n - 1) * p.ld_draft; };
 
-  // this CTA's slice, and the warp's share of it, whole vectors of a row that starts at one
-  const int step = ((V + cs * kWarps - 1) / (cs * kWarps) + 7) & ~7;
-  const int lo = min(V, (rank * kWarps + warp) * step), hi = min(V, lo + step);
-  for (int r = 0; r < rows; ++r) {
-    const T* row = r <= n ? target + r * p.ld : draft + (r - n - 1) * p.ld_draft;
-    const Part part = scan<T, kGreedy>(row, lo, hi, lane);
-    if (lane == 0) sh.part[r][warp] = part;
+  // a draft's token and its logits (lane: draft), on their way while the sums are made
+  int x = -1;
+  float zx = 0.f, wx = 0.f, u = 0.f;
+  if (warp == 0 && lane < n) {
+    x = p.ids[s * D + lane];
+    if (!kGreedy) u = p.uniform[s * D + lane];
+    if (x >= 0 && x < V) {
+      zx = to_f(target[lane * p.ld + x]);
+      if (draft != nullptr) wx = to_f(draft[lane * p.ld_draft + x]);
+    }
   }
-  __syncthreads();
-  for (int r = threadIdx.x; r < rows; r += kThreads) {
-    Part all = sh.part[r][0];
-    for (int w = 1; w < kWarps; ++w) merge<kGreedy>(all, sh.part[r][w]);
-    sh.cta[r] = all;
+
+  // slices of a row: so many that the warps of the cluster have kRounds each where all drafts are there
+  const int warps = cs * kWarps, most = p.draft != nullptr ? 2 * D + 1 : D + 1;
+  const int slices = max(1, (warps >= 16 * most ? warps : kRounds * warps) / most);
+  for (int i = rank * kWarps + warp, k = 0; i < rows * slices; i += warps, ++k) {
+    const int r = i / slices, j = i - r * slices;
+    const int lo = static_cast<int>(static_cast<long long>(V) * j / slices), hi = static_cast<int>(static_cast<long long>(V) * (j + 1) / slices);
+    const Part part = scan<T, kGreedy>(row_at(r), lo, hi, lane);
+    if (lane == 0) sh.part[warp][k] = part;
   }
   if (cs > 1) cluster_sync_all(); else __syncthreads();
-  for (int r = threadIdx.x; r < rows; r += kThreads) {
-    Part all = sh.cta[r];
-    if (cs > 1)
-      for (int c = 0; c < cs; ++c) {
-        Part o;
-        o.m = ld_cluster(&sh.cta[r].m, c);
-        o.s = ld_cluster(&sh.cta[r].s, c);
-        if (kGreedy) {
-          o.best.v = ld_cluster(&sh.cta[r].best.v, c);
-          o.best.i = ld_cluster(&sh.cta[r].best.i, c);
-        }
-        if (c == 0) all = o; else merge<kGreedy>(all, o);
+  // a warp a row, a lane a slice of it
+  for (int r = warp; r < rows; r += kWarps) {
+    Part all;
+    for (int j = lane; j < slices; j += 32) {
+      const int i = r * slices + j, w = i % warps;
+      const Part* from = &sh.part[w % kWarps][i / warps];
+      Part o;
+      const int c = w / kWarps;
+      o.m = c == rank ? from->m : ld_cluster(&from->m, c);
+      o.s = c == rank ? from->s : ld_cluster(&from->s, c);
+      if (kGreedy) {
+        o.best.v = c == rank ? from->best.v : ld_cluster(&from->best.v, c);
+        o.best.i = c == rank ? from->best.i : ld_cluster(&from->best.i, c);
       }
-    // a row of nothing but -inf: its sum is 0
-    sh.m[r] = all.s == 0.f ? -INFINITY : all.m;
-    sh.c[r] = all.s == 0.f ? 0.f : logf(all.s);
-    sh.top[r] = all.best.i == INT_MAX ? 0 : all.best.i;  // (nothing but NaN)
+      merge<kGreedy>(all, o);
+    }
+    all = warp_merge<kGreedy>(all);
+    if (lane == 0) {
+      // a row of nothing but -inf: its sum is 0
+      sh.m[r] = all.s == 0.f ? -INFINITY : all.m;
+      sh.c[r] = all.s == 0.f ? 0.f : logf(all.s);
+      sh.top[r] = all.best.i == INT_MAX ? 0 : all.best.i;  // (nothing but NaN)
+    }
   }
   __syncthreads();
 
-  // log-probability of token x in row r (the sums are in fp32; what is made of them here in 64 bits)
-  auto log_p = [&](const T* row, int r, int x) {
-    return static_cast<double>(to_f(row[x])) - sh.m[r] - sh.c[r];
-  };
+  // log-probability of logit z in row r (the sums are in fp32; what is made of them here in 64 bits)
+  auto log_p = [&](float z, int r) { return static_cast<double>(z) - sh.m[r] - sh.c[r]; };
   if (warp == 0) {
     float a = 0.f;
     bool keep = false;
     if (lane < n) {
-      const int x = p.ids[s * D + lane];
       if (x < 0 || x >= V) {
         a = __int_as_float(0x7fffffff);
         if (rank == 0) record_error(p.err, kDevBadTokenId);
@@ -219,18 +250,14 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, in
         keep = sh.top[lane] == x;
         a = keep ? 1.f : 0.f;
       } else {
-        const T* row = target + lane * p.ld;
-        if (sh.m[lane] == -INFINITY || to_f(row[x]) == -INFINITY) {
+        if (sh.m[lane] == -INFINITY || zx == -INFINITY) {
           a = 0.f;
         } else {
-          double d = log_p(row, lane, x);
-          if (draft != nullptr) {
-            const T* q = draft + lane * p.ld_draft;
-            d = sh.m[n + 1 + lane] == -INFINITY ? INFINITY : d - log_p(q, n + 1 + lane, x);
-          }
+          double d = log_p(zx, lane);
+          if (draft != nullptr) d = sh.m[n + 1 + lane] == -INFINITY ? INFINITY : d - log_p(wx, n + 1 + lane);
           a = d >= 0.0 ? 1.f : expf(static_cast<float>(d));
         }
-        keep = p.uniform[s * D + lane] < a;
+        keep = u < a;
       }
     }
     const unsigned refused = __ballot_sync(0xffffffffu, !keep);
@@ -247,21 +274,33 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, in
     const float* noise = p.gumbel + s * p.ld_gumbel;
     const bool refused = kept < n;
     const T* q = refused && draft != nullptr ? draft + kept * p.ld_draft : nullptr;
-    const int x = refused ? p.ids[s * D + kept] : -1;
+    const int gone = refused ? p.ids[s * D + kept] : -1;
     const float pm = sh.m[kept], pc = sh.c[kept];
     const float qm = q != nullptr ? sh.m[n + 1 + kept] : 0.f, qc = q != nullptr ? sh.c[n + 1 + kept] : 0.f;
     Best rest, whole;
     const int mine = (V + cs - 1) / cs, from = min(V, rank * mine), to = min(V, from + mine);
-    for (int v = from + threadIdx.x; v < to; v += kThreads) {
-      const float z = to_f(last[v]), g = noise[v];
-      whole.take(z + g, v);
-      if (q != nullptr) {
-        const float pv = z == -INFINITY ? 0.f : expf((z - pm) - pc);
-        const float w = to_f(q[v]);
-        const float r = pv - (w == -INFINITY ? 0.f : expf((w - qm) - qc));
-        if (r > 0.f) rest.take(logf(r) + g, v);
-      } else if (refused && v != x && z > -INFINITY) {
-        rest.take(z + g, v);
+    constexpr int kDeep = 8;  // of a thread, on their way (rows start anywhere: element by element)
+#pragma unroll 1
+    for (int at = from + threadIdx.x; at < to; at += kThreads * kDeep) {
+      float z[kDeep], g[kDeep], w[kDeep];
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        const int v = at + kThreads * i;
+        z[i] = v < to ? to_f(last[v]) : -INFINITY;
+        g[i] = v < to ? noise[v] : 0.f;
+        w[i] = q != nullptr && v < to ? to_f(q[v]) : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < kDeep; ++i) {
+        const int v = at + kThreads * i;
+        if (v >= to) continue;
+        whole.take(z[i] + g[i], v);
+        if (q != nullptr) {
+          const float r = (z[i] == -INFINITY ? 0.f : expf((z[i] - pm) - pc)) - (w[i] == -INFINITY ? 0.f : expf((w[i] - qm) - qc));
+          if (r > 0.f) rest.take(logf(r) + g[i], v);
+        } else if (refused && v != gone && z[i] > -INFINITY) {
+          rest.take(z[i] + g[i], v);
+        }
       }
     }
 #pragma unroll
@@ -297,7 +336,7 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, in
       if (p.logp != nullptr)
         p.logp[s * (D + 1) + i] = i > kept                ? 0.f
                                   : sh.m[i] == -INFINITY ? -INFINITY
-                                                          : static_cast<float>(log_p(target + i * p.ld, i, tok));
+                                                          : static_cast<float>(log_p(to_f(target[i * p.ld + tok]), i));
     }
     if (threadIdx.x == 0) p.accepted[s] = kept;
   }
@@ -306,9 +345,9 @@ __global__ void __launch_bounds__(kThreads) verify_kernel(const VerifyArgs p, in
 
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // the fewest CTAs a sequence that fill the device, none with under 1000 tokens
+  // as many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row
   int cs = 1;
-  while (cs < kMaxCluster && a.S * cs < 2 * std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
+  while (cs < kMaxCluster && 2 * a.S * cs <= 2 * std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.S * cs));
   cfg.blockDim = dim3(kThreads);

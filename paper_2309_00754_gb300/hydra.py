@@ -725,51 +725,51 @@ class KvCache:
             raise ValueError(f"data must have {n_pages} pages of {size} bytes, got {data.numel()} bytes")
         self.data, self.kind, self.n_pages, self.page = data, kind, n_pages, page
         self.n_kv_heads, self.head_dim, self.page_bytes = n_kv_heads, head_dim, size
+        self.device = data.get_device()
         self.c = KvCacheC(data.data_ptr(), n_pages, page, n_kv_heads, head_dim, kind)
+        self.ref = ctypes.byref(self.c)
 
 
 def _kv_args(cache, table, cached, lengths, S, L, dev):
-    """What every call with a cache begins with."""
-    if cache.data.get_device() != dev:
-        _on_device(cache.data)
-    if table.dtype is not torch.int32 or table.get_device() != dev:
+    """What every call with a cache begins with. One condition where all is well, as in _arg."""
+    shape, stride = table.shape, table.stride()
+    if not (len(shape) == 2 and table.dtype is torch.int32 and table.get_device() == dev == cache.device and shape[0] == S
+            and (stride[1] == 1 or shape[1] == 1)):
         if table.dtype is not torch.int32 or not table.is_cuda:
             raise ValueError(f"table must be an int32 CUDA tensor, got {table.dtype} on {table.device}")
-        _on_device(table)
-    if table.dim() != 2 or table.shape[0] != S:
-        raise ValueError(f"table must have {S} rows, got shape {tuple(table.shape)}")
-    ld, step = table.stride()
-    if step != 1 and table.shape[1] > 1:
-        raise ValueError("table rows must be unit-stride")
+        _on_device(table, cache.data)
+        raise ValueError(f"table must have {S} rows of unit stride, got shape {tuple(shape)}, strides {stride}")
+    width = shape[1]
     i32 = torch.int32
-    return (ctypes.byref(cache.c), table.data_ptr(), ld if S > 1 else max(ld, table.shape[1]), table.shape[1],
+    return (cache.ref, table.data_ptr(), stride[0] if S > 1 else width, width,
             _arg(cached, i32, S, dev, "cached"), _arg(lengths, i32, S, dev, "lengths"), S, L)
 
 
 def _heads(t, rows, head_dim, dtype, dev, name):
     """(pointer, heads, row stride) of rows of heads, which may be columns of a wider matrix."""
-    if t.dtype is not dtype or t.get_device() != dev:
-        if t.dtype is not dtype or not t.is_cuda:
-            raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
-        _on_device(t)
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] % head_dim != 0:
-        raise ValueError(f"{name} must have {rows} rows of heads of {head_dim}, got shape {tuple(t.shape)}")
-    ld, step = t.stride()
-    if step != 1:
-        raise ValueError(f"{name} rows must be unit-stride")
-    return t.data_ptr(), t.shape[1] // head_dim, ld if rows > 1 else t.shape[1]
+    shape, stride = t.shape, t.stride()
+    if (len(shape) == 2 and t.dtype is dtype and t.get_device() == dev and shape[0] == rows and stride[1] == 1
+            and shape[1] % head_dim == 0):
+        return t.data_ptr(), shape[1] // head_dim, stride[0] if rows > 1 else shape[1]
+    if t.dtype is not dtype or not t.is_cuda:
+        raise ValueError(f"{name} must be a {dtype} CUDA tensor, got {t.dtype} on {t.device}")
+    _on_device(t)
+    raise ValueError(f"{name} must have {rows} unit-stride rows of heads of {head_dim}, got shape {tuple(shape)}, "
+                     f"strides {stride}")
 
 
 def _kv_pair(k, v, rows, cache, dtype, dev, names):
     """(k, v, row stride) of two outputs or inputs of the cache's heads with one stride; either may be None."""
-    got = [None if t is None else _heads(t, rows, cache.head_dim, dtype, dev, n) for t, n in zip((k, v), names)]
-    for g, n in zip(got, names):
-        if g is not None and g[1] != cache.n_kv_heads:
-            raise ValueError(f"{n} must have {cache.n_kv_heads} heads, got {g[1]}")
-    strides = {g[2] for g in got if g is not None}
-    if len(strides) > 1:
-        raise ValueError(f"{names[0]} and {names[1]} must have one row stride")
-    return (*(None if g is None else g[0] for g in got), strides.pop() if strides else cache.n_kv_heads * cache.head_dim)
+    D, heads = cache.head_dim, cache.n_kv_heads
+    pk, hk, ld_k = (None, heads, 0) if k is None else _heads(k, rows, D, dtype, dev, names[0])
+    pv, hv, ld_v = (None, heads, ld_k) if v is None else _heads(v, rows, D, dtype, dev, names[1])
+    if hk != heads or hv != heads:
+        raise ValueError(f"{names[0]} and {names[1]} must have {heads} heads, got {hk} and {hv}")
+    if k is None:
+        ld_k = ld_v
+    if ld_k != ld_v:
+        raise ValueError(f"{names[0]} and {names[1]} must have one row stride, got {ld_k} and {ld_v}")
+    return pk, pv, ld_k or heads * D
 
 
 def hydra_kv_append(cache, table, cached, lengths, S, L, q, k, v, rope_table=None, q_out=None, stream=None):
