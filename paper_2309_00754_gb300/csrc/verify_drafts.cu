@@ -27,22 +27,34 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kMaxRows = 2 * kVerifyMaxDrafts + 1;  // target rows 0..n, then draft rows 0..n-1
 
-// A value with its index; the larger one, of equal ones the lower index.
+// A value with its index, and a logit beside it; the larger value, of equal ones the lower index.
 struct Best {
   float v = -INFINITY;
   int i = INT_MAX;
-  __device__ __forceinline__ void take(float ov, int oi) {
+  float z = -INFINITY;
+  __device__ __forceinline__ void take(float ov, int oi, float oz) {
     if (ov > v || (ov == v && oi < i)) {
       v = ov;
       i = oi;
+      z = oz;
     }
+  }
+  __device__ __forceinline__ void take_lanes(int most) {
+    for (int o = most / 2; o > 0; o >>= 1)
+      take(__shfl_xor_sync(0xffffffffu, v, o), __shfl_xor_sync(0xffffffffu, i, o), __shfl_xor_sync(0xffffffffu, z, o));
   }
 };
 
 // Part of a row: maximum (-FLT_MAX where there is none), sum of exp(z - maximum); greedy: its argmax.
 struct Part {
-  float m = -FLT_MAX, s = 0.f;
-  Best best;
+  float m = -FLT_MAX, s = 0.f, best = -INFINITY;
+  int i = INT_MAX;
+  __device__ __forceinline__ void take(float ov, int oi) {
+    if (ov > best || (ov == best && oi < i)) {
+      best = ov;
+      i = oi;
+    }
+  }
 };
 
 constexpr int kRounds = 4;  // slices of a warp, where there are not many more warps than rows
@@ -85,9 +97,9 @@ __device__ __forceinline__ void add(Part& p, const float (&x)[N], int first) {
 #pragma unroll
   for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
   if constexpr (kArg) {
-    if (top > p.best.v || p.best.i == INT_MAX)
+    if (top > p.best || p.i == INT_MAX)
 #pragma unroll
-      for (int e = 0; e < N; ++e) p.best.take(x[e], first + e);
+      for (int e = 0; e < N; ++e) p.take(x[e], first + e);
   }
   const float now = fmaxf(p.m, top);
   p.s *= exp_fast(p.m - now);
@@ -98,7 +110,7 @@ __device__ __forceinline__ void add(Part& p, const float (&x)[N], int first) {
 
 template <bool kArg>
 __device__ __forceinline__ void merge(Part& p, const Part& o) {
-  if constexpr (kArg) p.best.take(o.best.v, o.best.i);
+  if constexpr (kArg) p.take(o.best, o.i);
   const float now = fmaxf(p.m, o.m);
   p.s = p.s * exp_fast(p.m - now) + o.s * exp_fast(o.m - now);
   p.m = now;
@@ -112,18 +124,18 @@ __device__ __forceinline__ Part warp_merge(Part p) {
     other.m = __shfl_xor_sync(0xffffffffu, p.m, o);
     other.s = __shfl_xor_sync(0xffffffffu, p.s, o);
     if constexpr (kArg) {
-      other.best.v = __shfl_xor_sync(0xffffffffu, p.best.v, o);
-      other.best.i = __shfl_xor_sync(0xffffffffu, p.best.i, o);
+      other.best = __shfl_xor_sync(0xffffffffu, p.best, o);
+      other.i = __shfl_xor_sync(0xffffffffu, p.i, o);
     }
     merge<kArg>(p, other);
   }
   return p;
 }
 
-// [lo, hi) of a row by a warp.
-template <typename T, bool kArg>
+// [lo, hi) of a row by a warp, kDeep vectors a lane on their way.
+template <typename T, bool kArg, int kDeep>
 __device__ __forceinline__ Part scan(const T* row, int lo, int hi, int lane) {
-  constexpr int E = 16 / sizeof(T), kDeep = 4;  // vectors of a lane on their way
+  constexpr int E = 16 / sizeof(T);
   Part p;
   const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row + lo) & 15) / sizeof(T));
   const int head = min(off == 0 ? 0 : E - off, hi - lo);
@@ -171,8 +183,9 @@ __device__ __forceinline__ int ld_cluster(const int* local, unsigned rank) {
   return __float_as_int(ld_cluster_f32(reinterpret_cast<const float*>(local), rank));
 }
 
-template <typename T, bool kGreedy>
-__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p, int cs) {
+// kAlone: a CTA has an SM for itself, and twice the loads on their way.
+template <typename T, bool kGreedy, bool kAlone>
+__global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const VerifyArgs p, int cs) {
   extern __shared__ uint8_t raw_shared[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_shared);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -201,13 +214,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
     }
   }
 
-  // slices of a row: so many that the warps of the cluster have kRounds each where all drafts are there
+  // slices of a row: one for a warp of the cluster, or kRounds where they would not come out even, with all drafts there
   const int warps = cs * kWarps, most = p.draft != nullptr ? 2 * D + 1 : D + 1;
-  const int slices = max(1, (warps >= 16 * most ? warps : kRounds * warps) / most);
+  const int slices = max(1, (warps >= 8 * most ? warps : kRounds * warps) / most);
   for (int i = rank * kWarps + warp, k = 0; i < rows * slices; i += warps, ++k) {
     const int r = i / slices, j = i - r * slices;
     const int lo = static_cast<int>(static_cast<long long>(V) * j / slices), hi = static_cast<int>(static_cast<long long>(V) * (j + 1) / slices);
-    const Part part = scan<T, kGreedy>(row_at(r), lo, hi, lane);
+    const Part part = scan<T, kGreedy, kAlone ? 8 : 4>(row_at(r), lo, hi, lane);
     if (lane == 0) sh.part[warp][k] = part;
   }
   if (cs > 1) cluster_sync_all(); else __syncthreads();
@@ -222,8 +235,8 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
       o.m = c == rank ? from->m : ld_cluster(&from->m, c);
       o.s = c == rank ? from->s : ld_cluster(&from->s, c);
       if (kGreedy) {
-        o.best.v = c == rank ? from->best.v : ld_cluster(&from->best.v, c);
-        o.best.i = c == rank ? from->best.i : ld_cluster(&from->best.i, c);
+        o.best = c == rank ? from->best : ld_cluster(&from->best, c);
+        o.i = c == rank ? from->i : ld_cluster(&from->i, c);
       }
       merge<kGreedy>(all, o);
     }
@@ -232,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
       // a row of nothing but -inf: its sum is 0
       sh.m[r] = all.s == 0.f ? -INFINITY : all.m;
       sh.c[r] = all.s == 0.f ? 0.f : logf(all.s);
-      sh.top[r] = all.best.i == INT_MAX ? 0 : all.best.i;  // (nothing but NaN)
+      sh.top[r] = all.i == INT_MAX ? 0 : all.i;  // (nothing but NaN)
     }
   }
   __syncthreads();
@@ -269,6 +282,7 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
   const int kept = sh.kept;
   const T* last = target + kept * p.ld;
   int next = sh.top[kept];
+  float next_z = 0.f;
 
   if constexpr (!kGreedy) {
     const float* noise = p.gumbel + s * p.ld_gumbel;
@@ -280,74 +294,92 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
     Best rest, whole;
     const int mine = (V + cs - 1) / cs, from = min(V, rank * mine), to = min(V, from + mine);
     constexpr int kDeep = 8;  // of a thread, on their way (rows start anywhere: element by element)
+    // log r is at most log p: where that does not reach the warp's best so far, r is not worked out (it takes as long as all
+    // else). The slack covers the roundings of the bound.
+    float reach = -INFINITY;
 #pragma unroll 1
-    for (int at = from + threadIdx.x; at < to; at += kThreads * kDeep) {
+    for (int first = from + (threadIdx.x & ~31); first < to; first += kThreads * kDeep) {
       float z[kDeep], g[kDeep], w[kDeep];
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) {
-        const int v = at + kThreads * i;
+        const int v = first + lane + kThreads * i;
         z[i] = v < to ? to_f(last[v]) : -INFINITY;
         g[i] = v < to ? noise[v] : 0.f;
         w[i] = q != nullptr && v < to ? to_f(q[v]) : -INFINITY;
       }
 #pragma unroll
       for (int i = 0; i < kDeep; ++i) {
-        const int v = at + kThreads * i;
-        if (v >= to) continue;
-        whole.take(z[i] + g[i], v);
+        const int v = first + lane + kThreads * i;
+        const float t = z[i] + g[i];
+        if (v < to) whole.take(t, v, z[i]);
         if (q != nullptr) {
-          const float r = (z[i] == -INFINITY ? 0.f : expf((z[i] - pm) - pc)) - (w[i] == -INFINITY ? 0.f : expf((w[i] - qm) - qc));
-          if (r > 0.f) rest.take(logf(r) + g[i], v);
+          if (t - pm - pc + 1e-3f + 1e-6f * (fabsf(t) + fabsf(pm)) > reach) {  // (not in a row's end: -inf)
+            const float r = expf((z[i] - pm) - pc) - (w[i] == -INFINITY ? 0.f : expf((w[i] - qm) - qc));
+            if (r > 0.f) rest.take(logf(r) + g[i], v, z[i]);
+          }
         } else if (refused && v != gone && z[i] > -INFINITY) {
-          rest.take(z[i] + g[i], v);
+          rest.take(t, v, z[i]);
         }
       }
-    }
+      if (q != nullptr) {
+        reach = rest.v;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      rest.take(__shfl_xor_sync(0xffffffffu, rest.v, o), __shfl_xor_sync(0xffffffffu, rest.i, o));
-      whole.take(__shfl_xor_sync(0xffffffffu, whole.v, o), __shfl_xor_sync(0xffffffffu, whole.i, o));
+        for (int o = 16; o > 0; o >>= 1) reach = fmaxf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
+      }
     }
+    rest.take_lanes(32);
+    whole.take_lanes(32);
     if (lane == 0) {
       sh.best[0][warp] = rest;
       sh.best[1][warp] = whole;
     }
     __syncthreads();
-    if (threadIdx.x < 2) {
-      Best b = sh.best[threadIdx.x][0];
-      for (int w = 1; w < kWarps; ++w) b.take(sh.best[threadIdx.x][w].v, sh.best[threadIdx.x][w].i);
-      sh.cta_best[threadIdx.x] = b;
+    if (warp < 2) {  // one each
+      Best b = sh.best[warp][lane & (kWarps - 1)];
+      b.take_lanes(kWarps);
+      if (lane == 0) sh.cta_best[warp] = b;
     }
     if (cs > 1) cluster_sync_all(); else __syncthreads();
-    rest = sh.cta_best[0];
-    whole = sh.cta_best[1];
-    if (cs > 1 && rank == 0)
-      for (int c = 1; c < cs; ++c) {
-        rest.take(ld_cluster(&sh.cta_best[0].v, c), ld_cluster(&sh.cta_best[0].i, c));
-        whole.take(ld_cluster(&sh.cta_best[1].v, c), ld_cluster(&sh.cta_best[1].i, c));
-      }
-    // nothing of the residual is left: from the row itself
-    next = refused && rest.i != INT_MAX ? rest.i : whole.i != INT_MAX ? whole.i : 0;
+    if (rank == 0 && warp == 0) {
+      const int c = lane & (cs - 1);
+      auto of = [&](const Best& b) {
+        Best o;
+        o.v = c == 0 ? b.v : ld_cluster(&b.v, c);
+        o.i = c == 0 ? b.i : ld_cluster(&b.i, c);
+        o.z = c == 0 ? b.z : ld_cluster(&b.z, c);
+        o.take_lanes(cs);
+        return o;
+      };
+      const Best r = of(sh.cta_best[0]), all = of(sh.cta_best[1]);
+      // nothing of the residual is left: from the row itself
+      const Best& b = refused && r.i != INT_MAX ? r : all;
+      next = b.i != INT_MAX ? b.i : 0;  // (nothing but NaN)
+      next_z = b.i != INT_MAX ? b.z : to_f(last[0]);
+    }
   }
-  if (rank == 0) {
-    for (int i = threadIdx.x; i <= D; i += kThreads) {
-      const int tok = i < kept ? p.ids[s * D + i] : i == kept ? next : -1;
-      p.tokens[s * (D + 1) + i] = tok;
+  if (rank == 0 && warp == 0) {
+    if constexpr (kGreedy) next_z = to_f(last[next]);
+    for (int i = lane; i <= D; i += 32) {  // (lane: the draft that it has, and D beyond 31)
+      const bool draft_kept = i < kept;
+      p.tokens[s * (D + 1) + i] = draft_kept ? x : i == kept ? next : -1;
       if (p.logp != nullptr)
         p.logp[s * (D + 1) + i] = i > kept                ? 0.f
                                   : sh.m[i] == -INFINITY ? -INFINITY
-                                                          : static_cast<float>(log_p(to_f(target[i * p.ld + tok]), i));
+                                                          : static_cast<float>(log_p(draft_kept ? zx : next_z, i));
     }
-    if (threadIdx.x == 0) p.accepted[s] = kept;
+    if (lane == 0) p.accepted[s] = kept;
   }
   if (cs > 1) cluster_sync_all();  // nobody leaves while its memory is read
 }
 
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // as many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row
+  // as many CTAs a sequence as the device holds at once, none with under 1000 tokens of a row: one an SM, or where that leaves
+  // SMs idle two
+  const int sms = std::max(1, sm_count());
   int cs = 1;
-  while (cs < kMaxCluster && 2 * a.S * cs <= 2 * std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
+  while (cs < kMaxCluster && a.S * cs <= sms && a.V >= 2000 * cs) cs *= 2;
+  const bool alone = a.S * cs <= sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.S * cs));
   cfg.blockDim = dim3(kThreads);
@@ -362,7 +394,8 @@ cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, cs);
+  return alone ? cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy, true>, a, cs)
+               : cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy, false>, a, cs);
 }
 
 }  // namespace
