@@ -13,6 +13,7 @@
 // exchange before every one of them knows where the drafts end. (Cut alike, equal rows have equal sums: a draft model that
 // is the target is never refused.) The row that the last token is drawn from is read a second time, from L2 as a rule.
 #include <algorithm>
+#include <atomic>
 #include <cfloat>
 #include <climits>
 
@@ -57,55 +58,95 @@ struct Part {
   }
 };
 
-constexpr int kRounds = 4;  // slices of a warp, where there are not many more warps than rows
-constexpr int kMaxSlices = kMaxRows / kWarps + 1;
-static_assert(kMaxSlices >= kRounds, "a warp's slices");
+constexpr int kMaxSlices = 6;  // of a warp
+static_assert(kMaxSlices * kWarps >= kMaxRows, "a warp's slices");
 
-struct Shared {
+struct alignas(16) Shared {
   Part part[kWarps][kMaxSlices];  // read by the cluster
   float m[kMaxRows], c[kMaxRows];  // of whole rows: maximum, log of the sum
   int top[kMaxRows];
-  Best best[2][kWarps];
-  Best cta_best[2];  // drawn from the residual, from the row; read by the cluster
+  Best best[kWarps];
+  Best cta_best[2];  // of the first draw, of a second; read by the cluster
   int kept;
 };
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
+// (off by two units in the last place at most, and zero below 2^-126, which no sum of at least 1 sees)
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp_fast(float x) { return exp2_fast(x * kLog2e); }
+
+// Largest of a vector's logits, in their own type for two at once.
 template <typename T>
-__device__ __forceinline__ void unpack(const uint4& v, float (&f)[16 / sizeof(T)]) {
-  const uint32_t r[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    if constexpr (sizeof(T) == 4) {
-      f[q] = __uint_as_float(r[q]);
-    } else {
-      const float2 x = unpack_bf16x2(r[q]);
-      f[2 * q] = x.x;
-      f[2 * q + 1] = x.y;
-    }
+__device__ __forceinline__ float top_of(const uint4& v) {
+  if constexpr (sizeof(T) == 4) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  } else {
+    const auto h = [](const uint32_t& r) { return reinterpret_cast<const __nv_bfloat162&>(r); };
+    const __nv_bfloat162 m = __hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
   }
 }
 
-__device__ __forceinline__ float exp_fast(float x) { return exp2f(x * 1.4426950408889634f); }
-
-// N neighbouring logits more, the first at index `first`.
-template <bool kArg, int N>
-__device__ __forceinline__ void add(Part& p, const float (&x)[N], int first) {
-  float top = x[0];
+// The sum of exp(z - m) of a vector's logits, in two halves.
+template <typename T>
+__device__ __forceinline__ float2 exp_sum(const uint4& v, float m, float2 sum) {
+  const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+  const float2 minus = {-m, -m}, log2e = {kLog2e, kLog2e};
+  auto two = [&](float2 z) {
+    const float2 e = mul2(add2(z, minus), log2e);
+    sum = add2(sum, make_float2(exp2_fast(e.x), exp2_fast(e.y)));
+  };
+  if constexpr (sizeof(T) == 4) {
+    two(make_float2(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    two(make_float2(__uint_as_float(r[2]), __uint_as_float(r[3])));
+  } else {
 #pragma unroll
-  for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
-  if constexpr (kArg) {
-    if (top > p.best || p.i == INT_MAX)
-#pragma unroll
-      for (int e = 0; e < N; ++e) p.take(x[e], first + e);
+    for (int q = 0; q < 4; ++q) two(unpack_bf16x2(r[q]));
   }
-  const float now = fmaxf(p.m, top);
-  p.s *= exp_fast(p.m - now);
-  p.m = now;
+  return sum;
+}
+
+// kN vectors more, that of x[q] from index first + q stride on. Of the largest logit only the vector is kept.
+template <typename T, bool kArg, int kN>
+__device__ __forceinline__ void add(Part& p, const uint4 (&x)[kN], int first, int stride) {
+  float top = p.m;
 #pragma unroll
-  for (int e = 0; e < N; ++e) p.s += exp_fast(x[e] - now);
+  for (int q = 0; q < kN; ++q) {
+    const float t = top_of<T>(x[q]);
+    top = fmaxf(top, t);
+    if constexpr (kArg) {
+      if (t > p.best) {
+        p.best = t;
+        p.i = first + q * stride;
+      }
+    }
+  }
+  float2 sum = {0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < kN; ++q) sum = exp_sum<T>(x[q], top, sum);
+  p.s = p.s * exp_fast(p.m - top) + (sum.x + sum.y);
+  p.m = top;
 }
 
 template <bool kArg>
@@ -117,64 +158,121 @@ __device__ __forceinline__ void merge(Part& p, const Part& o) {
 }
 
 template <bool kArg>
-__device__ __forceinline__ Part warp_merge(Part p) {
+__device__ __forceinline__ Part warp_merge(const Part& p) {
+  Part all = p;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) all.m = fmaxf(all.m, __shfl_xor_sync(0xffffffffu, all.m, o));
+  all.s = p.s * exp_fast(p.m - all.m);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    Part other;
-    other.m = __shfl_xor_sync(0xffffffffu, p.m, o);
-    other.s = __shfl_xor_sync(0xffffffffu, p.s, o);
+    all.s += __shfl_xor_sync(0xffffffffu, all.s, o);
     if constexpr (kArg) {
-      other.best = __shfl_xor_sync(0xffffffffu, p.best, o);
-      other.i = __shfl_xor_sync(0xffffffffu, p.i, o);
+      const float best = __shfl_xor_sync(0xffffffffu, all.best, o);
+      all.take(best, __shfl_xor_sync(0xffffffffu, all.i, o));
     }
-    merge<kArg>(p, other);
   }
-  return p;
+  return all;
 }
 
-// [lo, hi) of a row by a warp, kDeep vectors a lane on their way.
-template <typename T, bool kArg, int kDeep>
-__device__ __forceinline__ Part scan(const T* row, int lo, int hi, int lane) {
+// A warp's slices as a stream of rounds: kVecs 16-byte vectors for each of 32 lanes, kAhead rounds on their way in a ring in
+// shared memory, over the ends of slices, too. A lane reads what it put there itself: -inf behind a row's last vector.
+constexpr int kVecs = 4, kAhead = 2, kStages = kAhead + 1;
+constexpr int kRoundVecs = kVecs * 32, kRoundBytes = kRoundVecs * 16;
+
+// A row as 16-byte vectors, with the logits before the first of them and behind the last.
+template <typename T>
+struct Row {
+  static constexpr int E = 16 / sizeof(T);
+  const T* at;
+  int head, vecs, tail;
+  __device__ __forceinline__ Row(const T* row, int V) : at(row) {
+    const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    head = min(off == 0 ? 0 : E - off, V);
+    vecs = (V - head) / E;
+    tail = V - head - vecs * E;
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void fetch(bool there, uint8_t* dst, const T* src) {
+  constexpr uint32_t kNone = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %0, 0;\n\t@p cp.async.cg.shared.global [%1], [%2], 16;\n\t"
+      "@!p st.shared.v4.b32 [%1], {%3, %3, %3, %3};\n\t}" ::"r"(static_cast<uint32_t>(there)),
+      "r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(src)), "r"(kNone)
+      : "memory");
+}
+
+// Slices first, first + step, ... below `total` by a warp, `slices` of `rounds` rounds a row (the last one shorter);
+// done(k, part) for the k-th of them.
+template <typename T, bool kArg, typename RowAt, typename Done>
+__device__ __forceinline__ void scan(int first, int step, int total, int slices, int rounds, int V, uint8_t* ring, int lane,
+                                     RowAt row_at, Done done) {
   constexpr int E = 16 / sizeof(T);
-  Part p;
-  const int off = static_cast<int>((reinterpret_cast<uintptr_t>(row + lo) & 15) / sizeof(T));
-  const int head = min(off == 0 ? 0 : E - off, hi - lo);
-  const int vecs = (hi - lo - head) / E, body = lo + head;
-  if (lane < head) {
-    const float x[1] = {to_f(row[lo + lane])};
-    add<kArg>(p, x, lo + lane);
-  }
-  const uint4* at = reinterpret_cast<const uint4*>(row + body);
-  int v = lane;
+  ring += lane * 16;
+  // what is fetched next: a round of slice `next`, from this lane's `from` with `left` vectors to the row's end
+  int next = first, left = 0, ahead = 0, fill = 0;
+  const T* from = nullptr;
+  auto open = [&]() {
+    for (ahead = 0; next < total; next += step) {
+      const int r = next / slices, skip = (next - r * slices) * rounds * kRoundVecs;
+      const Row<T> row(row_at(r), V);
+      left = row.vecs - skip;
+      ahead = min(rounds, (left + kRoundVecs - 1) / kRoundVecs);
+      if (ahead > 0) {
+        left -= lane;
+        from = row.at + row.head + static_cast<long long>(skip + lane) * E;
+        break;
+      }
+    }
+  };
+  auto produce = [&]() {
+    if (ahead > 0) {
+#pragma unroll
+      for (int q = 0; q < kVecs; ++q) fetch(q * 32 < left, ring + fill * kRoundBytes + q * 512, from + q * 32 * E);
+      from += kRoundVecs * E;
+      left -= kRoundVecs;
+      if (--ahead == 0) {
+        next += step;
+        open();
+      }
+    }
+    fill = fill + 1 == kStages ? 0 : fill + 1;
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  open();
 #pragma unroll 1
-  for (; v + 32 * (kDeep - 1) < vecs; v += 32 * kDeep) {
-    uint4 raw[kDeep];
+  for (int i = 0; i < kAhead; ++i) produce();
+  int take = 0;
+#pragma unroll 1
+  for (int i = first, k = 0; i < total; i += step, ++k) {
+    const int r = i / slices, j = i - r * slices, skip = j * rounds * kRoundVecs;
+    const Row<T> row(row_at(r), V);
+    // the logits before the first vector with the first slice, those behind the last with the last
+    int edge = -1;
+    if (j == 0 && lane < row.head) edge = lane;
+    if (j == slices - 1 && lane >= 16 && lane - 16 < row.tail) edge = V - row.tail + lane - 16;
+    const float edge_z = edge >= 0 ? to_f(row.at[edge]) : -INFINITY;
+    const int mine = min(rounds, (row.vecs - skip + kRoundVecs - 1) / kRoundVecs);
+    Part p;
+#pragma unroll 1
+    for (int v = 0; v < mine; ++v) {
+      produce();
+      asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
+      uint4 x[kVecs];
 #pragma unroll
-    for (int d = 0; d < kDeep; ++d) raw[d] = at[v + 32 * d];
-#pragma unroll
-    for (int d = 0; d < kDeep; ++d) {
-      float x[E];
-      unpack<T>(raw[d], x);
-      add<kArg>(p, x, body + (v + 32 * d) * E);
+      for (int q = 0; q < kVecs; ++q) x[q] = *reinterpret_cast<const uint4*>(ring + take * kRoundBytes + q * 512);
+      take = take + 1 == kStages ? 0 : take + 1;
+      add<T, kArg>(p, x, row.head + (skip + v * kRoundVecs + lane) * E, 32 * E);
     }
-  }
-  uint4 raw[kDeep];
-#pragma unroll
-  for (int d = 0; d < kDeep; ++d)
-    if (v + 32 * d < vecs) raw[d] = at[v + 32 * d];
-#pragma unroll
-  for (int d = 0; d < kDeep; ++d)
-    if (v + 32 * d < vecs) {
-      float x[E];
-      unpack<T>(raw[d], x);
-      add<kArg>(p, x, body + (v + 32 * d) * E);
+    if (edge >= 0) {
+      if constexpr (kArg) p.take(edge_z, edge);
+      const float now = fmaxf(p.m, edge_z);
+      p.s = p.s * exp_fast(p.m - now) + exp_fast(edge_z - now);
+      p.m = now;
     }
-  const int tail = body + vecs * E + lane;
-  if (tail < hi) {
-    const float x[1] = {to_f(row[tail])};
-    add<kArg>(p, x, tail);
+    done(k, warp_merge<kArg>(p));
   }
-  return warp_merge<kArg>(p);
 }
 
 // (the address of `local` in another CTA)
@@ -183,10 +281,9 @@ __device__ __forceinline__ int ld_cluster(const int* local, unsigned rank) {
   return __float_as_int(ld_cluster_f32(reinterpret_cast<const float*>(local), rank));
 }
 
-// kAlone: a CTA has an SM for itself, and twice the loads on their way.
-template <typename T, bool kGreedy, bool kAlone>
-__global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const VerifyArgs p, int cs) {
-  extern __shared__ uint8_t raw_shared[];
+template <typename T, bool kGreedy>
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p, int cs, int slices, int rounds) {
+  extern __shared__ __align__(16) uint8_t raw_shared[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_shared);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = cs > 1 ? static_cast<int>(cluster_rank()) : 0;
@@ -214,15 +311,12 @@ __global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const 
     }
   }
 
-  // slices of a row: one for a warp of the cluster, or kRounds where they would not come out even, with all drafts there
-  const int warps = cs * kWarps, most = p.draft != nullptr ? 2 * D + 1 : D + 1;
-  const int slices = max(1, (warps >= 8 * most ? warps : kRounds * warps) / most);
-  for (int i = rank * kWarps + warp, k = 0; i < rows * slices; i += warps, ++k) {
-    const int r = i / slices, j = i - r * slices;
-    const int lo = static_cast<int>(static_cast<long long>(V) * j / slices), hi = static_cast<int>(static_cast<long long>(V) * (j + 1) / slices);
-    const Part part = scan<T, kGreedy, kAlone ? 8 : 4>(row_at(r), lo, hi, lane);
-    if (lane == 0) sh.part[warp][k] = part;
-  }
+  const int warps = cs * kWarps;
+  scan<T, kGreedy>(
+      rank * kWarps + warp, warps, rows * slices, slices, rounds, V,
+      raw_shared + sizeof(Shared) + warp * kStages * kRoundBytes, lane, row_at, [&](int k, const Part& part) {
+        if (lane == 0) sh.part[warp][k] = part;
+      });
   if (cs > 1) cluster_sync_all(); else __syncthreads();
   // a warp a row, a lane a slice of it
   for (int r = warp; r < rows; r += kWarps) {
@@ -241,6 +335,10 @@ __global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const 
       merge<kGreedy>(all, o);
     }
     all = warp_merge<kGreedy>(all);
+    if (kGreedy && all.i != INT_MAX) {  // which one of the vector
+      const int i = all.i + lane;
+      all.i += __ffs(__ballot_sync(0xffffffffu, lane < 16 / static_cast<int>(sizeof(T)) && i < V && to_f(row_at(r)[min(i, V - 1)]) == all.best)) - 1;
+    }
     if (lane == 0) {
       // a row of nothing but -inf: its sum is 0
       sh.m[r] = all.s == 0.f ? -INFINITY : all.m;
@@ -288,74 +386,94 @@ __global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const 
     const float* noise = p.gumbel + s * p.ld_gumbel;
     const bool refused = kept < n;
     const T* q = refused && draft != nullptr ? draft + kept * p.ld_draft : nullptr;
-    const int gone = refused ? p.ids[s * D + kept] : -1;
     const float pm = sh.m[kept], pc = sh.c[kept];
     const float qm = q != nullptr ? sh.m[n + 1 + kept] : 0.f, qc = q != nullptr ? sh.c[n + 1 + kept] : 0.f;
-    Best rest, whole;
     const int mine = (V + cs - 1) / cs, from = min(V, rank * mine), to = min(V, from + mine);
     constexpr int kDeep = 8;  // of a thread, on their way (rows start anywhere: element by element)
-    // log r is at most log p: where that does not reach the warp's best so far, r is not worked out (it takes as long as all
-    // else). The slack covers the roundings of the bound.
-    float reach = -INFINITY;
+    // from the residual; where nothing is left of it, once more from the row itself
+    Best b;
+    for (bool residual = refused;; residual = false) {
+      b = Best();
+      if (residual && q != nullptr) {
+        // log r is at most log p: where that does not reach the warp's best so far, r is not worked out (it takes as long as
+        // all else). The slack covers the roundings of the bound.
+        auto bound = [&](float t) { return t - pm - pc + 1e-3f + 1e-6f * (fabsf(t) + fabsf(pm)); };
+        auto draw = [&](float z, float g, float w, int v) {
+          const float r = expf((z - pm) - pc) - (w == -INFINITY ? 0.f : expf((w - qm) - qc));
+          if (r > 0.f) b.take(logf(r) + g, v, z);
+        };
+        float reach = -INFINITY;
 #pragma unroll 1
-    for (int first = from + (threadIdx.x & ~31); first < to; first += kThreads * kDeep) {
-      float z[kDeep], g[kDeep], w[kDeep];
+        for (int first = from + (threadIdx.x & ~31); first < to; first += kThreads * kDeep) {
+          float z[kDeep], g[kDeep], w[kDeep];
 #pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        const int v = first + lane + kThreads * i;
-        z[i] = v < to ? to_f(last[v]) : -INFINITY;
-        g[i] = v < to ? noise[v] : 0.f;
-        w[i] = q != nullptr && v < to ? to_f(q[v]) : -INFINITY;
-      }
-#pragma unroll
-      for (int i = 0; i < kDeep; ++i) {
-        const int v = first + lane + kThreads * i;
-        const float t = z[i] + g[i];
-        if (v < to) whole.take(t, v, z[i]);
-        if (q != nullptr) {
-          if (t - pm - pc + 1e-3f + 1e-6f * (fabsf(t) + fabsf(pm)) > reach) {  // (not in a row's end: -inf)
-            const float r = expf((z[i] - pm) - pc) - (w[i] == -INFINITY ? 0.f : expf((w[i] - qm) - qc));
-            if (r > 0.f) rest.take(logf(r) + g[i], v, z[i]);
+          for (int i = 0; i < kDeep; ++i) {
+            const int v = first + lane + kThreads * i;
+            z[i] = v < to ? to_f(last[v]) : -INFINITY;
+            g[i] = v < to ? noise[v] : 0.f;
+            w[i] = v < to ? to_f(q[v]) : -INFINITY;
           }
-        } else if (refused && v != gone && z[i] > -INFINITY) {
-          rest.take(t, v, z[i]);
+          // a lane's likeliest first
+          float top = -INFINITY, top_z = -INFINITY, top_w = 0.f, top_g = 0.f;
+          int top_i = -1;
+#pragma unroll
+          for (int i = 0; i < kDeep; ++i)
+            if (z[i] + g[i] > top) {
+              top = z[i] + g[i];
+              top_z = z[i];
+              top_g = g[i];
+              top_w = w[i];
+              top_i = i;
+            }
+          if (bound(top) > reach) draw(top_z, top_g, top_w, first + lane + kThreads * top_i);
+          reach = fmaxf(reach, b.v);
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) reach = fmaxf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
+#pragma unroll
+          for (int i = 0; i < kDeep; ++i)
+            if (i != top_i && bound(z[i] + g[i]) > reach) draw(z[i], g[i], w[i], first + lane + kThreads * i);
+        }
+      } else {
+        const int gone = residual ? p.ids[s * D + kept] : -1;
+#pragma unroll 1
+        for (int first = from + static_cast<int>(threadIdx.x); first < to; first += kThreads * kDeep) {
+          float z[kDeep], g[kDeep];
+#pragma unroll
+          for (int i = 0; i < kDeep; ++i) {
+            const int v = first + kThreads * i;
+            z[i] = v < to ? to_f(last[v]) : -INFINITY;
+            g[i] = v < to ? noise[v] : 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < kDeep; ++i)
+            if (const int v = first + kThreads * i; z[i] + g[i] > b.v && v != gone) {
+              b.v = z[i] + g[i];
+              b.i = v;
+              b.z = z[i];
+            }
         }
       }
-      if (q != nullptr) {
-        reach = rest.v;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) reach = fmaxf(reach, __shfl_xor_sync(0xffffffffu, reach, o));
+      b.take_lanes(32);
+      if (lane == 0) sh.best[warp] = b;
+      __syncthreads();
+      if (warp == 0) {
+        b = sh.best[lane & (kWarps - 1)];
+        b.take_lanes(kWarps);
+        if (lane == 0) sh.cta_best[residual] = b;
       }
+      if (cs > 1) cluster_sync_all(); else __syncthreads();
+      if (residual || (rank == 0 && warp == 0)) {
+        const int c = lane & (cs - 1);
+        const Best& of = sh.cta_best[residual];
+        b.v = c == rank ? of.v : ld_cluster(&of.v, c);
+        b.i = c == rank ? of.i : ld_cluster(&of.i, c);
+        b.z = c == rank ? of.z : ld_cluster(&of.z, c);
+        b.take_lanes(cs);
+      }
+      if (!residual || b.i != INT_MAX) break;
     }
-    rest.take_lanes(32);
-    whole.take_lanes(32);
-    if (lane == 0) {
-      sh.best[0][warp] = rest;
-      sh.best[1][warp] = whole;
-    }
-    __syncthreads();
-    if (warp < 2) {  // one each
-      Best b = sh.best[warp][lane & (kWarps - 1)];
-      b.take_lanes(kWarps);
-      if (lane == 0) sh.cta_best[warp] = b;
-    }
-    if (cs > 1) cluster_sync_all(); else __syncthreads();
-    if (rank == 0 && warp == 0) {
-      const int c = lane & (cs - 1);
-      auto of = [&](const Best& b) {
-        Best o;
-        o.v = c == 0 ? b.v : ld_cluster(&b.v, c);
-        o.i = c == 0 ? b.i : ld_cluster(&b.i, c);
-        o.z = c == 0 ? b.z : ld_cluster(&b.z, c);
-        o.take_lanes(cs);
-        return o;
-      };
-      const Best r = of(sh.cta_best[0]), all = of(sh.cta_best[1]);
-      // nothing of the residual is left: from the row itself
-      const Best& b = refused && r.i != INT_MAX ? r : all;
-      next = b.i != INT_MAX ? b.i : 0;  // (nothing but NaN)
-      next_z = b.i != INT_MAX ? b.z : to_f(last[0]);
-    }
+    next = b.i != INT_MAX ? b.i : 0;  // (nothing but NaN and -inf)
+    next_z = b.i != INT_MAX ? b.z : to_f(last[0]);
   }
   if (rank == 0 && warp == 0) {
     if constexpr (kGreedy) next_z = to_f(last[next]);
@@ -374,16 +492,36 @@ __global__ void __launch_bounds__(kThreads, kAlone ? 1 : 2) verify_kernel(const 
 
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // as many CTAs a sequence as the device holds at once, none with under 1000 tokens of a row: one an SM, or where that leaves
-  // SMs idle two
-  const int sms = std::max(1, sm_count());
+  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row
   int cs = 1;
-  while (cs < kMaxCluster && a.S * cs <= sms && a.V >= 2000 * cs) cs *= 2;
-  const bool alone = a.S * cs <= sms;
+  while (cs < kMaxCluster && a.S * cs <= std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
+  // Slices of a row: t for each of the cluster's warps with all drafts there, t such that they come out with the fewest rounds,
+  // a slice's end counted as one.
+  const int warps = cs * kWarps, most = static_cast<int>(a.draft != nullptr ? 2 * a.D + 1 : a.D + 1);
+  const int all = static_cast<int>((a.V + kRoundVecs * Row<T>::E - 1) / (kRoundVecs * Row<T>::E));  // rounds of a row
+  int slices = 1, rounds = all, least = INT_MAX;
+  for (int t = 1; t <= kMaxSlices; ++t) {
+    if (t * warps < most) continue;
+    const int of = (all + t * warps / most - 1) / (t * warps / most);
+    if (t * (of + 1) < least) {
+      least = t * (of + 1);
+      rounds = of;
+      slices = (all + of - 1) / of;
+    }
+  }
+  constexpr int kSmem = sizeof(Shared) + kWarps * kStages * kRoundBytes;
+  static std::atomic<bool> attr_set[64];  // the shared-memory limit is a per-device attribute; host threads may ask at once
+  int dev = 0;
+  if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess || dev >= 64) return e == cudaSuccess ? cudaErrorInvalidDevice : e;
+  if (!attr_set[dev]) {
+    if (cudaError_t e = cudaFuncSetAttribute(verify_kernel<T, kGreedy>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); e != cudaSuccess)
+      return e;
+    attr_set[dev] = true;
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(a.S * cs));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Shared);
+  cfg.dynamicSmemBytes = kSmem;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -394,8 +532,7 @@ cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return alone ? cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy, true>, a, cs)
-               : cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy, false>, a, cs);
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, cs, slices, rounds);
 }
 
 }  // namespace
