@@ -10,15 +10,12 @@
 namespace hydra {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kPer = 4;  // heads of a warp, where there are many
+constexpr int64_t kManyUnits = 20000;
+constexpr int kBlock = 8;  // tokens of a warp, from a multiple of 8 on: half of a tile
 
-// The 16 channels of a lane: 8 from 8 j on, and 8 from D/2 + 8 j on.
-template <int kDh>
-struct Half {
-  static constexpr int kLanes = kDh / 16;  // of a head
-};
-
-__device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
+__device__ __forceinline__ void unpack8(const uint4& v, float* f) {
   const uint32_t r[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -27,173 +24,340 @@ __device__ __forceinline__ void unpack8(const uint4& v, float (&f)[8]) {
     f[2 * i + 1] = x.y;
   }
 }
-__device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
+__device__ __forceinline__ uint4 pack8(const float* f) {
   return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
 }
 
-// Of a group of channels, from the least and the largest value (0 among them).
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// Of a group of channels: the least and the largest value (0 among them); `hi` is NaN where one of them is.
+struct Range {
+  float lo = 0.f, hi = 0.f;
+  __device__ __forceinline__ void take(float x) {
+    lo = fminf(lo, x);
+    hi = max_or_nan(hi, x);
+  }
+};
+// over the lanes that differ in the bits of kFrom, 2 kFrom, ... kTo
+template <int kFrom, int kTo, int kN>
+__device__ __forceinline__ void take_lanes(Range (&r)[kN]) {
+#pragma unroll
+  for (int o = kFrom; o <= kTo; o <<= 1)
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      r[i].lo = fminf(r[i].lo, __shfl_xor_sync(0xffffffffu, r[i].lo, o));
+      r[i].hi = max_or_nan(r[i].hi, __shfl_xor_sync(0xffffffffu, r[i].hi, o));
+    }
+}
+
 struct Quant {
-  float scale, zero;
-  __device__ __forceinline__ Quant(float lo, float hi) {
+  float scale, zero;  // scale 0 or NaN: all codes are 0
+  __device__ __forceinline__ explicit Quant(const Range& r) {
     // (halves: the difference of two large values passes fp32)
-    scale = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(hi * 0.5f, lo * 0.5f), 2.0f / 15.0f)));
-    zero = scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-lo, scale)), 0.f), 15.f) : 0.f;
+    scale = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(r.hi * 0.5f, r.lo * 0.5f), 2.0f / 15.0f)));
+    scale = fmaf(scale, 0.f, scale);  // infinite only with an infinity among the channels: NaN then, too
+    zero = scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-r.lo, scale)), 0.f), 15.f) : 0.f;
   }
   __device__ __forceinline__ uint32_t code(float x) const {
     if (!(scale > 0.f)) return 0;
     return static_cast<uint32_t>(fminf(fmaxf(rintf(__fdiv_rn(x, scale)) + zero, 0.f), 15.f));
   }
+  // Codes of 8 channels, the first in the lowest bits. By the reciprocal, x / scale is off by less than 2^-19 (it is at
+  // most 16); where that could turn the rounding, by the division.
+  __device__ __forceinline__ uint32_t codes(const float* x) const {
+    constexpr float kMagic = 12582912.f;  // 1.5 2^23: what is added to it is rounded to an integer in the low bits
+    constexpr uint32_t kMagicBits = 0x4b400000u;
+    const bool usual = scale > 1e-30f && scale < 1e30f;
+    const float inv = __frcp_rn(scale), magic = kMagic + zero;
+    uint32_t w = 0;
+    float off = 0.f;
+#pragma unroll
+    for (int i = 7; i >= 0; --i) {
+      const float t = fmaf(x[i], inv, magic);
+      off = fmaxf(off, fabsf(fmaf(x[i], inv, magic - t)));
+      w = w * 16 + __float_as_uint(fminf(fmaxf(t, kMagic), kMagic + 15.f));
+    }
+    w -= kMagicBits * 0x11111111u;
+    if (!usual || off > 0.49999f) {
+      uint32_t close = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float t = fmaf(x[i], inv, magic);
+        if (!usual || fabsf(fmaf(x[i], inv, magic - t)) > 0.49999f) close |= 1u << i;
+      }
+#pragma unroll 1
+      for (; close != 0; close &= close - 1) {  // (one copy of the division: a short call waits for its instructions)
+        const int at = __ffs(close) - 1;
+        float one = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) one = at == i ? x[i] : one;
+        w = (w & ~(15u << (4 * at))) | code(one) << (4 * at);
+      }
+    }
+    return w;
+  }
+  __device__ __forceinline__ uint32_t scale_bits() const { return __bfloat16_as_ushort(__float2bfloat16_rn(scale)); }
+  __device__ __forceinline__ uint32_t zero_bits() const { return 17u * static_cast<uint32_t>(zero); }
 };
 
-// A token's head to its place in the tile. `a`, `b`: the lane's channels from 8 j and D/2 + 8 j on.
-template <int kDh, bool kInt4>
-__device__ __forceinline__ void store_head(uint8_t* tile, int token, bool value, int j, const float (&a)[8],
-                                           const float (&b)[8], bool there) {
-  using Tile = KvTile<kDh, kInt4>;
-  constexpr int kLanes = Half<kDh>::kLanes;
-  if constexpr (kInt4) {
-    constexpr int kGroups = Tile::kGroups;
-    // NaN, which fmin and fmax drop, and infinities make the scale NaN
-    float lo[2] = {0.f, 0.f}, hi[2] = {0.f, 0.f}, sick[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      lo[0] = fminf(lo[0], a[i]);
-      hi[0] = fmaxf(hi[0], a[i]);
-      lo[1] = fminf(lo[1], b[i]);
-      hi[1] = fmaxf(hi[1], b[i]);
-      sick[0] += a[i] * 0.f;
-      sick[1] += b[i] * 0.f;
-    }
-    if constexpr (kGroups == 1) {
-      lo[0] = fminf(lo[0], lo[1]);
-      hi[0] = fmaxf(hi[0], hi[1]);
-      sick[0] += sick[1];
-    }
-#pragma unroll
-    for (int off = kLanes / 2; off > 0; off >>= 1)
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) {
-        lo[g] = fminf(lo[g], __shfl_xor_sync(0xffffffffu, lo[g], off));
-        hi[g] = fmaxf(hi[g], __shfl_xor_sync(0xffffffffu, hi[g], off));
-        sick[g] += __shfl_xor_sync(0xffffffffu, sick[g], off);
-      }
-    if (!there) return;
-    Quant qa(lo[0], hi[0]), qb(lo[kGroups - 1], hi[kGroups - 1]);
-    qa.scale += sick[0];
-    qb.scale += sick[kGroups - 1];
-    uint32_t wa = 0, wb = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      wa |= qa.code(a[i]) << (4 * i);
-      wb |= qb.code(b[i]) << (4 * i);
-    }
-    const int da = 8 * j, db = kDh / 2 + 8 * j;
-    if (!value) {
-      *reinterpret_cast<uint32_t*>(tile + Tile::key(token, da)) = wa;
-      *reinterpret_cast<uint32_t*>(tile + Tile::key(token, db)) = wb;
-    } else {
-      *reinterpret_cast<uint16_t*>(tile + Tile::value(token, da)) = static_cast<uint16_t>(wa);
-      *reinterpret_cast<uint16_t*>(tile + Tile::value(token, da + 4)) = static_cast<uint16_t>(wa >> 16);
-      *reinterpret_cast<uint16_t*>(tile + Tile::value(token, db)) = static_cast<uint16_t>(wb);
-      *reinterpret_cast<uint16_t*>(tile + Tile::value(token, db + 4)) = static_cast<uint16_t>(wb >> 16);
-    }
-    if (j < kGroups) {
-      const Quant& q = j == 0 ? qa : qb;
-      *reinterpret_cast<__nv_bfloat16*>(tile + Tile::scale(token, value, j)) = __float2bfloat16_rn(q.scale);
-      *reinterpret_cast<uint16_t*>(tile + Tile::zero(token, value, j)) =
-          static_cast<uint16_t>(17u * static_cast<uint32_t>(q.scale > 0.f ? q.zero : 0.f));
-    }
-  } else {
-    if (!there) return;
-    const int d[2] = {8 * j, kDh / 2 + 8 * j};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const float(&x)[8] = h == 0 ? a : b;
-      if (!value) {
-        *reinterpret_cast<uint4*>(tile + Tile::key(token, d[h])) = pack8(x);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *reinterpret_cast<__nv_bfloat16*>(tile + Tile::value(token, d[h] + (i & 4)) + 4 * (i & 3)) = __float2bfloat16_rn(x[i]);
-      }
-    }
+// The tokens of a warp: `slot` of the first (maybe below 0), and what the call says of their sequence.
+struct Block {
+  int s, first;
+  KvSeq seq;
+  __device__ __forceinline__ Block(const KvBatch& b, int blocks, long long positions, int* err) {
+    s = static_cast<int>(blockIdx.x) / blocks;
+    seq = kv_seq(b, s, positions, err);
+    first = (static_cast<int>(blockIdx.x) - s * blocks) * kBlock - (seq.cached & (kBlock - 1));
   }
-}
+};
 
-// One row (token slot) a CTA in x, kThreads / kLanes heads in y: the queries', then the keys' and values'.
+// A warp has 8 tokens of up to `per` heads of a kind. Queries and keys: lane (token lane / 4, part t = lane % 4) has channels
+// D/8 t .. and D/2 + D/8 t .., which rotate together. Values: lane (g = lane / 4, t = lane % 4) has tokens 2 t and 2 t + 1,
+// channels 8 g .. of each 64. So a lane's codes are 16 bytes of the tile (D = 64: 8) where it has both tokens, and a warp's
+// lie side by side.
 template <int kDh, bool kInt4>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs p) {
-  constexpr int kLanes = Half<kDh>::kLanes;
-  const int j = threadIdx.x % kLanes;
-  const int head = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes;
-  const int heads = static_cast<int>(p.n_heads), kv = p.cache.kv_heads;
-  const long long row = blockIdx.x;
-  const int s = static_cast<int>(row / p.batch.L), t = static_cast<int>(row % p.batch.L);
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs p, int blocks, int per) {
+  using Tile = KvTile<kDh, kInt4>;
+  constexpr int kGroups = kDh / kKvGroup, kRun = kDh / 8, kRaw = 2 * kGroups;
+  const int lane = threadIdx.x & 31, quad = lane >> 2, t = lane & 3;
+  const int heads = p.q_out != nullptr ? static_cast<int>(p.n_heads) : 0, kv = p.cache.kv_heads;
+  const int q_units = (heads + per - 1) / per, kv_units = (kv + per - 1) / per;
+  const int unit = blockIdx.y * kWarps + (threadIdx.x >> 5);
   pdl_wait();
   pdl_launch_dependents();
-  const bool there = head < heads + 2 * kv;
-  const bool query = head < heads, value = head >= heads + kv;
+  if (unit >= q_units + 2 * kv_units) return;
+  const bool value = unit < kv_units, query = unit >= 2 * kv_units;  // (what takes longest first)
+  int head = per * (value ? unit : query ? unit - 2 * kv_units : unit - kv_units);
+  const int end = min(head + per, query ? heads : kv);
   const long long positions = p.batch.max_pages << p.cache.page_bits;
-  const KvSeq seq = kv_seq(p.batch, s, p.rope != nullptr ? min(positions, static_cast<long long>(p.rope_len)) : positions, p.err);
-  if (t >= seq.n || !seq.ok) {
-    if (there && query && p.q_out != nullptr) {
-      const uint32_t fill = t < seq.n ? 0x7fff7fffu : 0u;  // NaN, or an empty slot
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.q_out) + row * p.ld_q_out + head * kDh + 8 * j;
-      *reinterpret_cast<uint4*>(out) = make_uint4(fill, fill, fill, fill);
-      *reinterpret_cast<uint4*>(out + kDh / 2) = make_uint4(fill, fill, fill, fill);
+  const Block at(p.batch, blocks, p.rope != nullptr ? min(positions, static_cast<long long>(p.rope_len)) : positions, p.err);
+  const int n = at.seq.ok ? at.seq.n : 0, L = static_cast<int>(p.batch.L);
+  const long long row0 = static_cast<long long>(at.s) * L;
+
+  if (!value) {
+    const int slot = at.first + quad, pos = at.seq.cached + slot;
+    const long long row = row0 + slot;
+    const bool there = slot >= 0 && slot < n;
+    __nv_bfloat16* q_out = static_cast<__nv_bfloat16*>(p.q_out) + row * p.ld_q_out + kRun * t;
+    if (query && !there && slot >= 0 && slot < L) {
+      const uint32_t fill = slot < at.seq.n ? 0x7fff7fffu : 0u;  // NaN, or an empty slot
+      for (int h = head; h < end; ++h)
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i)
+          *reinterpret_cast<uint4*>(q_out + h * kDh + (i / kGroups) * (kDh / 2) + (i % kGroups) * 8) = make_uint4(fill, fill, fill, fill);
+    }
+    if (!__any_sync(0xffffffffu, there)) return;
+    const __nv_bfloat16* x = query ? static_cast<const __nv_bfloat16*>(p.q) + row * p.ld_q : static_cast<const __nv_bfloat16*>(p.k) + row * p.ld_kv;
+    x += kRun * t;
+    uint4 raw[kRaw] = {};
+    auto load = [&](int h) {
+      if (there)
+#pragma unroll
+        for (int i = 0; i < kRaw; ++i)
+          raw[i] = *reinterpret_cast<const uint4*>(x + h * kDh + (i / kGroups) * (kDh / 2) + (i % kGroups) * 8);
+    };
+    load(head);
+    float4 rope[kRun / 2] = {};
+    if (p.rope != nullptr && there) {
+      const float4* r = reinterpret_cast<const float4*>(p.rope + (static_cast<long long>(pos) * (kDh / 2) + kRun * t) * 2);
+#pragma unroll
+      for (int i = 0; i < kRun / 2; ++i) rope[i] = r[i];
+    }
+    const int page = there && !query ? kv_page(p.batch, p.cache, at.s, pos, p.err) : -1;
+#pragma unroll 1
+    for (; head < end; ++head) {
+      float a[kRun], b[kRun];
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) {
+        unpack8(raw[i], a + 8 * i);
+        unpack8(raw[kGroups + i], b + 8 * i);
+      }
+      if (head + 1 < end) load(head + 1);
+      if (p.rope != nullptr) {
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          const float c = i & 1 ? rope[i / 2].z : rope[i / 2].x, sn = i & 1 ? rope[i / 2].w : rope[i / 2].y;
+          const float x1 = a[i], x2 = b[i];
+          a[i] = __fsub_rn(__fmul_rn(x1, c), __fmul_rn(x2, sn));
+          b[i] = __fadd_rn(__fmul_rn(x1, sn), __fmul_rn(x2, c));
+        }
+      }
+      if (query) {
+        if (there)
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            *reinterpret_cast<uint4*>(q_out + head * kDh + 8 * i) = pack8(a + 8 * i);
+            *reinterpret_cast<uint4*>(q_out + head * kDh + kDh / 2 + 8 * i) = pack8(b + 8 * i);
+          }
+        continue;
+      }
+      const int token = pos & (kKvTile - 1);
+      uint8_t* tile = page >= 0 ? kv_tile<Tile>(p.cache, page, head, pos) : nullptr;
+      if constexpr (!kInt4) {
+        if (tile != nullptr)
+#pragma unroll
+          for (int i = 0; i < kGroups; ++i) {
+            *reinterpret_cast<uint4*>(tile + Tile::key(token, kRun * t + 8 * i)) = pack8(a + 8 * i);
+            *reinterpret_cast<uint4*>(tile + Tile::key(token, kDh / 2 + kRun * t + 8 * i)) = pack8(b + 8 * i);
+          }
+      } else {
+        Range range[kGroups];
+#pragma unroll
+        for (int i = 0; i < kRun; ++i) {
+          range[0].take(a[i]);
+          range[kGroups - 1].take(b[i]);
+        }
+        take_lanes<1, 2>(range);
+        const Quant qa(range[0]), qb(range[kGroups - 1]);
+        if (tile != nullptr) {
+          if constexpr (kGroups == 2) {
+            *reinterpret_cast<uint4*>(tile + Tile::key(token, kRun * t)) = make_uint4(qa.codes(a), qa.codes(a + 8), qb.codes(b), qb.codes(b + 8));
+            if (t == 0) {
+              *reinterpret_cast<uint32_t*>(tile + Tile::scale(token, false, 0)) = qa.scale_bits() | qb.scale_bits() << 16;
+              *reinterpret_cast<uint32_t*>(tile + Tile::zero(token, false, 0)) = qa.zero_bits() | qb.zero_bits() << 16;
+            }
+          } else {
+            *reinterpret_cast<uint32_t*>(tile + Tile::key(token, kRun * t)) = qa.codes(a);
+            *reinterpret_cast<uint32_t*>(tile + Tile::key(token, kDh / 2 + kRun * t)) = qa.codes(b);
+            if (t == 0) {
+              *reinterpret_cast<uint16_t*>(tile + Tile::scale(token, false, 0)) = static_cast<uint16_t>(qa.scale_bits());
+              *reinterpret_cast<uint16_t*>(tile + Tile::zero(token, false, 0)) = static_cast<uint16_t>(qa.zero_bits());
+            }
+          }
+        }
+      }
     }
     return;
   }
-  const int pos = seq.cached + t;
-  float a[8] = {}, b[8] = {};
-  if (there) {
-    const __nv_bfloat16* x = query   ? static_cast<const __nv_bfloat16*>(p.q) + row * p.ld_q + head * kDh
-                             : value ? static_cast<const __nv_bfloat16*>(p.v) + row * p.ld_kv + (head - heads - kv) * kDh
-                                     : static_cast<const __nv_bfloat16*>(p.k) + row * p.ld_kv + (head - heads) * kDh;
-    unpack8(*reinterpret_cast<const uint4*>(x + 8 * j), a);
-    unpack8(*reinterpret_cast<const uint4*>(x + kDh / 2 + 8 * j), b);
-  }
-  if (p.rope != nullptr && there && !value) {
-    const float4* r = reinterpret_cast<const float4*>(p.rope + (static_cast<long long>(pos) * (kDh / 2) + 8 * j) * 2);
+
+  const int slot = at.first + 2 * t, pos = at.seq.cached + slot;  // of the first of two tokens (even)
+  const bool there[2] = {slot >= 0 && slot < n, slot + 1 >= 0 && slot + 1 < n};
+  const bool any[2] = {__any_sync(0xffffffffu, there[0]) != 0, __any_sync(0xffffffffu, there[1]) != 0};  // of the warp's
+  if (!any[0] && !any[1]) return;
+  const __nv_bfloat16* x = static_cast<const __nv_bfloat16*>(p.v) + (row0 + slot) * p.ld_kv + 8 * quad;
+  uint4 raw[2][kGroups] = {};
+  auto load = [&](int h) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float4 cs = r[i];
-      const float c[2] = {cs.x, cs.z}, sn[2] = {cs.y, cs.w};
+    for (int b = 0; b < 2; ++b)
+      if (there[b])
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float x1 = a[2 * i + e], x2 = b[2 * i + e];
-        a[2 * i + e] = __fsub_rn(__fmul_rn(x1, c[e]), __fmul_rn(x2, sn[e]));
-        b[2 * i + e] = __fadd_rn(__fmul_rn(x1, sn[e]), __fmul_rn(x2, c[e]));
+        for (int g = 0; g < kGroups; ++g) raw[b][g] = *reinterpret_cast<const uint4*>(x + b * p.ld_kv + h * kDh + g * kKvGroup);
+  };
+  load(head);
+  const int page = there[0] || there[1] ? kv_page(p.batch, p.cache, at.s, pos + (there[0] ? 0 : 1), p.err) : -1;
+  const int token = pos & (kKvTile - 1);
+#pragma unroll 1
+  for (; head < end; ++head) {
+    uint8_t* tile = page >= 0 ? kv_tile<Tile>(p.cache, page, head, pos) : nullptr;
+    if constexpr (!kInt4) {
+      if (tile != nullptr) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          const uint32_t r[2][4] = {{raw[0][g].x, raw[0][g].y, raw[0][g].z, raw[0][g].w}, {raw[1][g].x, raw[1][g].y, raw[1][g].z, raw[1][g].w}};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {  // 4 channels
+            uint8_t* to = tile + Tile::value(token, g * kKvGroup + 8 * quad + 4 * h);
+            if (there[0] && there[1]) {
+              *reinterpret_cast<uint4*>(to) = make_uint4(
+                  __byte_perm(r[0][2 * h], r[1][2 * h], 0x5410), __byte_perm(r[0][2 * h], r[1][2 * h], 0x7632),
+                  __byte_perm(r[0][2 * h + 1], r[1][2 * h + 1], 0x5410), __byte_perm(r[0][2 * h + 1], r[1][2 * h + 1], 0x7632));
+            } else {
+              const int b = there[0] ? 0 : 1;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const uint32_t two = b == 0 ? r[0][2 * h + i / 2] : r[1][2 * h + i / 2];
+                reinterpret_cast<uint16_t*>(to)[2 * i + b] = static_cast<uint16_t>(i & 1 ? two >> 16 : two);
+              }
+            }
+          }
+        }
+      }
+      if (head + 1 < end) load(head + 1);
+    } else {
+      float v[2][kGroups][8];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) unpack8(raw[b][g], v[b][g]);
+      if (head + 1 < end) load(head + 1);
+      uint32_t w[2][kGroups] = {}, scales[2] = {}, zeros[2] = {};
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        if (!(b == 0 ? any[0] : any[1])) continue;
+        Range range[kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) range[g].take(v[b][g][i]);
+        take_lanes<4, 16>(range);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          const Quant q(range[g]);
+          w[b][g] = q.codes(v[b][g]);
+          scales[b] |= q.scale_bits() << (16 * g);
+          zeros[g] |= q.zero_bits() << (16 * b);
+        }
+      }
+      if (tile != nullptr) {
+        uint8_t* to = tile + Tile::value(token, 8 * quad);
+        if (there[0] && there[1]) {
+          uint32_t piece[2 * kGroups];
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            piece[2 * g] = __byte_perm(w[0][g], w[1][g], 0x5410);
+            piece[2 * g + 1] = __byte_perm(w[0][g], w[1][g], 0x7632);
+          }
+          if constexpr (kGroups == 2)
+            *reinterpret_cast<uint4*>(to) = make_uint4(piece[0], piece[1], piece[2], piece[3]);
+          else
+            *reinterpret_cast<uint2*>(to) = make_uint2(piece[0], piece[1]);
+        } else {
+          const int b = there[0] ? 0 : 1;
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            const uint32_t one = b == 0 ? w[0][g] : w[1][g];
+            reinterpret_cast<uint16_t*>(to)[4 * g + b] = static_cast<uint16_t>(one);
+            reinterpret_cast<uint16_t*>(to)[4 * g + 2 + b] = static_cast<uint16_t>(one >> 16);
+          }
+        }
+        if (quad < 2 && there[quad]) {  // a lane a token
+          const uint32_t sc = quad == 0 ? scales[0] : scales[1];
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            *reinterpret_cast<uint16_t*>(tile + Tile::scale(token + quad, true, g)) = static_cast<uint16_t>(sc >> (16 * g));
+            *reinterpret_cast<uint16_t*>(tile + Tile::zero(token + quad, true, g)) = static_cast<uint16_t>(zeros[g] >> (16 * quad));
+          }
+        }
       }
     }
   }
-  if (there && query && p.q_out != nullptr) {
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.q_out) + row * p.ld_q_out + head * kDh + 8 * j;
-    *reinterpret_cast<uint4*>(out) = pack8(a);
-    *reinterpret_cast<uint4*>(out + kDh / 2) = pack8(b);
-  }
-  const int page = there && !query ? kv_page(p.batch, p.cache, s, pos, p.err) : -1;
-  uint8_t* tile = page < 0 ? nullptr
-                           : kv_tile<KvTile<kDh, kInt4>>(p.cache, page, value ? head - heads - kv : head - heads, pos);
-  store_head<kDh, kInt4>(tile, pos % kKvTile, value, j, a, b, page >= 0);  // (shuffles: by every lane)
 }
 
-__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) { *reinterpret_cast<uint4*>(p) = pack8(x); }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x) { *reinterpret_cast<uint4*>(p) = pack8(x); }
+__device__ __forceinline__ void store8(float* p, const float* x) {
   reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
   reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
 
-// Eight channels a thread, a row a CTA in x.
+// What 8 codes stand for, from a group's scale and zero point (17 times it).
+__device__ __forceinline__ void values8(uint32_t w, uint32_t scale_bits, uint32_t zero_bits, float* x) {
+  const float scale = __uint_as_float(scale_bits << 16), minus = -8388608.f - static_cast<float>(zero_bits & 15);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = scale * (__uint_as_float(0x4b000000u | ((w >> (4 * i)) & 15)) + minus);  // 2^23 + code
+}
+
+// A warp has 8 tokens of a head's keys or values, its lanes the channels as above (keys: those of one 16-byte piece).
 template <int kDh, bool kInt4, typename Out>
-__global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvReadArgs p) {
+__global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvReadArgs p, int blocks) {
   using Tile = KvTile<kDh, kInt4>;
-  constexpr int kLanes = kDh / 8;
-  const int j = threadIdx.x % kLanes;
-  const int unit = blockIdx.y * (kThreads / kLanes) + threadIdx.x / kLanes;
+  constexpr int kGroups = kDh / kKvGroup;
+  const int lane = threadIdx.x & 31, quad = lane >> 2, t = lane & 3;
   const int kv = p.cache.kv_heads;
-  const long long row = blockIdx.x;
-  const int s = static_cast<int>(row / p.batch.L), t = static_cast<int>(row % p.batch.L);
+  const int unit = blockIdx.y * kWarps + (threadIdx.x >> 5);
   pdl_wait();
   pdl_launch_dependents();
   if (unit >= 2 * kv) return;
@@ -201,49 +365,110 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvReadArgs p) {
   const int head = value ? unit - kv : unit;
   Out* out = static_cast<Out*>(value ? p.v : p.k);
   if (out == nullptr) return;
-  out += row * p.ld + head * kDh + 8 * j;
-  const KvSeq seq = kv_seq(p.batch, s, p.batch.max_pages << p.cache.page_bits, p.err);
-  float x[8] = {};
-  if (t < seq.n) {
-    const int pos = seq.cached + t, token = pos & (kKvTile - 1);
-    const int page = seq.ok ? kv_page(p.batch, p.cache, s, pos, p.err) : -1;
-    if (page < 0) {
+  const Block at(p.batch, blocks, p.batch.max_pages << p.cache.page_bits, p.err);
+  const int L = static_cast<int>(p.batch.L);
+  const int slot = at.first + (value ? 2 * t : quad), pos = at.seq.cached + slot, tokens = value ? 2 : 1;
+  bool any = false, in[2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = __int_as_float(0x7fffffff);
+  for (int b = 0; b < 2; ++b) {
+    in[b] = b < tokens && slot + b >= 0 && slot + b < L;
+    any |= in[b] && slot + b < at.seq.n;
+  }
+  const int valid = slot < 0 ? pos + 1 : pos;  // a position that is the sequence's
+  const int page = any && at.seq.ok ? kv_page(p.batch, p.cache, at.s, valid, p.err) : -1;
+  const uint8_t* tile = page >= 0 ? kv_tile<Tile>(p.cache, page, head, valid) : nullptr;
+  out += (static_cast<long long>(at.s) * L + slot) * p.ld + head * kDh;
+  const int token = pos & (kKvTile - 1);
+  // a token's 8 channels from d on
+  auto put = [&](int b, int d, float* x) {
+    if (!in[b]) return;
+    if (slot + b >= at.seq.n || tile == nullptr) {
+      const float fill = slot + b >= at.seq.n ? 0.f : __int_as_float(0x7fffffff);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = fill;
+    }
+    store8(out + b * p.ld + d, x);
+  };
+  if (!value) {
+    if constexpr (kInt4) {
+      uint32_t w[2 * kGroups] = {}, scale = 0, zero = 0;
+      if (tile != nullptr) {
+        if constexpr (kGroups == 2) {
+          const uint4 v = *reinterpret_cast<const uint4*>(tile + Tile::key(token, 16 * t));
+          w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+          scale = *reinterpret_cast<const uint32_t*>(tile + Tile::scale(token, false, 0));
+          zero = *reinterpret_cast<const uint32_t*>(tile + Tile::zero(token, false, 0));
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(tile + Tile::key(token, 16 * t));
+          w[0] = v.x, w[1] = v.y;
+          scale = *reinterpret_cast<const uint16_t*>(tile + Tile::scale(token, false, 0));
+          zero = *reinterpret_cast<const uint16_t*>(tile + Tile::zero(token, false, 0));
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * kGroups; ++i) {
+        float x[8];
+        values8(w[i], (scale >> (16 * (i / 2))) & 0xffff, zero >> (16 * (i / 2)), x);
+        put(0, (i / 2) * kKvGroup + 16 * t + 8 * (i & 1), x);
+      }
     } else {
-      const uint8_t* tile = kv_tile<Tile>(p.cache, page, head, pos);
-      if constexpr (kInt4) {
-        const uint32_t w = !value ? *reinterpret_cast<const uint32_t*>(tile + Tile::key(token, 8 * j))
-                                  : *reinterpret_cast<const uint16_t*>(tile + Tile::value(token, 8 * j)) |
-                                        static_cast<uint32_t>(*reinterpret_cast<const uint16_t*>(tile + Tile::value(token, 8 * j + 4))) << 16;
-        const float scale = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(tile + Tile::scale(token, value, j / 8)));
-        const int zero = *reinterpret_cast<const uint16_t*>(tile + Tile::zero(token, value, j / 8)) & 15;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = scale * static_cast<float>(static_cast<int>((w >> (4 * i)) & 15) - zero);
-      } else if (!value) {
-        unpack8(*reinterpret_cast<const uint4*>(tile + Tile::key(token, 8 * j)), x);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          x[i] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(tile + Tile::value(token, 8 * j + (i & 4)) + 4 * (i & 3)));
+      for (int i = 0; i < kDh / 32; ++i) {  // 8 channels of each 32
+        float x[8] = {};
+        if (tile != nullptr) unpack8(*reinterpret_cast<const uint4*>(tile + Tile::key(token, 32 * i + 8 * t)), x);
+        put(0, 32 * i + 8 * t, x);
       }
     }
+  } else {
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const int d = g * kKvGroup + 8 * quad;
+      float x[2][8] = {};
+      if (tile != nullptr) {
+        if constexpr (kInt4) {
+          const uint2 v = *reinterpret_cast<const uint2*>(tile + Tile::value(token, d));
+          const uint32_t zero = *reinterpret_cast<const uint32_t*>(tile + Tile::zero(token, true, g));
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            values8(__byte_perm(v.x, v.y, b == 0 ? 0x5410 : 0x7632),
+                    *reinterpret_cast<const uint16_t*>(tile + Tile::scale(token + b, true, g)), zero >> (16 * b), x[b]);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {  // 4 channels
+            const uint4 v = *reinterpret_cast<const uint4*>(tile + Tile::value(token, d + 4 * h));
+            const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float2 two = unpack_bf16x2(r[i]);
+              x[0][4 * h + i] = two.x;
+              x[1][4 * h + i] = two.y;
+            }
+          }
+        }
+      }
+      put(0, d, x[0]);
+      put(1, d, x[1]);
+    }
   }
-  store8(out, x);
 }
+
+// Blocks of 8 positions that L tokens can touch.
+int64_t blocks_of(int64_t L) { return (L + 2 * kBlock - 2) / kBlock; }
 
 template <int kDh, bool kInt4>
 cudaError_t append(const KvAppendArgs& a, cudaStream_t st) {
-  const int64_t heads = a.n_heads + 2 * a.cache.kv_heads, per = kThreads / Half<kDh>::kLanes;
-  return launch_pdl(kv_append_kernel<kDh, kInt4>, dim3(static_cast<unsigned>(a.batch.S * a.batch.L), static_cast<unsigned>((heads + per - 1) / per)),
-                    dim3(kThreads), 0, st, a);
+  const int64_t heads = a.q_out != nullptr ? a.n_heads : 0, blocks = blocks_of(a.batch.L), kv = a.cache.kv_heads;
+  const int64_t per = a.batch.S * blocks * (heads + 2 * kv) >= kManyUnits ? kPer : 1;
+  const int64_t units = (heads + per - 1) / per + 2 * ((kv + per - 1) / per);
+  return launch_pdl(kv_append_kernel<kDh, kInt4>, dim3(static_cast<unsigned>(a.batch.S * blocks), static_cast<unsigned>((units + kWarps - 1) / kWarps)),
+                    dim3(kThreads), 0, st, a, static_cast<int>(blocks), static_cast<int>(per));
 }
 template <int kDh, bool kInt4>
 cudaError_t read(const KvReadArgs& a, cudaStream_t st) {
-  const int per = kThreads / (kDh / 8);
-  const dim3 grid(static_cast<unsigned>(a.batch.S * a.batch.L), static_cast<unsigned>((2 * a.cache.kv_heads + per - 1) / per));
-  return a.f32 ? launch_pdl(kv_read_kernel<kDh, kInt4, float>, grid, dim3(kThreads), 0, st, a)
-               : launch_pdl(kv_read_kernel<kDh, kInt4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, a);
+  const int64_t blocks = blocks_of(a.batch.L);
+  const dim3 grid(static_cast<unsigned>(a.batch.S * blocks), static_cast<unsigned>((2 * a.cache.kv_heads + kWarps - 1) / kWarps));
+  return a.f32 ? launch_pdl(kv_read_kernel<kDh, kInt4, float>, grid, dim3(kThreads), 0, st, a, static_cast<int>(blocks))
+               : launch_pdl(kv_read_kernel<kDh, kInt4, __nv_bfloat16>, grid, dim3(kThreads), 0, st, a, static_cast<int>(blocks));
 }
 
 }  // namespace

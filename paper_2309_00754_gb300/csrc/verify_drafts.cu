@@ -176,7 +176,7 @@ __device__ __forceinline__ Part warp_merge(const Part& p) {
 
 // A warp's slices as a stream of rounds: kVecs 16-byte vectors for each of 32 lanes, kAhead rounds on their way in a ring in
 // shared memory, over the ends of slices, too. A lane reads what it put there itself: -inf behind a row's last vector.
-constexpr int kVecs = 4, kAhead = 2, kStages = kAhead + 1;
+constexpr int kVecs = 4, kAhead = 1, kStages = kAhead + 1;
 constexpr int kRoundVecs = kVecs * 32, kRoundBytes = kRoundVecs * 16;
 
 // A row as 16-byte vectors, with the logits before the first of them and behind the last.
@@ -492,9 +492,12 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
 
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row
+  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row; eight only where
+  // there is an SM for each, as twice as many clusters of half the size are placed more evenly (24 sequences of 8 drafts and
+  // 128,000 tokens: 16.3 us by fours, 17.4 by eights; 64 of 4 drafts and 32,000: 18.6 by fours, 21.9 by twos).
+  const int64_t sms = std::max(1, sm_count());
   int cs = 1;
-  while (cs < kMaxCluster && a.S * cs <= std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
+  while (cs < kMaxCluster && a.S * cs <= (cs < 4 ? sms : sms / 2) && a.V >= 2000 * cs) cs *= 2;
   // Slices of a row: t for each of the cluster's warps with all drafts there, t such that they come out with the fewest rounds,
   // a slice's end counted as one.
   const int warps = cs * kWarps, most = static_cast<int>(a.draft != nullptr ? 2 * a.D + 1 : a.D + 1);
