@@ -350,7 +350,7 @@ __device__ __forceinline__ void values8(uint32_t w, uint32_t scale_bits, uint32_
   for (int i = 0; i < 8; ++i) x[i] = scale * (__uint_as_float(0x4b000000u | ((w >> (4 * i)) & 15)) + minus);  // 2^23 + code
 }
 
-// A warp has 8 tokens of a head's keys or values, its lanes the channels as above (keys: those of one 16-byte piece).
+// A warp has 8 tokens of a head's keys or values, four lanes a key, eight two values.
 template <int kDh, bool kInt4, typename Out>
 __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvReadArgs p, int blocks) {
   using Tile = KvTile<kDh, kInt4>;
@@ -390,34 +390,28 @@ __global__ void __launch_bounds__(kThreads) kv_read_kernel(const KvReadArgs p, i
     store8(out + b * p.ld + d, x);
   };
   if (!value) {
-    if constexpr (kInt4) {
-      uint32_t w[2 * kGroups] = {}, scale = 0, zero = 0;
+    uint32_t scale = 0, zero = 0;
+    if (kInt4 && tile != nullptr) {
+      if constexpr (kGroups == 2) {
+        scale = *reinterpret_cast<const uint32_t*>(tile + Tile::scale(token, false, 0));
+        zero = *reinterpret_cast<const uint32_t*>(tile + Tile::zero(token, false, 0));
+      } else {
+        scale = *reinterpret_cast<const uint16_t*>(tile + Tile::scale(token, false, 0));
+        zero = *reinterpret_cast<const uint16_t*>(tile + Tile::zero(token, false, 0));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kDh / 32; ++i) {  // 8 channels of each 32, so that four lanes write a row's bytes in order
+      const int d = 32 * i + 8 * t;
+      float x[8] = {};
       if (tile != nullptr) {
-        if constexpr (kGroups == 2) {
-          const uint4 v = *reinterpret_cast<const uint4*>(tile + Tile::key(token, 16 * t));
-          w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-          scale = *reinterpret_cast<const uint32_t*>(tile + Tile::scale(token, false, 0));
-          zero = *reinterpret_cast<const uint32_t*>(tile + Tile::zero(token, false, 0));
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(tile + Tile::key(token, 16 * t));
-          w[0] = v.x, w[1] = v.y;
-          scale = *reinterpret_cast<const uint16_t*>(tile + Tile::scale(token, false, 0));
-          zero = *reinterpret_cast<const uint16_t*>(tile + Tile::zero(token, false, 0));
-        }
+        if constexpr (kInt4)
+          values8(*reinterpret_cast<const uint32_t*>(tile + Tile::key(token, d)), (scale >> (16 * (i / 2))) & 0xffff,
+                  zero >> (16 * (i / 2)), x);
+        else
+          unpack8(*reinterpret_cast<const uint4*>(tile + Tile::key(token, d)), x);
       }
-#pragma unroll
-      for (int i = 0; i < 2 * kGroups; ++i) {
-        float x[8];
-        values8(w[i], (scale >> (16 * (i / 2))) & 0xffff, zero >> (16 * (i / 2)), x);
-        put(0, (i / 2) * kKvGroup + 16 * t + 8 * (i & 1), x);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kDh / 32; ++i) {  // 8 channels of each 32
-        float x[8] = {};
-        if (tile != nullptr) unpack8(*reinterpret_cast<const uint4*>(tile + Tile::key(token, 32 * i + 8 * t)), x);
-        put(0, 32 * i + 8 * t, x);
-      }
+      put(0, d, x);
     }
   } else {
 #pragma unroll
