@@ -102,6 +102,12 @@ CASES = [
     dict(S=3, L=70, heads=7, kv=7, D=128, page=64, cached=[0, 63, 129], lengths=[70, 1, 33]),
     dict(S=2, L=150, heads=40, kv=3, D=64, page=128, cached=[5, 250], lengths=[150, 149]),
     dict(S=9, L=2, heads=5, kv=1, D=128, page=16, cached=list(range(11, 20)), lengths=[2, 1, 0] * 3),
+    # single tokens, a lane group a head: numbers of heads that fill no warp
+    dict(S=23, L=1, heads=13, kv=6, D=128, page=16, cached=list(range(23)), lengths=[1, 1, 0, 1, 1] * 4 + [1] * 3),
+    dict(S=4, L=1, heads=8, kv=9, D=64, page=32, cached=[31, 32, 7, 0]),
+    # a warp has several heads
+    dict(S=20, L=100, heads=50, kv=11, D=64, page=16, cached=list(range(0, 100, 5)), lengths=list(range(100, 0, -5))),
+    dict(S=4, L=129, heads=33, kv=130, D=128, page=64, cached=[0, 1, 77, 64], lengths=[129, 3, 0, 8]),
 ]
 
 
@@ -170,6 +176,23 @@ def test_values_where_a_scale_goes_wrong():
     H.hydra_kv_append(c["cache"], dev_i32(c["table"]), dev_i32(c["cached"]), None, 1, 1, None, k, v)
     _, k_ref, v_ref = want(c, rope=False)
     assert np.isnan(k_ref).sum() == 3 * 64
+    same(read(c)[0], k_ref)
+    same(read(c)[1], v_ref)
+
+
+def test_quotients_half_way_between_codes():
+    """Channels at whole and half codes of a scale of 1 (and 2^-20, 2^20): ties go to the even code, as rint has it."""
+    def halves(rng, like):
+        x = rng.integers(0, 31, like.size).reshape(-1, 64) / 2.0 - rng.integers(0, 16, (like.size // 64, 1))
+        lo = rng.integers(0, 16, (len(x), 1)) * -1.0
+        x = np.clip(x, lo, lo + 15)
+        x[:, :1], x[:, 1:2] = lo, lo + 15
+        return (x * rng.choice([1.0, 2.0 ** -20, 2.0 ** 20], (len(x), 1))).reshape(like.shape)
+
+    c = make(9, 1, 18, 0, 40, 128, 16, True, [3], values=halves)
+    _, k, v = parts(c, c["x"].cuda())
+    H.hydra_kv_append(c["cache"], dev_i32(c["table"]), dev_i32(c["cached"]), None, 1, 18, None, k, v)
+    _, k_ref, v_ref = want(c, rope=False)
     same(read(c)[0], k_ref)
     same(read(c)[1], v_ref)
 
