@@ -1,13 +1,17 @@
 """Attention over a paged cache against the fp64 oracle on the values that the cache holds.
 
-Tolerances, with u = 2^-24. A score is a sum of D products in fp32, off by at most (D + 16) u of the sum of their
-magnitudes (`reach`); in 4 bits a query is two e4m3, relative to its row's largest, between 2^7 and 2^8 then, of which the
-second has steps of 2^-9 at least: an element is off by 2^-10, 2^-17 of the largest, and a score by that times sum_d |k_jd|
-(`coarse`). So a weight is off by e = (D + 16) u reach + 2^-17 coarse relative, and the quotient of two sums of weights twice that. Weights enter the second product rounded to fp16 (half a step: 2^-11 relative) together with their value's scale, the
-largest such product of a row at 2^6 or more: below 2^-14 fp16 has steps of 2^-24, so a weight is off by 2^-25 at most, 2^-31
-of the largest product w sv. Times a code of up to 15, and sv <= max |v| / 7.5 (a scale is a fifteenth of its range),
-that is N 2^-30 max |v| over N tokens. (Two bf16, 2^-16 relative, in a bf16 cache.) The sums themselves are fp32 over N terms:
-at most N u, with 128 for the order and for logarithms of up to 128, rounded, by which parts are added up. So an output is off by
+Tolerances, with u = 2^-24. A score is a sum of D exact products in fp32. Sixteen at a time and the sum before are added
+aligned to the largest, cut off below its last place: 17 D / 16 terms, each off by 2 u of the largest partial sum at most, so
+2 (D + D / 16) u, with 16 u for scales and factors, of the sum of the products' magnitudes (`reach`); in 4 bits a query is
+fp16, relative to its row's largest, between 2^7 and 2^8 then, a part of its elements divided by 16: below 2^-14 fp16 has
+steps of 2^-24, so an element is off by 2^-21 at most, 2^-28 of the largest, and a score by that times sum_d |k_jd|
+(`coarse`). So a weight is off by e = (2 (D + D / 16) + 16) u reach + 2^-28 coarse relative, and the quotient of two sums of
+weights twice that. Weights enter the second product rounded to fp16 (half a step: 2^-11 relative) together with their
+value's scale, the largest such product of a row at 2^6 or more: below 2^-14 fp16 has steps of 2^-24, so a weight is off by
+2^-25 at most, 2^-31 of the largest product w sv. Times a code of up to 15, and sv <= max |v| / 7.5 (a scale is a fifteenth
+of its range), that is N 2^-30 max |v| over N tokens. (Two bf16, 2^-16 relative, in a bf16 cache.) The sums themselves are
+fp32 over N terms: at most N u, with 128 for the order and for logarithms of up to 128, rounded, by which parts are added up.
+So an output is off by
     (2^-11 + 2 e + (N + 128) u) sum_j p_j |v_j| + N 2^-30 max |v|,
 and rounded to bf16: half a step, 2^-8 of its value (and of what it is off by)."""
 import numpy as np
@@ -97,7 +101,7 @@ def check(c, got, scale=None, sick=None):
         ref, size, reach = O.cached_attention(q[s, :n], c["k"][s, :N], c["v"][s, :N], int(c["cached"][s]), scale)
         by = c["heads"] // c["kv"]
         coarse = np.abs(q[s, :n]).max(-1) * np.abs(c["k"][s, :N].astype(np.float64)).sum(-1).max(0).repeat(by)[None] * abs(scale)
-        e = ((D + 16) * U * reach + 2.0 ** -17 * coarse)[..., None]
+        e = ((2 * (D + D // 16) + 16) * U * reach + 2.0 ** -28 * coarse)[..., None]
         tol = (2.0 ** -11 + 2 * e + (N + 128) * U) * size + N * 2.0 ** -30 * np.abs(c["v"][s, :N]).max()
         tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
         off = np.abs(got[s, :n] - ref)
@@ -120,6 +124,11 @@ CASES = [
     dict(L=2, heads=5, kv=5, D=128, page=16, cached=list(range(0, 210, 3)), lengths=[2, 1] * 35),
     dict(L=1, heads=40, kv=1, D=64, page=16, cached=[700]),
     dict(L=4, heads=32, kv=1, D=128, page=32, cached=[90, 1]),             # 128 rows of one kv head
+    dict(L=2, heads=4, kv=2, D=64, page=16, cached=[37 * i % 1700 for i in range(40)]),  # equal parts, more than 32 sequences
+    dict(L=5, heads=32, kv=8, D=64, page=16, cached=[61 * i % 300 for i in range(16)], lengths=[5, 0, 1, 4] * 4),  # a row of units
+    dict(L=1, heads=2, kv=2, D=64, page=16, cached=[7 * i % 90 for i in range(300)], lengths=[1, 0, 1] * 100),
+    dict(L=2, heads=2, kv=2, D=64, page=16, cached=[40, 0, 7], lengths=[0, 0, 0]),
+    dict(L=1, heads=3, kv=1, D=128, page=16, cached=[20000, 1281]),
 ]
 
 
