@@ -634,10 +634,11 @@ hydra_status hydra_kv_read(const hydra_kv_cache* cache, const int32_t* table, in
  *   table, cached, lengths, S, L, cache : as the append of the same step.
  *   workspace : device, 16-byte aligned, >= hydra_paged_attention_workspace_size(...) bytes, caller-owned; no
  *             initial contents required; calls sharing a workspace must be stream-ordered.
- * It is made for decoding, where L is a few tokens and the cache's bytes are all that counts; any L works, but every 32
- * query rows (tokens times n_heads / n_kv_heads) of a kv head read the cache again.
+ * It is made for decoding, where L is a few tokens and the cache's bytes are all that counts; any L works, but every 8
+ * query rows (tokens times n_heads / n_kv_heads) of a kv head read the cache again (from L2, where it fits).
  * Bytes behind a sequence's last token may be anything, NaN among them, and what one query must not see does not
- * change it. Scores, their maximum and sums are fp32.
+ * change it. An infinity or NaN among the values that a query sees makes that channel of its output (in 4 bits its group of
+ * channels) infinite or NaN, one among its keys the whole head. Scores, their maximum and sums are fp32.
  * Bits: equal calls on one device give equal bits; a sequence's depend on the others' lengths (where work is cut).
  * Errors as hydra_kv_append; n_heads not a multiple of n_kv_heads -> HYDRA_ERR_SHAPE; scale not finite ->
  * HYDRA_ERR_RANGE; NULL q or out -> HYDRA_ERR_NULL; small, NULL or misaligned workspace -> HYDRA_ERR_WORKSPACE. A bad page

@@ -10,8 +10,8 @@
 //
 // Bound by the reads of the logits. A cluster of CTAs has a sequence. Every row is cut in the same number of slices, which its
 // warps take in turn, each in one pass with a running maximum and sum; the slices' (maximum, sum) pairs are all that the CTAs
-// exchange before every one of them knows where the drafts end. (Cut alike, equal rows have equal sums: a draft model that
-// is the target is never refused.) The row that the last token is drawn from is read a second time, from L2 as a rule.
+// exchange before every one of them knows where the drafts end. (Cut alike, equal rows that start alike modulo 16 bytes have
+// equal sums: a draft model that is the target is never refused.) The row that the last token is drawn from is read a second time, from L2 as a rule.
 #include <algorithm>
 #include <atomic>
 #include <cfloat>

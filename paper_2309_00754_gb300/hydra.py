@@ -723,11 +723,16 @@ class KvCache:
         _req(data, torch.uint8, "data")
         if data.numel() != n_pages * size:
             raise ValueError(f"data must have {n_pages} pages of {size} bytes, got {data.numel()} bytes")
-        self.data, self.kind, self.n_pages, self.page = data, kind, n_pages, page
+        self._data, self.kind, self.n_pages, self.page = data, kind, n_pages, page
         self.n_kv_heads, self.head_dim, self.page_bytes = n_kv_heads, head_dim, size
         self.device = data.get_device()
         self.c = KvCacheC(data.data_ptr(), n_pages, page, n_kv_heads, head_dim, kind)
         self.ref = ctypes.byref(self.c)
+
+    @property
+    def data(self):
+        """(read only: the calls know its address)"""
+        return self._data
 
 
 def _kv_args(cache, table, cached, lengths, S, L, dev):
