@@ -5,14 +5,21 @@
 // with every product and sum rounded to fp32 as hydra_rope rounds them. A bf16 cache takes bf16(r). A cache in 4 bits
 // takes, for each group of 64 channels, lo = min(0, r), hi = max(0, r), scale = bf16((hi / 2 - lo / 2) 2/15), the
 // zero point rint(-lo / scale) and the codes rint(r / scale) + zero, both within 0..15.
+//
+// Bound by bytes for prompts, by latency for a step's few tokens. 8 prompts of up to 512 tokens with 32 query heads and 32 for
+// keys and values of 128 channels: 26.2 us to append (4 bits), 14.5 us to read back; one token of 64 sequences 3.9 us, of one
+// 2.9 us.
 #include "kv_cache.cuh"
 
 namespace hydra {
 namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
-constexpr int kPer = 4;  // heads of a warp, where there are many
-constexpr int64_t kManyUnits = 20000;
+// Heads of a warp where there are many: it reads the rotation once for them and has the next head on its way while it works
+// (the 8 prompts above: 26 us with four heads, 30 with two, 40 with one; 1000 tokens of 32 + 16 heads, 6000 heads' blocks
+// in all, are the faster singly, 9.8 us against 11.3).
+constexpr int kPer = 4;
+constexpr int64_t kManyUnits = 20000;  // blocks of eight tokens times heads
 constexpr int kBlock = 8;  // tokens of a warp, from a multiple of 8 on: half of a tile
 
 __device__ __forceinline__ void unpack8(const uint4& v, float* f) {

