@@ -14,7 +14,7 @@
 // equal sums: a draft model that is the target is never refused.) The row that the last token is drawn from is read a second
 // time, from L2 as a rule.
 //
-// Measured: 64 sequences of up to 4 drafts and 32,000 fp32 logits (49 MB) in 18.7 us, 2.6 TB/s: a cluster has its rows in 6 to 8
+// Measured: 64 sequences of up to 4 drafts and 32,000 fp32 logits (49 MB) in 18.4 us, 2.7 TB/s: a cluster has its rows in 6 to 8
 // us of that and what follows is a chain of latencies (the pairs' exchange, the second read, the exchange of what it found),
 // 9 us where a single sequence is all there is.
 #include <algorithm>
@@ -288,7 +288,7 @@ __device__ __forceinline__ int ld_cluster(const int* local, unsigned rank) {
 }
 
 template <typename T, bool kGreedy>
-__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p, int cs, int slices, int rounds) {
+__global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p, int cs) {
   extern __shared__ __align__(16) uint8_t raw_shared[];
   Shared& sh = *reinterpret_cast<Shared*>(raw_shared);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -318,7 +318,13 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
     }
   }
 
-  const int warps = cs * kWarps;
+  // Slices of a row: t for each of the cluster's warps, t such that they come out with the fewest rounds, a slice's end counted
+  // as one (a lane a t). By the drafts that are there: cut for all D, a sequence of few leaves most warps idle.
+  const int warps = cs * kWarps, all = (V + kRoundVecs * Row<T>::E - 1) / (kRoundVecs * Row<T>::E);  // rounds of a row
+  const int t = lane + 1, least = max(1, t * warps / rows), mine_rounds = (all + least - 1) / least;
+  const unsigned cost = t <= kMaxSlices && t * warps >= rows ? static_cast<unsigned>(t * (mine_rounds + 1)) : UINT_MAX / 2;
+  const int best_t = __ffs(__ballot_sync(0xffffffffu, cost == __reduce_min_sync(0xffffffffu, cost))) - 1;
+  const int rounds = __shfl_sync(0xffffffffu, mine_rounds, best_t), slices = (all + rounds - 1) / rounds;
   scan<T, kGreedy>(
       rank * kWarps + warp, warps, rows * slices, slices, rounds, V,
       raw_shared + sizeof(Shared) + warp * kStages * kRoundBytes, lane, row_at, [&](int k, const Part& part) {
@@ -499,26 +505,10 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
 
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row; eight only where
-  // there is an SM for each, as twice as many clusters of half the size are placed more evenly (24 sequences of 8 drafts and
-  // 128,000 tokens: 16.3 us by fours, 17.4 by eights; 64 of 4 drafts and 32,000: 18.6 by fours, 21.9 by twos).
-  const int64_t sms = std::max(1, sm_count());
+  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row (64 sequences of 4 drafts
+  // and 32,000 tokens: 18.4 us by fours, 22.0 by twos, 24.9 by eights).
   int cs = 1;
-  while (cs < kMaxCluster && a.S * cs <= (cs < 4 ? sms : sms / 2) && a.V >= 2000 * cs) cs *= 2;
-  // Slices of a row: t for each of the cluster's warps with all drafts there, t such that they come out with the fewest rounds,
-  // a slice's end counted as one.
-  const int warps = cs * kWarps, most = static_cast<int>(a.draft != nullptr ? 2 * a.D + 1 : a.D + 1);
-  const int all = static_cast<int>((a.V + kRoundVecs * Row<T>::E - 1) / (kRoundVecs * Row<T>::E));  // rounds of a row
-  int slices = 1, rounds = all, least = INT_MAX;
-  for (int t = 1; t <= kMaxSlices; ++t) {
-    if (t * warps < most) continue;
-    const int of = (all + t * warps / most - 1) / (t * warps / most);
-    if (t * (of + 1) < least) {
-      least = t * (of + 1);
-      rounds = of;
-      slices = (all + of - 1) / of;
-    }
-  }
+  while (cs < kMaxCluster && a.S * cs <= std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
   constexpr int kSmem = sizeof(Shared) + kWarps * kStages * kRoundBytes;
   static std::atomic<bool> attr_set[64];  // the shared-memory limit is a per-device attribute; host threads may ask at once
   int dev = 0;
@@ -542,7 +532,7 @@ cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, cs, slices, rounds);
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, cs);
 }
 
 }  // namespace
