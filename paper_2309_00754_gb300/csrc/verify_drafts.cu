@@ -30,7 +30,6 @@ namespace {
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kMaxCluster = 8;
 constexpr int kMaxRows = 2 * kVerifyMaxDrafts + 1;  // target rows 0..n, then draft rows 0..n-1
 
 // A value with its index, and a logit beside it; the larger value, of equal ones the lower index.
@@ -503,36 +502,59 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
   if (cs > 1) cluster_sync_all();  // nobody leaves while its memory is read
 }
 
+constexpr int kSmem = sizeof(Shared) + kWarps * kStages * kRoundBytes;
+
+cudaLaunchConfig_t config(int64_t clusters, int cs, cudaStream_t st, cudaLaunchAttribute (&attr)[2]) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(clusters * cs));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(cs);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  return cfg;
+}
+
+// Clusters of 1 << bits CTAs that the device holds at once (0: none, or it does not say, which is not kept).
+template <typename T, bool kGreedy>
+int clusters_held(int dev, int bits) {
+  static std::atomic<int> held[64][4];  // and one more; host threads may ask at once
+  if (const int known = held[dev][bits]; known > 0) return known - 1;
+  cudaLaunchAttribute attr[2];
+  cudaLaunchConfig_t cfg = config(1, 1 << bits, nullptr, attr);
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, verify_kernel<T, kGreedy>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  held[dev][bits] = n + 1;
+  return n;
+}
+
 template <typename T, bool kGreedy>
 cudaError_t launch(const VerifyArgs& a, cudaStream_t st) {
-  // As many CTAs a sequence as the device holds at once (two an SM), none with under 1000 tokens of a row (64 sequences of 4 drafts
-  // and 32,000 tokens: 18.4 us by fours, 22.0 by twos, 24.9 by eights).
-  int cs = 1;
-  while (cs < kMaxCluster && a.S * cs <= std::max(1, sm_count()) && a.V >= 2000 * cs) cs *= 2;
-  constexpr int kSmem = sizeof(Shared) + kWarps * kStages * kRoundBytes;
   static std::atomic<bool> attr_set[64];  // the shared-memory limit is a per-device attribute; host threads may ask at once
   int dev = 0;
-  if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess || dev >= 64) return e == cudaSuccess ? cudaErrorInvalidDevice : e;
+  if (cudaError_t e = cudaGetDevice(&dev); e != cudaSuccess || dev < 0 || dev >= 64) return e == cudaSuccess ? cudaErrorInvalidDevice : e;
   if (!attr_set[dev]) {
     if (cudaError_t e = cudaFuncSetAttribute(verify_kernel<T, kGreedy>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem); e != cudaSuccess)
       return e;
     attr_set[dev] = true;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(a.S * cs));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmem;
-  cfg.stream = st;
+  // As many CTAs a sequence as the device holds for all at once, none with under 1000 tokens of a row (64 sequences of 4 drafts and
+  // 32,000 tokens: 18.4 us by fours, 22.0 by twos, 24.9 by eights, of which 35 fit).
+  int bits = 3;
+  while (bits > 0 && (a.V < (1000LL << bits) || a.S > clusters_held<T, kGreedy>(dev, bits))) --bits;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(cs);
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, cs);
+  const cudaLaunchConfig_t cfg = config(a.S, 1 << bits, st, attr);
+  return cudaLaunchKernelEx(&cfg, verify_kernel<T, kGreedy>, a, 1 << bits);
 }
 
 }  // namespace
