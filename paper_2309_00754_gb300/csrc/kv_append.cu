@@ -49,26 +49,32 @@ struct Range {
     hi = max_or_nan(hi, x);
   }
 };
-// over the lanes that differ in the bits of kFrom, 2 kFrom, ... kTo
-template <int kFrom, int kTo, int kN>
-__device__ __forceinline__ void take_lanes(Range (&r)[kN]) {
-#pragma unroll
-  for (int o = kFrom; o <= kTo; o <<= 1)
-#pragma unroll
-    for (int i = 0; i < kN; ++i) {
-      r[i].lo = fminf(r[i].lo, __shfl_xor_sync(0xffffffffu, r[i].lo, o));
-      r[i].hi = max_or_nan(r[i].hi, __shfl_xor_sync(0xffffffffu, r[i].hi, o));
-    }
+// over the lanes that differ in the bit `off`: of one range, and of two, of which the lane goes on with the one of its bit
+__device__ __forceinline__ Range met(const Range& mine, const Range& sent, int off) {
+  Range r;
+  r.lo = fminf(mine.lo, __shfl_xor_sync(0xffffffffu, sent.lo, off));
+  r.hi = max_or_nan(mine.hi, __shfl_xor_sync(0xffffffffu, sent.hi, off));
+  return r;
+}
+__device__ __forceinline__ Range met(const Range& r, int off) { return met(r, r, off); }
+__device__ __forceinline__ Range halved(const Range& zero, const Range& one, int off) {
+  const bool bit = (threadIdx.x & off) != 0;
+  return met(bit ? one : zero, bit ? zero : one, off);
 }
 
 struct Quant {
   float scale, zero;  // scale 0 or NaN: all codes are 0
+  float inv;          // 1 / scale, or NaN where codes are not to come from it
   __device__ __forceinline__ explicit Quant(const Range& r) {
     // (halves: the difference of two large values passes fp32)
     scale = __bfloat162float(__float2bfloat16_rn(__fmul_rn(__fsub_rn(r.hi * 0.5f, r.lo * 0.5f), 2.0f / 15.0f)));
     scale = fmaf(scale, 0.f, scale);  // infinite only with an infinity among the channels: NaN then, too
     zero = scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(-r.lo, scale)), 0.f), 15.f) : 0.f;
+    inv = scale > 1e-30f && scale < 1e30f ? __frcp_rn(scale) : __int_as_float(0x7fffffff);
   }
+  // that of another lane
+  __device__ __forceinline__ Quant(const Quant& q, int lane)
+      : scale(__shfl_sync(0xffffffffu, q.scale, lane)), zero(__shfl_sync(0xffffffffu, q.zero, lane)), inv(__shfl_sync(0xffffffffu, q.inv, lane)) {}
   __device__ __forceinline__ uint32_t code(float x) const {
     if (!(scale > 0.f)) return 0;
     return static_cast<uint32_t>(fminf(fmaxf(rintf(__fdiv_rn(x, scale)) + zero, 0.f), 15.f));
@@ -78,8 +84,8 @@ struct Quant {
   __device__ __forceinline__ uint32_t codes(const float* x) const {
     constexpr float kMagic = 12582912.f;  // 1.5 2^23: what is added to it is rounded to an integer in the low bits
     constexpr uint32_t kMagicBits = 0x4b400000u;
-    const bool usual = scale > 1e-30f && scale < 1e30f;
-    const float inv = __frcp_rn(scale), magic = kMagic + zero;
+    const bool usual = inv == inv;
+    const float magic = kMagic + zero;
     uint32_t w = 0;
     float off = 0.f;
 #pragma unroll
@@ -230,22 +236,19 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs 
           range[0].take(a[i]);
           range[kGroups - 1].take(b[i]);
         }
-        take_lanes<1, 2>(range);
-        const Quant qa(range[0]), qb(range[kGroups - 1]);
+        // (D = 128: a lane works out one of the two groups; the other comes from its neighbour)
+        const Quant own(met(kGroups == 2 ? halved(range[0], range[kGroups - 1], 1) : met(range[0], 1), 2));
+        const Quant qa(kGroups == 2 ? Quant(own, lane & ~1) : own), qb(kGroups == 2 ? Quant(own, lane | 1) : own);
+        if (tile != nullptr && t < kGroups) {
+          *reinterpret_cast<uint16_t*>(tile + Tile::scale(token, false, t)) = static_cast<uint16_t>(own.scale_bits());
+          *reinterpret_cast<uint16_t*>(tile + Tile::zero(token, false, t)) = static_cast<uint16_t>(own.zero_bits());
+        }
         if (tile != nullptr) {
           if constexpr (kGroups == 2) {
             *reinterpret_cast<uint4*>(tile + Tile::key(token, kRun * t)) = make_uint4(qa.codes(a), qa.codes(a + 8), qb.codes(b), qb.codes(b + 8));
-            if (t == 0) {
-              *reinterpret_cast<uint32_t*>(tile + Tile::scale(token, false, 0)) = qa.scale_bits() | qb.scale_bits() << 16;
-              *reinterpret_cast<uint32_t*>(tile + Tile::zero(token, false, 0)) = qa.zero_bits() | qb.zero_bits() << 16;
-            }
           } else {
             *reinterpret_cast<uint32_t*>(tile + Tile::key(token, kRun * t)) = qa.codes(a);
             *reinterpret_cast<uint32_t*>(tile + Tile::key(token, kDh / 2 + kRun * t)) = qa.codes(b);
-            if (t == 0) {
-              *reinterpret_cast<uint16_t*>(tile + Tile::scale(token, false, 0)) = static_cast<uint16_t>(qa.scale_bits());
-              *reinterpret_cast<uint16_t*>(tile + Tile::zero(token, false, 0)) = static_cast<uint16_t>(qa.zero_bits());
-            }
           }
         }
       }
@@ -304,23 +307,26 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs 
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) unpack8(raw[b][g], v[b][g]);
       if (step < steps) load(head + 1);
-      uint32_t w[2][kGroups] = {}, scales[2] = {}, zeros[2] = {};
+      Range range[2][kGroups];
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        if (!(b == 0 ? any[0] : any[1])) continue;
-        Range range[kGroups];
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) range[g].take(v[b][g][i]);
-        take_lanes<4, 16>(range);
+          for (int i = 0; i < 8; ++i) range[b][g].take(v[b][g][i]);
+      // a lane works out the token of bit 2 of its number and (D = 128) the group of bit 3; the others come from their lanes
+      Range mine = halved(range[0][0], range[1][0], 4);
+      if constexpr (kGroups == 2)
+        mine = halved(mine, halved(range[0][1], range[1][1], 4), 8);
+      else
+        mine = met(mine, 8);
+      const Quant own(met(mine, 16));
+      uint32_t w[2][kGroups] = {};
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          const Quant q(range[g]);
-          w[b][g] = q.codes(v[b][g]);
-          scales[b] |= q.scale_bits() << (16 * g);
-          zeros[g] |= q.zero_bits() << (16 * b);
-        }
+      for (int b = 0; b < 2; ++b) {
+        if (!(b == 0 ? any[0] : any[1])) continue;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) w[b][g] = Quant(own, t + 4 * b + 8 * g).codes(v[b][g]);
       }
       if (tile != nullptr) {
         uint8_t* to = tile + Tile::value(token, 8 * quad);
@@ -344,13 +350,9 @@ __global__ void __launch_bounds__(kThreads) kv_append_kernel(const KvAppendArgs 
             reinterpret_cast<uint16_t*>(to)[4 * g + 2 + b] = static_cast<uint16_t>(one >> 16);
           }
         }
-        if (quad < 2 && there[quad]) {  // a lane a token
-          const uint32_t sc = quad == 0 ? scales[0] : scales[1];
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) {
-            *reinterpret_cast<uint16_t*>(tile + Tile::scale(token + quad, true, g)) = static_cast<uint16_t>(sc >> (16 * g));
-            *reinterpret_cast<uint16_t*>(tile + Tile::zero(token + quad, true, g)) = static_cast<uint16_t>(zeros[g] >> (16 * quad));
-          }
+        if (quad < 2 * kGroups && there[quad & 1]) {  // a lane a token and group
+          *reinterpret_cast<uint16_t*>(tile + Tile::scale(token + (quad & 1), true, quad >> 1)) = static_cast<uint16_t>(own.scale_bits());
+          *reinterpret_cast<uint16_t*>(tile + Tile::zero(token + (quad & 1), true, quad >> 1)) = static_cast<uint16_t>(own.zero_bits());
         }
       }
     }
