@@ -7,8 +7,8 @@
 // zero point rint(-lo / scale) and the codes rint(r / scale) + zero, both within 0..15.
 //
 // Bound by bytes for prompts, by latency for a step's few tokens. 8 prompts of up to 512 tokens with 32 query heads and 32 for
-// keys and values of 128 channels: 26.2 us to append (4 bits), 14.5 us to read back; one token of 64 sequences 3.9 us, of one
-// 2.9 us.
+// keys and values of 128 channels: 25.0 us to append (4 bits), 14.5 us to read back; one token of 64 sequences 3.7 us, of one
+// 2.8 us.
 #include "kv_cache.cuh"
 
 namespace hydra {
@@ -16,10 +16,10 @@ namespace {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 // Heads of a warp where there are many: it reads the rotation once for them and has the next head on its way while it works
-// (the 8 prompts above: 26 us with four heads, 30 with two, 40 with one; 1000 tokens of 32 + 16 heads, 6000 heads' blocks
-// in all, are the faster singly, 9.8 us against 11.3).
+// (the 8 prompts above: 25.0 us with four heads, 28.6 with two, 39.1 with one; 2 such prompts, 12,000 blocks times heads, 10.2
+// with four and 13.1 with one; 4 of 128 tokens in bf16, 6500, are the faster singly, 7.6 against 8.1).
 constexpr int kPer = 4;
-constexpr int64_t kManyUnits = 20000;  // blocks of eight tokens times heads
+constexpr int64_t kManyUnits = 10000;  // blocks of eight tokens times heads
 constexpr int kBlock = 8;  // tokens of a warp, from a multiple of 8 on: half of a tile
 
 __device__ __forceinline__ void unpack8(const uint4& v, float* f) {
@@ -129,7 +129,7 @@ struct Block {
 };
 
 // The warps of a block of tokens: up to `per` heads of a kind for each; where there is a single token, a head for each of the
-// lanes' tokens (64 sequences of 32 + 64 heads: 3.9 us; with 7 of 8 lanes idle 7.6).
+// lanes' tokens (64 sequences of 32 + 64 heads: 3.7 us; with 7 of 8 lanes idle 7.6).
 struct Units {
   int per, v_per, q, k, v;
   __host__ __device__ Units(int heads, int kv, bool single, int per_)

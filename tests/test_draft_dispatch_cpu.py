@@ -59,6 +59,7 @@ def test_appended_tokens_go_by_blocks_of_eight_positions(fake):
     assert grid(3, 1) == (3, 2)                     # single tokens: eight heads a warp, four of values: 4 + 1 + 2 warps
     assert grid(3, 1, heads=0, kv=1) == (3, 1)
     assert grid(64, 64, kv=32) == (64 * 9, 6)       # many: four heads a warp
+    assert grid(2, 512, kv=32)[1] == 6 and grid(4, 128, kv=32)[1] == 24
     assert grid((1 << 31) - 1, 1, heads=4096, kv=4096)[1] == (4096 // 8 * 2 + 4096 // 4) // 4  # within a grid's limits
 
 
