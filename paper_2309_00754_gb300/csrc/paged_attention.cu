@@ -46,7 +46,10 @@ constexpr int kRows = 8;          // query rows of an item: the columns of a pro
 // 8.5 with four, which leave warps idle).
 constexpr int kMinUnits = 2;
 // Tokens of a table up to which a CTA takes an item alone, without the second kernel, where there are CTAs for all (one sequence, 32
-// heads: 300 tokens 7.8 us against 12.0, 1100 tokens 11.9 against 13.2, 2200 tokens 17.5 against 15.3).
+// heads: 300 tokens 7.8 us against 12.0, 1100 tokens 11.9 against 13.2, 2200 tokens 17.5 against 14.4). Twice as many where a quarter
+// of the CTAs have an item and a tile costs less than in 4 bits with 128 channels (bf16, 13 sequences of 2000 tokens, 156 items of 64
+// channels, 15.1 us against 16.6; 4 of 2000, 128 of 128 channels, 20.7 against 22.8; one of 2200, 32 items, 18.2 against 15.9;
+// 4 bits with 128 channels, 8 of 2400, 256 items, 26.2 against 23.7).
 constexpr int64_t kAlignedTokens = 1280;
 // What an item costs beside its tiles, in tiles (16 sequences x 20 rows over up to 4096 tokens: 35 us with 6 or 12, 36 with 3, 52
 // with 0; 64 sequences of up to 800, 32 heads: 47, 48, 48, 65).
@@ -79,13 +82,13 @@ struct Config {
   using Parts = Part<kDh>;
   using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
-  static constexpr int kCtasPerSm = kInt4 ? 2 : 1;
+  static constexpr int kCtasPerSm = kInt4 || kDh == 64 ? 2 : 1;
   static constexpr int kPair = kInt4 ? 2 : 1;  // tiles that are taken together
   static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that are copied together
   static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
   // a warp's ring also takes its last part at the end
   static constexpr int kLeast = (kRows * kDh * 4 + kStageBytes - 1) / kStageBytes;
-  static constexpr int kStages = kLeast > 2 || (!kInt4 && kDh == 64) ? 4 : 2;
+  static constexpr int kStages = kLeast > 2 ? 4 : 2;
   static_assert(kLeast <= kStages, "a part fits the ring");
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kQ = kRows * kDh * 2;  // a warp's queries, as rows and then as fragments
@@ -1198,7 +1201,8 @@ int launch(const PagedAttentionArgs& a, cudaStream_t st) {
   const int ctas = std::min(kMaxCtas, std::max(1, sm_count()) * C::kCtasPerSm);
   const int64_t rows = a.n_heads / a.cache.kv_heads * a.batch.L;
   const int64_t items = a.batch.S * a.cache.kv_heads * ((rows + kRows - 1) / kRows);
-  const bool aligned = items <= ctas && (a.batch.max_pages << a.cache.page_bits) <= kAlignedTokens;
+  const int64_t tokens = (!kInt4 || kDh == 64) && 4 * items >= ctas ? 2 * kAlignedTokens : kAlignedTokens;
+  const bool aligned = items <= ctas && (a.batch.max_pages << a.cache.page_bits) <= tokens;
   if (aligned)
     return launch_pdl(paged_attention_kernel<kDh, kInt4>, dim3(static_cast<unsigned>(items)), dim3(kThreads), C::kSmem, st, a, true) ==
                    cudaSuccess

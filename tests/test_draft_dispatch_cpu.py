@@ -76,7 +76,7 @@ def test_attention_of_short_tables_is_one_launch_else_two(fake):
     for int4, ctas in ((True, 304), (False, 152)):
         for S, L, pages, one in ((4, 1, 80, True), (4, 1, 81, False), (ctas // 8, 1, 80, True), (ctas // 8 + 1, 1, 80, False),
                                  (1, 2 * ctas // 8, 80, True), (1, 2 * ctas // 8 + 1, 80, False)):
-            launches = attend(fake, S, L, int4=int4, pages=pages)
+            launches = attend(fake, S, L, int4=int4, pages=pages if pages == 80 or int4 else 2 * pages)
             items = S * 8 * -(-4 * L // 8)
             if one:
                 ((name, x, *_),) = launches
@@ -84,6 +84,10 @@ def test_attention_of_short_tables_is_one_launch_else_two(fake):
             else:
                 (_, x, *_), (name, jx, jy, *_) = launches
                 assert x == jx == ctas and jy == min(8, 4 * L) and "join" in name, (S, L, pages)
+    # twice the tokens for light tiles where a quarter of the CTAs have an item
+    for dh, int4, S, pages, one in ((64, True, 9, 160, False), (64, True, 10, 160, True), (64, True, 10, 161, False), (64, False, 10, 160, True),
+                                    (128, True, 20, 160, False), (128, False, 4, 160, False), (128, False, 5, 160, True)):
+        assert len(attend(fake, S, 1, dh=dh, int4=int4, pages=pages)) == (1 if one else 2), (dh, int4, S, pages)
     # the workspace holds the parts of any device's grid
     fake.device(device=1, sms=1000)
     assert attend(fake, 900, 1)[0][1] == 320
