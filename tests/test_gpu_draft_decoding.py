@@ -5,6 +5,10 @@ by the next step, sequences that end at different times, and the step as one cap
 The model is a single layer whose query, key and value are a bf16 row of a table for each token, so that the oracle knows
 them bit for bit; attention has the tolerance derived in test_gpu_paged_attention.py, and verification is compared on the
 logits that the device made."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -71,12 +75,15 @@ class Server:
         H.hydra_kv_append(self.cache, self.table, None, lengths, S, n, None, k, v, self.rope_dev)
         self.cached.copy_(lengths)
 
+    def matmul(self):
+        torch.matmul(self.o.float(), self.out, out=self.logits)
+
     def step(self):
         x = self.rows_dev[self.tokens.reshape(-1).long()]
         q, k, v = x[:, :HEADS * D], x[:, HEADS * D:(HEADS + KV) * D], x[:, (HEADS + KV) * D:]
         H.hydra_kv_append(self.cache, self.table, self.cached, self.lengths, S, L, q, k, v, self.rope_dev, self.q)
         H.hydra_paged_attention(self.cache, self.table, self.cached, self.lengths, S, L, self.q, self.o, D ** -0.5, self.ws)
-        torch.matmul(self.o.float(), self.out, out=self.logits)
+        self.matmul()
         H.hydra_verify_drafts(self.logits, self.draft, self.ids, self.n_draft, self.uniform, self.gumbel, S, DRAFTS, self.next,
                               self.accepted)
         # the tokens that stay; the refused ones are written over
@@ -138,6 +145,26 @@ def compare(server, texts, ids, n_draft, live):
     for s in np.flatnonzero(live):
         assert server.accepted[s].item() == want["accepted"][s]
         assert server.next[s].tolist() == want["tokens"][s].tolist()
+
+
+def test_the_first_call_of_a_process_may_be_captured():
+    """What a call looks up once for a device can be looked up while a stream is captured."""
+    code = (
+        "import torch; from tests.test_gpu_draft_decoding import Server\n"
+        "for mode, int4 in (('draft', True), ('greedy', False)):\n"
+        "    s = Server(3, mode, int4)\n"
+        "    s.matmul()\n"
+        "    torch.cuda.synchronize()\n"
+        "    g = torch.cuda.CUDAGraph()\n"
+        "    with torch.cuda.graph(g):\n"
+        "        s.step()\n"
+        "    s.lengths.fill_(1)\n"
+        "    g.replay()\n"
+        "    torch.cuda.synchronize()\n"
+        "    assert s.cached.tolist() == [1] * len(s.cached)\n")
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    run = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0, run.stderr[-2000:]
 
 
 @pytest.mark.parametrize("int4", [True, False])

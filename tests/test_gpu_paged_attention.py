@@ -129,6 +129,7 @@ CASES = [
     dict(L=1, heads=2, kv=2, D=64, page=16, cached=[7 * i % 90 for i in range(300)], lengths=[1, 0, 1] * 100),
     dict(L=2, heads=2, kv=2, D=64, page=16, cached=[40, 0, 7], lengths=[0, 0, 0]),
     dict(L=1, heads=3, kv=1, D=128, page=16, cached=[20000, 1281]),
+    dict(L=300, heads=8, kv=2, D=64, page=64, cached=[0, 40], lengths=[300, 77]),  # prompts
 ]
 
 
