@@ -145,6 +145,19 @@ def test_rows_that_leave_nothing():
         assert o["tokens"][2].tolist() == [7, -1]  # refused, but nothing else is left
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,ld,shift", [(1, 1, 0), (2, 3, 1), (6, 11, 8), (23, 25, 3), (1003, 1007, 5)])
+def test_rows_of_nothing_give_token_0_wherever_they_start(V, ld, shift, dtype):
+    """Greedy and drawn; the first logits and the last ones of a row lie outside its whole vectors."""
+    S = 9
+    for mode in ("greedy", "given"):
+        c = make(50, S, 1, V, dtype, mode, ld=ld, shift=shift, n_draft=None)
+        c["z"][:] = -INF
+        o = run(c)
+        check(c, o)
+        assert (o["tokens"][:, 0] == 0).all() and (o["logp"][:, 0] == -INF).all()
+
+
 def test_ties_go_to_the_lowest_index():
     V, S = 3001, 3
     z = np.zeros((S * 3, V))
