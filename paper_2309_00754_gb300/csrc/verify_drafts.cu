@@ -271,7 +271,7 @@ __device__ __forceinline__ void scan(int first, int step, int total, int slices,
       add<T, kArg>(p, x, row.head + (skip + v * kRoundVecs + lane) * E, 32 * E);
     }
     if (edge >= 0) {
-      if constexpr (kArg) p.take(edge_z, edge);
+      if (kArg && edge_z > -INFINITY) p.take(edge_z, edge);  // (a row of nothing else has no largest)
       const float now = fmaxf(p.m, edge_z);
       p.s = p.s * exp_fast(p.m - now) + exp_fast(edge_z - now);
       p.m = now;
