@@ -672,9 +672,10 @@ hydra_status hydra_paged_attention(const hydra_kv_cache* cache, const int32_t* t
  *   logp     : fp32 [S, D+1] log-probability of each of these tokens under the target, then 0; may be NULL.
  *   accept   : fp32 [S, D] of every draft i < n (greedy: 1 or 0), then 0; may be NULL.
  * Rows past n are not read. Masked logits: -inf cannot be drawn; a target row of nothing but -inf gives token 0 with
- * logp -inf. A NaN or +inf logit makes its row's accept and logp NaN and refuses its draft; the token after is then some
- * token in [0, V). Sums are fp32 and depend on nothing but the row, its start modulo 16 bytes, S, V, n, whether there are
- * draft logits, and the device.
+ * logp -inf. A NaN or +inf logit in target or draft row i, greedy or not and whatever the drafted token's own logit is, makes
+ * accept_i NaN and refuses the draft; in a target row it makes logp NaN, and the token after is then some token in [0, V).
+ * Sums are fp32 and depend on nothing but the row, its start modulo 16 bytes, S, V, n, whether there are draft logits, and the
+ * device.
  * Errors: logits_dtype, D, or draft_logits without gumbel -> HYDRA_ERR_RANGE; S < 0, S > 2^24, V < 1, V > 2^30 or a stride below
  * V -> HYDRA_ERR_SHAPE; a needed pointer NULL, or (D > 0) one of uniform and gumbel alone -> HYDRA_ERR_NULL; logits not
  * aligned to their element -> HYDRA_ERR_ALIGN. On the device: a drafted id out of range -> 0x201, accept NaN, refused; n_draft

@@ -369,6 +369,8 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
       if (x < 0 || x >= V) {
         a = __int_as_float(0x7fffffff);
         if (rank == 0) record_error(p.err, kDevBadTokenId);
+      } else if (isnan(sh.c[lane]) || (draft != nullptr && isnan(sh.c[n + 1 + lane]))) {
+        a = __int_as_float(0x7fffffff);  // a NaN or +inf logit, which makes its row's sum NaN: refused, whatever the draft's own is
       } else if (kGreedy) {
         keep = sh.top[lane] == x;
         a = keep ? 1.f : 0.f;

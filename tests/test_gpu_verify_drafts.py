@@ -191,6 +191,43 @@ def test_sick_logits_and_bad_arguments_on_the_device():
     assert torch.equal(o["tokens"][1:], ref["tokens"][1:])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mode", ["draft", "given", "greedy"])
+@pytest.mark.parametrize("what", [NAN, INF])
+@pytest.mark.parametrize("V,ld,shift,at", [(900, 900, 0, 450), (901, 907, 3, 0), (901, 907, 3, 900)])
+def test_sick_rows_refuse_their_drafts(V, ld, shift, at, what, mode, dtype):
+    """`what` at one token of target row 1 of three: the drafted token is the row's largest finite logit, masked, or the sick one
+    itself; a masked token under a sick draft row; a sick target row beside a draft row of nothing but -inf. With u = 0
+    everything else is kept."""
+    S, D = 6, 3
+    c = make(14, S, D, V, dtype, mode, ld=ld, shift=shift, n_draft=None)
+    z = c["z"].view(S, D + 1, V)
+    c["ids"] = z[:, :D].double().cpu().numpy().argmax(-1)
+    if c["u"] is not None:
+        c["u"][:] = 0.0
+    masked = (at + 7) % V
+    z[:4, 1, at] = what
+    finite = z[:, 1].double().cpu().numpy()
+    finite[:4, at] = -INF
+    c["ids"][:, 1] = finite.argmax(-1)
+    c["ids"][1, 1], c["ids"][2, 1] = masked, at
+    z[1, 1, masked] = -INF
+    sick = [0, 1, 2, 3]
+    if mode == "draft":
+        w = c["w"].view(S, D, V)
+        w[3, 1] = -INF
+        z[4, 1, masked], w[4, 1, at] = -INF, what
+        c["ids"][4, 1] = masked
+        sick.append(4)
+    o = {k: v.cpu() for k, v in run(c).items()}
+    for s in range(S):
+        kept = 1 if s in sick else 3
+        assert o["accepted"][s] == kept and o["tokens"][s, :kept].tolist() == c["ids"][s, :kept].tolist(), s
+        assert 0 <= o["tokens"][s, kept] < V and (o["tokens"][s, kept + 1:] == -1).all(), s
+        assert torch.isnan(o["accept"][s]).tolist() == [False, s in sick, False], s
+        assert torch.isnan(o["logp"][s, :4]).tolist() == [False, s < 4, False, False], s
+
+
 def test_frequencies_are_the_targets():
     """20000 sequences with one draft each over five tokens: the first token is the target's draw. A count of n draws
     with probability p is off by 5 sqrt(n p (1 - p)) less than once in a million."""
