@@ -709,7 +709,8 @@ def verify_drafts(z, w, ids, n_draft, uniform, gumbel, S, D):
                     else:
                         rest = np.log(np.maximum(np.exp(lp[kept]) - np.exp(lq[kept]), 0.0))
                     score = rest if rest.max() > -np.inf else score
-                score = score + np.asarray(gumbel[s], dtype=np.float64)
+                top = score.max()  # (off first: what is added to the type's lowest value leaves it as it is)
+                score = (score - top if np.isfinite(top) else score) + np.asarray(gumbel[s], dtype=np.float64)
             row = [int(x) for x in ids[s][:kept]] + [int(np.argmax(score))]
             out["accepted"][s] = kept
             for i, x in enumerate(row):

@@ -459,12 +459,15 @@ __global__ void __launch_bounds__(kThreads, 2) verify_kernel(const VerifyArgs p,
             g[i] = v < to ? noise[v] : 0.f;
           }
 #pragma unroll
-          for (int i = 0; i < kDeep; ++i)
-            if (const int v = first + kThreads * i; z[i] + g[i] > b.v && v != gone) {
-              b.v = z[i] + g[i];
+          for (int i = 0; i < kDeep; ++i) {
+            // (the maximum off first: beside logits of 10^5 noise would be left with steps of 1/128)
+            const float score = (z[i] - pm) + g[i];
+            if (const int v = first + kThreads * i; score > b.v && v != gone) {
+              b.v = score;
               b.i = v;
               b.z = z[i];
             }
+          }
         }
       }
       b.take_lanes(32);

@@ -228,6 +228,31 @@ def test_sick_rows_refuse_their_drafts(V, ld, shift, at, what, mode, dtype):
         assert torch.isnan(o["logp"][s, :4]).tolist() == [False, s < 4, False, False], s
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mode", ["draft", "given"])
+@pytest.mark.parametrize("base", [1e6, -3e5, 3e37, "lowest"])
+def test_noise_counts_beside_logits_of_any_size(base, mode, dtype):
+    """Draws from a row of large logits, some of which are equal: the noise decides between them as between small ones."""
+    S, D, V = 200, 2, 1000
+    c = make(15, S, D, V, dtype, mode, n_draft=np.arange(S) % (D + 1))
+    if base == "lowest":
+        for x in (c["z"], c["w"]):
+            if x is not None:
+                x.fill_(torch.finfo(TYPES[dtype]).min)
+    else:
+        step = 2.0 ** np.floor(np.log2(abs(base))) * (2.0 ** -22 if dtype == "f32" else 2.0 ** -7)
+        rng = np.random.default_rng(16)
+        for x in (c["z"], c["w"]):
+            if x is not None:
+                x.copy_(torch.from_numpy(base + step * rng.integers(0, 3, tuple(x.shape))).cuda())
+    o = run(c)
+    check(c, o)
+    if base == "lowest" and mode == "draft":  # equal rows: all is kept, and the token after is the noise's largest
+        n = c["n"]
+        assert (o["accepted"].cpu().numpy() == n).all()
+        assert (o["tokens"].cpu().numpy()[np.arange(S), n] == c["g"].argmax(-1)).all()
+
+
 def test_frequencies_are_the_targets():
     """20000 sequences with one draft each over five tokens: the first token is the target's draw. A count of n draws
     with probability p is off by 5 sqrt(n p (1 - p)) less than once in a million."""
