@@ -774,7 +774,7 @@ def _kv_pair(k, v, rows, cache, dtype, dev, names):
         ld_k = ld_v
     if ld_k != ld_v:
         raise ValueError(f"{names[0]} and {names[1]} must have one row stride, got {ld_k} and {ld_v}")
-    return pk, pv, ld_k or heads * D
+    return pk, pv, ld_k
 
 
 def hydra_kv_append(cache, table, cached, lengths, S, L, q, k, v, rope_table=None, q_out=None, stream=None):

@@ -203,6 +203,24 @@ def test_binding_refuses_tensors_off_the_gpu_and_of_other_shapes(lib):
         H.hydra_verify_drafts(torch.zeros(4, 10), None, None, None, None, None, 1, 3, None, None)
 
 
+def test_rows_that_are_one_row_repeated_are_refused(lib):
+    """Keys and values (or outputs) expanded from a single row: their stride of 0 goes to the library as it is, which refuses it.
+    As the stride of dense rows, rows past the first would lie outside the tensor."""
+    class Two:
+        n_kv_heads, head_dim = 2, 128
+    bf16 = torch.bfloat16
+    one, dense = torch.zeros(1, 256, dtype=bf16), torch.zeros(6, 256, dtype=bf16)
+    for k, v in ((one.expand(6, 256),) * 2, (None, one.expand(6, 256)), (one.expand(6, 256), None)):
+        *_, ld = H._kv_pair(k, v, 6, Two, bf16, -1, ("k", "v"))
+        assert ld == 0
+    assert _append(lib, ld_kv=0) == 2 and _read(lib, ld=0) == 2
+    with pytest.raises(ValueError):
+        H._kv_pair(one.expand(6, 256), dense, 6, Two, bf16, -1, ("k", "v"))
+    assert H._kv_pair(dense, dense, 6, Two, bf16, -1, ("k", "v"))[2] == 256
+    assert H._kv_pair(one, None, 1, Two, bf16, -1, ("k", "v"))[2] == 256
+    assert H._kv_pair(dense[:0], dense[:0], 0, Two, bf16, -1, ("k", "v"))[2] == 256
+
+
 def test_cache_struct_layout_is_the_headers():
     assert ctypes.sizeof(H.KvCacheC) == 48
     assert [getattr(H.KvCacheC, n).offset for n in ("data", "n_pages", "page", "n_kv_heads", "head_dim", "kind")] == [0, 8, 16, 24, 32, 40]
