@@ -11,10 +11,13 @@
 // In 4 bits a code enters as the fp16 integer code - zero: its bits over those of 1024 (or 16 times it over 1024, for the
 // upper nibble of a byte) are a float, less 1024 + zero, all exact; what is 16 times too large is undone in q and at
 // the end. So keys' products are exact up to the sums, their scale is multiplied in fp32 after, and a value's scale goes
-// into its probability, which is the one thing that is rounded (to fp16, 2^-12; bf16's 2^-9 would add as much again to the
-// error as the output's own rounding). To keep that in fp16's range, m is not the largest score but that of probability
-// times scale, and moved only when a row's passes the range, which a vote finds: the pass would spend its time on
-// maxima else. A bf16 cache takes the probability as two bf16.
+// into its probability, which is the one thing that is rounded: to fp16, 2^-12, which adds a hundredth to the error that the
+// output's own rounding makes. (bf16's 2^-9 would add as much again; what the rounding leaves as a second fp16 number is 10 to
+// 15 % of the time: 53.7, 38.2 and 71.2 us for 64 sequences of 800 tokens, 16 of 4096 and 3 of 131,072, against 47.4, 34.6 and
+// 61.8.) To keep that in fp16's range, each row has a power of two for each group of channels (`lift`) by which the group's
+// weights are held, so that a group's precision is its own, whatever the other's scales are. m, a whole number, and the lifts
+// are moved only when a row's weights pass the range, which a vote finds: the pass would spend its time on maxima else. A bf16
+// cache takes the probability as two bf16.
 //
 // A bf16 cache is bound by its bytes (8 sequences of up to 32,768 tokens, 8 heads: 580 MB in 92 us, 6.3 TB/s). In 4 bits the
 // copies are hidden and what a tile costs to unpack and multiply, 360 instructions of a warp for 2304 bytes, is as much as
@@ -55,10 +58,11 @@ constexpr int64_t kAlignedTokens = 1280;
 // with 0; 64 sequences of up to 800, 32 heads: 47, 48, 48, 65).
 constexpr int kItemUnits = 6;
 constexpr float kFar = -1e30f;    // a maximum of nothing
-// Exponents relative to m. bf16: a probability up to 2^8. 4 bits: probability times scale from 2^6, when m is set, up to 2^14
-// (fp16 ends at 2^16, and keeps 11 bits down to 2^-14); the probability alone, whose scale may be 0, up to 2^108. (For
-// values' scales above 2^100 probabilities far below the largest are flushed.)
-constexpr float kSlack = 8.f, kTop = 6.f, kMost = 14.f, kAlone = 100.f;
+// Exponents: of a probability relative to m up to 2^8; in 4 bits of probability times scale times the group's lift, of which the
+// largest is put between 2^6 and 2^7 when the lift is set, up to 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14). A
+// lift is at most 2^118, so that its product with a probability is finite, and at least 2^-126.
+constexpr float kSlack = 8.f, kMost = 14.f;
+constexpr int kTop = 7, kLiftMost = 118, kLiftLeast = -126;
 
 // What a CTA leaves for the second kernel.
 struct Desc {
@@ -133,9 +137,10 @@ __device__ __forceinline__ float ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-__device__ __forceinline__ float lg2(float x) {
+// (-inf below 2^-126)
+__device__ __forceinline__ float lg2_or_none(float x) {
   float y;
-  asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 __device__ __forceinline__ uint32_t max_f16(uint32_t a, uint32_t b) {
@@ -163,8 +168,16 @@ __device__ __forceinline__ uint32_t add_f16(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
+  return r;
+}
 // 2^e, e in [-126, 127]
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
+__device__ __forceinline__ float pow2_or_0(int e) { return pow2(max(e, -127)); }  // 0 below 2^-126
 
 // (w & mask) | bits in one instruction: `bits` comes from a register, as two constants in one would take two instructions
 template <uint32_t kMask>
@@ -493,7 +506,9 @@ struct Rows {
   int first_limit, last_limit;  // the least and the largest of the rows'
   // fragments of 16 channels; in 4 bits fp16, of which the second word is a sixteenth
   const uint2* q;
+  static constexpr int kGroups = kInt4 ? kDh / kKvGroup : 1;  // of channels that have a scale of their own
   float o[C::kMTiles][4], m[2], l[2];
+  float lift[2][kGroups];  // 4 bits: powers of two by which a group's weights are held (o with them) for fp16's range
   uint32_t plus1024, minus1024;  // kFp16Of1024, kFp16OfMinus1024 in registers
 
   __device__ __forceinline__ uint2 query(int step, int lane) const { return q[step * 32 + lane]; }
@@ -567,6 +582,8 @@ struct Rows {
                     (geo.group == geo.rows ? 0 : min((c.rt * kRows + 2 * t + e) / geo.group, c.seq.n - 1));
       m[e] = kFar;
       l[e] = 0.f;
+#pragma unroll
+      for (int gr = 0; gr < kGroups; ++gr) lift[e][gr] = 1.f;
     }
 #pragma unroll
     for (int j = 0; j < C::kMTiles; ++j)
@@ -581,7 +598,6 @@ struct Rows {
   template <int kN, bool kMasked>
   __device__ __forceinline__ void take(const uint8_t* first_tile, int pos, int lane) {
     using Tile = typename C::Tile;
-    constexpr int kGroups = kInt4 ? kDh / kKvGroup : 1;  // that have a scale of their own
     constexpr int kWords = kDh / 32;
     const int g = lane >> 2, t = lane & 3;
     // ---- scores: S^T = K q^T
@@ -682,20 +698,20 @@ struct Rows {
         for (int e = 0; e < 4; ++e) {
           float ex = fmaf(sc[i][e], factor[e & 1], -m[e & 1]);
           if (hidden(i, e)) ex = -INFINITY;
-          far |= ex > (kInt4 ? kAlone + kSlack : kSlack);
+          far |= ex > kSlack;
           pr[i][e] = ex2(ex);
         }
         if constexpr (kInt4) {
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
-            float w[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              w[e] = pr[i][e] * sv[i][e >> 1][gr];
-              if (hidden(i, e)) w[e] = 0.f;  // whatever its scale is
+            for (int h = 0; h < 2; ++h) {  // (both rows at once: 64 sequences of up to 800 tokens 47.4 us, singly 48.8)
+              float2 w = mul2(mul2(make_float2(pr[i][2 * h], pr[i][2 * h + 1]), make_float2(lift[0][gr], lift[1][gr])),
+                              make_float2(sv[i][h][gr], sv[i][h][gr]));
+              if (hidden(i, 2 * h)) w.x = 0.f;  // whatever its scale is
+              if (hidden(i, 2 * h + 1)) w.y = 0.f;
+              pf[i][gr][h] = pack_f16(w.x, w.y);
             }
-            pf[i][gr][0] = pack_f16(w[0], w[1]);
-            pf[i][gr][1] = pack_f16(w[2], w[3]);
             most = max_f16(most, max_f16(pf[i][gr][0], pf[i][gr][1]));
           }
         }
@@ -704,33 +720,72 @@ struct Rows {
       return far;
     };
     if (__any_sync(0xffffffffu, probabilities())) {
+      // (both rows at once: this runs at every item's start)
+      float score[kN][4], top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          score[i][e] = hidden(i, e) ? -INFINITY : sc[i][e] * factor[e & 1];
+          top[e & 1] = fmaxf(top[e & 1], score[i][e]);
+        }
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) top[e] = fmaxf(top[e], __shfl_xor_sync(0xffffffffu, top[e], off));
+      // (a row of which nothing passes its range keeps what it has: what it does not see must not change it; whole exponents, so
+      // that what is added up is scaled without a rounding)
+      int up[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float top = -INFINITY, top_w = -INFINITY;
+        const bool moves = top[e] - m[e] > kSlack;
+        const float now = moves ? ceilf(top[e]) : m[e];
+        up[e] = moves ? static_cast<int>(fminf(now - m[e], 1000.f)) : 0;
+        m[e] = now;
+        l[e] *= pow2_or_0(-up[e]);
+      }
+      if constexpr (kInt4) {
+        float most[2][kGroups];
 #pragma unroll
-        for (int i = 0; i < kN; ++i)
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const float x = hidden(i, e + 2 * h) ? -INFINITY : sc[i][e + 2 * h] * factor[e];
-            top = fmaxf(top, x);
-            if constexpr (kInt4) top_w = fmaxf(top_w, x + lg2(fmaxf(sv[i][h][0], sv[i][h][kGroups - 1])));
+          for (int gr = 0; gr < kGroups; ++gr) {
+            most[e][gr] = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kN; ++i)
+#pragma unroll
+              for (int h = 0; h < 2; ++h) most[e][gr] = fmaxf(most[e][gr], score[i][e + 2 * h] - m[e] + lg2_or_none(sv[i][h][gr]));
           }
 #pragma unroll
-        for (int off = 4; off < 32; off <<= 1) {
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-          if constexpr (kInt4) top_w = fmaxf(top_w, __shfl_xor_sync(0xffffffffu, top_w, off));
-        }
-        // (the other rows keep theirs: what a row does not see must not change it)
-        if (kInt4 ? top_w - m[e] > kMost || top - m[e] > kAlone + kSlack : top - m[e] > kSlack) {
-          const float now = kInt4 ? fmaxf(top_w - kTop, top - kAlone) : top, by = ex2(m[e] - now);
-          m[e] = now;
-          l[e] *= by;
+        for (int off = 4; off < 32; off <<= 1)
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int gr = 0; gr < kGroups; ++gr) most[e][gr] = fmaxf(most[e][gr], __shfl_xor_sync(0xffffffffu, most[e][gr], off));
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int gr = 0; gr < kGroups; ++gr) {
+            // what is held stays what it is when m moves, as far as the lift reaches
+            const int was = (__float_as_int(lift[e][gr]) >> 23) - 127 + up[e];
+            const int by = min(most[e][gr] + static_cast<float>(was) > kMost ? max(kTop - static_cast<int>(ceilf(most[e][gr])), kLiftLeast) : was,
+                               kLiftMost);
+            lift[e][gr] = pow2(by);
+            const float held = pow2_or_0(by - was);
+#pragma unroll
+            for (int j = gr * 4; j < gr * 4 + 4; ++j) {
+              o[j][e] *= held;
+              o[j][e + 2] *= held;
+            }
+          }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
 #pragma unroll
           for (int j = 0; j < C::kMTiles; ++j) {
-            o[j][e] *= by;
-            o[j][e + 2] *= by;
+            o[j][e] *= pow2_or_0(-up[e]);
+            o[j][e + 2] *= pow2_or_0(-up[e]);
           }
-        }
       }
       probabilities();
     }
@@ -865,9 +920,14 @@ struct Rows {
     const int g = lane >> 2;
     const float high = kInt4 ? by * 0.0625f : by;
 #pragma unroll
-    for (int j = 0; j < C::kMTiles; j += 2)
-      f(kInt4 ? 64 * (j >> 2) + 8 * g + 2 * (j & 3) : 32 * (j >> 1) + 4 * g,
-        make_float4(o[j][e] * by, o[j][e + 2] * high, o[j + 1][e] * by, o[j + 1][e + 2] * high));
+    for (int j = 0; j < C::kMTiles; j += 2) {
+      float4 v = make_float4(o[j][e] * by, o[j][e + 2] * high, o[j + 1][e] * by, o[j + 1][e + 2] * high);
+      if constexpr (kInt4) {
+        const float held = pow2(127 - (__float_as_int(lift[e][j >> 2]) >> 23));  // its reciprocal
+        v = make_float4(v.x * held, v.y * held, v.z * held, v.w * held);
+      }
+      f(kInt4 ? 64 * (j >> 2) + 8 * g + 2 * (j & 3) : 32 * (j >> 1) + 4 * g, v);
+    }
   }
 };
 
