@@ -984,7 +984,8 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
     rows.minus1024 = held(kFp16OfMinus1024);
     int used = 0;  // stages
     int lo = 0, tile = 0, hi = 0, live = 0;  // the warp's part of the present item, the next tile; rows with a token
-    bool open = false, poison = false;
+    bool open = false;
+    int bad_from = INT_MAX;  // first position of the item whose page is none of the cache's
     // (one place each where a stage is filled, an item begun and ended: what runs rarely runs from a cold instruction cache)
     int fast = 0;  // stages that need no second look, neither when taken nor (copying) when filled again
     bool copying = false;
@@ -1015,6 +1016,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
             float sum = rows.l[e];
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            const bool poison = rows.limit[e] >= bad_from;  // (a row that ends before it is what it is)
             const float by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
             if (whole) {
               if (row < slots) {
@@ -1058,7 +1060,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
         left -= units_of_item(c.tiles) - lo;
         live = R::live_rows(geo, c);
         open = true;
-        poison = false;
+        bad_from = INT_MAX;
         commit_copies();
         wait_copies<0>();
         rows.begin(p, geo, c, live, lane, queries);
@@ -1078,7 +1080,8 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
         const uint8_t* const at = ring + (used & (C::kStages - 1)) * C::kStageBytes;
         wait_copies<C::kStages - 1>();
         if (loader.bad)  // rare: whether it is these tiles' pages
-          for (int i = 0; i < n; ++i) poison |= kv_page(p.batch, p.cache, take.s, pos + i * kKvTile, nullptr) < 0;
+          for (int i = 0; i < n; ++i)
+            if (kv_page(p.batch, p.cache, take.s, pos + i * kKvTile, nullptr) < 0) bad_from = min(bad_from, pos + i * kKvTile);
 #pragma unroll 1
         for (int i = 0; i < n; ++i) rows.template take<1, true>(at + i * Tile::kBytes, pos + i * kKvTile, lane);
         __syncwarp();

@@ -1,5 +1,5 @@
-"""Attention over a paged cache where single precision or a half's range could run out: groups of channels of very different
-size. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
+"""Attention over a paged cache at its limits: groups of channels of very different size, bad pages that only some rows of
+an item read. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
 fp16's least step adds: a weight is off by 2^-25 at most where the largest product of probability and scale that the row has
 met in that group of 64 channels is 2^6 or more. Relative to the row's largest product over all tokens it is off by 2^-31, times a
 code of up to 15, and a scale is at most max |v| / 7.5 of its token and group, so over N tokens
@@ -27,14 +27,16 @@ def lib():
     assert H.device_error(clear=True) == 0
 
 
-def check_groups(c, got):
-    """Every channel against its own group's tolerance."""
+def check_groups(c, got, rows=None):
+    """Every channel against its own group's tolerance; `rows`: of the first so many new tokens of each sequence."""
     S, L, D, heads, kv = c["S"], c["L"], c["D"], c["heads"], c["kv"]
     got = got.double().cpu().numpy().reshape(S, L, heads, D)
     q = c["q"].double().numpy().reshape(S, L, heads, D)
     scale, by = D ** -0.5, heads // kv
     for s in range(S):
-        n, at = int(c["lengths"][s]), int(c["cached"][s])
+        n, at = int(c["lengths"][s] if rows is None else rows[s]), int(c["cached"][s])
+        if n == 0:
+            continue
         N = at + n
         k, v = (c[x][s, :N].astype(np.float64) for x in ("k", "v"))
         ref, size, reach = O.cached_attention(q[s, :n], k, v, at, scale)
@@ -90,3 +92,22 @@ def test_values_near_the_ends_of_bf16(D):
 
     c = make(62, 2, 4, 2, D, 16, True, [200] * 3, change=change)
     check_groups(c, attend(c))
+
+
+@pytest.mark.parametrize("int4", [True, False])
+@pytest.mark.parametrize("page,cached,L,bad", [(16, [12, 11, 2009], 8, 1), (32, [29, 1, 3101], 40, 1), (16, [0, 9, 33], 17, 0)])
+def test_rows_that_end_before_a_bad_page_keep_theirs(page, cached, L, bad, int4):
+    """The new tokens cross into a page that the table does not name (`bad` pages past the one that the first of them is in): those
+    before it are what they should be, those behind it NaN. Sequences that are cut between CTAs among them."""
+    c = make(63, L, 8, 2, 64, page, int4, cached)
+    first = []
+    for s in range(3):
+        entry = cached[s] // page + bad
+        c["table"][s, entry] = -1 if s % 2 else c["cache"].n_pages
+        first.append(max(0, entry * page - cached[s]))
+    got = attend(c)
+    assert H.device_error(clear=True) == 0x203
+    check_groups(c, got, first)
+    got = got.cpu().view(3, L, -1)
+    for s in range(3):
+        assert torch.isnan(got[s, first[s]:]).all() and first[s] < L, s
