@@ -57,7 +57,8 @@ constexpr int64_t kAlignedTokens = 1280;
 // What an item costs beside its tiles, in tiles (16 sequences x 20 rows over up to 4096 tokens: 35 us with 6 or 12, 36 with 3, 52
 // with 0; 64 sequences of up to 800, 32 heads: 47, 48, 48, 65).
 constexpr int kItemUnits = 6;
-constexpr float kFar = -1e30f;    // a maximum of nothing
+constexpr float kFar = -1e30f;           // a maximum of nothing
+constexpr float kNothing = -INFINITY;    // mass of a part whose scores are all -inf
 // Exponents: of a probability relative to m up to 2^8; in 4 bits of probability times scale times the group's lift, of which the
 // largest is put between 2^6 and 2^7 when the lift is set, up to 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14). A
 // lift is at most 2^118, so that its product with a probability is finite, and at least 2^-126.
@@ -1017,7 +1018,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
 #pragma unroll
             for (int off = 4; off < 32; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
             const bool poison = rows.limit[e] >= bad_from;  // (a row that ends before it is what it is)
-            const float by = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? 0.f : 1.f / sum;
+            const float by = poison ? __int_as_float(0x7fffffff) : 1.f / sum;  // (NaN where all scores are -inf)
             if (whole) {
               if (row < slots) {
                 __nv_bfloat16* dst = out_row(p, geo, c.s, row0 + row, c.h, kDh);
@@ -1031,7 +1032,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
             } else if (row < live) {
               rows.each(e, by, lane, [&](int d, const float4& v) { *reinterpret_cast<float4*>(part_o + row * kDh + d) = v; });
               if (g == 0)
-                part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kFar : rows.m[e] + log2f(sum);
+                part_mass[row] = poison ? __int_as_float(0x7fffffff) : sum == 0.f ? kNothing : rows.m[e] + log2f(sum);
             }
           }
           if (!whole) {
@@ -1136,7 +1137,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
       const Parts* far_part = warp_part<kDh>(p, w0);
       const float* row_at = there && !near ? far_part->o[row]
                                            : reinterpret_cast<const float*>(smem + w0 * (C::kStages * C::kStageBytes)) + row * kDh;
-      const float mass = !there ? kFar : near ? sh.mass[w0][row] : far_part->mass[row];
+      const float mass = !there ? kNothing : near ? sh.mass[w0][row] : far_part->mass[row];
       Vec in[kWarps];
 #pragma unroll
       for (int w = 0; w < kWarps; ++w)
@@ -1144,11 +1145,11 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
       float top = mass;
 #pragma unroll
       for (int off = 4; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-      const float weight = mass == kFar ? 0.f : ex2(mass - top);
+      const float weight = mass == kNothing ? 0.f : ex2(mass - top);
       float sum = weight;
 #pragma unroll
       for (int off = 4; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      const float share = sum == 0.f ? 0.f : weight / sum;
+      const float share = weight / sum;  // (0 / 0 where all scores are -inf: NaN, which the mass keeps from counting beside others)
       float out[kE];
 #pragma unroll
       for (int i = 0; i < kE; ++i) out[i] = 0.f;
@@ -1169,7 +1170,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
 #pragma unroll
         for (int i = 0; i < kE; ++i) to->o[row][lane * kE + i] = out[i];
         const float total = __shfl_sync(0xffffffffu, sum, 0), highest = __shfl_sync(0xffffffffu, top, 0);
-        if (lane == 0) to->mass[row] = total == 0.f ? kFar : highest + log2f(total);
+        if (lane == 0) to->mass[row] = total == 0.f ? kNothing : highest + log2f(total);
       }
     }
     turn += shown;
@@ -1215,7 +1216,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   using Vec = std::conditional_t<kDh == 128, float4, float2>;
   constexpr int kE = kDh / 32;
   const int n = end - b;
-  float mass = kFar, top, sum = 0.f, out[kE];
+  float mass = kNothing, top, sum = 0.f, out[kE];
   for (int i = lane; i < n; i += 32) mass = fmaxf(mass, cta_part<kDh>(p, b + i, i == 0 ? mine.slot : 0)->mass[row]);
   top = mass;
 #pragma unroll
@@ -1226,7 +1227,7 @@ __global__ void __launch_bounds__(kThreads) paged_attention_join_kernel(const Pa
   for (int i = warp; i < n; i += kWarps) {
     const Part<kDh>* part = cta_part<kDh>(p, b + i, i == 0 ? mine.slot : 0);
     const Vec x = reinterpret_cast<const Vec*>(part->o[row])[lane];
-    const float m = part->mass[row], weight = m == kFar ? 0.f : ex2(m - top);
+    const float m = part->mass[row], weight = m == kNothing ? 0.f : ex2(m - top);
     sum += weight;
 #pragma unroll
     for (int e = 0; e < kE; ++e)

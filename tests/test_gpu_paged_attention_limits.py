@@ -1,5 +1,5 @@
 """Attention over a paged cache at its limits: groups of channels of very different size, bad pages that only some rows of
-an item read. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
+an item read, infinite keys. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
 fp16's least step adds: a weight is off by 2^-25 at most where the largest product of probability and scale that the row has
 met in that group of 64 channels is 2^6 or more. Relative to the row's largest product over all tokens it is off by 2^-31, times a
 code of up to 15, and a scale is at most max |v| / 7.5 of its token and group, so over N tokens
@@ -16,6 +16,8 @@ from tests.test_gpu_paged_attention import U, attend, make
 
 pytestmark = pytest.mark.gpu
 
+INF, NAN = float("inf"), float("nan")
+
 
 @pytest.fixture(scope="module", autouse=True)
 def lib():
@@ -27,32 +29,41 @@ def lib():
     assert H.device_error(clear=True) == 0
 
 
+def check_one(q, k, v, cached, scale, got, what=""):
+    """Rows [n, heads, D] of one sequence over held keys and values [cached + n, kv heads, D]: every channel against its own
+    group's tolerance."""
+    n, heads, D = q.shape
+    N, kv = k.shape[:2]
+    by = heads // kv
+    ref, size, reach = O.cached_attention(q, k, v, cached, scale)
+    coarse = np.abs(q).max(-1) * np.abs(k).sum(-1).max(0).repeat(by)[None] * scale
+    e = ((2 * (D + D // 16) + 16) * U * reach + 2.0 ** -28 * coarse)[..., None]
+    largest = np.abs(v).reshape(N, kv, D // 64, 64).max(-1)  # of a token, head and group
+    most = np.zeros((n, heads, D // 64))
+    for t in range(n):
+        for h in range(heads):
+            z = k[:cached + t + 1, h // by] @ q[t, h] * scale
+            p = np.exp(z - z.max())
+            most[t, h] = (p[:, None] / p.sum() * largest[:cached + t + 1, h // by]).max(0)
+    tol = (2.0 ** -11 + 2 * e + (N + 128) * U) * size + N * 2.0 ** -30 * most.repeat(64, -1)
+    tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
+    off = np.abs(got - ref)
+    assert np.isfinite(got).all() and (off <= tol).all(), f"{what}: {np.max(off / np.maximum(tol, 1e-300)):.3g}"
+
+
+def fp64(c, got):
+    """(queries, output) [S, L, heads, D]"""
+    return (x.double().cpu().numpy().reshape(c["S"], c["L"], c["heads"], c["D"]) for x in (c["q"], got))
+
+
 def check_groups(c, got, rows=None):
-    """Every channel against its own group's tolerance; `rows`: of the first so many new tokens of each sequence."""
-    S, L, D, heads, kv = c["S"], c["L"], c["D"], c["heads"], c["kv"]
-    got = got.double().cpu().numpy().reshape(S, L, heads, D)
-    q = c["q"].double().numpy().reshape(S, L, heads, D)
-    scale, by = D ** -0.5, heads // kv
-    for s in range(S):
+    """`rows`: of the first so many new tokens of each sequence."""
+    q, got = fp64(c, got)
+    for s in range(c["S"]):
         n, at = int(c["lengths"][s] if rows is None else rows[s]), int(c["cached"][s])
-        if n == 0:
-            continue
-        N = at + n
-        k, v = (c[x][s, :N].astype(np.float64) for x in ("k", "v"))
-        ref, size, reach = O.cached_attention(q[s, :n], k, v, at, scale)
-        coarse = np.abs(q[s, :n]).max(-1) * np.abs(k).sum(-1).max(0).repeat(by)[None] * scale
-        e = ((2 * (D + D // 16) + 16) * U * reach + 2.0 ** -28 * coarse)[..., None]
-        largest = np.abs(v).reshape(N, kv, D // 64, 64).max(-1)  # of a token, head and group
-        most = np.zeros((n, heads, D // 64))
-        for t in range(n):
-            for h in range(heads):
-                z = k[:at + t + 1, h // by] @ q[s, t, h] * scale
-                p = np.exp(z - z.max())
-                most[t, h] = (p[:, None] / p.sum() * largest[:at + t + 1, h // by]).max(0)
-        tol = (2.0 ** -11 + 2 * e + (N + 128) * U) * size + N * 2.0 ** -30 * most.repeat(64, -1)
-        tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
-        off = np.abs(got[s, :n] - ref)
-        assert np.isfinite(got[s, :n]).all() and (off <= tol).all(), f"sequence {s}: {np.max(off / np.maximum(tol, 1e-300)):.3g}"
+        k, v = (c[x][s, :at + n].astype(np.float64) for x in ("k", "v"))
+        if n > 0:
+            check_one(q[s, :n], k, v, at, c["D"] ** -0.5, got[s, :n], f"sequence {s}")
 
 
 @pytest.mark.parametrize("cached", [[500, 37, 0], [5000, 900]])
@@ -111,3 +122,52 @@ def test_rows_that_end_before_a_bad_page_keep_theirs(page, cached, L, bad, int4)
     got = got.cpu().view(3, L, -1)
     for s in range(3):
         assert torch.isnan(got[s, first[s]:]).all() and first[s] < L, s
+
+
+@pytest.mark.parametrize("cached", [[1, 37, 200], [1, 3100, 37], [4, 12]])  # (a CTA an item, shared ones, few tiles)
+@pytest.mark.parametrize("what", [INF, -INF])
+@pytest.mark.parametrize("D", [64, 128])
+def test_an_infinite_key_in_a_bf16_cache(D, what, cached):
+    """Token 1 of each sequence has it in one channel: its score is +inf or -inf by the query's sign there, which makes the
+    head NaN or drops the token."""
+    def change(k, v):
+        k[:, 1, :, 9] = what
+
+    c = make(64, 2, 4, 2, D, 16, False, cached, change=change)
+    q, got = fp64(c, attend(c))
+    assert (q[..., 9] != 0).all()
+    for s, at in enumerate(cached):
+        k, v = (np.delete(c[x][s, :at + 2].astype(np.float64), 1, axis=0) for x in ("k", "v"))
+        for h in range(4):
+            for t in range(2):
+                if np.sign(q[s, t, h, 9]) == np.sign(what):
+                    assert np.isnan(got[s, t, h]).all(), (s, t, h)
+                else:
+                    check_one(q[s, t:t + 1, h:h + 1], k[:at + t, h // 2:h // 2 + 1], v[:at + t, h // 2:h // 2 + 1], at + t - 1, D ** -0.5,
+                              got[s, t:t + 1, h:h + 1], f"{s}, {t}, {h}")
+
+
+@pytest.mark.parametrize("cached", [[0, 37, 200], [0, 3100, 37], [500] * 40])
+@pytest.mark.parametrize("what", [INF, -INF, NAN])
+@pytest.mark.parametrize("int4", [True, False])
+def test_keys_that_leave_a_query_nothing(int4, what, cached):
+    """Every key has it: all scores are infinite or NaN, however the work is cut."""
+    def change(k, v):
+        k[..., 9] = what
+
+    c = make(65, 2, 4, 2, 64, 16, int4, cached, change=change)
+    assert torch.isnan(attend(c)).all()
+
+
+@pytest.mark.parametrize("what", [INF, -INF, NAN])
+@pytest.mark.parametrize("kind", ["int4", "bf16"])
+def test_one_sick_key_and_the_queries_before_it(kind, what):
+    """The last but one of four new tokens: queries before it are what they were; in 4 bits the others are NaN."""
+    def change(k, v):
+        k[:, -2, :, 9] = what
+
+    c, calm = (make(66, 4, 4, 2, 64, 16, kind == "int4", [29, 29], change=f) for f in (change, None))
+    got, ref = (attend(x).view(2, 4, -1) for x in (c, calm))
+    assert torch.equal(got[:, :2], ref[:, :2])
+    if kind == "int4" or what != what:
+        assert torch.isnan(got[:, 2:]).all()
