@@ -33,6 +33,7 @@
 // as fp16 numbers below the normal range, whose zero points come off the sums, are 295 instructions a tile and no faster.)
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -57,7 +58,7 @@ constexpr int64_t kAlignedTokens = 1280;
 // What an item costs beside its tiles, in tiles (16 sequences x 20 rows over up to 4096 tokens: 35 us with 6 or 12, 36 with 3, 52
 // with 0; 64 sequences of up to 800, 32 heads: 47, 48, 48, 65).
 constexpr int kItemUnits = 6;
-constexpr float kFar = -1e30f;           // a maximum of nothing
+constexpr float kLowest = -FLT_MAX;      // a maximum of nothing yet, which the least finite score does not lie below
 constexpr float kNothing = -INFINITY;    // mass of a part whose scores are all -inf
 // Exponents: of a probability relative to m up to 2^8; in 4 bits of probability times scale times the group's lift, of which the
 // largest is put between 2^6 and 2^7 when the lift is set, up to 2^14 (fp16 ends at 2^16, and keeps 11 bits down to 2^-14). A
@@ -581,7 +582,7 @@ struct Rows {
       factor[e] = __shfl_sync(0xffffffffu, by_row, (2 * t + e) * 4);
       limit[e] = c.seq.cached +
                     (geo.group == geo.rows ? 0 : min((c.rt * kRows + 2 * t + e) / geo.group, c.seq.n - 1));
-      m[e] = kFar;
+      m[e] = kLowest;
       l[e] = 0.f;
 #pragma unroll
       for (int gr = 0; gr < kGroups; ++gr) lift[e][gr] = 1.f;
@@ -690,14 +691,15 @@ struct Rows {
     float pr[kN][4];
     uint32_t pf[kN][2][2];
     auto hidden = [&](int i, int e) { return kMasked && pos + kKvTile * i + g + 8 * (e >> 1) > limit[e & 1]; };
-    auto probabilities = [&]() {
+    // (rounded: with the scores rounded as the maximum was, which the single rounding passes by more than the range beyond 2^25)
+    auto probabilities = [&](bool rounded) {
       bool far = false;
       uint32_t most = 0;
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float ex = fmaf(sc[i][e], factor[e & 1], -m[e & 1]);
+          float ex = rounded ? __fsub_rn(__fmul_rn(sc[i][e], factor[e & 1]), m[e & 1]) : fmaf(sc[i][e], factor[e & 1], -m[e & 1]);
           if (hidden(i, e)) ex = -INFINITY;
           far |= ex > kSlack;
           pr[i][e] = ex2(ex);
@@ -720,14 +722,14 @@ struct Rows {
       if constexpr (kInt4) far |= above_f16(most);
       return far;
     };
-    if (__any_sync(0xffffffffu, probabilities())) {
+    if (__any_sync(0xffffffffu, probabilities(false))) {
       // (both rows at once: this runs at every item's start)
       float score[kN][4], top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int i = 0; i < kN; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          score[i][e] = hidden(i, e) ? -INFINITY : sc[i][e] * factor[e & 1];
+          score[i][e] = hidden(i, e) ? -INFINITY : __fmul_rn(sc[i][e], factor[e & 1]);
           top[e & 1] = fmaxf(top[e & 1], score[i][e]);
         }
 #pragma unroll
@@ -788,7 +790,7 @@ struct Rows {
             o[j][e + 2] *= pow2_or_0(-up[e]);
           }
       }
-      probabilities();
+      probabilities(true);
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) {

@@ -1,5 +1,5 @@
 """Attention over a paged cache at its limits: groups of channels of very different size, bad pages that only some rows of
-an item read, infinite keys. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
+an item read, infinite keys, scores of any size. Tolerances as tests/test_gpu_paged_attention.py derives them, with u = 2^-24 and e for a score's error, but for what
 fp16's least step adds: a weight is off by 2^-25 at most where the largest product of probability and scale that the row has
 met in that group of 64 channels is 2^6 or more. Relative to the row's largest product over all tokens it is off by 2^-31, times a
 code of up to 15, and a scale is at most max |v| / 7.5 of its token and group, so over N tokens
@@ -171,3 +171,40 @@ def test_one_sick_key_and_the_queries_before_it(kind, what):
     assert torch.equal(got[:, :2], ref[:, :2])
     if kind == "int4" or what != what:
         assert torch.isnan(got[:, 2:]).all()
+
+
+@pytest.mark.parametrize("cached", [[70, 0, 200], [3000, 37]])
+@pytest.mark.parametrize("sign", [0, 1, -1])
+@pytest.mark.parametrize("size", [1e4, 1e6, 1e9, 1e14, 1e33])
+@pytest.mark.parametrize("int4", [True, False])
+def test_scores_of_any_size(int4, size, sign, cached):
+    """Scores of about +-size (of one sign, or both): where the largest leads by more than the others can be off, its value is the
+    output. A score is off by e as above and by a product's rounding; then its weight is 1 of all but 2^-30, and enters the sum rounded
+    (2^-11 and 16 u), as does its value to bf16."""
+    def change(k, v):
+        if sign:
+            k[:] = np.abs(k)
+
+    by = np.sqrt(size)
+    c = make(67, 2, 4, 2, 128, 16, int4, cached, k_by=by, q_by=by, change=change)
+    if sign:
+        c["q"] = c["q"].abs() * sign
+    q, got = fp64(c, attend(c))
+    assert np.isfinite(got).all()
+    led = 0
+    for s, at in enumerate(cached):
+        for t in range(2):
+            for h in range(4):
+                k, v = (c[x][s, :at + t + 1, h // 2].astype(np.float64) for x in ("k", "v"))
+                z = k @ q[s, t, h] * 128 ** -0.5
+                reach = (np.abs(k) @ np.abs(q[s, t, h])).max() * 128 ** -0.5
+                coarse = np.abs(q[s, t, h]).max() * np.abs(k).sum(-1).max() * 128 ** -0.5
+                e = (2 * (128 + 8) + 16) * U * reach + 2.0 ** -28 * coarse + 4 * U * np.abs(z).max()
+                lead = np.partition(z, -2)[-2:] if len(z) > 1 else np.array([-np.inf, z[0]])
+                if lead[1] - lead[0] <= 2 * e + np.log(len(z) * 2.0 ** 30):
+                    continue
+                led += 1
+                one = v[z.argmax()]
+                tol = (2.0 ** -11 + 16 * U) * np.abs(one) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(one) + 2.0 ** -30 * np.abs(v).max()
+                assert (np.abs(got[s, t, h] - one) <= tol).all(), (s, t, h)
+    assert led >= 8
