@@ -640,9 +640,11 @@ hydra_status hydra_kv_read(const hydra_kv_cache* cache, const int32_t* table, in
  * change it. An infinity or NaN among the values that a query sees makes that channel of its output (in 4 bits its group of
  * channels) infinite or NaN. A NaN among its keys makes the whole head NaN, and in 4 bits an infinity as well; in a bf16 cache
  * a key's infinity makes a score infinite: +inf makes the head NaN, a token with -inf weighs nothing, and where all that a query
- * sees have -inf the head is NaN. Scores, their maximum and sums are fp32. Weights enter
- * the sum over values rounded: from a cache in 4 bits a weight times its value's scale in fp16 (2^-12 of it, and where it is less
- * than 2^-20 of the largest such product of its row and its 64 channels, 2^-31 of that), from a bf16 cache as two bf16 (2^-16).
+ * sees have -inf the head is NaN.
+ * Scores, their maximum and sums are fp32. A cache in 4 bits takes queries as they are down to 2^-28 of their head's largest
+ * channel, what is less with an error of 2^-35 of it, and a weight times its value's scale in fp16 (2^-12 of it, and where it is
+ * less than 2^-20 of the largest such product of its row and its 64 channels, 2^-31 of that); a bf16 cache takes weights as two
+ * bf16 (2^-16).
  * Bits: equal calls on one device give equal bits; a sequence's depend on the others' lengths (where work is cut) and on
  * whether one of the call's pages is bad.
  * Errors as hydra_kv_append; n_heads not a multiple of n_kv_heads -> HYDRA_ERR_SHAPE; scale not finite ->

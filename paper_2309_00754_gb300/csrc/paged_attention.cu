@@ -532,8 +532,8 @@ struct Rows {
     }
   }
 
-  // The queries' fragments; in 4 bits each row times a power of two that makes its largest 2^7 to 2^8 (fp16 holds all bits
-  // of a bf16 down to 2^-21 of that; a row with an infinity or NaN is NaN).
+  // The queries' fragments; in 4 bits each row times a power of two that makes its largest 2^14 to 2^15 (fp16 holds all bits of a
+  // bf16 down to 2^-28 of that, of the part that is a sixteenth, too; a row with an infinity or NaN is NaN).
   __device__ __forceinline__ void begin(const PagedAttentionArgs& p, const Geometry& geo, const Place& c, int live, int lane,
                                         uint2* shared) {
     const int g = lane >> 2, t = lane & 3;
@@ -561,7 +561,7 @@ struct Rows {
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
       const int exponent = (__float_as_int(top) >> 23) - 127;  // -127 for 0 and what is below 2^-126
-      const int by = min(126, 7 - exponent);
+      const int by = min(126, 14 - exponent);
       by_row = exponent > 127 ? __int_as_float(0x7fffffff) : by_row * pow2(max(-by, -126));
       const float up = pow2(by);
 #pragma unroll

@@ -29,7 +29,7 @@ def lib():
     assert H.device_error(clear=True) == 0
 
 
-def check_one(q, k, v, cached, scale, got, what=""):
+def check_one(q, k, v, cached, scale, got, what="", step=2.0 ** -28):
     """Rows [n, heads, D] of one sequence over held keys and values [cached + n, kv heads, D]: every channel against its own
     group's tolerance."""
     n, heads, D = q.shape
@@ -37,7 +37,7 @@ def check_one(q, k, v, cached, scale, got, what=""):
     by = heads // kv
     ref, size, reach = O.cached_attention(q, k, v, cached, scale)
     coarse = np.abs(q).max(-1) * np.abs(k).sum(-1).max(0).repeat(by)[None] * scale
-    e = ((2 * (D + D // 16) + 16) * U * reach + 2.0 ** -28 * coarse)[..., None]
+    e = ((2 * (D + D // 16) + 16) * U * reach + step * coarse)[..., None]
     largest = np.abs(v).reshape(N, kv, D // 64, 64).max(-1)  # of a token, head and group
     most = np.zeros((n, heads, D // 64))
     for t in range(n):
@@ -208,3 +208,25 @@ def test_scores_of_any_size(int4, size, sign, cached):
                 tol = (2.0 ** -11 + 16 * U) * np.abs(one) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(one) + 2.0 ** -30 * np.abs(v).max()
                 assert (np.abs(got[s, t, h] - one) <= tol).all(), (s, t, h)
     assert led >= 8
+
+
+@pytest.mark.parametrize("loud", [0, 1])
+@pytest.mark.parametrize("D,channels", [(128, 64), (128, 16), (64, 16)])
+@pytest.mark.parametrize("int4", [True, False])
+def test_small_channels_of_a_query_that_meet_large_keys(int4, D, channels, loud):
+    """The first (or last) channels have queries of 2^-26 and (where they are a group of their own) keys of 2^26 times the others'. A
+    query is off by 2^-35 of its head's largest at most, as its largest is put at 2^14 or more and a sixteenth of it has
+    steps of 2^-24 then; scores' other errors as above."""
+    def change(k, v):
+        if channels == 64:
+            k[..., at:at + 64] *= 2.0 ** 26
+
+    at = D - channels if loud else 0
+    c = make(68, 2, 4, 2, D, 16, int4, [300, 0, 37], change=change)
+    x = c["q"].view(-1, 4, D)
+    x[..., at:at + channels] *= 2.0 ** -26
+    q, got = fp64(c, attend(c))
+    for s in range(3):
+        n, old = 2, int(c["cached"][s])
+        k, v = (c[y][s, :old + n].astype(np.float64) for y in ("k", "v"))
+        check_one(q[s], k, v, old, D ** -0.5, got[s], f"sequence {s}", step=2.0 ** -35)
