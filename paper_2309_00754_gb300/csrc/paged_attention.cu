@@ -89,13 +89,10 @@ struct Config {
   using Vec = std::conditional_t<kDh == 128, float4, float2>;  // a lane's channels where a warp has a row
   static constexpr int kMTiles = kDh / 16;
   static constexpr int kCtasPerSm = kInt4 || kDh == 64 ? 2 : 1;
-  static constexpr int kPair = kInt4 ? 2 : 1;  // tiles that are taken together
-  static constexpr int kStageTiles = kInt4 ? 2 : 1;       // that are copied together
+  static constexpr int kStageTiles = kInt4 ? 2 : 1;  // that are copied and taken together
   static constexpr int kStageBytes = kStageTiles * Tile::kBytes;
-  // a warp's ring also takes its last part at the end
-  static constexpr int kLeast = (kRows * kDh * 4 + kStageBytes - 1) / kStageBytes;
-  static constexpr int kStages = kLeast > 2 ? 4 : 2;
-  static_assert(kLeast <= kStages, "a part fits the ring");
+  static constexpr int kStages = 2;  // a power of two
+  static_assert(kRows * kDh * 4 <= kStages * kStageBytes, "a warp's ring takes its last part at the end");
   static constexpr int kRing = kWarps * kStages * kStageBytes;
   static constexpr int kQ = kRows * kDh * 2;  // a warp's queries, as rows and then as fragments
   static constexpr int kSmem = kRing + kWarps * kQ;
@@ -1096,12 +1093,7 @@ __global__ void __launch_bounds__(kThreads, Config<kDh, kInt4>::kCtasPerSm)
       --fast;
       const uint8_t* const at = ring + (used & (C::kStages - 1)) * C::kStageBytes;
       wait_copies<C::kStages - 1>();
-      if constexpr (C::kPair == C::kStageTiles) {
-        rows.template take<C::kPair, false>(at, tile * kKvTile, lane);
-      } else {
-#pragma unroll 1
-        for (int i = 0; i < C::kStageTiles; ++i) rows.template take<1, false>(at + i * Tile::kBytes, (tile + i) * kKvTile, lane);
-      }
+      rows.template take<C::kStageTiles, false>(at, tile * kKvTile, lane);
       __syncwarp();
       ++used;
       tile += C::kStageTiles;
