@@ -174,6 +174,14 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
       : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)));
   return r;
 }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<unsigned long long&>(r))
+      : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)),
+        "l"(reinterpret_cast<unsigned long long&>(c)));
+  return r;
+}
 // 2^e, e in [-126, 127]
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }
 __device__ __forceinline__ float pow2_or_0(int e) { return pow2(max(e, -127)); }  // 0 below 2^-126
@@ -600,6 +608,8 @@ struct Rows {
     constexpr int kWords = kDh / 32;
     const int g = lane >> 2, t = lane & 3;
     // ---- scores: S^T = K q^T
+    // (as exponents of 2, and numbers of their own: a product that is rounded only when the maximum comes off lies, beyond 2^25,
+    // further from the maximum than the range that follows)
     float sc[kN][4], sv[kN][2][kGroups];  // values' scales of tokens g and g + 8
 #pragma unroll
     for (int i = 0; i < kN; ++i) {
@@ -660,9 +670,13 @@ struct Rows {
             if (step == 0) first_mma_f16(part[gr], a, f.x, f.y); else mma_f16(part[gr], a, f.x, f.y);
           }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          sc[i][e] = part[0][e] * sk[e >> 1][0];
-          if constexpr (kGroups == 2) sc[i][e] = fmaf(part[1][e], sk[e >> 1][1], sc[i][e]);
+        for (int h = 0; h < 2; ++h) {  // (the row's factor before the keys' scales: the sums of large keys alone would pass fp32)
+          const float2 f = make_float2(factor[0], factor[1]);
+          float2 s = mul2(mul2(make_float2(part[0][2 * h], part[0][2 * h + 1]), f), make_float2(sk[h][0], sk[h][0]));
+          if constexpr (kGroups == 2)
+            s = fma2(mul2(make_float2(part[1][2 * h], part[1][2 * h + 1]), f), make_float2(sk[h][1], sk[h][1]), s);
+          sc[i][2 * h] = s.x;
+          sc[i][2 * h + 1] = s.y;
         }
       } else {
 #pragma unroll
@@ -679,7 +693,7 @@ struct Rows {
           }
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[i][e] = part[0][e];
+        for (int e = 0; e < 4; ++e) sc[i][e] = __fmul_rn(part[0][e], factor[e & 1]);
       }
     }
 
@@ -688,15 +702,14 @@ struct Rows {
     float pr[kN][4];
     uint32_t pf[kN][2][2];
     auto hidden = [&](int i, int e) { return kMasked && pos + kKvTile * i + g + 8 * (e >> 1) > limit[e & 1]; };
-    // (rounded: with the scores rounded as the maximum was, which the single rounding passes by more than the range beyond 2^25)
-    auto probabilities = [&](bool rounded) {
+    auto probabilities = [&]() {
       bool far = false;
       uint32_t most = 0;
 #pragma unroll
       for (int i = 0; i < kN; ++i) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          float ex = rounded ? __fsub_rn(__fmul_rn(sc[i][e], factor[e & 1]), m[e & 1]) : fmaf(sc[i][e], factor[e & 1], -m[e & 1]);
+          float ex = sc[i][e] - m[e & 1];
           if (hidden(i, e)) ex = -INFINITY;
           far |= ex > kSlack;
           pr[i][e] = ex2(ex);
@@ -719,14 +732,14 @@ struct Rows {
       if constexpr (kInt4) far |= above_f16(most);
       return far;
     };
-    if (__any_sync(0xffffffffu, probabilities(false))) {
+    if (__any_sync(0xffffffffu, probabilities())) {
       // (both rows at once: this runs at every item's start)
       float score[kN][4], top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int i = 0; i < kN; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          score[i][e] = hidden(i, e) ? -INFINITY : __fmul_rn(sc[i][e], factor[e & 1]);
+          score[i][e] = hidden(i, e) ? -INFINITY : sc[i][e];
           top[e & 1] = fmaxf(top[e & 1], score[i][e]);
         }
 #pragma unroll
@@ -787,7 +800,7 @@ struct Rows {
             o[j][e + 2] *= pow2_or_0(-up[e]);
           }
       }
-      probabilities(true);
+      probabilities();
     }
 #pragma unroll
     for (int i = 0; i < kN; ++i) {

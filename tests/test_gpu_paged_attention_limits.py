@@ -230,3 +230,12 @@ def test_small_channels_of_a_query_that_meet_large_keys(int4, D, channels, loud)
         n, old = 2, int(c["cached"][s])
         k, v = (c[y][s, :old + n].astype(np.float64) for y in ("k", "v"))
         check_one(q[s], k, v, old, D ** -0.5, got[s], f"sequence {s}", step=2.0 ** -35)
+
+
+@pytest.mark.parametrize("k_by,q_by", [(1e33, 1e-33), (1e35, 1e-35), (1e-35, 1e35), (1e-30, 1e33), (1e20, 1e-20)])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("int4", [True, False])
+def test_large_keys_and_small_queries(int4, D, k_by, q_by):
+    """And the other way round: what counts is that the score is a number."""
+    c = make(69, 3, 4, 2, D, 16, int4, [200, 0, 37], k_by=k_by, q_by=q_by / (k_by * q_by if k_by * q_by > 1 else 1))
+    check_groups(c, attend(c))
