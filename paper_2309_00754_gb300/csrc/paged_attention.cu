@@ -21,7 +21,7 @@
 //
 // A bf16 cache is bound by its bytes (8 sequences of up to 32,768 tokens, 8 heads: 580 MB in 92 us, 6.3 TB/s). In 4 bits the
 // copies are hidden and what a tile costs to unpack and multiply, 360 instructions of a warp for 2304 bytes, is as much as
-// its bytes or more: 3 sequences of up to 131,072 tokens, 8 heads: 283 MB in 62 us, 4.6 TB/s; 64 sequences of up to 800, 32
+// its bytes or more: 3 sequences of up to 131,072 tokens, 8 heads: 283 MB in 62 us, 4.5 TB/s; 64 sequences of up to 800, 32
 // heads: 146 MB in 47 us. Half of the issue slots are used, the rest goes to dependent instructions and their fetch.
 //
 // Work is cut evenly: the tiles of all (sequence, eight rows, head) items in a row, a contiguous part for each warp, which
