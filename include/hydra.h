@@ -642,7 +642,7 @@ hydra_status hydra_kv_read(const hydra_kv_cache* cache, const int32_t* table, in
  * a key's infinity makes a score infinite: +inf makes the head NaN, a token with -inf weighs nothing, and where all that a query
  * sees have -inf the head is NaN.
  * Scores, their maximum and sums are fp32. A cache in 4 bits takes queries as they are down to 2^-28 of their head's largest
- * channel, what is less with an error of 2^-35 of it, and a weight times its value's scale in fp16 (2^-12 of it, and where it is
+ * channel, what is less with an error of 2^-35 of it, and a weight times its value's scale in fp16 (2^-11 of it, and where it is
  * less than 2^-20 of the largest such product of its row and its 64 channels, 2^-31 of that); a bf16 cache takes weights as two
  * bf16 (2^-16).
  * Bits: equal calls on one device give equal bits; a sequence's depend on the others' lengths (where work is cut) and on

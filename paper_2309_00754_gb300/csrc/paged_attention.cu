@@ -11,8 +11,8 @@
 // In 4 bits a code enters as the fp16 integer code - zero: its bits over those of 1024 (or 16 times it over 1024, for the
 // upper nibble of a byte) are a float, less 1024 + zero, all exact; what is 16 times too large is undone in q and at
 // the end. So keys' products are exact up to the sums, their scale is multiplied in fp32 after, and a value's scale goes
-// into its probability, which is the one thing that is rounded: to fp16, 2^-12, which adds a hundredth to the error that the
-// output's own rounding makes. (bf16's 2^-9 would add as much again; what the rounding leaves as a second fp16 number is 10 to
+// into its probability, which is the one thing that is rounded: to fp16, 2^-11, which adds a hundredth to the error that the
+// output's own rounding makes. (bf16's 2^-8 would add as much again; what the rounding leaves as a second fp16 number is 10 to
 // 15 % of the time: 53.7, 38.2 and 71.2 us for 64 sequences of 800 tokens, 16 of 4096 and 3 of 131,072, against 47.4, 34.6 and
 // 61.8.) To keep that in fp16's range, each row has a power of two for each group of channels (`lift`) by which the group's
 // weights are held, so that a group's precision is its own, whatever the other's scales are. m, a whole number, and the lifts
